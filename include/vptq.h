@@ -58,6 +58,7 @@ extern "C" {
 #define VPTQ_DTYPE_FP16 0
 #define VPTQ_DTYPE_BF16 1
 #define VPTQ_DTYPE_FP32 2
+#define VPTQ_DTYPE_E4M3 3   /* 8-bit floating point (vptq_fp8_* and vptq_linear_fp8 only)              */
 
 #define VPTQ_FLAG_SCALE_BIAS   1  /* scale and bias are present                                     */
 #define VPTQ_FLAG_SCALE_ROWS   2  /* scale/bias are per OUTPUT row ([M]) instead of per input column */
@@ -430,6 +431,56 @@ int64_t vptq_kmeans_update_workspace_bytes(int32_t v, int32_t k);
 int vptq_kmeans_update(const void *W, int32_t M, int32_t N, int32_t v, const int32_t *idx,
                        const float *col_weight, int32_t k, void *codebook,
                        void *workspace, size_t workspace_bytes, void *stream);
+
+/* ---- 8-bit floating point: operands with block scales, and the product over them -------- */
+
+/* The paper has no counterpart: it restores weights to FP16 for prompts (App. D.2).  On B200 the tensor cores take e4m3 operands
+ * at twice the FP16 rate, so a layer that is restored once to e4m3 (vptq_dequant_fp8: one byte a weight) runs its prompts
+ * faster than any kernel that makes FP16 tiles of it, and checkpoints that come in this format run as they are.
+ *
+ * An e4m3 matrix is [rows][pitch] bytes, pitch = vptq_fp8_row_bytes(cols) = cols rounded up to a multiple of 16, pad bytes zero;
+ * e4m3 is the format without infinities (largest value 448, NaN 0x7F / 0xFF).  Its scales are FP32,
+ * [ceil(rows / block_rows)][ceil(cols / 128)], block_rows = 1 (activations) or 128 (weights); value = e4m3 * scale.
+ * The rule of the quantization, in FP32 with every operation rounded by itself:
+ *   a = max |x| over the block, at least 2^-100;  scale = a / 448;  r = 448 / a;
+ *   e4m3 = round(x * r), ties to even.
+ * A block with an infinity or a NaN gets an infinite or NaN scale, and every value of it reads as NaN.
+ *
+ * vptq_fp8_quantize: x [rows][cols] of x_dtype (FP16, BF16 or FP32), its rows `ld` values apart (ld >= cols; any alignment of a
+ *   value of the type), to q and scale (16-byte aligned, q packed at the pitch above).  block_rows is 1 or 128, else VPTQ_E_SHAPE.
+ *   rows = 0 does nothing. */
+int64_t vptq_fp8_row_bytes(int32_t n_cols);
+int vptq_fp8_quantize(const void *x, int32_t x_dtype, int32_t n_rows, int32_t n_cols, int64_t ld, int32_t block_rows,
+                      uint8_t *q, float *scale, void *stream);
+/* A vector-quantized layer as an e4m3 weight: the FP16 values of vptq_dequant, bit for bit, quantized by the rule with
+ * block_rows = 128; the FP16 matrix is not written anywhere.  q [M][pitch(N)], scale [ceil(M / 128)][ceil(N / 128)].  Layers with a
+ * stored column order (VPTQ_FLAG_COL_PERM) need vptq_dequant_fp8_workspace_bytes() bytes of workspace, others none. */
+int64_t vptq_dequant_fp8_workspace_bytes(const vptq_layer_desc *desc);
+int vptq_dequant_fp8(const vptq_layer_desc *desc, const vptq_layer_ptrs *p, uint8_t *q, float *scale,
+                     void *workspace, size_t workspace_bytes, void *stream);
+
+/* out[B][M] = x[B][N] * W^T over an e4m3 weight (block_rows = 128): FP32 sums of exact products, a block's sum multiplied by its two
+ * scales, the result rounded once to out_dtype.
+ *   x_dtype VPTQ_DTYPE_E4M3: x [B][pitch(N)] with x_scale [B][ceil(N / 128)] (block_rows = 1)
+ *           VPTQ_DTYPE_FP16 / _BF16: x [B][N], quantized inside the call by the rule (x_scale is not read): the same operands, and
+ *           so the same result, as vptq_fp8_quantize followed by the call above
+ *   out_dtype FP16, BF16 or FP32;  flags: VPTQ_FLAG_CONCURRENT and VPTQ_FLAG_DETERMINISTIC are accepted and change nothing (no CTA
+ *           waits for another launch's, every sum has a fixed order).
+ * At most 16 tokens take the kernel "fp8_decode", more "fp8_tcgen05" (vptq_linear_fp8_path; by M, N, B and the types alone), whose
+ * workspace starts with a status word (vptq_workspace_status); that kernel's waits are bounded.  The workspace is
+ * 256-byte aligned; its contents on entry are irrelevant; calls that may overlap must not share one. */
+typedef struct vptq_fp8_desc {
+    int32_t M, N;        /* out_features, in_features */
+    int32_t x_dtype;     /* VPTQ_DTYPE_E4M3, _FP16 or _BF16 */
+    int32_t out_dtype;   /* VPTQ_DTYPE_FP16, _BF16 or _FP32 */
+    int32_t flags;       /* VPTQ_FLAG_CONCURRENT, VPTQ_FLAG_DETERMINISTIC or 0 */
+} vptq_fp8_desc;
+int64_t vptq_linear_fp8_workspace_bytes(const vptq_fp8_desc *desc, int32_t B);
+int vptq_linear_fp8(const vptq_fp8_desc *desc, const void *x, const float *x_scale, int32_t B,
+                    const uint8_t *w, const float *w_scale, void *out,
+                    void *workspace, size_t workspace_bytes, void *stream);
+const char *vptq_linear_fp8_path(const vptq_fp8_desc *desc, int32_t B);
+int vptq_linear_fp8_launches(const vptq_fp8_desc *desc, int32_t B);
 
 /* ---- diagnostics ------------------------------------------------------------------ */
 

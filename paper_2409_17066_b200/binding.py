@@ -32,13 +32,14 @@ OK = 0
 E_NULL, E_SHAPE, E_ALIGN, E_UNSUPPORTED, E_WORKSPACE, E_INDEX_RANGE, E_CUDA, E_TIMEOUT = range(-1, -9, -1)
 E_SCRATCH_LIMIT = -9
 NOALLOC_SCRATCH_BYTES = 1 << 20
-DTYPE_FP16, DTYPE_BF16, DTYPE_FP32 = 0, 1, 2
+DTYPE_FP16, DTYPE_BF16, DTYPE_FP32, DTYPE_E4M3 = 0, 1, 2, 3
 FLAG_SCALE_BIAS, FLAG_SCALE_ROWS, FLAG_FORCE_GENERIC, FLAG_COL_PERM, FLAG_PREPARED = 1, 2, 4, 8, 16
 FLAG_CONCURRENT = 32
 FLAG_DETERMINISTIC = 64
 
 _DT = {"fp16": DTYPE_FP16, "bf16": DTYPE_BF16, "fp32": DTYPE_FP32}
 _TORCH_DT = {DTYPE_FP16: torch.float16, DTYPE_BF16: torch.bfloat16, DTYPE_FP32: torch.float32}
+_DT_OF_TORCH = {torch.float16: DTYPE_FP16, torch.bfloat16: DTYPE_BF16, torch.float32: DTYPE_FP32, torch.float8_e4m3fn: DTYPE_E4M3}
 
 
 class LayerDesc(C.Structure):
@@ -55,6 +56,11 @@ class LayerPtrs(C.Structure):
                 ("res_idx", C.c_void_p), ("res_codebook", C.c_void_p),
                 ("outlier_idx", C.c_void_p), ("outlier_codebook", C.c_void_p),
                 ("scale", C.c_void_p), ("bias", C.c_void_p), ("col_perm", C.c_void_p), ("prepared", C.c_void_p)]
+
+
+class Fp8Desc(C.Structure):
+    """vptq_fp8_desc"""
+    _fields_ = [("M", C.c_int32), ("N", C.c_int32), ("x_dtype", C.c_int32), ("out_dtype", C.c_int32), ("flags", C.c_int32)]
 
 
 EXPORTS = {
@@ -95,6 +101,17 @@ EXPORTS = {
                                       C.c_void_p]),
     "vptq_linear_noalloc": (C.c_int, [C.POINTER(LayerDesc), C.c_void_p, C.c_int32, C.POINTER(LayerPtrs),
                                       C.c_void_p, C.c_void_p]),
+    "vptq_fp8_row_bytes": (C.c_int64, [C.c_int32]),
+    "vptq_fp8_quantize": (C.c_int, [C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int64, C.c_int32, C.c_void_p, C.c_void_p,
+                                    C.c_void_p]),
+    "vptq_dequant_fp8_workspace_bytes": (C.c_int64, [C.POINTER(LayerDesc)]),
+    "vptq_dequant_fp8": (C.c_int, [C.POINTER(LayerDesc), C.POINTER(LayerPtrs), C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t,
+                                   C.c_void_p]),
+    "vptq_linear_fp8_workspace_bytes": (C.c_int64, [C.POINTER(Fp8Desc), C.c_int32]),
+    "vptq_linear_fp8": (C.c_int, [C.POINTER(Fp8Desc), C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p,
+                                  C.c_void_p, C.c_size_t, C.c_void_p]),
+    "vptq_linear_fp8_path": (C.c_char_p, [C.POINTER(Fp8Desc), C.c_int32]),
+    "vptq_linear_fp8_launches": (C.c_int, [C.POINTER(Fp8Desc), C.c_int32]),
     "vptq_status_string": (C.c_char_p, [C.c_int]),
     "vptq_last_cuda_error": (C.c_char_p, []),
     "vptq_workspace_status": (C.c_int, [C.c_void_p, C.c_void_p]),
@@ -375,6 +392,52 @@ def vptq_linear_launches(desc: LayerDesc, B: int) -> int:
     return lib.vptq_linear_launches(C.byref(desc), B)
 
 
+# ---- 8-bit floating point ----------------------------------------------------------------
+
+def vptq_fp8_row_bytes(n_cols: int) -> int:
+    return lib.vptq_fp8_row_bytes(n_cols)
+
+
+def make_fp8_desc(M, N, x_dtype="fp16", out_dtype="fp16", flags=0) -> Fp8Desc:
+    return Fp8Desc(M, N, DTYPE_E4M3 if x_dtype == "e4m3" else _DT[x_dtype], _DT[out_dtype], flags)
+
+
+def vptq_fp8_quantize(x: torch.Tensor, block_rows: int = 1):
+    """(q, scale) of x [rows][cols] (fp16, bf16 or fp32; the columns adjacent, any distance between rows): q float8_e4m3fn
+    [rows][cols rounded up to 16], scale fp32 [ceil(rows / block_rows)][ceil(cols / 128)]; block_rows 1 (activations) or 128."""
+    return _native.fp8_quantize(x, block_rows)
+
+
+def vptq_dequant_fp8(desc: LayerDesc, ptrs: LayerPtrs, workspace: Optional[torch.Tensor] = None):
+    """(q, scale) of a vector-quantized layer, as vptq_fp8_quantize(W, 128) of its restored FP16 weight gives them."""
+    return _native.dequant_fp8(desc, ptrs, workspace)
+
+
+def vptq_linear_fp8_workspace_bytes(desc: Fp8Desc, B: int) -> int:
+    n = lib.vptq_linear_fp8_workspace_bytes(C.byref(desc), B)
+    if n < 0:
+        raise VptqError(int(n))
+    return n
+
+
+def vptq_linear_fp8(x: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, x_scale: Optional[torch.Tensor] = None,
+                    out_dtype: Optional[str] = None, out: Optional[torch.Tensor] = None,
+                    workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """out [B][M] = x * W^T over an e4m3 weight w [M][pitch], w_scale [ceil(M / 128)][ceil(N / 128)].  x is fp16 or bf16 [B][N]
+    (quantized inside the call) or e4m3 [B][pitch] with x_scale [B][ceil(N / 128)].  out_dtype "fp16", "bf16" or "fp32" (default:
+    that of `out`, else of x, else "bf16").  Contiguous tensors of one device, the current one.  A workspace is only taken from the caller to
+    read its status word afterwards (vptq_workspace_status); without one the call allocates its own."""
+    return _native.linear_fp8(x, w, w_scale, x_scale, None if out_dtype is None else _DT[out_dtype], out, workspace)
+
+
+def vptq_linear_fp8_path(desc: Fp8Desc, B: int) -> str:
+    return lib.vptq_linear_fp8_path(C.byref(desc), B).decode()
+
+
+def vptq_linear_fp8_launches(desc: Fp8Desc, B: int) -> int:
+    return lib.vptq_linear_fp8_launches(C.byref(desc), B)
+
+
 # ---- a quantized layer resident on the device ------------------------------------------
 
 class DeviceLayer:
@@ -473,6 +536,10 @@ class DeviceLayer:
     def dequant(self) -> torch.Tensor:
         W = torch.empty((self.spec.M, self.spec.N), dtype=torch.float16, device=self.device)
         return vptq_dequant(self.desc, self.ptrs, W)
+
+    def dequant_fp8(self):
+        """(q, scale): the restored weight in e4m3 with 128 x 128 block scales, an operand of vptq_linear_fp8."""
+        return vptq_dequant_fp8(self.desc, self.ptrs)
 
     def linear(self, x: torch.Tensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         y = _native.layer_linear(self.desc, self.ptrs, self._ws, x, out)

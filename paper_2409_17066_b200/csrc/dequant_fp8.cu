@@ -1,0 +1,206 @@
+// A vector-quantized layer restored straight to an e4m3 weight with 128 x 128 block scales: the FP16 values of vptq_dequant, bit for
+// bit (FP32, three separately rounded operations, then FP16), quantized by the rule of fp8_quantize.cu, without the FP16 matrix in
+// global memory.
+//
+// A CTA makes one 128 x 128 block: its threads look up the (vector row, column) pairs that meet the block, ITEMS at a time so that
+// as many table reads are in flight, and leave the FP16 values in shared memory; the block's maximum and the rounding follow.
+// A vector row that crosses a block's edge is looked up by both blocks (v = 8 never does; v = 6: 23 rows instead of 21.3).
+#include "fp8.cuh"
+
+namespace vptq {
+
+namespace {
+
+constexpr int THREADS = 256;
+constexpr int COL_LANES = THREADS / FP8_BLOCK;            // vector rows of a block taken at a time
+constexpr int ITEMS = 4;
+constexpr int TILE_STRIDE = FP8_BLOCK + 8;                // halves; 16-byte rows, half warps read them without conflicts
+
+struct DequantFp8Params {
+    LayerView L;
+    uint8_t *q;
+    float *scale;
+    const int *inverse;       // stored column of every input feature (-1: none names it), or null
+    long long pitch;
+    int col_blocks;
+};
+
+// V = 0: any length, component by component
+template <int V> struct Row { uint32_t w[V > 0 ? V / 2 : 1]; };
+template <int V>
+__device__ __forceinline__ Row<V> table_row(const __half *__restrict__ tab, long long e)
+{
+    Row<V> r;
+    if constexpr (V == 8) {
+        const uint4 q = __ldg(reinterpret_cast<const uint4 *>(tab) + e);
+        r.w[0] = q.x; r.w[1] = q.y; r.w[2] = q.z; r.w[3] = q.w;
+    } else if constexpr (V % 4 == 0 && V > 0) {
+#pragma unroll
+        for (int i = 0; i < V / 4; i++) {
+            const uint2 q = __ldg(reinterpret_cast<const uint2 *>(tab) + e * (V / 4) + i);
+            r.w[2 * i] = q.x; r.w[2 * i + 1] = q.y;
+        }
+    } else if constexpr (V > 0) {
+#pragma unroll
+        for (int i = 0; i < V / 2; i++) r.w[i] = __ldg(reinterpret_cast<const uint32_t *>(tab) + e * (V / 2) + i);
+    }
+    return r;
+}
+template <int V>
+__device__ __forceinline__ float component(const Row<V> &r, const __half *__restrict__ tab, long long e, int v, int j)
+{
+    if constexpr (V > 0) {
+        const uint32_t w = r.w[j / 2];
+        return __half2float(__ushort_as_half((unsigned short)((j & 1) ? w >> 16 : w & 0xFFFFu)));
+    } else {
+        return __half2float(__ldg(tab + e * v + j));
+    }
+}
+
+__device__ __forceinline__ float finish(float t, bool has_scale, float s, float b)
+{
+    return has_scale ? __fadd_rn(__fmul_rn(t, s), b) : t;              // never contracted to an FMA
+}
+
+template <int V>
+__global__ void __launch_bounds__(THREADS)
+dequant_fp8_kernel(const __grid_constant__ DequantFp8Params P)
+{
+    __shared__ __align__(16) __half tile[FP8_BLOCK][TILE_STRIDE];
+    __shared__ uint32_t part[THREADS / 32];
+    const LayerView &L = P.L;
+    const int cb = blockIdx.x % P.col_blocks, rb = blockIdx.x / P.col_blocks;
+    const int m0 = rb * FP8_BLOCK, m1 = min(L.M, m0 + FP8_BLOCK);
+    const int v = V > 0 ? V : L.v;
+    {
+        const int c = threadIdx.x % FP8_BLOCK, sub = threadIdx.x / FP8_BLOCK;
+        const int f = cb * FP8_BLOCK + c;                                 // input feature
+        const int n = f >= L.N ? -1 : P.inverse ? __ldg(P.inverse + f) : f;      // stored column
+        float sc = 1.f, bi = 0.f;
+        if (n >= 0 && L.has_scale && !L.scale_rows) { sc = __half2float(__ldg(L.scale + n)); bi = __half2float(__ldg(L.bias + n)); }
+        auto put = [&](int m, float t) {
+            float s = sc, b = bi;
+            if (L.has_scale && L.scale_rows) { s = __half2float(__ldg(L.scale + m)); b = __half2float(__ldg(L.bias + m)); }
+            tile[m - m0][c] = __float2half_rn(finish(t, L.has_scale, s, b));
+        };
+        if (n < 0) {
+            for (int m = m0 + sub; m < m1; m += COL_LANES) tile[m - m0][c] = __float2half_rn(0.f);
+        } else if (n < L.n_out) {
+            for (int r = m0 / L.v0 + sub; r * L.v0 < m1; r += COL_LANES) {
+                const int i0 = clamp_index(load_index(L.s0.ptr + (long long)r * L.s0.stride, n, L.s0.bits), L.k0);
+                for (int j = 0; j < L.v0; j++) {
+                    const int m = r * L.v0 + j;
+                    if (m >= m0 && m < m1) put(m, __half2float(__ldg(L.c0 + (long long)i0 * L.v0 + j)));
+                }
+            }
+        } else {
+            const int col = n - L.n_out, group = L.G > 1 ? col / L.cpg : 0;
+            const bool res = L.k2 > 0;
+            const int r1 = (m1 + v - 1) / v;                              // (m1 <= M: rows that exist)
+            for (int r0 = m0 / v + sub; r0 < r1; r0 += COL_LANES * ITEMS) {
+                long long e1[ITEMS], e2[ITEMS];
+                Row<V> w1[ITEMS], w2[ITEMS];
+#pragma unroll
+                for (int i = 0; i < ITEMS; i++) {
+                    const int r = min(r0 + i * COL_LANES, r1 - 1);
+                    e1[i] = (long long)group * L.k1 + clamp_index(load_index(L.s1.ptr + (long long)r * L.s1.stride, col, L.s1.bits), L.k1);
+                    e2[i] = res ? (long long)group * L.k2 + clamp_index(load_index(L.s2.ptr + (long long)r * L.s2.stride, col, L.s2.bits), L.k2) : 0;
+                }
+#pragma unroll
+                for (int i = 0; i < ITEMS; i++) {
+                    w1[i] = table_row<V>(L.c1, e1[i]);
+                    if (res) w2[i] = table_row<V>(L.c2, e2[i]);
+                }
+#pragma unroll
+                for (int i = 0; i < ITEMS; i++) {
+                    const int r = r0 + i * COL_LANES;
+                    if (r >= r1) break;
+                    auto one = [&](int j) {
+                        const int m = r * v + j;
+                        if (m < m0 || m >= m1) return;
+                        float t = component<V>(w1[i], L.c1, e1[i], v, j);
+                        if (res) t = __fadd_rn(t, component<V>(w2[i], L.c2, e2[i], v, j));
+                        put(m, t);
+                    };
+                    if constexpr (V > 0) {
+#pragma unroll
+                        for (int j = 0; j < V; j++) one(j);
+                    } else {
+                        for (int j = 0; j < v; j++) one(j);
+                    }
+                }
+            }
+        }
+    }
+    __syncthreads();
+    // 16 lanes a row, eight columns a lane (rows beyond M were not written: left out)
+    constexpr int ROWS = THREADS / 16, ROUNDS = FP8_BLOCK / ROWS;
+    const int lane = threadIdx.x & 15, sub = threadIdx.x >> 4, c = cb * FP8_BLOCK + lane * 8;
+    uint4 w[ROUNDS];
+    uint32_t most = 0;
+#pragma unroll
+    for (int i = 0; i < ROUNDS; i++) {
+        const int row = i * ROWS + sub;
+        w[i] = m0 + row < m1 ? *reinterpret_cast<const uint4 *>(&tile[row][lane * 8]) : make_uint4(0, 0, 0, 0);
+        most = __vmaxu2(most, __vmaxu2(__vmaxu2(w[i].x & 0x7FFF7FFFu, w[i].y & 0x7FFF7FFFu), __vmaxu2(w[i].z & 0x7FFF7FFFu, w[i].w & 0x7FFF7FFFu)));
+    }
+    most = __reduce_max_sync(0xffffffffu, max(most & 0xFFFFu, most >> 16));
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = most;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < THREADS / 32; i++) most = max(most, part[i]);
+    const Fp8Scale s = fp8_scale(__half2float(__ushort_as_half((unsigned short)most)));
+    if (threadIdx.x == 0) P.scale[blockIdx.x] = s.scale;
+    if (c >= P.pitch) return;
+#pragma unroll
+    for (int i = 0; i < ROUNDS; i++) {
+        const int row = i * ROWS + sub;
+        if (m0 + row >= m1) break;
+        const uint32_t h[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+        uint32_t o[2];
+#pragma unroll
+        for (int k = 0; k < 2; k++) {
+            const float2 a = Act<VPTQ_DTYPE_FP16>::two(h[2 * k]), b = Act<VPTQ_DTYPE_FP16>::two(h[2 * k + 1]);
+            o[k] = fp8_quad(a.x * s.factor, a.y * s.factor, b.x * s.factor, b.y * s.factor);
+        }
+        uint8_t *dst = P.q + (long long)(m0 + row) * P.pitch + c;
+        *reinterpret_cast<uint2 *>(dst) = make_uint2(o[0], o[1]);
+        if (c + 8 > L.N)
+            for (int j = max(0, L.N - c); j < 8; j++) dst[j] = 0;         // pad bytes are zeros, whatever the factor
+    }
+}
+
+// stored column order -> the stored column of every feature; a list that is no permutation: the largest column that names it, -1 none
+__global__ void __launch_bounds__(256)
+inverse_order_kernel(LayerView L, int *inverse)
+{
+    const int j = blockIdx.x * 256 + threadIdx.x;
+    if (j < L.N) atomicMax(inverse + in_col(L, j), j);
+}
+
+}  // namespace
+
+cudaError_t launch_dequant_fp8(const LayerView &L, uint8_t *q, float *scale, int *inverse, cudaStream_t st)
+{
+    DequantFp8Params P;
+    P.L = L; P.q = q; P.scale = scale; P.inverse = nullptr;
+    P.pitch = fp8_row_bytes(L.N);
+    P.col_blocks = ceil_div(L.N, FP8_BLOCK);
+    if (L.perm != nullptr) {
+        cudaError_t e = cudaMemsetAsync(inverse, 0xFF, 4ull * L.N, st);
+        if (e != cudaSuccess) return e;
+        inverse_order_kernel<<<ceil_div(L.N, 256), 256, 0, st>>>(L, inverse);
+        if ((e = cudaGetLastError()) != cudaSuccess) return e;
+        P.inverse = inverse;
+    }
+    const unsigned blocks = (unsigned)((long long)ceil_div(L.M, FP8_BLOCK) * P.col_blocks);
+    switch (L.v) {
+    case 8: dequant_fp8_kernel<8><<<blocks, THREADS, 0, st>>>(P); break;
+    case 6: dequant_fp8_kernel<6><<<blocks, THREADS, 0, st>>>(P); break;
+    case 12: dequant_fp8_kernel<12><<<blocks, THREADS, 0, st>>>(P); break;
+    default: dequant_fp8_kernel<0><<<blocks, THREADS, 0, st>>>(P);
+    }
+    return cudaGetLastError();
+}
+
+}  // namespace vptq

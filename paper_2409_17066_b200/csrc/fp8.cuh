@@ -1,0 +1,120 @@
+// Matrices in 8-bit floating point (e4m3) with a scale per block of 128 columns: the rule of the quantization and the pieces that
+// the kernels over them share.
+#pragma once
+#include "common.cuh"
+
+namespace vptq {
+
+constexpr int FP8_BLOCK = 128;                            // columns (and rows, for weights) that share a scale
+constexpr int FP8_MAX_SIZE = 1 << 30;                     // rows, columns, tokens: sums of a few of them stay in an int
+constexpr float FP8_MAX = 448.f;                          // largest e4m3 value
+constexpr float FP8_AMAX_MIN = 7.888609052210118e-31f;    // 2^-100: a block's largest value counts as at least this
+
+inline long long fp8_row_bytes(long long cols) { return (cols + 15) / 16 * 16; }
+
+// activations (or results) of `rows` rows to e4m3 with a scale per 128 columns of a row (block_rows = 1) or per 128 x 128 values
+// (block_rows = 128); ld = distance of x's rows in values; `status` (may be null) is cleared.  `early`: the kernel behind this one
+// on the stream waits for it by itself before it touches q or scale.
+cudaError_t launch_fp8_quantize(const void *x, int x_dtype, int rows, int cols, long long ld, int block_rows, uint8_t *q, float *scale,
+                                int *status, bool early, cudaStream_t st);
+
+// a vector-quantized layer to e4m3 with 128 x 128 blocks; inverse: null or N words of scratch (a stored column order needs them)
+cudaError_t launch_dequant_fp8(const LayerView &L, uint8_t *q, float *scale, int *inverse, cudaStream_t st);
+
+struct Fp8Linear {
+    int M, N, B;
+    int x_dtype, out_dtype;
+    const void *x;
+    const float *x_scale;      // e4m3 activations only
+    const uint8_t *w;          // [M][fp8_row_bytes(N)]
+    const float *w_scale;      // [ceil(M / 128)][ceil(N / 128)]
+    void *out;
+};
+
+constexpr int FP8_DECODE_MAX_B = 16;
+cudaError_t launch_linear_fp8_decode(const Fp8Linear &P, cudaStream_t st);
+
+long long linear_fp8_workspace_bytes(int M, int N, int B, int x_dtype);
+int linear_fp8_launches(int M, int N, int B, int x_dtype);
+const char *linear_fp8_path(int M, int N, int B, int x_dtype);
+cudaError_t launch_linear_fp8(const Fp8Linear &P, void *ws, cudaStream_t st);
+
+#ifdef __CUDACC__
+// scale of a block whose largest magnitude is amax, and the factor its values are multiplied by before they are rounded to e4m3
+struct Fp8Scale { float scale, factor; };
+__device__ __forceinline__ Fp8Scale fp8_scale(float amax)
+{
+    const float a = amax < FP8_AMAX_MIN ? FP8_AMAX_MIN : amax;          // (a NaN stays)
+    return {__fdiv_rn(a, FP8_MAX), __fdiv_rn(FP8_MAX, a)};
+}
+
+// Two values to e4m3, nearest, ties to even; beyond 448: 448; NaN: NaN.  lo in the low byte.
+__device__ __forceinline__ uint32_t fp8_pair(float lo, float hi)
+{
+    uint16_t r;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ uint32_t fp8_quad(float a, float b, float c, float d) { return fp8_pair(a, b) | fp8_pair(c, d) << 16; }
+
+// Types of activations.  `magnitude` keeps the largest magnitude of packed values as bits, in an order in which NaN > infinity >
+// every number, so that one NaN or infinity shows in the block's scale.
+template <int DT> struct Act;
+template <> struct Act<VPTQ_DTYPE_FP16> {
+    static constexpr int BYTES = 2;
+    static __device__ __forceinline__ float2 two(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2 *>(&w)); }
+    static __device__ __forceinline__ float one(const void *p, long long i) { return __half2float(reinterpret_cast<const __half *>(p)[i]); }
+};
+template <> struct Act<VPTQ_DTYPE_BF16> {
+    static constexpr int BYTES = 2;
+    static __device__ __forceinline__ float2 two(uint32_t w) { return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u)); }
+    static __device__ __forceinline__ float one(const void *p, long long i)
+    {
+        return __uint_as_float((uint32_t)reinterpret_cast<const uint16_t *>(p)[i] << 16);
+    }
+};
+template <> struct Act<VPTQ_DTYPE_FP32> {
+    static constexpr int BYTES = 4;
+    static __device__ __forceinline__ float one(const void *p, long long i) { return reinterpret_cast<const float *>(p)[i]; }
+};
+
+// N consecutive values of a row, the first at column c of `cols` (zeros beyond); VEC: 16-byte loads (c and the row are aligned for
+// them, and the values beyond `cols` in the last of them belong to the row's next block or are not read: cols % (16 / bytes) == 0).
+template <int DT, bool VEC, int N>
+__device__ __forceinline__ void load_values(const void *row, int c, int cols, float (&v)[N])
+{
+    if constexpr (VEC && DT == VPTQ_DTYPE_FP32) {
+#pragma unroll
+        for (int i = 0; i < N; i += 4) {
+            const float4 q = c + i < cols ? __ldg(reinterpret_cast<const float4 *>(reinterpret_cast<const float *>(row) + c + i)) : make_float4(0.f, 0.f, 0.f, 0.f);
+            v[i] = q.x; v[i + 1] = q.y; v[i + 2] = q.z; v[i + 3] = q.w;
+        }
+    } else if constexpr (VEC) {
+#pragma unroll
+        for (int i = 0; i < N; i += 8) {
+            const uint4 q = c + i < cols ? __ldg(reinterpret_cast<const uint4 *>(reinterpret_cast<const uint16_t *>(row) + c + i)) : make_uint4(0, 0, 0, 0);
+            const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+                const float2 f = Act<DT>::two(w[j]);
+                v[i + 2 * j] = f.x; v[i + 2 * j + 1] = f.y;
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; i++) v[i] = c + i < cols ? Act<DT>::one(row, c + i) : 0.f;
+    }
+}
+
+// largest magnitude of N values as bits
+template <int N>
+__device__ __forceinline__ uint32_t magnitude(const float (&v)[N])
+{
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < N; i++) m = max(m, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+    return m;
+}
+#endif
+
+}  // namespace vptq

@@ -6,6 +6,7 @@
 #include <Python.h>
 
 #include <ATen/ops/empty.h>
+#include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -207,6 +208,155 @@ PyObject *py_dequant(PyObject *, PyObject *const *a, Py_ssize_t n)
     return a[2];
 }
 
+// ---- 8-bit floating point: these allocate their results (and workspaces) themselves, from torch's allocator -----------------
+
+// a contiguous CUDA tensor on the device of the current stream
+bool on_current_device(const at::Tensor &t) { return t.is_cuda() && t.get_device() == c10::cuda::current_device(); }
+bool plain(const at::Tensor &t) { return on_current_device(t) && t.is_contiguous(); }
+
+// runs a call that may throw (torch's allocator) and turns what it throws into a Python error
+template <typename F>
+PyObject *guarded(F f)
+{
+    try {
+        return f();
+    } catch (const std::exception &e) {
+        if (!PyErr_Occurred()) PyErr_SetString(PyExc_RuntimeError, e.what());
+        return nullptr;
+    }
+}
+
+PyObject *pair_of(const at::Tensor &a, const at::Tensor &b)
+{
+    PyObject *x = THPVariable_Wrap(a), *y = THPVariable_Wrap(b);
+    PyObject *r = x && y ? PyTuple_Pack(2, x, y) : nullptr;
+    Py_XDECREF(x);
+    Py_XDECREF(y);
+    return r;
+}
+
+// tensors of an e4m3 matrix: [rows][pitch] and its scales
+struct Fp8Tensors { at::Tensor q, scale; };
+Fp8Tensors empty_fp8(int64_t rows, int64_t cols, int64_t block_rows, const at::TensorOptions &options)
+{
+    return {at::empty({rows, (cols + 15) / 16 * 16}, options.dtype(at::kFloat8_e4m3fn)),
+            at::empty({(rows + block_rows - 1) / block_rows, (cols + 127) / 128}, options.dtype(at::kFloat))};
+}
+
+// [rows][pitch] e4m3 with [ceil(rows / block_rows)][ceil(pitch / 128)] FP32 scales
+bool is_fp8(const at::Tensor &q, const at::Tensor &scale, int64_t rows, int64_t pitch, int64_t block_rows)
+{
+    return plain(q) && plain(scale) && q.scalar_type() == at::kFloat8_e4m3fn && scale.scalar_type() == at::kFloat && q.dim() == 2 && scale.dim() == 2 &&
+           q.size(0) == rows && q.size(1) == pitch && scale.size(0) == (rows + block_rows - 1) / block_rows && scale.size(1) == (pitch + 127) / 128;
+}
+
+int32_t code_of(at::ScalarType t)
+{
+    return t == at::kHalf ? VPTQ_DTYPE_FP16 : t == at::kBFloat16 ? VPTQ_DTYPE_BF16 : t == at::kFloat ? VPTQ_DTYPE_FP32 : t == at::kFloat8_e4m3fn ? VPTQ_DTYPE_E4M3 : -1;
+}
+
+constexpr int64_t MAX_INT = 0x7FFFFFFF;
+
+// fp8_quantize(x, block_rows) -> (q, scale)
+PyObject *py_fp8_quantize(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (n != 2) { PyErr_SetString(PyExc_TypeError, "fp8_quantize takes 2 arguments"); return nullptr; }
+    const at::Tensor *x = tensor_of(a[0]);
+    const long block_rows = x ? PyLong_AsLong(a[1]) : -1;
+    if (!x || (block_rows == -1 && PyErr_Occurred())) return nullptr;
+    if (block_rows != 1 && block_rows != 128) return fail(VPTQ_E_SHAPE);
+    if (!on_current_device(*x)) return assertion("a CUDA tensor of the current device");
+    if (x->dim() != 2 || x->size(1) < 1 || x->size(0) > MAX_INT || x->size(1) > MAX_INT) return assertion("x [rows][cols]");
+    const int64_t rows = x->size(0), cols = x->size(1), ld = rows > 1 ? x->stride(0) : cols;
+    if ((cols > 1 && x->stride(1) != 1) || ld < cols) return assertion("a row's columns next to each other, rows apart");
+    return guarded([&]() -> PyObject * {
+        const Fp8Tensors r = empty_fp8(rows, cols, block_rows, x->options());
+        int rc;
+        Py_BEGIN_ALLOW_THREADS
+        rc = vptq_fp8_quantize(x->data_ptr(), code_of(x->scalar_type()), (int32_t)rows, (int32_t)cols, ld, (int32_t)block_rows,
+                               static_cast<uint8_t *>(r.q.data_ptr()), static_cast<float *>(r.scale.data_ptr()), current_stream());
+        Py_END_ALLOW_THREADS
+        return rc != VPTQ_OK ? fail(rc) : pair_of(r.q, r.scale);
+    });
+}
+
+// dequant_fp8(desc, ptrs, workspace or None) -> (q, scale)
+PyObject *py_dequant_fp8(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (n != 3) { PyErr_SetString(PyExc_TypeError, "dequant_fp8 takes 3 arguments"); return nullptr; }
+    const vptq_layer_desc *d = struct_of<vptq_layer_desc>(a[0]);
+    const vptq_layer_ptrs *p = d ? struct_of<vptq_layer_ptrs>(a[1]) : nullptr;
+    void *ws = nullptr;
+    size_t ws_bytes = 0;
+    if (!p || !workspace_of(a[2], &ws, &ws_bytes)) return nullptr;
+    const int64_t need = vptq_dequant_fp8_workspace_bytes(d);
+    if (need < 0) return fail((int)need);
+    return guarded([&]() -> PyObject * {
+        const at::TensorOptions options = at::TensorOptions().device(at::kCUDA, c10::cuda::current_device());
+        const Fp8Tensors r = empty_fp8(d->M, d->N, 128, options);
+        at::Tensor own;
+        if (need > 0 && ws == nullptr) {
+            own = at::empty({need}, options.dtype(at::kByte));
+            ws = own.data_ptr();
+            ws_bytes = (size_t)need;
+        }
+        int rc;
+        Py_BEGIN_ALLOW_THREADS
+        rc = vptq_dequant_fp8(d, p, static_cast<uint8_t *>(r.q.data_ptr()), static_cast<float *>(r.scale.data_ptr()), ws, ws_bytes, current_stream());
+        Py_END_ALLOW_THREADS
+        return rc != VPTQ_OK ? fail(rc) : pair_of(r.q, r.scale);
+    });
+}
+
+// linear_fp8(x, w, w_scale, x_scale or None, out dtype or None, out or None, workspace or None) -> out
+PyObject *py_linear_fp8(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (n != 7) { PyErr_SetString(PyExc_TypeError, "linear_fp8 takes 7 arguments"); return nullptr; }
+    const at::Tensor *x = tensor_of(a[0]), *w = x ? tensor_of(a[1]) : nullptr, *ws_t = w ? tensor_of(a[2]) : nullptr;
+    const at::Tensor *xs = nullptr, *out = nullptr;
+    if (!ws_t || (a[3] != Py_None && !(xs = tensor_of(a[3]))) || (a[5] != Py_None && !(out = tensor_of(a[5])))) return nullptr;
+    vptq_fp8_desc d = {};
+    d.x_dtype = code_of(x->scalar_type());
+    const bool e4m3 = d.x_dtype == VPTQ_DTYPE_E4M3;
+    if (x->dim() != 2 || w->dim() != 2 || !plain(*x) || x->size(0) > MAX_INT || x->size(1) > MAX_INT || w->size(0) > MAX_INT)
+        return assertion("x [B][N] and w [M][pitch], contiguous tensors of the current device");
+    const int64_t B = x->size(0), N = x->size(1), M = w->size(0);
+    if (!is_fp8(*w, *ws_t, M, (N + 15) / 16 * 16, 128)) return assertion("w e4m3 [M][N rounded up to 16] with FP32 scales [ceil(M / 128)][ceil(N / 128)]");
+    if (e4m3 != (xs != nullptr)) return assertion("x_scale comes with e4m3 activations, and with no others");
+    if (e4m3 && !is_fp8(*x, *xs, B, (N + 15) / 16 * 16, 1)) return assertion("x e4m3 [B][pitch] with FP32 scales [B][ceil(N / 128)]");
+    d.M = (int32_t)M; d.N = (int32_t)N;
+    if (a[4] != Py_None) {
+        d.out_dtype = (int32_t)PyLong_AsLong(a[4]);
+        if (PyErr_Occurred()) return nullptr;
+    } else {
+        d.out_dtype = out ? code_of(out->scalar_type()) : e4m3 ? VPTQ_DTYPE_BF16 : d.x_dtype;
+    }
+    if (out && (!plain(*out) || out->dim() != 2 || out->size(0) != B || out->size(1) != M || code_of(out->scalar_type()) != d.out_dtype))
+        return assertion("out [B][M], contiguous, of the type asked for");
+    void *ws;
+    size_t ws_bytes;
+    if (!workspace_of(a[6], &ws, &ws_bytes)) return nullptr;
+    const int64_t need = vptq_linear_fp8_workspace_bytes(&d, (int32_t)B);
+    if (need < 0) return fail((int)need);
+    return guarded([&]() -> PyObject * {
+        at::Tensor own, result = out ? *out : at::empty({B, M}, x->options().dtype(dtype_of(d.out_dtype)));
+        if (need > 0 && ws == nullptr) {
+            own = at::empty({need}, x->options().dtype(at::kByte));
+            ws = own.data_ptr();
+            ws_bytes = (size_t)need;
+        }
+        int rc;
+        Py_BEGIN_ALLOW_THREADS
+        rc = vptq_linear_fp8(&d, x->data_ptr(), xs ? static_cast<const float *>(xs->data_ptr()) : nullptr, (int32_t)B,
+                             static_cast<const uint8_t *>(w->data_ptr()), static_cast<const float *>(ws_t->data_ptr()), result.data_ptr(), ws, ws_bytes,
+                             current_stream());
+        Py_END_ALLOW_THREADS
+        if (rc != VPTQ_OK) return fail(rc);
+        if (out) { Py_INCREF(a[5]); return a[5]; }
+        return THPVariable_Wrap(result);
+    });
+}
+
 PyObject *py_set_error_class(PyObject *, PyObject *cls)
 {
     Py_INCREF(cls);
@@ -219,6 +369,9 @@ PyMethodDef methods[] = {
     {"dequant", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_dequant)), METH_FASTCALL, "vptq_dequant on torch tensors"},
     {"layer_linear", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_layer_linear)), METH_FASTCALL, "DeviceLayer.linear"},
     {"fused_linear", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_fused_linear)), METH_FASTCALL, "FusedLayers.linear"},
+    {"fp8_quantize", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_fp8_quantize)), METH_FASTCALL, "vptq_fp8_quantize on torch tensors"},
+    {"dequant_fp8", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_dequant_fp8)), METH_FASTCALL, "vptq_dequant_fp8 on torch tensors"},
+    {"linear_fp8", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_linear_fp8)), METH_FASTCALL, "vptq_linear_fp8 on torch tensors"},
     {"set_error_class", py_set_error_class, METH_O, "exception raised for VPTQ_E_* codes"},
     {nullptr, nullptr, 0, nullptr}};
 

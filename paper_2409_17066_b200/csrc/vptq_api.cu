@@ -9,6 +9,7 @@
 #include "paths.cuh"
 #include "assign.cuh"
 #include "prepared.cuh"
+#include "fp8.cuh"
 
 #include <vector>
 
@@ -537,6 +538,103 @@ int vptq_linear_fused_host_io(const vptq_layer_desc *descs, const vptq_layer_ptr
         if (e != cudaSuccess) return cuda_fail(e);
     }
     return VPTQ_OK;
+}
+
+int64_t vptq_fp8_row_bytes(int32_t n_cols)
+{
+    if (n_cols < 0) return VPTQ_E_SHAPE;
+    return fp8_row_bytes(n_cols);
+}
+
+int vptq_fp8_quantize(const void *x, int32_t x_dtype, int32_t n_rows, int32_t n_cols, int64_t ld, int32_t block_rows,
+                      uint8_t *q, float *scale, void *stream)
+{
+    if (n_rows < 0 || n_cols <= 0 || n_cols > FP8_MAX_SIZE || ld < n_cols || (block_rows != 1 && block_rows != FP8_BLOCK)) return VPTQ_E_SHAPE;
+    if (x_dtype != VPTQ_DTYPE_FP16 && x_dtype != VPTQ_DTYPE_BF16 && x_dtype != VPTQ_DTYPE_FP32) return VPTQ_E_UNSUPPORTED;
+    if (n_rows == 0) return VPTQ_OK;
+    if (x == nullptr || q == nullptr || scale == nullptr) return VPTQ_E_NULL;
+    if (!aligned16(q) || !aligned16(scale) || (reinterpret_cast<uintptr_t>(x) & (x_dtype == VPTQ_DTYPE_FP32 ? 3u : 1u))) return VPTQ_E_ALIGN;
+    const cudaError_t e = launch_fp8_quantize(x, x_dtype, n_rows, n_cols, ld, block_rows, q, scale, nullptr, false,
+                                              reinterpret_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? VPTQ_OK : cuda_fail(e);
+}
+
+int64_t vptq_dequant_fp8_workspace_bytes(const vptq_layer_desc *desc)
+{
+    const int rc = check_desc(desc);
+    if (rc != VPTQ_OK) return rc;
+    return (desc->flags & VPTQ_FLAG_COL_PERM) ? (4ll * desc->N + 255) / 256 * 256 : 0;
+}
+
+int vptq_dequant_fp8(const vptq_layer_desc *desc, const vptq_layer_ptrs *p, uint8_t *q, float *scale,
+                     void *workspace, size_t workspace_bytes, void *stream)
+{
+    int rc = check_desc(desc);
+    if (rc != VPTQ_OK) return rc;
+    rc = check_ptrs(desc, p);
+    if (rc != VPTQ_OK) return rc;
+    if (desc->M > FP8_MAX_SIZE || desc->N > FP8_MAX_SIZE) return VPTQ_E_SHAPE;
+    if (q == nullptr || scale == nullptr) return VPTQ_E_NULL;
+    if (!aligned16(q) || !aligned16(scale)) return VPTQ_E_ALIGN;
+    const int64_t need = vptq_dequant_fp8_workspace_bytes(desc);
+    if (need > 0) {
+        if (workspace == nullptr || (int64_t)workspace_bytes < need) return VPTQ_E_WORKSPACE;
+        if ((reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return VPTQ_E_ALIGN;
+    }
+    const LayerView L = make_view(desc, p);
+    const cudaError_t e = launch_dequant_fp8(L, q, scale, reinterpret_cast<int *>(workspace), reinterpret_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? VPTQ_OK : cuda_fail(e);
+}
+
+static int check_fp8_desc(const vptq_fp8_desc *d, int32_t B)
+{
+    if (d == nullptr) return VPTQ_E_NULL;
+    if (d->M <= 0 || d->N <= 0 || B <= 0 || d->M > FP8_MAX_SIZE || d->N > FP8_MAX_SIZE || B > FP8_MAX_SIZE) return VPTQ_E_SHAPE;
+    if (d->x_dtype != VPTQ_DTYPE_E4M3 && d->x_dtype != VPTQ_DTYPE_FP16 && d->x_dtype != VPTQ_DTYPE_BF16) return VPTQ_E_UNSUPPORTED;
+    if (d->out_dtype != VPTQ_DTYPE_FP16 && d->out_dtype != VPTQ_DTYPE_BF16 && d->out_dtype != VPTQ_DTYPE_FP32) return VPTQ_E_UNSUPPORTED;
+    if (d->flags & ~(VPTQ_FLAG_CONCURRENT | VPTQ_FLAG_DETERMINISTIC)) return VPTQ_E_UNSUPPORTED;
+    return VPTQ_OK;
+}
+
+int64_t vptq_linear_fp8_workspace_bytes(const vptq_fp8_desc *desc, int32_t B)
+{
+    const int rc = check_fp8_desc(desc, B);
+    if (rc != VPTQ_OK) return rc;
+    return linear_fp8_workspace_bytes(desc->M, desc->N, B, desc->x_dtype);
+}
+
+int vptq_linear_fp8(const vptq_fp8_desc *desc, const void *x, const float *x_scale, int32_t B,
+                    const uint8_t *w, const float *w_scale, void *out,
+                    void *workspace, size_t workspace_bytes, void *stream)
+{
+    const int rc = check_fp8_desc(desc, B);
+    if (rc != VPTQ_OK) return rc;
+    const bool e4m3 = desc->x_dtype == VPTQ_DTYPE_E4M3;
+    if (x == nullptr || w == nullptr || w_scale == nullptr || out == nullptr || (e4m3 && x_scale == nullptr)) return VPTQ_E_NULL;
+    if (!aligned16(x) || !aligned16(w) || !aligned16(w_scale) || !aligned16(out) || (e4m3 && !aligned16(x_scale))) return VPTQ_E_ALIGN;
+    const long long need = linear_fp8_workspace_bytes(desc->M, desc->N, B, desc->x_dtype);
+    if (need > 0) {
+        if (workspace == nullptr || (long long)workspace_bytes < need) return VPTQ_E_WORKSPACE;
+        if ((reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return VPTQ_E_ALIGN;
+    }
+    Fp8Linear P;
+    P.M = desc->M; P.N = desc->N; P.B = B; P.x_dtype = desc->x_dtype; P.out_dtype = desc->out_dtype;
+    P.x = x; P.x_scale = e4m3 ? x_scale : nullptr; P.w = w; P.w_scale = w_scale; P.out = out;
+    const cudaError_t e = launch_linear_fp8(P, workspace, reinterpret_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? VPTQ_OK : cuda_fail(e);
+}
+
+const char *vptq_linear_fp8_path(const vptq_fp8_desc *desc, int32_t B)
+{
+    if (check_fp8_desc(desc, B) != VPTQ_OK) return "invalid";
+    return linear_fp8_path(desc->M, desc->N, B, desc->x_dtype);
+}
+
+int vptq_linear_fp8_launches(const vptq_fp8_desc *desc, int32_t B)
+{
+    const int rc = check_fp8_desc(desc, B);
+    if (rc != VPTQ_OK) return rc;
+    return linear_fp8_launches(desc->M, desc->N, B, desc->x_dtype);
 }
 
 const char *vptq_status_string(int code)
