@@ -13,10 +13,10 @@ constexpr float FP8_AMAX_MIN = 7.888609052210118e-31f;    // 2^-100: a block's l
 inline long long fp8_row_bytes(long long cols) { return (cols + 15) / 16 * 16; }
 
 // activations (or results) of `rows` rows to e4m3 with a scale per 128 columns of a row (block_rows = 1) or per 128 x 128 values
-// (block_rows = 128); ld = distance of x's rows in values; `status` (may be null) is cleared.  `early`: the kernel behind this one
-// on the stream waits for it by itself before it touches q or scale.
+// (block_rows = 128); ld = distance of x's rows in values.  `early`: the kernel behind this one on the stream waits for it by itself
+// before it touches q or scale.
 cudaError_t launch_fp8_quantize(const void *x, int x_dtype, int rows, int cols, long long ld, int block_rows, uint8_t *q, float *scale,
-                                int *status, bool early, cudaStream_t st);
+                                bool early, cudaStream_t st);
 
 // a vector-quantized layer to e4m3 with 128 x 128 blocks; inverse: null or N words of scratch (a stored column order needs them)
 cudaError_t launch_dequant_fp8(const LayerView &L, uint8_t *q, float *scale, int *inverse, cudaStream_t st);
@@ -34,9 +34,9 @@ struct Fp8Linear {
 constexpr int FP8_DECODE_MAX_B = 16;
 cudaError_t launch_linear_fp8_decode(const Fp8Linear &P, cudaStream_t st);
 
-long long linear_fp8_workspace_bytes(int M, int N, int B, int x_dtype);
-int linear_fp8_launches(int M, int N, int B, int x_dtype);
-const char *linear_fp8_path(int M, int N, int B, int x_dtype);
+long long linear_fp8_workspace_bytes(int N, int B, int x_dtype);
+int linear_fp8_launches(int B, int x_dtype);
+const char *linear_fp8_path(int B);
 cudaError_t launch_linear_fp8(const Fp8Linear &P, void *ws, cudaStream_t st);
 
 #ifdef __CUDACC__

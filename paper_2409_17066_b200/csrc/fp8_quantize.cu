@@ -22,7 +22,6 @@ struct QuantizeParams {
     int col_blocks;
     uint8_t *q;
     float *scale;
-    int *status;
     int early;
 };
 
@@ -48,7 +47,6 @@ quantize_rows_kernel(const __grid_constant__ QuantizeParams P)
 {
     if (P.early) pdl_launch_dependents();
     pdl_wait();
-    if (P.status != nullptr && blockIdx.x == 0 && threadIdx.x == 0) *P.status = 0;
     const long long n = (long long)P.rows * P.col_blocks;
     const int lane = threadIdx.x & 15;
     const long long first = ((long long)blockIdx.x * THREADS + threadIdx.x) >> 4, step = ((long long)gridDim.x * THREADS) >> 4;
@@ -145,12 +143,12 @@ cudaError_t launch(const QuantizeParams &P, int block_rows, cudaStream_t st)
 }  // namespace
 
 cudaError_t launch_fp8_quantize(const void *x, int x_dtype, int rows, int cols, long long ld, int block_rows, uint8_t *q, float *scale,
-                                int *status, bool early, cudaStream_t st)
+                                bool early, cudaStream_t st)
 {
     QuantizeParams P;
     P.x = x; P.rows = rows; P.cols = cols; P.ld = ld; P.pitch = fp8_row_bytes(cols);
     P.col_blocks = ceil_div(cols, FP8_BLOCK);
-    P.q = q; P.scale = scale; P.status = status; P.early = early ? 1 : 0;
+    P.q = q; P.scale = scale; P.early = early ? 1 : 0;
     const int bytes = x_dtype == VPTQ_DTYPE_FP32 ? 4 : 2, per = 16 / bytes;
     const bool vec = (reinterpret_cast<uintptr_t>(x) & 15u) == 0 && cols % per == 0 && (rows == 1 || ld % per == 0);
     switch (x_dtype) {

@@ -1,25 +1,44 @@
 // vptq_linear_fp8: which kernels a call takes.
 #include "fp8.cuh"
+#include "fp8_tcgen05.cuh"
 
 namespace vptq {
 
-long long linear_fp8_workspace_bytes(int M, int N, int B, int x_dtype) { return 0; }
-int linear_fp8_launches(int M, int N, int B, int x_dtype) { return ceil_div(B, FP8_DECODE_MAX_B); }
-const char *linear_fp8_path(int M, int N, int B, int x_dtype) { return "fp8_decode"; }
+namespace {
+
+bool decodes(int B) { return B <= FP8_DECODE_MAX_B; }
+
+// workspace of the tensor-core kernel: the status word, then (16-bit activations) the activations' scales and e4m3 values
+struct Workspace { long long scales, values, bytes; };
+Workspace workspace_of(int N, int B, int x_dtype)
+{
+    Workspace w = {256, 256, 256};
+    if (x_dtype != VPTQ_DTYPE_E4M3) {
+        w.values = w.scales + (4ll * B * ceil_div(N, FP8_BLOCK) + 255) / 256 * 256;
+        w.bytes = w.values + B * fp8_row_bytes(N);
+    }
+    return w;
+}
+
+}  // namespace
+
+long long linear_fp8_workspace_bytes(int N, int B, int x_dtype) { return decodes(B) ? 0 : workspace_of(N, B, x_dtype).bytes; }
+int linear_fp8_launches(int B, int x_dtype) { return decodes(B) || x_dtype == VPTQ_DTYPE_E4M3 ? 1 : 2; }
+const char *linear_fp8_path(int B) { return decodes(B) ? "fp8_decode" : "fp8_tcgen05"; }
 
 cudaError_t launch_linear_fp8(const Fp8Linear &P, void *ws, cudaStream_t st)
 {
-    const long long x_row = P.x_dtype == VPTQ_DTYPE_E4M3 ? fp8_row_bytes(P.N) : 2ll * P.N, out_row = (P.out_dtype == VPTQ_DTYPE_FP32 ? 4ll : 2ll) * P.M;
-    for (int b = 0; b < P.B; b += FP8_DECODE_MAX_B) {
-        Fp8Linear Q = P;
-        Q.B = P.B - b < FP8_DECODE_MAX_B ? P.B - b : FP8_DECODE_MAX_B;
-        Q.x = reinterpret_cast<const uint8_t *>(P.x) + b * x_row;
-        if (P.x_scale != nullptr) Q.x_scale = P.x_scale + (long long)b * ceil_div(P.N, FP8_BLOCK);
-        Q.out = reinterpret_cast<uint8_t *>(P.out) + b * out_row;
-        const cudaError_t e = launch_linear_fp8_decode(Q, st);
+    if (decodes(P.B)) return launch_linear_fp8_decode(P, st);
+    uint8_t *w8 = reinterpret_cast<uint8_t *>(ws);
+    Fp8Linear Q = P;
+    if (P.x_dtype != VPTQ_DTYPE_E4M3) {
+        const Workspace w = workspace_of(P.N, P.B, P.x_dtype);
+        const cudaError_t e = launch_fp8_quantize(P.x, P.x_dtype, P.B, P.N, P.N, 1, w8 + w.values, reinterpret_cast<float *>(w8 + w.scales), true, st);
         if (e != cudaSuccess) return e;
+        Q.x = w8 + w.values;
+        Q.x_scale = reinterpret_cast<const float *>(w8 + w.scales);
     }
-    return cudaSuccess;
+    return launch_linear_fp8_tcgen05(Q, reinterpret_cast<int *>(ws), st);
 }
 
 }  // namespace vptq

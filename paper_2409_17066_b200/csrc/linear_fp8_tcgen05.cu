@@ -1,0 +1,494 @@
+// out = x W^T for more than 16 tokens over an e4m3 weight with 128 x 128 block scales, on the tensor cores.
+//
+// D[token][feature] per block of 128 columns is one group of four tcgen05.mma (kind::f8f6f4, 128 tokens x TN features x 32 columns
+// each) into a TMEM buffer of its own; the block's two scales differ from the next block's, so the sum over blocks is formed in
+// registers: acc += D * (x_scale[token][block] * w_scale[feature block][block]).  A TMEM lane is a token: its scale is one register of
+// the lane, the weight's is the same for 128 columns, and the update is one packed fma per two values.
+//
+// Warps by role: 0 loads (TMA, 128-byte swizzle, zeros beyond the matrices' edges), 1 issues the MMAs, 2..9 read the buffers and hold
+// the sums (two warps per lane quarter, the features shared between them).  Two TMEM buffers: one fills while the other is read.
+// CTAs are persistent over tiles, tokens fastest, so that those that run together share weight tiles in L2.
+// Few tiles: SPLIT CTAs of a cluster share a tile's columns, leave their sums in shared memory, and each adds up its share of the
+// tile's rows in rank order: one launch, no scratch, and a result that does not depend on timing.
+// Every wait is bounded; one that gives up sets the status word of the workspace.
+#include "fp8.cuh"
+#include "fp8_tcgen05.cuh"
+#include "tcgen05_ptx.cuh"
+
+#include <cuda.h>
+
+namespace vptq {
+
+namespace {
+
+using namespace tc;
+
+constexpr int TM = 128;                                   // tokens of a tile
+constexpr int ACC_WARP0 = 2, ACC_WARPS = 8;
+constexpr int THREADS = 32 * (ACC_WARP0 + ACC_WARPS);
+constexpr int X_BYTES = TM * FP8_BLOCK;                   // a stage's activations
+constexpr int STAGING = 4096;                             // per accumulating warp: 32 rows x 32 columns on their way out
+constexpr int SMEM_MAX = 232448 - 1024;                  // (the static part takes a multiple of the dynamic part's alignment)
+constexpr int BARRIERS = 256;
+
+template <int TN> constexpr int stage_bytes() { return X_BYTES + TN * FP8_BLOCK; }
+template <int TN> constexpr int stages()
+{
+    const int n = (SMEM_MAX - BARRIERS - ACC_WARPS * STAGING) / stage_bytes<TN>();
+    return n < 8 ? n : 8;
+}
+template <int TN> constexpr int smem_bytes() { return stages<TN>() * stage_bytes<TN>() + ACC_WARPS * STAGING + BARRIERS; }
+// features of the first of the two warps of a lane quarter (the second has the rest)
+template <int TN> constexpr int first_share() { return (TN / 2 + 31) / 32 * 32; }
+
+struct Params {
+    int M, B, kbs;
+    int tiles_t, tiles;
+    const float *x_scale, *w_scale;
+    void *out;
+    int out_dtype;
+    int tma_out;           // rows of `out` are 16-byte aligned: stored by TMA
+    int *status;
+};
+
+__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void tma_store(const CUtensorMap *map, uint32_t src, int x, int y)
+{
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];"
+                 ::"l"(map), "r"(src), "r"(x), "r"(y) : "memory");
+}
+__device__ __forceinline__ void mma_f8(uint32_t d_tmem, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(d_tmem), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+// 16 consecutive FP32 accumulator columns of this lane's row: started here, read after tmem_wait16 of the same registers
+__device__ __forceinline__ void tmem_start16(uint32_t taddr, uint32_t (&r)[16])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+                   "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                 : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_wait16(uint32_t (&r)[16])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
+                   "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
+                 :: "memory");
+}
+__device__ __forceinline__ uint64_t pack2(uint32_t lo, uint32_t hi)
+{
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(lo), "r"(hi));
+    return r;
+}
+__device__ __forceinline__ float2 unpack2(uint64_t v)
+{
+    uint32_t lo, hi;
+    asm("mov.b64 {%0, %1}, %2;" : "=r"(lo), "=r"(hi) : "l"(v));
+    return make_float2(__uint_as_float(lo), __uint_as_float(hi));
+}
+__device__ __forceinline__ void fma2(uint64_t &acc, uint64_t a, uint64_t b) { asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(acc) : "l"(a), "l"(b)); }
+
+__device__ __forceinline__ uint32_t cluster_rank()
+{
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ float4 load_peer(uint32_t addr, uint32_t rank)
+{
+    uint32_t at;
+    float4 v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(addr), "r"(rank));
+    asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint32_t pair16(float a, float b, int dtype)
+{
+    if (dtype == VPTQ_DTYPE_FP16) {
+        const __half2 h = __floats2half2_rn(a, b);
+        return *reinterpret_cast<const uint32_t *>(&h);
+    }
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+
+template <int TN, int SPLIT>
+__global__ void __launch_bounds__(THREADS, 1)
+linear_fp8_tcgen05_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_out,
+                          const __grid_constant__ Params P)
+{
+    constexpr int ST = stages<TN>(), SB = stage_bytes<TN>();
+    constexpr int C0 = first_share<TN>(), C1 = TN - C0;
+    extern __shared__ __align__(1024) uint8_t sm[];
+    __shared__ uint32_t tmem_slot;
+    const uint32_t base = smem_addr(sm), staging0 = base + ST * SB, bars = staging0 + ACC_WARPS * STAGING;
+    auto bar_full = [&](int s) { return bars + 8u * s; };
+    auto bar_empty = [&](int s) { return bars + 8u * (ST + s); };
+    auto bar_acc_full = [&](int b) { return bars + 8u * (2 * ST + b); };
+    auto bar_acc_empty = [&](int b) { return bars + 8u * (2 * ST + 2 + b); };
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < ST; s++) { mbar_init(bar_full(s), 1); mbar_init(bar_empty(s), 1); }
+        for (int b = 0; b < 2; b++) { mbar_init(bar_acc_full(b), 1); mbar_init(bar_acc_empty(b), ACC_WARPS); }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&tmem_slot)), "r"(512) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_slot;
+    pdl_launch_dependents();
+
+    // this CTA's tiles and columns
+    const int rank = SPLIT > 1 ? (int)cluster_rank() : 0;
+    const int first = SPLIT > 1 ? (int)blockIdx.x / SPLIT : (int)blockIdx.x;
+    const int step = SPLIT > 1 ? P.tiles : (int)gridDim.x;
+    const int kb0 = SPLIT > 1 ? (int)((long long)P.kbs * rank / SPLIT) : 0, kb1 = SPLIT > 1 ? (int)((long long)P.kbs * (rank + 1) / SPLIT) : P.kbs;
+    uint32_t gave_up = 0;
+
+    if (warp == 0) {
+        // ---- loads ----
+        uint32_t it = 0;
+        // the first stages' weights are no one's output: they may come in while the preceding kernel still runs
+        uint32_t early = 0;
+        if (first < P.tiles)
+            for (int kb = kb0; kb < kb1 && early < ST; kb++, early++)
+                if (elect_one()) {
+                    mbar_expect_tx(bar_full(early), SB);
+                    tma_load(base + early * SB + X_BYTES, &map_w, kb * FP8_BLOCK, first / P.tiles_t * TN, bar_full(early));
+                }
+        pdl_wait();
+        for (int tile = first; tile < P.tiles; tile += step) {
+            const int t0 = tile % P.tiles_t * TM, n0 = tile / P.tiles_t * TN;
+            for (int kb = kb0; kb < kb1; kb++, it++) {
+                const uint32_t s = it % ST;
+                if (it >= early) mbar_wait_uniform(bar_empty(s), ((it / ST) & 1) ^ 1u, gave_up);
+                if (gave_up) break;
+                if (elect_one()) {
+                    if (it >= early) {
+                        mbar_expect_tx(bar_full(s), SB);
+                        tma_load(base + s * SB + X_BYTES, &map_w, kb * FP8_BLOCK, n0, bar_full(s));
+                    }
+                    tma_load(base + s * SB, &map_x, kb * FP8_BLOCK, t0, bar_full(s));
+                }
+                __syncwarp();
+            }
+            if (gave_up) break;
+        }
+        // copies still in flight (only after a wait that ran out) get a bounded time to land before the CTA exits
+        if (gave_up)
+            for (uint32_t j = it > ST ? it - ST : 0; j < it; j++) {
+                const long long c0 = clock64();
+                while (!mbar_try(bar_full(j % ST), (j / ST) & 1) && clock64() - c0 < 20000000ll) {}
+            }
+    } else if (warp == 1) {
+        // ---- MMAs ----
+        constexpr uint32_t IDESC = (1u << 4) | ((uint32_t)(TN >> 3) << 17) | ((uint32_t)(TM >> 4) << 24);      // e4m3 x e4m3 -> FP32, both K-major
+        const uint64_t a0 = make_smem_desc(base, 16, 1024, LAYOUT_SW128), b0 = make_smem_desc(base + X_BYTES, 16, 1024, LAYOUT_SW128);
+        uint32_t it = 0;
+        for (int tile = first; tile < P.tiles; tile += step)
+            for (int kb = kb0; kb < kb1; kb++, it++) {
+                const uint32_t s = it % ST, buf = it & 1;
+                mbar_wait_uniform(bar_acc_empty(buf), ((it >> 1) & 1) ^ 1u, gave_up);
+                mbar_wait_uniform(bar_full(s), (it / ST) & 1, gave_up);
+                tc_fence_after();
+                if (elect_one()) {
+                    const uint64_t at = (uint64_t)((s * SB) >> 4);
+#pragma unroll
+                    for (int k = 0; k < FP8_BLOCK / 32; k++) mma_f8(tmem + buf * 256, a0 + at + 2 * k, b0 + at + 2 * k, IDESC, k > 0);
+                    umma_commit(bar_empty(s));
+                    umma_commit(bar_acc_full(buf));
+                }
+                __syncwarp();
+            }
+    } else {
+        // ---- sums ----
+        const int w = warp - ACC_WARP0, q = warp & 3, share = w >> 2;          // TMEM lane quarter this warp may read, its part of the features
+        const int c_first = share ? C0 : 0, c_count = share ? C1 : C0;
+        const uint32_t taddr = tmem + ((uint32_t)(32 * q) << 16) + c_first;
+        const uint32_t staging = staging0 + w * STAGING;
+        uint8_t *staging_p = sm + ST * SB + w * STAGING;
+        pdl_wait();                                                            // the activations' scales may be the preceding kernel's
+        if (blockIdx.x == 0 && threadIdx.x == 32 * ACC_WARP0) *P.status = 0;
+        uint32_t it = 0, pieces = 0;
+        for (int tile = first; tile < P.tiles; tile += step) {
+            const int t0 = tile % P.tiles_t * TM, n0 = tile / P.tiles_t * TN;
+            const int token = t0 + 32 * q + lane;
+            const float *xs = P.x_scale + (long long)min(token, P.B - 1) * P.kbs;
+            // 128-row blocks of the weight that the features lie in: one, or two from feature `second` on
+            const int nb = (n0 + c_first) / FP8_BLOCK, nb_last = (P.M - 1) / FP8_BLOCK;
+            const int second = FP8_BLOCK - (n0 + c_first) % FP8_BLOCK;
+            const float *ws0 = P.w_scale + (long long)min(nb, nb_last) * P.kbs, *ws1 = P.w_scale + (long long)min(nb + 1, nb_last) * P.kbs;
+            uint64_t acc[C0 / 2];
+#pragma unroll
+            for (int i = 0; i < C0 / 2; i++) acc[i] = 0;
+            float x_next = kb0 < kb1 ? __ldg(xs + kb0) : 0.f, w0_next = kb0 < kb1 ? __ldg(ws0 + kb0) : 0.f, w1_next = kb0 < kb1 ? __ldg(ws1 + kb0) : 0.f;
+            for (int kb = kb0; kb < kb1; kb++, it++) {
+                const uint32_t buf = it & 1;
+                const float s0 = x_next * w0_next, s1 = x_next * w1_next;
+                if (kb + 1 < kb1) { x_next = __ldg(xs + kb + 1); w0_next = __ldg(ws0 + kb + 1); w1_next = __ldg(ws1 + kb + 1); }
+                mbar_wait_uniform(bar_acc_full(buf), (it >> 1) & 1, gave_up);
+                tc_fence_after();
+                uint32_t d[2][16];
+                tmem_start16(taddr + buf * 256, d[0]);
+#pragma unroll
+                for (int j = 0; j < C0 / 16; j++) {
+                    if (16 * j < c_count) {
+                        tmem_wait16(d[j & 1]);
+                        if (16 * (j + 1) < C0 && 16 * (j + 1) < c_count) tmem_start16(taddr + buf * 256 + 16 * (j + 1), d[(j + 1) & 1]);
+                        else {
+                            // everything read: the buffer is the MMA warp's again
+                            tc_fence_before();
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive(bar_acc_empty(buf));
+                        }
+                        const float sf = 16 * j < second ? s0 : s1;
+                        const uint64_t ss = pack2(__float_as_uint(sf), __float_as_uint(sf));
+#pragma unroll
+                        for (int i = 0; i < 8; i++) fma2(acc[8 * j + i], pack2(d[j & 1][2 * i], d[j & 1][2 * i + 1]), ss);
+                    }
+                }
+            }
+            if constexpr (SPLIT > 1) {
+                // the tile's sums over this CTA's columns: [128][TN] FP32 where the stages were (all of them have been read), 16-byte
+                // pieces of a row exchanged so that the lanes of a quarter warp write different banks
+#pragma unroll
+                for (int j = 0; j < C0 / 4; j++)
+                    if (4 * j < c_count) {
+                        const float2 a = unpack2(acc[2 * j]), b = unpack2(acc[2 * j + 1]);
+                        const int row = 32 * q + lane, piece = (c_first / 4 + j) ^ (lane & 7);
+                        *reinterpret_cast<float4 *>(sm + (row * TN + 4 * piece) * 4) = make_float4(a.x, a.y, b.x, b.y);
+                    }
+            } else {
+                // 32 features at a time through the warp's staging rows (64 or 128 bytes, swizzled as the store's map says)
+                const bool wide = P.out_dtype == VPTQ_DTYPE_FP32;
+#pragma unroll
+                for (int j = 0; j < C0 / 32; j++) {
+                    if (32 * j >= c_count) continue;
+                    // (16-bit pieces take turns at two halves of the staging; every piece is a group of its own, stored or not)
+                    const uint32_t at = wide ? 0u : (pieces++ & 1) * (STAGING / 2);
+                    if (P.tma_out && lane == 0) {
+                        if (wide) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                        else asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+                    }
+                    __syncwarp();
+                    if (wide) {
+#pragma unroll
+                        for (int c = 0; c < 8; c++) {
+                            const float2 a = unpack2(acc[16 * j + 2 * c]), b = unpack2(acc[16 * j + 2 * c + 1]);
+                            *reinterpret_cast<float4 *>(staging_p + lane * 128 + ((c ^ (lane & 7)) << 4)) = make_float4(a.x, a.y, b.x, b.y);
+                        }
+                    } else {
+#pragma unroll
+                        for (int c = 0; c < 4; c++) {
+                            uint32_t h[4];
+#pragma unroll
+                            for (int i = 0; i < 4; i++) {
+                                const float2 a = unpack2(acc[16 * j + 4 * c + i]);
+                                h[i] = pair16(a.x, a.y, P.out_dtype);
+                            }
+                            *reinterpret_cast<uint4 *>(staging_p + at + lane * 64 + ((c ^ ((lane >> 1) & 3)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
+                        }
+                    }
+                    const int col = n0 + c_first + 32 * j;
+                    if (P.tma_out) {
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                        __syncwarp();
+                        if (lane == 0) {
+                            if (col < P.M && t0 + 32 * q < P.B) tma_store(&map_out, staging + at, col, t0 + 32 * q);
+                            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                        }
+                    } else {
+                        __syncwarp();
+                        for (int r = 0; r < 32 && t0 + 32 * q + r < P.B; r++) {
+                            if (col + lane >= P.M) break;
+                            const long long o = (long long)(t0 + 32 * q + r) * P.M + col + lane;
+                            if (wide) reinterpret_cast<float *>(P.out)[o] = *reinterpret_cast<const float *>(staging_p + r * 128 + (((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4);
+                            else reinterpret_cast<uint16_t *>(P.out)[o] = *reinterpret_cast<const uint16_t *>(staging_p + at + r * 64 + (((lane >> 3) ^ ((r >> 1) & 3)) << 4) + (lane & 7) * 2);
+                        }
+                        __syncwarp();
+                    }
+                }
+            }
+        }
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+    }
+    if (__any_sync(0xffffffffu, gave_up != 0) && lane == 0) {
+        pdl_wait();
+        atomicExch(P.status, VPTQ_E_TIMEOUT);
+    }
+    __syncwarp();
+    if constexpr (SPLIT > 1) {
+        cluster_sync();
+        // rows of the tile that are tokens, dealt out over the ranks; four features a thread, the ranks' sums added in order
+        const int t0 = first % P.tiles_t * TM, n0 = first / P.tiles_t * TN;
+        const int rows = min(TM, P.B - t0), r0 = rows * rank / SPLIT, r1 = rows * (rank + 1) / SPLIT;
+        constexpr int PIECES = TN / 4;
+        for (int i = threadIdx.x; i < (r1 - r0) * PIECES; i += THREADS) {
+            const int row = r0 + i / PIECES, p = i % PIECES, col = n0 + 4 * p;
+            const uint32_t at = base + (uint32_t)(row * TN + 4 * (p ^ (row & 7))) * 4u;
+            float4 v[SPLIT];
+#pragma unroll
+            for (int r = 0; r < SPLIT; r++) v[r] = load_peer(at, (uint32_t)r);
+#pragma unroll
+            for (int r = 1; r < SPLIT; r++) { v[0].x += v[r].x; v[0].y += v[r].y; v[0].z += v[r].z; v[0].w += v[r].w; }
+            const long long o = (long long)(t0 + row) * P.M + col;
+            if (P.tma_out && col + 4 <= P.M) {                                 // rows of 16-byte multiples: a thread's four values are aligned
+                if (P.out_dtype == VPTQ_DTYPE_FP32) *reinterpret_cast<float4 *>(reinterpret_cast<float *>(P.out) + o) = v[0];
+                else *reinterpret_cast<uint2 *>(reinterpret_cast<uint16_t *>(P.out) + o) = make_uint2(pair16(v[0].x, v[0].y, P.out_dtype), pair16(v[0].z, v[0].w, P.out_dtype));
+            } else {
+                const float e[4] = {v[0].x, v[0].y, v[0].z, v[0].w};
+#pragma unroll
+                for (int k = 0; k < 4; k++)
+                    if (col + k < P.M) store_out(P.out, o + k, e[k], P.out_dtype);
+            }
+        }
+        __syncwarp();
+        cluster_sync();                                                        // a peer may still read this CTA's sums
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+    }
+}
+
+// ---- host side ----------------------------------------------------------------------------------------
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
+                                  const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
+                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiledFn get_encode_fn()
+{
+    static EncodeTiledFn fn = []() -> EncodeTiledFn {
+        void *p = nullptr;
+        cudaDriverEntryPointQueryResult qres;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &qres) == cudaSuccess &&
+            qres == cudaDriverEntryPointSuccess)
+            return reinterpret_cast<EncodeTiledFn>(p);
+        return nullptr;
+    }();
+    return fn;
+}
+
+bool encode_2d(CUtensorMap *map, CUtensorMapDataType type, const void *p, uint64_t cols, uint64_t rows, uint64_t row_bytes,
+               uint32_t box_cols, uint32_t box_rows, CUtensorMapSwizzle swizzle)
+{
+    const EncodeTiledFn encode = get_encode_fn();
+    if (encode == nullptr) return false;
+    const cuuint64_t dim[2] = {cols, rows}, stride[1] = {row_bytes};
+    const cuuint32_t box[2] = {box_cols, box_rows}, unit[2] = {1, 1};
+    return encode(map, type, 2, const_cast<void *>(p), dim, stride, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
+                  CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int TN, int SPLIT>
+cudaError_t run(const Fp8Linear &L, const Params &P0, cudaStream_t st)
+{
+    Params P = P0;
+    const long long pitch = fp8_row_bytes(L.N), out_bytes = L.out_dtype == VPTQ_DTYPE_FP32 ? 4 : 2;
+    CUtensorMap map_x, map_w, map_out;
+    if (!encode_2d(&map_x, CU_TENSOR_MAP_DATA_TYPE_UINT8, L.x, pitch, L.B, pitch, FP8_BLOCK, TM, CU_TENSOR_MAP_SWIZZLE_128B) ||
+        !encode_2d(&map_w, CU_TENSOR_MAP_DATA_TYPE_UINT8, L.w, pitch, L.M, pitch, FP8_BLOCK, TN, CU_TENSOR_MAP_SWIZZLE_128B))
+        return cudaErrorNotSupported;
+    map_out = map_x;                                      // (not read unless tma_out)
+    P.tma_out = L.M * out_bytes % 16 == 0 ? 1 : 0;
+    if (P.tma_out &&
+        !encode_2d(&map_out, out_bytes == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16, L.out, L.M, L.B, L.M * out_bytes, 32, 32,
+                   out_bytes == 4 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B))
+        return cudaErrorNotSupported;
+    P.tiles_t = ceil_div(L.B, TM);
+    P.tiles = P.tiles_t * ceil_div(L.M, TN);
+    auto kern = linear_fp8_tcgen05_kernel<TN, SPLIT>;
+    const cudaError_t e = allow_dynamic_smem(reinterpret_cast<const void *>(kern), smem_bytes<TN>());
+    if (e != cudaSuccess) return e;
+    const int sms = device_sm_count();
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(SPLIT > 1 ? P.tiles * SPLIT : P.tiles < sms ? P.tiles : sms));
+    cfg.blockDim = dim3(THREADS);
+    cfg.dynamicSmemBytes = smem_bytes<TN>();
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    int n = 0;
+    if (SPLIT > 1) {
+        attr[n].id = cudaLaunchAttributeClusterDimension;
+        attr[n].val.clusterDim.x = SPLIT; attr[n].val.clusterDim.y = 1; attr[n].val.clusterDim.z = 1;
+        n++;
+    }
+    if (pdl_enabled("linear_fp8")) {
+        attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[n].val.programmaticStreamSerializationAllowed = 1;
+        n++;
+    }
+    cfg.attrs = attr; cfg.numAttrs = n;
+    return cudaLaunchKernelEx(&cfg, kern, map_x, map_w, map_out, P);
+}
+
+struct Choice { int tn, split; };
+
+// Tile width and split by estimated time, in clocks per SM: a block of 128 columns takes 2 TN on the tensor cores, and its bytes come
+// in at most about 48 a clock; a tile ends with about 1500 for its results, a split one with 2500 for the meeting.
+Choice choose(int M, int B, int kbs)
+{
+    const int sms = device_sm_count(), widths[6] = {256, 224, 192, 160, 128, 64}, splits[4] = {1, 2, 4, 8};
+    Choice best = {256, 1};
+    double best_time = 1e300;
+    for (int i = 0; i < 6; i++)
+        for (int j = 0; j < 4; j++) {
+            const int tn = widths[i], split = splits[j];
+            if (split > 1 && (tn > 128 || kbs < 2 * split)) continue;
+            const long long tiles = (long long)ceil_div(B, TM) * ceil_div(M, tn);
+            if (split > 1 && tiles * split > sms) continue;
+            const long long waves = (tiles * split + sms - 1) / sms;
+            const double block = 2.0 * tn > (TM + tn) * 128 / 48.0 ? 2.0 * tn : (TM + tn) * 128 / 48.0;
+            const double time = waves * (ceil_div(kbs, split) * block + (split > 1 ? 2500 : 1500)) + 2000;
+            if (time < best_time) { best_time = time; best = {tn, split}; }
+        }
+    return best;
+}
+
+}  // namespace
+
+cudaError_t launch_linear_fp8_tcgen05(const Fp8Linear &L, int *status, cudaStream_t st)
+{
+    Params P;
+    P.M = L.M; P.B = L.B; P.kbs = ceil_div(L.N, FP8_BLOCK);
+    P.x_scale = L.x_scale; P.w_scale = L.w_scale; P.out = L.out; P.out_dtype = L.out_dtype; P.status = status;
+    P.tiles_t = P.tiles = P.tma_out = 0;
+    const Choice c = choose(L.M, L.B, P.kbs);
+    switch (c.tn * 10 + c.split) {
+    case 2561: return run<256, 1>(L, P, st);
+    case 2241: return run<224, 1>(L, P, st);
+    case 1921: return run<192, 1>(L, P, st);
+    case 1601: return run<160, 1>(L, P, st);
+    case 1281: return run<128, 1>(L, P, st);
+    case 1282: return run<128, 2>(L, P, st);
+    case 1284: return run<128, 4>(L, P, st);
+    case 1288: return run<128, 8>(L, P, st);
+    case 641: return run<64, 1>(L, P, st);
+    case 642: return run<64, 2>(L, P, st);
+    case 644: return run<64, 4>(L, P, st);
+    default: return run<64, 8>(L, P, st);
+    }
+}
+
+}  // namespace vptq

@@ -554,7 +554,7 @@ int vptq_fp8_quantize(const void *x, int32_t x_dtype, int32_t n_rows, int32_t n_
     if (n_rows == 0) return VPTQ_OK;
     if (x == nullptr || q == nullptr || scale == nullptr) return VPTQ_E_NULL;
     if (!aligned16(q) || !aligned16(scale) || (reinterpret_cast<uintptr_t>(x) & (x_dtype == VPTQ_DTYPE_FP32 ? 3u : 1u))) return VPTQ_E_ALIGN;
-    const cudaError_t e = launch_fp8_quantize(x, x_dtype, n_rows, n_cols, ld, block_rows, q, scale, nullptr, false,
+    const cudaError_t e = launch_fp8_quantize(x, x_dtype, n_rows, n_cols, ld, block_rows, q, scale, false,
                                               reinterpret_cast<cudaStream_t>(stream));
     return e == cudaSuccess ? VPTQ_OK : cuda_fail(e);
 }
@@ -600,7 +600,7 @@ int64_t vptq_linear_fp8_workspace_bytes(const vptq_fp8_desc *desc, int32_t B)
 {
     const int rc = check_fp8_desc(desc, B);
     if (rc != VPTQ_OK) return rc;
-    return linear_fp8_workspace_bytes(desc->M, desc->N, B, desc->x_dtype);
+    return linear_fp8_workspace_bytes(desc->N, B, desc->x_dtype);
 }
 
 int vptq_linear_fp8(const vptq_fp8_desc *desc, const void *x, const float *x_scale, int32_t B,
@@ -612,7 +612,7 @@ int vptq_linear_fp8(const vptq_fp8_desc *desc, const void *x, const float *x_sca
     const bool e4m3 = desc->x_dtype == VPTQ_DTYPE_E4M3;
     if (x == nullptr || w == nullptr || w_scale == nullptr || out == nullptr || (e4m3 && x_scale == nullptr)) return VPTQ_E_NULL;
     if (!aligned16(x) || !aligned16(w) || !aligned16(w_scale) || !aligned16(out) || (e4m3 && !aligned16(x_scale))) return VPTQ_E_ALIGN;
-    const long long need = linear_fp8_workspace_bytes(desc->M, desc->N, B, desc->x_dtype);
+    const long long need = linear_fp8_workspace_bytes(desc->N, B, desc->x_dtype);
     if (need > 0) {
         if (workspace == nullptr || (long long)workspace_bytes < need) return VPTQ_E_WORKSPACE;
         if ((reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return VPTQ_E_ALIGN;
@@ -627,14 +627,14 @@ int vptq_linear_fp8(const vptq_fp8_desc *desc, const void *x, const float *x_sca
 const char *vptq_linear_fp8_path(const vptq_fp8_desc *desc, int32_t B)
 {
     if (check_fp8_desc(desc, B) != VPTQ_OK) return "invalid";
-    return linear_fp8_path(desc->M, desc->N, B, desc->x_dtype);
+    return linear_fp8_path(B);
 }
 
 int vptq_linear_fp8_launches(const vptq_fp8_desc *desc, int32_t B)
 {
     const int rc = check_fp8_desc(desc, B);
     if (rc != VPTQ_OK) return rc;
-    return linear_fp8_launches(desc->M, desc->N, B, desc->x_dtype);
+    return linear_fp8_launches(B, desc->x_dtype);
 }
 
 const char *vptq_status_string(int code)
