@@ -173,6 +173,26 @@ def test_linear_many_tokens(b, M, N, B, x_type):
     check_linear(b, M, N, B, x_type, "fp32")
 
 
+# (tiles of every width, alone and in pairs, and tiles split over 2, 4 and 8 CTAs; rows of the result that are no multiple of 16 bytes)
+@pytest.mark.parametrize("M,N,B,out", [(128, 4096, 40, "fp32"), (1000, 2048, 77, "fp16"), (2048, 1024, 128, "bf16"), (4096, 1024, 64, "fp16"), (4099, 512, 100, "fp32"),
+                                       (9472, 256, 128, "fp16"), (18944, 272, 100, "bf16"), (37888, 160, 17, "fp16"), (33152, 128, 33, "bf16"), (9472, 400, 512, "fp16"),
+                                       (18944, 144, 300, "fp32"), (14208, 256, 512, "bf16"), (16576, 384, 513, "fp16"), (28416, 128, 385, "fp32"), (1001, 1000, 1111, "bf16"), (18990, 128, 40, "fp16"),
+                                       (4744, 128, 133, "bf16"), (4741, 200, 133, "fp32"), (9760, 128, 150, "fp16"), (15120, 144, 200, "fp32"), (15121, 128, 129, "bf16")])
+def test_linear_tiles(b, M, N, B, out):
+    N = ref.pitch(N)
+    check_linear(b, M, N, B, "e4m3", out)
+
+
+@pytest.mark.parametrize("B", [17, 100, 600])
+def test_linear_reports_no_error(b, B):
+    w, ws, x, _, _ = operands(500, 640, B, "fp16", 3)
+    desc = b.make_fp8_desc(500, 640, "fp16", "fp16")
+    room = torch.full((b.vptq_linear_fp8_workspace_bytes(desc, B),), 255, dtype=torch.uint8, device="cuda")       # what it held before does not matter
+    y = b.vptq_linear_fp8(x, w, ws, workspace=room)
+    assert b.vptq_linear_fp8_path(desc, B) == "fp8_tcgen05" and b.vptq_workspace_status(room) == b.OK
+    assert same(y, b.vptq_linear_fp8(x, w, ws))
+
+
 @pytest.mark.parametrize("out", ["fp16", "bf16"])
 @pytest.mark.parametrize("M,N,B", [(130, 1030, 5), (256, 512, 16), (300, 1000, 48), (264, 768, 200)])
 def test_linear_result_types(b, M, N, B, out):
