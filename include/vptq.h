@@ -466,9 +466,10 @@ int vptq_dequant_fp8(const vptq_layer_desc *desc, const vptq_layer_ptrs *p, uint
  *           so the same result, as vptq_fp8_quantize followed by the call above
  *   out_dtype FP16, BF16 or FP32;  flags: VPTQ_FLAG_CONCURRENT and VPTQ_FLAG_DETERMINISTIC are accepted and change nothing (no CTA
  *           waits for another launch's, every sum has a fixed order).
- * At most 16 tokens take the kernel "fp8_decode", more "fp8_tcgen05" (vptq_linear_fp8_path; by M, N, B and the types alone), whose
- * workspace starts with a status word (vptq_workspace_status); that kernel's waits are bounded.  The workspace is
- * 256-byte aligned; its contents on entry are irrelevant; calls that may overlap must not share one. */
+ * At most 8 tokens take the kernel "fp8_decode" (no workspace), more "fp8_tcgen05" (vptq_linear_fp8_path), whose workspace, 256-byte
+ * aligned, starts with a status word (vptq_workspace_status); its contents on entry are irrelevant, calls that may overlap must not
+ * share one.  All device-side waits are bounded: one that gives up leaves VPTQ_E_TIMEOUT in the status word, or NaN in the results of
+ * "fp8_decode". */
 typedef struct vptq_fp8_desc {
     int32_t M, N;        /* out_features, in_features */
     int32_t x_dtype;     /* VPTQ_DTYPE_E4M3, _FP16 or _BF16 */

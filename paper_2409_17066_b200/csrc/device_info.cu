@@ -1,5 +1,6 @@
 // Per-device facts the launch plans depend on, looked up once per device ordinal.
 #include "common.cuh"
+#include "tma_2d.cuh"
 
 #include <atomic>
 #include <mutex>
@@ -126,6 +127,29 @@ bool pdl_enabled(const char *family)
     static const char *off = getenv("VPTQ_NO_PDL");          // read once
     if (off == nullptr || off[0] == 0) return true;
     return strstr(off, "all") == nullptr && strstr(off, family) == nullptr;
+}
+
+namespace {
+typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
+                                  const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
+                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+}
+
+bool encode_tensor_map(CUtensorMap *map, CUtensorMapDataType type, const void *p, uint64_t cols, uint64_t rows, uint64_t row_bytes, uint64_t layers,
+                       uint64_t layer_bytes, uint32_t box_cols, uint32_t box_rows, uint32_t box_layers, CUtensorMapSwizzle swizzle)
+{
+    static const EncodeTiledFn encode = []() -> EncodeTiledFn {
+        void *f = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess)
+            return nullptr;
+        return reinterpret_cast<EncodeTiledFn>(f);
+    }();
+    if (encode == nullptr) return false;
+    const cuuint64_t dim[3] = {cols, rows, layers}, stride[2] = {row_bytes, layer_bytes};
+    const cuuint32_t box[3] = {box_cols, box_rows, box_layers}, unit[3] = {1, 1, 1};
+    return encode(map, type, layers > 0 ? 3 : 2, const_cast<void *>(p), dim, stride, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
+                  CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 }  // namespace vptq

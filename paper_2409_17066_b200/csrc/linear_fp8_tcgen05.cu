@@ -15,8 +15,7 @@
 #include "fp8.cuh"
 #include "fp8_tcgen05.cuh"
 #include "tcgen05_ptx.cuh"
-
-#include <cuda.h>
+#include "tma_2d.cuh"
 
 namespace vptq {
 
@@ -64,8 +63,7 @@ __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap *map, i
         asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
                      ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
     else
-        asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
-                     ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+        tma_load_2d(dst, map, x, y, bar);
 }
 __device__ __forceinline__ void tma_store(const CUtensorMap *map, uint32_t src, int x, int y)
 {
@@ -476,48 +474,20 @@ linear_fp8_tcgen05_kernel(const __grid_constant__ CUtensorMap map_x, const __gri
 
 // ---- host side ----------------------------------------------------------------------------------------
 
-typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
-                                  const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeTiledFn get_encode_fn()
-{
-    static EncodeTiledFn fn = []() -> EncodeTiledFn {
-        void *p = nullptr;
-        cudaDriverEntryPointQueryResult qres;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &qres) == cudaSuccess &&
-            qres == cudaDriverEntryPointSuccess)
-            return reinterpret_cast<EncodeTiledFn>(p);
-        return nullptr;
-    }();
-    return fn;
-}
-
-bool encode_2d(CUtensorMap *map, CUtensorMapDataType type, const void *p, uint64_t cols, uint64_t rows, uint64_t row_bytes,
-               uint32_t box_cols, uint32_t box_rows, CUtensorMapSwizzle swizzle)
-{
-    const EncodeTiledFn encode = get_encode_fn();
-    if (encode == nullptr) return false;
-    const cuuint64_t dim[2] = {cols, rows}, stride[1] = {row_bytes};
-    const cuuint32_t box[2] = {box_cols, box_rows}, unit[2] = {1, 1};
-    return encode(map, type, 2, const_cast<void *>(p), dim, stride, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
-                  CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 template <int TN, int SPLIT, int PAIR>
 cudaError_t run(const Fp8Linear &L, const Params &P0, cudaStream_t st)
 {
     Params P = P0;
     const long long pitch = fp8_row_bytes(L.N), out_bytes = L.out_dtype == VPTQ_DTYPE_FP32 ? 4 : 2;
     CUtensorMap map_x, map_w, map_out;
-    if (!encode_2d(&map_x, CU_TENSOR_MAP_DATA_TYPE_UINT8, L.x, pitch, L.B, pitch, FP8_BLOCK, TM, CU_TENSOR_MAP_SWIZZLE_128B) ||
-        !encode_2d(&map_w, CU_TENSOR_MAP_DATA_TYPE_UINT8, L.w, pitch, L.M, pitch, FP8_BLOCK, TN / PAIR, CU_TENSOR_MAP_SWIZZLE_128B))
+    if (!encode_tensor_map(&map_x, CU_TENSOR_MAP_DATA_TYPE_UINT8, L.x, pitch, L.B, pitch, 0, 0, FP8_BLOCK, TM, 1, CU_TENSOR_MAP_SWIZZLE_128B) ||
+        !encode_tensor_map(&map_w, CU_TENSOR_MAP_DATA_TYPE_UINT8, L.w, pitch, L.M, pitch, 0, 0, FP8_BLOCK, TN / PAIR, 1, CU_TENSOR_MAP_SWIZZLE_128B))
         return cudaErrorNotSupported;
     map_out = map_x;                                      // (not read unless tma_out)
     P.tma_out = L.M * out_bytes % 16 == 0 ? 1 : 0;
     if (P.tma_out &&
-        !encode_2d(&map_out, out_bytes == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16, L.out, L.M, L.B, L.M * out_bytes, 16, 32,
-                   out_bytes == 4 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_32B))
+        !encode_tensor_map(&map_out, out_bytes == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16, L.out, L.M, L.B, L.M * out_bytes, 0, 0, 16, 32, 1,
+                           out_bytes == 4 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_32B))
         return cudaErrorNotSupported;
     P.tiles_t = ceil_div(L.B, PAIR * TM);
     P.tiles = P.tiles_t * ceil_div(L.M, TN);

@@ -87,7 +87,15 @@ def test_linear_fp8_refusals(b):
     assert call(bad) == b.E_UNSUPPORTED
     assert call(b.make_fp8_desc(64, 64, flags=b.FLAG_SCALE_BIAS)) == b.E_UNSUPPORTED
     assert b.vptq_linear_fp8_path(bad, 1) == "invalid"
-    assert b.vptq_linear_fp8_path(d, 1) == "fp8_decode" and b.vptq_linear_fp8_path(d, 16) == "fp8_decode"
+    assert b.vptq_linear_fp8_path(d, 8) == "fp8_decode" and b.vptq_linear_fp8_path(d, 9) == "fp8_tcgen05"
+    h = b.make_fp8_desc(100, 300, "bf16", "fp32")
+    assert b.vptq_linear_fp8_workspace_bytes(h, 8) == 0 and b.vptq_linear_fp8_workspace_bytes(d, 9) == 256
+    need = b.vptq_linear_fp8_workspace_bytes(h, 9)
+    assert need >= 256 + 9 * (304 + 4 * 3)                          # status word, e4m3 rows, scales
+    assert f(C.byref(h), p, None, 9, p, p, p, None, 0, None) == b.E_WORKSPACE
+    assert f(C.byref(h), p, None, 9, p, p, p, p, need - 1, None) == b.E_WORKSPACE
+    assert f(C.byref(h), p, None, 9, p, p, p, p + 16, need, None) == b.E_ALIGN
+    assert [b.vptq_linear_fp8_launches(x, B) for x in (d, h) for B in (8, 9)] == [1, 1, 1, 2]
     assert b.vptq_linear_fp8_launches(d, 1) == 1 and b.vptq_linear_fp8_launches(d, 0) == b.E_SHAPE
 
 
