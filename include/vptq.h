@@ -483,6 +483,36 @@ int vptq_linear_fp8(const vptq_fp8_desc *desc, const void *x, const float *x_sca
 const char *vptq_linear_fp8_path(const vptq_fp8_desc *desc, int32_t B);
 int vptq_linear_fp8_launches(const vptq_fp8_desc *desc, int32_t B);
 
+/* A mixture-of-experts layer for a few tokens over experts in this format:
+ *   logits = x * router^T (FP32), p = softmax(logits) over all experts, the top_k largest logits of every token (of equal ones the
+ *   lowest expert), weight = p, or with VPTQ_FLAG_MOE_RENORMALIZE p / the sum of the chosen ones' p;
+ *   h = silu(x * gate_e^T) * (x * up_e^T), out = sum over the choices of weight * (h * down_e^T),
+ * the three products as in vptq_linear_fp8: x and h (FP32) are quantized by the rule with block_rows = 1; silu(v) = v / (1 + exp(-v)).
+ *   x [T][hidden], router [n_experts][hidden]: x_dtype (FP16 or BF16); out [T][hidden]: out_dtype (FP16, BF16 or FP32)
+ *   gate, up    n_experts e4m3 matrices [inner][pitch(hidden)], one after the other, scales [n_experts][ceil(inner / 128)][ceil(hidden / 128)]
+ *   down        n_experts e4m3 matrices [hidden][pitch(inner)], scales [n_experts][ceil(hidden / 128)][ceil(inner / 128)]
+ * 1 <= T <= VPTQ_MOE_MAX_TOKENS, n_experts <= VPTQ_MOE_MAX_EXPERTS, top_k <= VPTQ_MOE_MAX_TOP and <= n_experts, n_experts * inner and
+ * n_experts * hidden < 2^30, else VPTQ_E_SHAPE.  Two kernels; only the chosen experts' weights are read.  Every sum has a fixed order, no
+ * CTA waits for one outside its cluster.  The workspace is 256-byte aligned, its contents on entry are irrelevant; calls that may overlap
+ * must not share one.  A bounded device-side wait that gives up leaves NaN in the results. */
+#define VPTQ_MOE_MAX_TOKENS  32
+#define VPTQ_MOE_MAX_EXPERTS 256
+#define VPTQ_MOE_MAX_TOP     16
+#define VPTQ_FLAG_MOE_RENORMALIZE 128   /* weights of a token's choices are divided by their sum */
+typedef struct vptq_moe_desc {
+    int32_t hidden, inner, n_experts, top_k;
+    int32_t x_dtype, out_dtype;
+    int32_t flags;       /* VPTQ_FLAG_MOE_RENORMALIZE, VPTQ_FLAG_CONCURRENT, VPTQ_FLAG_DETERMINISTIC (the last two change nothing) */
+} vptq_moe_desc;
+typedef struct vptq_moe_ptrs {
+    const void    *router;
+    const uint8_t *gate, *up, *down;
+    const float   *gate_scale, *up_scale, *down_scale;
+} vptq_moe_ptrs;
+int64_t vptq_moe_fp8_workspace_bytes(const vptq_moe_desc *desc, int32_t T);
+int vptq_moe_fp8(const vptq_moe_desc *desc, const vptq_moe_ptrs *p, const void *x, int32_t T, void *out,
+                 void *workspace, size_t workspace_bytes, void *stream);
+
 /* ---- diagnostics ------------------------------------------------------------------ */
 
 const char *vptq_status_string(int code);

@@ -36,6 +36,8 @@ DTYPE_FP16, DTYPE_BF16, DTYPE_FP32, DTYPE_E4M3 = 0, 1, 2, 3
 FLAG_SCALE_BIAS, FLAG_SCALE_ROWS, FLAG_FORCE_GENERIC, FLAG_COL_PERM, FLAG_PREPARED = 1, 2, 4, 8, 16
 FLAG_CONCURRENT = 32
 FLAG_DETERMINISTIC = 64
+FLAG_MOE_RENORMALIZE = 128
+MOE_MAX_TOKENS, MOE_MAX_EXPERTS, MOE_MAX_TOP = 32, 256, 16
 
 _DT = {"fp16": DTYPE_FP16, "bf16": DTYPE_BF16, "fp32": DTYPE_FP32}
 _TORCH_DT = {DTYPE_FP16: torch.float16, DTYPE_BF16: torch.bfloat16, DTYPE_FP32: torch.float32}
@@ -61,6 +63,18 @@ class LayerPtrs(C.Structure):
 class Fp8Desc(C.Structure):
     """vptq_fp8_desc"""
     _fields_ = [("M", C.c_int32), ("N", C.c_int32), ("x_dtype", C.c_int32), ("out_dtype", C.c_int32), ("flags", C.c_int32)]
+
+
+class MoeDesc(C.Structure):
+    """vptq_moe_desc"""
+    _fields_ = [("hidden", C.c_int32), ("inner", C.c_int32), ("n_experts", C.c_int32), ("top_k", C.c_int32), ("x_dtype", C.c_int32),
+                ("out_dtype", C.c_int32), ("flags", C.c_int32)]
+
+
+class MoePtrs(C.Structure):
+    """vptq_moe_ptrs"""
+    _fields_ = [("router", C.c_void_p), ("gate", C.c_void_p), ("up", C.c_void_p), ("down", C.c_void_p), ("gate_scale", C.c_void_p),
+                ("up_scale", C.c_void_p), ("down_scale", C.c_void_p)]
 
 
 EXPORTS = {
@@ -112,6 +126,9 @@ EXPORTS = {
                                   C.c_void_p, C.c_size_t, C.c_void_p]),
     "vptq_linear_fp8_path": (C.c_char_p, [C.POINTER(Fp8Desc), C.c_int32]),
     "vptq_linear_fp8_launches": (C.c_int, [C.POINTER(Fp8Desc), C.c_int32]),
+    "vptq_moe_fp8_workspace_bytes": (C.c_int64, [C.POINTER(MoeDesc), C.c_int32]),
+    "vptq_moe_fp8": (C.c_int, [C.POINTER(MoeDesc), C.POINTER(MoePtrs), C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_size_t,
+                               C.c_void_p]),
     "vptq_status_string": (C.c_char_p, [C.c_int]),
     "vptq_last_cuda_error": (C.c_char_p, []),
     "vptq_workspace_status": (C.c_int, [C.c_void_p, C.c_void_p]),
@@ -436,6 +453,26 @@ def vptq_linear_fp8_path(desc: Fp8Desc, B: int) -> str:
 
 def vptq_linear_fp8_launches(desc: Fp8Desc, B: int) -> int:
     return lib.vptq_linear_fp8_launches(C.byref(desc), B)
+
+
+def make_moe_desc(hidden, inner, n_experts, top_k, x_dtype="bf16", out_dtype="bf16", flags=FLAG_MOE_RENORMALIZE) -> MoeDesc:
+    return MoeDesc(hidden, inner, n_experts, top_k, _DT[x_dtype], _DT[out_dtype], flags)
+
+
+def vptq_moe_fp8_workspace_bytes(desc: MoeDesc, T: int) -> int:
+    n = lib.vptq_moe_fp8_workspace_bytes(C.byref(desc), T)
+    if n < 0:
+        raise VptqError(int(n))
+    return n
+
+
+def vptq_moe_fp8(x: torch.Tensor, router: torch.Tensor, gate: torch.Tensor, gate_scale: torch.Tensor, up: torch.Tensor,
+                 up_scale: torch.Tensor, down: torch.Tensor, down_scale: torch.Tensor, top_k: int, renormalize: bool = True,
+                 out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """A mixture-of-experts layer for T <= MOE_MAX_TOKENS tokens: x [T][hidden] and router [E][hidden] fp16 or bf16; gate and up e4m3
+    [E][inner][pitch(hidden)], down e4m3 [E][hidden][pitch(inner)], each with its 128 x 128 block scales (fp32, [E][row blocks][column
+    blocks]).  Returns out [T][hidden] (of x's type unless `out` has another)."""
+    return _native.moe_fp8(x, router, gate, gate_scale, up, up_scale, down, down_scale, top_k, renormalize, out, workspace)
 
 
 # ---- a quantized layer resident on the device ------------------------------------------

@@ -1,0 +1,553 @@
+// A mixture-of-experts layer for a few tokens over experts in e4m3 with 128 x 128 block scales, in two kernels:
+//   logits = x Wr^T, p = softmax(logits), the k largest logits of a token (equal ones: the lowest expert) with weights p, or p divided
+//   by the chosen ones' sum;  h = silu(x Wg^T) * (x Wu^T) per token and choice;  out = sum over the choices of weight * (h Wd^T).
+//
+// moe_gate_up_kernel: clusters of four CTAs compute all logits, a quarter each, exchange them, and every CTA makes the choices and the
+// list of experts in use by itself: no wait for another cluster and no launch for the router.  Then the units (16 gate and the 16 up
+// rows of an expert in use) are dealt out over all CTAs; a warp takes every sixteenth 128-column block of up to two units at a time
+// into a stage of its own (as in linear_fp8_decode.cu), multiplies it with up to 8 of the expert's tokens (fp8_mma.cuh), and
+// the warps' sums meet in shared memory, where h is formed (FP32, to the workspace).
+// moe_down_kernel: a CTA owns 16 or 32 rows of the result; its warps share the blocks of all the experts in use, quantizing h on the way;
+// per expert a warp adds weight * sums to a slot of its own for each token, and the slots are added in warp order.  No atomics: a result
+// does not depend on timing.
+// Bound by HBM: the weights of the experts in use, each once (once for every 8 of its tokens), and for one token of small experts by
+// the way through router, two launches and two reductions.
+// Every wait is bounded; a warp whose wait gives up leaves NaN.
+#include "fp8_mma.cuh"
+#include "moe_fp8.cuh"
+#include "tcgen05_ptx.cuh"
+#include "tma_2d.cuh"
+
+namespace vptq {
+
+namespace {
+
+using namespace tc;
+
+constexpr int GROUP = 16, GROUP_BYTES = GROUP * FP8_BLOCK;
+constexpr int WARPS = 16, THREADS = 32 * WARPS;
+constexpr int CLUSTER = 4;
+constexpr int UNITS = 2;                                  // of a pass: 16 gate and 16 up rows each
+constexpr int UP_GROUPS = 2 * UNITS;
+constexpr int TOKENS = 8;                                 // of an expert at a time
+constexpr int MAX_ENTRIES = MOE_MAX_TOKENS * MOE_MAX_TOP;
+constexpr int DOWN_GROUPS = 2;                            // groups of a CTA's pass of the down kernel
+
+// The experts in use, up to 8 of an expert's (token, choice) pairs to an entry; pair = token * top + choice.
+struct Plan {
+    int entries;
+    int pad[3];
+    float weight[MAX_ENTRIES];                            // of every pair
+    int16_t expert[MAX_ENTRIES];
+    int16_t count[MAX_ENTRIES];
+    int16_t pair[MAX_ENTRIES][TOKENS];
+};
+
+struct Params {
+    MoeFp8 L;
+    Plan *plan;            // in the workspace
+    float *h;              // [T * top][h_stride]
+    int h_stride;
+    int down_groups;       // groups of a pass of the down kernel
+    int down_passes, down_run_shift;
+};
+
+__device__ __forceinline__ uint4 load_shared16(uint32_t a)
+{
+    uint4 q;
+    asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(q.x), "=r"(q.y), "=r"(q.z), "=r"(q.w) : "r"(a));
+    return q;
+}
+__device__ __forceinline__ void cluster_sync()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void store_peer(float *at, uint32_t rank, float v)
+{
+    uint32_t a;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_addr(at)), "r"(rank));
+    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(a), "f"(v) : "memory");
+}
+
+// logits of this CTA's quarter of the experts, to all four CTAs: a warp an expert and up to four tokens at a time
+template <int DT, bool VEC>
+__device__ __forceinline__ void router(const MoeFp8 &L, float *logits, uint32_t rank, int warp, int lane)
+{
+    const int n = (L.experts + CLUSTER - 1) / CLUSTER, quads = (L.T + 3) / 4;
+    for (int i = warp; i < n * quads; i += WARPS) {
+        const int e = (int)rank + CLUSTER * (i / quads), t0 = i % quads * 4;
+        if (e >= L.experts) continue;                     // (whole warps)
+        const uint8_t *w = reinterpret_cast<const uint8_t *>(L.router) + (long long)e * L.hidden * 2;
+        const uint8_t *x[4];
+#pragma unroll
+        for (int j = 0; j < 4; j++) x[j] = reinterpret_cast<const uint8_t *>(L.x) + (long long)min(t0 + j, L.T - 1) * L.hidden * 2;
+        float sum[4] = {};
+        if (VEC) {
+#pragma unroll 4
+            for (int c = lane * 8; c < L.hidden; c += 256) {
+                float a[8], b[8];
+                load_values<DT, true, 8>(w, c, L.hidden, a);
+#pragma unroll
+                for (int j = 0; j < 4; j++) {
+                    if (t0 + j >= L.T) break;
+                    load_values<DT, true, 8>(x[j], c, L.hidden, b);
+#pragma unroll
+                    for (int q = 0; q < 8; q++) sum[j] = __fmaf_rn(a[q], b[q], sum[j]);
+                }
+            }
+        } else {
+            for (int c = lane; c < L.hidden; c += 32) {
+                const float a = Act<DT>::one(w, c);
+#pragma unroll
+                for (int j = 0; j < 4; j++)
+                    if (t0 + j < L.T) sum[j] = __fmaf_rn(a, Act<DT>::one(x[j], c), sum[j]);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 4; j++)
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], o);
+        // lane 4 j + r: token t0 + j to CTA r
+        const int j = lane >> 2;
+        const float v = j == 0 ? sum[0] : j == 1 ? sum[1] : j == 2 ? sum[2] : sum[3];
+        if (j < 4 && t0 + j < L.T) store_peer(logits + (t0 + j) * L.experts + e, (uint32_t)(lane & 3), v);
+    }
+}
+
+// an order of FP32 values as unsigned integers
+__device__ __forceinline__ uint32_t order_of(float v)
+{
+    const uint32_t b = __float_as_uint(v);
+    return (b & 0x80000000u) ? ~b : b | 0x80000000u;
+}
+
+// a warp: token t's choices and their weights
+__device__ __forceinline__ void choose_experts(const MoeFp8 &L, const float *logits, int t, int lane, int16_t *chosen, float *weight)
+{
+    constexpr int MOST = MOE_MAX_EXPERTS / 32;
+    float v[MOST];
+    float top = -__int_as_float(0x7F800000), total = 0.f;
+#pragma unroll
+    for (int i = 0; i < MOST; i++) {
+        const int e = lane + 32 * i;
+        v[i] = e < L.experts ? logits[t * L.experts + e] : 0.f;
+        if (e < L.experts) top = fmaxf(top, v[i]);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    uint32_t free_experts = 0;                            // of this lane's
+#pragma unroll
+    for (int i = 0; i < MOST; i++)
+        if (lane + 32 * i < L.experts) { total += expf(v[i] - top); free_experts |= 1u << i; }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+    float picked = 0.f, mine = 0.f;                       // sum of the chosen ones' p; lane j: choice j's
+    for (int j = 0; j < L.top; j++) {
+        uint32_t best = 0;
+        int e = 0x7FFFFFFF;
+#pragma unroll
+        for (int i = 0; i < MOST; i++) {
+            const uint32_t o = order_of(v[i]);
+            if ((free_experts >> i & 1u) && (e == 0x7FFFFFFF || o > best)) { best = o; e = lane + 32 * i; }
+        }
+        const uint32_t most = __reduce_max_sync(0xffffffffu, e == 0x7FFFFFFF ? 0u : best);
+        const int winner = (int)__reduce_min_sync(0xffffffffu, (uint32_t)(e != 0x7FFFFFFF && best == most ? e : 0x7FFFFFFF));
+        float p = 0.f;
+#pragma unroll
+        for (int i = 0; i < MOST; i++)
+            if (winner == lane + 32 * i) { p = expf(v[i] - top) / total; free_experts &= ~(1u << i); }
+        p = __shfl_sync(0xffffffffu, p, winner & 31);
+        picked += p;
+        if (lane == j) { mine = p; chosen[t * L.top + j] = (int16_t)winner; }
+    }
+    if (lane < L.top) weight[t * L.top + lane] = L.renormalize ? mine / picked : mine;
+}
+
+// all threads: the entries, experts ascending, an expert's pairs ascending
+__device__ __forceinline__ void list_entries(const MoeFp8 &L, const int16_t *chosen, Plan *plan, int *warp_total)
+{
+    const int e = threadIdx.x, warp = e >> 5, lane = e & 31, pairs = L.T * L.top;
+    int count = 0;
+    if (e < L.experts)
+        for (int p = 0; p < pairs; p++) count += chosen[p] == e ? 1 : 0;
+    const int entries = (count + TOKENS - 1) / TOKENS;
+    int before = entries;                                 // inclusive sum over the warp, then over the warps
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int other = __shfl_up_sync(0xffffffffu, before, o);
+        if (lane >= o) before += other;
+    }
+    if (lane == 31) warp_total[warp] = before;
+    __syncthreads();
+    int all = 0;
+    for (int w = 0; w < WARPS; w++) {
+        if (w < warp) before += warp_total[w];
+        all += warp_total[w];
+    }
+    if (threadIdx.x == 0) plan->entries = all;
+    int at = before - entries, n = 0;
+    if (count > 0)
+        for (int p = 0; p < pairs; p++)
+            if (chosen[p] == e) {
+                plan->pair[at][n] = (int16_t)p;
+                if (++n == TOKENS) { plan->expert[at] = (int16_t)e; plan->count[at++] = TOKENS; n = 0; }
+            }
+    if (n > 0) { plan->expert[at] = (int16_t)e; plan->count[at] = (int16_t)n; }
+    __syncthreads();
+}
+
+// ---- shared memory: [ring: a stage a warp][sums][plan][choices][barriers]; the logits lie in the ring until that is used --------
+constexpr int UP_STAGE = UP_GROUPS * GROUP_BYTES, UP_STRIDE = UP_GROUPS * GROUP + 4;
+constexpr int UP_PART = WARPS * TOKENS * UP_STRIDE * 4;
+constexpr int OFF_PART = WARPS * UP_STAGE, OFF_PLAN = OFF_PART + UP_PART, OFF_CHOSEN = OFF_PLAN + (int)sizeof(Plan),
+              OFF_UP_BARS = OFF_CHOSEN + MAX_ENTRIES * 2, UP_SMEM = OFF_UP_BARS + WARPS * 8 + WARPS * 4;
+static_assert(UP_SMEM <= 232448 && MOE_MAX_TOKENS * MOE_MAX_EXPERTS * 4 <= OFF_PART && sizeof(Plan) % 16 == 0, "");
+
+template <int DT, bool VEC>
+__global__ void __launch_bounds__(THREADS, 1)
+moe_gate_up_kernel(const __grid_constant__ CUtensorMap map_gate, const __grid_constant__ CUtensorMap map_up, const __grid_constant__ Params P)
+{
+    extern __shared__ __align__(1024) uint8_t sm[];
+    const MoeFp8 &L = P.L;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    float *logits = reinterpret_cast<float *>(sm), *part = reinterpret_cast<float *>(sm + OFF_PART);
+    Plan *plan = reinterpret_cast<Plan *>(sm + OFF_PLAN);
+    int16_t *chosen = reinterpret_cast<int16_t *>(sm + OFF_CHOSEN);
+    int *warp_total = reinterpret_cast<int *>(sm + OFF_UP_BARS + WARPS * 8);
+    const uint32_t bar = smem_addr(sm + OFF_UP_BARS) + 8 * warp, stage = smem_addr(sm) + warp * UP_STAGE;
+    if (lane == 0) {
+        mbar_init(bar, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    uint32_t rank;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+    __syncwarp();
+    cluster_sync();                                       // every CTA of the cluster runs: its memory may be written
+    pdl_launch_dependents();
+    pdl_wait();
+    router<DT, VEC>(L, logits, rank, warp, lane);
+    __syncwarp();
+    cluster_sync();
+    for (int t = warp; t < L.T; t += WARPS) choose_experts(L, logits, t, lane, chosen, plan->weight);
+    __syncthreads();
+    list_entries(L, chosen, plan, warp_total);
+    if (blockIdx.x == 0)                                  // for the second kernel
+        for (int i = threadIdx.x; i < (int)(sizeof(Plan) / 16); i += THREADS)
+            reinterpret_cast<uint4 *>(P.plan)[i] = reinterpret_cast<const uint4 *>(plan)[i];
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");                   // the logits were written where the copies go
+    __syncthreads();
+
+    // this CTA's units
+    const int per_entry = (L.inner + GROUP - 1) / GROUP, kbs = (L.hidden + FP8_BLOCK - 1) / FP8_BLOCK;
+    const long long all = (long long)plan->entries * per_entry;
+    const long long begin = all * blockIdx.x / gridDim.x, end = all * (blockIdx.x + 1) / gridDim.x;
+    uint32_t gave_up = 0;
+    // a pass: up to UNITS of one entry; and the next one
+    struct Pass { int entry, unit, n; long long left; };
+    auto cut = [&](Pass &p) { p.n = (int)min((long long)min(UNITS, per_entry - p.unit), p.left); };
+    auto advance = [&](Pass &p) {
+        p.unit += p.n;
+        p.left -= p.n;
+        if (p.unit == per_entry) { p.unit = 0; p.entry++; }
+        cut(p);
+    };
+    Pass now = {(int)(begin / per_entry), (int)(begin % per_entry), 0, end - begin};
+    cut(now);
+    // this warp's loads, in order: blocks warp, warp + 16, ... of one pass after the other; always a box of UNITS units (rows that a pass does
+    // not have are read with it and dropped)
+    Pass ahead = now;
+    int load_kb = warp;
+    auto load = [&]() {
+        const int row = plan->expert[ahead.entry] * L.inner + ahead.unit * GROUP;
+        mbar_expect_tx(bar, UP_STAGE);
+        tma_load_2d(stage, &map_gate, load_kb * FP8_BLOCK, row, bar);
+        tma_load_2d(stage + UP_STAGE / 2, &map_up, load_kb * FP8_BLOCK, row, bar);
+    };
+    auto next_load = [&]() {
+        load_kb += WARPS;
+        if (load_kb >= kbs) { load_kb = warp; advance(ahead); }
+    };
+    if (warp >= kbs) ahead.n = 0;
+    if (ahead.n > 0) {
+        if (lane == 0) load();
+        next_load();
+    }
+
+    const int g = lane >> 2, t = lane & 3;
+    const int row = (g >> 1) | ((g & 1) << 2);            // (see linear_fp8_decode.cu)
+    const uint32_t at0 = (uint32_t)(row * FP8_BLOCK + ((t ^ row) << 4)), at1 = (uint32_t)(row * FP8_BLOCK + (((t + 4) ^ row) << 4));
+    const int iterations = warp < kbs ? (kbs - warp + WARPS - 1) / WARPS : 0, scale_rows = (L.inner + FP8_BLOCK - 1) / FP8_BLOCK;
+    uint32_t parity = 0;
+    bool first = true;
+    for (; now.n > 0; advance(now)) {
+        const int expert = plan->expert[now.entry], count = plan->count[now.entry];
+        const uint8_t *x_row = g < count ? reinterpret_cast<const uint8_t *>(L.x) + (long long)(plan->pair[now.entry][g] / L.top) * L.hidden * 2 : nullptr;
+        // (a pass's units lie in one 128-row block, or the second of them in the next)
+        const int b0 = now.unit / (FP8_BLOCK / GROUP), b1 = min((now.unit + 1) / (FP8_BLOCK / GROUP), scale_rows - 1);
+        const long long of_expert = (long long)expert * scale_rows;
+        // scales of the warp's blocks j, 8 of them at a time: lane 8 r + j holds group r's
+        const float *scales = (lane < 16 ? L.gate_scale : L.up_scale) + (of_expert + (lane & 8 ? b1 : b0)) * kbs + warp;
+        auto block_scales = [&](int i) { return i + (lane & 7) < iterations ? __ldg(scales + (i + (lane & 7)) * WARPS) : 0.f; };
+        float ws = block_scales(0);
+        TokenRaw<DT, VEC> x = load_token<DT, VEC>(iterations > 0 ? x_row : nullptr, t, warp, L.hidden);
+        float acc[UP_GROUPS][1][4] = {};
+#pragma unroll 1
+        for (int i = 0; i < iterations; i++) {
+            if ((i & 7) == 0 && i > 0) ws = block_scales(i);
+            const TokenFrag b[1] = {quantize_token<DT, VEC>(x, 0.f)};
+            const float2 s = scales_of_columns(b[0].scale, t);
+            x = load_token<DT, VEC>(i + 1 < iterations ? x_row : nullptr, t, warp + (i + 1) * WARPS, L.hidden);
+            mbar_wait_uniform(bar, parity, gave_up);
+            parity ^= 1u;
+#pragma unroll
+            for (int r0 = 0; r0 < UP_GROUPS; r0 += UNITS) {
+                WeightFrag a[UNITS];
+                float w[UNITS];
+#pragma unroll
+                for (int r = 0; r < UNITS; r++) {
+                    const uint32_t box = stage + (r0 + r) * GROUP_BYTES;
+                    a[r].q[0][0] = load_shared16(box + at0); a[r].q[1][0] = load_shared16(box + 8 * FP8_BLOCK + at0);
+                    a[r].q[0][1] = load_shared16(box + at1); a[r].q[1][1] = load_shared16(box + 8 * FP8_BLOCK + at1);
+                    w[r] = __shfl_sync(0xffffffffu, ws, 8 * (r0 + r) + (i & 7));
+                }
+                block_products<UNITS, 1>(&acc[r0], a, b, [&](int r, int) { return make_float2(s.x * w[r], s.y * w[r]); });
+            }
+            __syncwarp();                                 // every lane has read the stage
+            if (ahead.n > 0 && !__any_sync(0xffffffffu, gave_up != 0)) {
+                if (lane == 0) load();
+                next_load();
+            }
+        }
+        if (!first) __syncthreads();                      // the last pass's sums have been read
+        first = false;
+        float *mine = part + warp * TOKENS * UP_STRIDE;
+#pragma unroll
+        for (int r = 0; r < UP_GROUPS; r++)
+#pragma unroll
+            for (int i = 0; i < 4; i++) mine[(2 * t + (i & 1)) * UP_STRIDE + r * GROUP + row + 8 * (i >> 1)] = gave_up ? __int_as_float(0x7FFFFFFF) : acc[r][0][i];
+        __syncthreads();
+        for (int i = threadIdx.x; i < count * now.n * GROUP; i += THREADS) {
+            const int token = i / (now.n * GROUP), m = i % (now.n * GROUP), col = now.unit * GROUP + m;
+            float gate = 0.f, up = 0.f;
+#pragma unroll
+            for (int w = 0; w < WARPS; w++) {
+                gate += part[(w * TOKENS + token) * UP_STRIDE + m];
+                up += part[(w * TOKENS + token) * UP_STRIDE + UNITS * GROUP + m];
+            }
+            // (columns up to the row's end in the workspace are zeros)
+            if (col < P.h_stride) P.h[(long long)plan->pair[now.entry][token] * P.h_stride + col] = col < L.inner ? gate / (1.f + expf(-gate)) * up : 0.f;
+        }
+    }
+    if (gave_up) {                                        // copies in flight get a bounded time to land before the CTA exits
+        const long long c0 = clock64();
+        while (clock64() - c0 < 20000000ll) {}
+    }
+}
+
+// ---- the down projection -----------------------------------------------------------------------------------
+// shared memory: [ring: stages][slots: [warp][token][groups * 16 + 4]][plan][barriers]
+__host__ __device__ inline int down_slot_floats(int tokens, int groups) { return tokens * (groups * GROUP + 4); }
+
+__global__ void __launch_bounds__(THREADS, 1)
+moe_down_kernel(const __grid_constant__ CUtensorMap map_down, const __grid_constant__ Params P, int stages)
+{
+    extern __shared__ __align__(1024) uint8_t sm[];
+    const MoeFp8 &L = P.L;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int block_bytes = P.down_groups * GROUP_BYTES, run_shift = P.down_run_shift, run = 1 << run_shift, stage_bytes = block_bytes << run_shift;
+    const int stride = P.down_groups * GROUP + 4;
+    float *slots = reinterpret_cast<float *>(sm + (long long)WARPS * stages * stage_bytes), *mine = slots + warp * down_slot_floats(L.T, P.down_groups);
+    Plan *plan = reinterpret_cast<Plan *>(slots + WARPS * down_slot_floats(L.T, P.down_groups));
+    const uint32_t bars = smem_addr(plan + 1) + (uint32_t)(8 * warp * stages), ring = smem_addr(sm) + (uint32_t)(warp * stages * stage_bytes);
+    if (lane == 0) {
+        for (int s = 0; s < stages; s++) mbar_init(bars + 8 * s, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    pdl_launch_dependents();
+    pdl_wait();                                           // the plan and h are the first kernel's
+    for (int i = threadIdx.x; i < (int)(sizeof(Plan) / 16); i += THREADS)
+        reinterpret_cast<uint4 *>(plan)[i] = __ldcg(reinterpret_cast<const uint4 *>(P.plan) + i);
+    __syncthreads();
+
+    const int groups = (L.hidden + GROUP - 1) / GROUP, kbs = (L.inner + FP8_BLOCK - 1) / FP8_BLOCK, runs = (kbs + run - 1) >> run_shift;
+    const int first = (int)((long long)groups * blockIdx.x / gridDim.x), count = (int)((long long)groups * (blockIdx.x + 1) / gridDim.x) - first;
+    const int pass_groups = count / P.down_passes, larger = count - pass_groups * P.down_passes;
+    auto pass_begin = [&](int p) { return first + p * pass_groups + min(p, larger); };
+    const int scale_rows = (L.hidden + FP8_BLOCK - 1) / FP8_BLOCK;
+    // this warp's loads, in order: runs warp, warp + 16, ... of the entries one after the other, pass by pass
+    struct At { int pass, entry, r; };
+    auto settle = [&](At &a) {                            // r counts on from the entry before
+        while (a.pass < P.down_passes && a.r >= runs) {
+            a.r -= runs;
+            if (++a.entry == plan->entries) { a.entry = 0; a.pass++; a.r = warp; }
+        }
+    };
+    At ahead = {0, 0, warp};
+    settle(ahead);
+    uint32_t gave_up = 0;
+    auto load = [&](uint32_t slot) {
+        const uint32_t bar = bars + 8 * slot, to = ring + slot * stage_bytes;
+        const int row = plan->expert[ahead.entry] * L.hidden + pass_begin(ahead.pass) * GROUP;
+        mbar_expect_tx(bar, (uint32_t)stage_bytes);
+        if (run_shift > 0) tma_load_3d(to, &map_down, 0, row, ahead.r << run_shift, bar);
+        else tma_load_2d(to, &map_down, ahead.r * FP8_BLOCK, row, bar);
+    };
+    for (int s = 0; s < stages && ahead.pass < P.down_passes; s++) {
+        if (lane == 0) load((uint32_t)s);
+        ahead.r += WARPS;
+        settle(ahead);
+    }
+    __syncwarp();
+
+    const int g = lane >> 2, t = lane & 3;
+    const int row = (g >> 1) | ((g & 1) << 2);
+    const uint32_t at0 = (uint32_t)(row * FP8_BLOCK + ((t ^ row) << 4)), at1 = (uint32_t)(row * FP8_BLOCK + (((t + 4) ^ row) << 4));
+    uint32_t slot = 0, parity = 0;
+    At now = {0, 0, warp};
+    settle(now);
+    for (int p = 0; p < P.down_passes; p++) {
+        const int g0 = pass_begin(p), n_groups = pass_begin(p + 1) - g0;
+        const int b0 = g0 / (FP8_BLOCK / GROUP), b1 = min((g0 + 1) / (FP8_BLOCK / GROUP), scale_rows - 1);
+        for (int i = lane; i < down_slot_floats(L.T, P.down_groups); i += 32) mine[i] = 0.f;
+        __syncwarp();
+        while (now.pass == p) {
+            // this warp's runs of one entry
+            const int entry = now.entry, n = plan->count[entry];
+            const long long of_expert = (long long)plan->expert[entry] * scale_rows;
+            const float *ws0 = L.down_scale + (of_expert + b0) * kbs, *ws1 = L.down_scale + (of_expert + b1) * kbs;
+            const float *h_row = g < n ? P.h + (long long)plan->pair[entry][g] * P.h_stride : nullptr;
+            float acc[DOWN_GROUPS][1][4] = {};
+            while (now.pass == p && now.entry == entry) {
+                const int kb0 = now.r << run_shift, kb1 = min(kbs, kb0 + run);
+                TokenRaw<VPTQ_DTYPE_FP32, true> x = load_token<VPTQ_DTYPE_FP32, true>(h_row, t, kb0, P.h_stride);
+                float w0 = __ldg(ws0 + kb0), w1 = __ldg(ws1 + kb0);
+                for (int kb = kb0; kb < kb1; kb++) {
+                    const TokenFrag b[1] = {quantize_token<VPTQ_DTYPE_FP32, true>(x, 0.f)};
+                    const float2 s = scales_of_columns(b[0].scale, t);
+                    const float c0 = w0, c1 = w1;
+                    if (kb + 1 < kb1) {
+                        x = load_token<VPTQ_DTYPE_FP32, true>(h_row, t, kb + 1, P.h_stride);
+                        w0 = __ldg(ws0 + kb + 1);
+                        w1 = __ldg(ws1 + kb + 1);
+                    }
+                    if (kb == kb0) mbar_wait_uniform(bars + 8 * slot, parity, gave_up);
+                    WeightFrag a[DOWN_GROUPS];
+#pragma unroll
+                    for (int r = 0; r < DOWN_GROUPS; r++) {
+                        // (one group: the other's operands are whatever lies behind, dropped)
+                        const uint32_t box = ring + slot * stage_bytes + (uint32_t)((kb - kb0) * block_bytes + r * GROUP_BYTES);
+                        a[r].q[0][0] = load_shared16(box + at0); a[r].q[1][0] = load_shared16(box + 8 * FP8_BLOCK + at0);
+                        a[r].q[0][1] = load_shared16(box + at1); a[r].q[1][1] = load_shared16(box + 8 * FP8_BLOCK + at1);
+                    }
+                    block_products<DOWN_GROUPS, 1>(acc, a, b, [&](int r, int) { return r == 0 ? make_float2(s.x * c0, s.y * c0) : make_float2(s.x * c1, s.y * c1); });
+                }
+                __syncwarp();                             // every lane has read the stage
+                if (ahead.pass < P.down_passes && !__any_sync(0xffffffffu, gave_up != 0)) {
+                    if (lane == 0) load(slot);
+                    ahead.r += WARPS;
+                    settle(ahead);
+                }
+                if (++slot == (uint32_t)stages) { slot = 0; parity ^= 1u; }
+                now.r += WARPS;
+                settle(now);
+            }
+            // each (row, token) of the entry is one lane's: an expert has a token once
+#pragma unroll
+            for (int r = 0; r < DOWN_GROUPS; r++)
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    const int j = 2 * t + (i & 1);
+                    if (r < n_groups && j < n) {
+                        const int pair = plan->pair[entry][j];
+                        float *to = mine + pair / L.top * stride + r * GROUP + row + 8 * (i >> 1);
+                        *to = __fmaf_rn(plan->weight[pair], gave_up ? __int_as_float(0x7FFFFFFF) : acc[r][0][i], *to);
+                    }
+                }
+            __syncwarp();
+        }
+        __syncthreads();
+        const int rows = n_groups * GROUP, m0 = g0 * GROUP;
+        for (int i = threadIdx.x; i < L.T * rows; i += THREADS) {
+            const int token = i / rows, m = i % rows;
+            if (m0 + m >= L.hidden) continue;
+            float sum = 0.f;
+#pragma unroll
+            for (int w = 0; w < WARPS; w++) sum += slots[w * down_slot_floats(L.T, P.down_groups) + token * stride + m];
+            store_out(L.out, (long long)token * L.hidden + m0 + m, sum, L.out_dtype);
+        }
+        __syncthreads();
+    }
+    if (gave_up) {
+        const long long c0 = clock64();
+        while (clock64() - c0 < 20000000ll) {}
+    }
+}
+
+int h_stride_of(int inner) { return (inner + 3) / 4 * 4; }
+long long plan_bytes() { return ((long long)sizeof(Plan) + 255) / 256 * 256; }
+
+}  // namespace
+
+long long moe_fp8_workspace_bytes(int inner, int top, int T) { return plan_bytes() + 4ll * T * top * h_stride_of(inner); }
+
+cudaError_t launch_moe_fp8(const MoeFp8 &L, void *ws, cudaStream_t st)
+{
+    Params P;
+    P.L = L;
+    P.plan = reinterpret_cast<Plan *>(ws);
+    P.h = reinterpret_cast<float *>(reinterpret_cast<uint8_t *>(ws) + plan_bytes());
+    P.h_stride = h_stride_of(L.inner);
+    const int sms = device_sm_count();
+    const long long pitch_h = fp8_row_bytes(L.hidden), pitch_i = fp8_row_bytes(L.inner);
+    const int down_all = ceil_div(L.hidden, GROUP), down_grid = down_all < sms ? down_all : sms, most = ceil_div(down_all, down_grid);
+    const int down_kbs = ceil_div(L.inner, FP8_BLOCK);
+    P.down_passes = ceil_div(most, DOWN_GROUPS);
+    P.down_groups = ceil_div(most, P.down_passes);
+    P.down_run_shift = 0;
+    if (L.inner % FP8_BLOCK == 0 && P.down_groups * 2 <= 4 && (long long)down_kbs * L.top >= 2 * WARPS) P.down_run_shift = 1;
+    CUtensorMap gate, up, down;
+    const long long rows_i = (long long)L.experts * L.inner, rows_h = (long long)L.experts * L.hidden;
+    if (!encode_tensor_map(&gate, CU_TENSOR_MAP_DATA_TYPE_UINT8, L.gate, pitch_h, rows_i, pitch_h, 0, 0, FP8_BLOCK, UNITS * GROUP, 1, CU_TENSOR_MAP_SWIZZLE_128B) ||
+        !encode_tensor_map(&up, CU_TENSOR_MAP_DATA_TYPE_UINT8, L.up, pitch_h, rows_i, pitch_h, 0, 0, FP8_BLOCK, UNITS * GROUP, 1, CU_TENSOR_MAP_SWIZZLE_128B) ||
+        !(P.down_run_shift > 0 ? encode_tensor_map(&down, CU_TENSOR_MAP_DATA_TYPE_UINT8, L.down, FP8_BLOCK, rows_h, pitch_i, down_kbs, FP8_BLOCK, FP8_BLOCK,
+                                                   P.down_groups * GROUP, 1 << P.down_run_shift, CU_TENSOR_MAP_SWIZZLE_128B)
+                               : encode_tensor_map(&down, CU_TENSOR_MAP_DATA_TYPE_UINT8, L.down, pitch_i, rows_h, pitch_i, 0, 0, FP8_BLOCK, P.down_groups * GROUP, 1,
+                                                   CU_TENSOR_MAP_SWIZZLE_128B)))
+        return cudaErrorNotSupported;
+
+    const bool vec = L.hidden % 8 == 0;
+    auto kern = L.x_dtype == VPTQ_DTYPE_BF16 ? (vec ? moe_gate_up_kernel<VPTQ_DTYPE_BF16, true> : moe_gate_up_kernel<VPTQ_DTYPE_BF16, false>)
+                                             : (vec ? moe_gate_up_kernel<VPTQ_DTYPE_FP16, true> : moe_gate_up_kernel<VPTQ_DTYPE_FP16, false>);
+    cudaError_t e = allow_dynamic_smem(reinterpret_cast<const void *>(kern), UP_SMEM);
+    if (e != cudaSuccess) return e;
+    const int clusters = max_resident_clusters(reinterpret_cast<const void *>(kern), CLUSTER, THREADS, UP_SMEM);
+    if (clusters < 1) return cudaErrorNotSupported;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(CLUSTER * clusters));
+    cfg.blockDim = dim3(THREADS);
+    cfg.dynamicSmemBytes = UP_SMEM;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = CLUSTER; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr; cfg.numAttrs = pdl_enabled("moe_fp8") ? 2 : 1;
+    e = cudaLaunchKernelEx(&cfg, kern, gate, up, P);
+    if (e != cudaSuccess) return e;
+
+    const int stage = P.down_groups * GROUP_BYTES << P.down_run_shift;
+    const int fixed = WARPS * down_slot_floats(L.T, P.down_groups) * 4 + (int)sizeof(Plan) + WARPS * 8 * 8;
+    int stages = (232448 - fixed) / (WARPS * stage);
+    if (stages > 8) stages = 8;
+    const int smem = stages * WARPS * stage + fixed;
+    e = allow_dynamic_smem(reinterpret_cast<const void *>(moe_down_kernel), 232448);
+    if (e != cudaSuccess) return e;
+    cfg.gridDim = dim3((unsigned)down_grid);
+    cfg.dynamicSmemBytes = smem;
+    cfg.attrs = attr + 1; cfg.numAttrs = pdl_enabled("moe_fp8") ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, moe_down_kernel, down, P, stages);
+}
+
+}  // namespace vptq

@@ -357,6 +357,60 @@ PyObject *py_linear_fp8(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
+// an operand of all experts: [experts][rows][cols rounded up to 16] with [experts][ceil(rows / 128)][ceil(cols / 128)] FP32 scales
+bool is_expert_operand(const at::Tensor &q, const at::Tensor &scale, int64_t experts, int64_t rows, int64_t cols)
+{
+    return plain(q) && plain(scale) && q.scalar_type() == at::kFloat8_e4m3fn && scale.scalar_type() == at::kFloat && q.dim() == 3 && scale.dim() == 3 &&
+           q.size(0) == experts && q.size(1) == rows && q.size(2) == (cols + 15) / 16 * 16 && scale.size(0) == experts &&
+           scale.size(1) == (rows + 127) / 128 && scale.size(2) == (cols + 127) / 128;
+}
+
+// moe_fp8(x, router, gate, gate_scale, up, up_scale, down, down_scale, top_k, renormalize, out or None, workspace or None) -> out
+PyObject *py_moe_fp8(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (n != 12) { PyErr_SetString(PyExc_TypeError, "moe_fp8 takes 12 arguments"); return nullptr; }
+    const at::Tensor *t[8], *out = nullptr;
+    for (int i = 0; i < 8; i++)
+        if (!(t[i] = tensor_of(a[i]))) return nullptr;
+    const long top = PyLong_AsLong(a[8]);
+    const int renormalize = PyObject_IsTrue(a[9]);
+    if ((top == -1 && PyErr_Occurred()) || renormalize < 0 || (a[10] != Py_None && !(out = tensor_of(a[10])))) return nullptr;
+    const at::Tensor &x = *t[0], &router = *t[1], &gate = *t[2];
+    if (!plain(x) || !plain(router) || x.dim() != 2 || router.dim() != 2 || gate.dim() != 3 || router.scalar_type() != x.scalar_type() || router.size(1) != x.size(1))
+        return assertion("x [T][hidden], router [experts][hidden] of one type, gate [experts][inner][pitch], contiguous tensors of the current device");
+    const int64_t T = x.size(0), hidden = x.size(1), experts = router.size(0), inner = gate.size(1);
+    if (T > MAX_INT || hidden > MAX_INT || experts > MAX_INT || inner > MAX_INT) return fail(VPTQ_E_SHAPE);
+    if (!is_expert_operand(gate, *t[3], experts, inner, hidden) || !is_expert_operand(*t[4], *t[5], experts, inner, hidden) ||
+        !is_expert_operand(*t[6], *t[7], experts, hidden, inner))
+        return assertion("gate, up [experts][inner][pitch(hidden)], down [experts][hidden][pitch(inner)] in e4m3 with their FP32 block scales");
+    vptq_moe_desc d = {(int32_t)hidden, (int32_t)inner, (int32_t)experts, (int32_t)(top > MAX_INT || top < 0 ? 0 : top), code_of(x.scalar_type()),
+                       code_of(out ? out->scalar_type() : x.scalar_type()), renormalize ? VPTQ_FLAG_MOE_RENORMALIZE : 0};
+    if (out && (!plain(*out) || out->dim() != 2 || out->size(0) != T || out->size(1) != hidden)) return assertion("out [T][hidden], contiguous");
+    void *ws;
+    size_t ws_bytes;
+    if (!workspace_of(a[11], &ws, &ws_bytes)) return nullptr;
+    const int64_t need = vptq_moe_fp8_workspace_bytes(&d, (int32_t)T);
+    if (need < 0) return fail((int)need);
+    const vptq_moe_ptrs p = {router.data_ptr(), static_cast<const uint8_t *>(gate.data_ptr()), static_cast<const uint8_t *>(t[4]->data_ptr()),
+                             static_cast<const uint8_t *>(t[6]->data_ptr()), static_cast<const float *>(t[3]->data_ptr()),
+                             static_cast<const float *>(t[5]->data_ptr()), static_cast<const float *>(t[7]->data_ptr())};
+    return guarded([&]() -> PyObject * {
+        at::Tensor own, result = out ? *out : at::empty({T, hidden}, x.options());
+        if (ws == nullptr) {
+            own = at::empty({need}, x.options().dtype(at::kByte));
+            ws = own.data_ptr();
+            ws_bytes = (size_t)need;
+        }
+        int rc;
+        Py_BEGIN_ALLOW_THREADS
+        rc = vptq_moe_fp8(&d, &p, x.data_ptr(), (int32_t)T, result.data_ptr(), ws, ws_bytes, current_stream());
+        Py_END_ALLOW_THREADS
+        if (rc != VPTQ_OK) return fail(rc);
+        if (out) { Py_INCREF(a[10]); return a[10]; }
+        return THPVariable_Wrap(result);
+    });
+}
+
 PyObject *py_set_error_class(PyObject *, PyObject *cls)
 {
     Py_INCREF(cls);
@@ -372,6 +426,7 @@ PyMethodDef methods[] = {
     {"fp8_quantize", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_fp8_quantize)), METH_FASTCALL, "vptq_fp8_quantize on torch tensors"},
     {"dequant_fp8", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_dequant_fp8)), METH_FASTCALL, "vptq_dequant_fp8 on torch tensors"},
     {"linear_fp8", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_linear_fp8)), METH_FASTCALL, "vptq_linear_fp8 on torch tensors"},
+    {"moe_fp8", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_moe_fp8)), METH_FASTCALL, "vptq_moe_fp8 on torch tensors"},
     {"set_error_class", py_set_error_class, METH_O, "exception raised for VPTQ_E_* codes"},
     {nullptr, nullptr, 0, nullptr}};
 

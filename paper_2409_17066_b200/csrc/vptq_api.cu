@@ -10,6 +10,7 @@
 #include "assign.cuh"
 #include "prepared.cuh"
 #include "fp8.cuh"
+#include "moe_fp8.cuh"
 
 #include <vector>
 
@@ -635,6 +636,47 @@ int vptq_linear_fp8_launches(const vptq_fp8_desc *desc, int32_t B)
     const int rc = check_fp8_desc(desc, B);
     if (rc != VPTQ_OK) return rc;
     return linear_fp8_launches(B, desc->x_dtype);
+}
+
+static int check_moe_desc(const vptq_moe_desc *d, int32_t T)
+{
+    if (d == nullptr) return VPTQ_E_NULL;
+    if (d->hidden <= 0 || d->inner <= 0 || d->n_experts <= 0 || d->n_experts > VPTQ_MOE_MAX_EXPERTS || T <= 0 || T > VPTQ_MOE_MAX_TOKENS) return VPTQ_E_SHAPE;
+    if (d->top_k <= 0 || d->top_k > VPTQ_MOE_MAX_TOP || d->top_k > d->n_experts) return VPTQ_E_SHAPE;
+    if ((int64_t)d->n_experts * d->inner >= FP8_MAX_SIZE || (int64_t)d->n_experts * d->hidden >= FP8_MAX_SIZE) return VPTQ_E_SHAPE;
+    if (d->x_dtype != VPTQ_DTYPE_FP16 && d->x_dtype != VPTQ_DTYPE_BF16) return VPTQ_E_UNSUPPORTED;
+    if (d->out_dtype != VPTQ_DTYPE_FP16 && d->out_dtype != VPTQ_DTYPE_BF16 && d->out_dtype != VPTQ_DTYPE_FP32) return VPTQ_E_UNSUPPORTED;
+    if (d->flags & ~(VPTQ_FLAG_MOE_RENORMALIZE | VPTQ_FLAG_CONCURRENT | VPTQ_FLAG_DETERMINISTIC)) return VPTQ_E_UNSUPPORTED;
+    return VPTQ_OK;
+}
+
+int64_t vptq_moe_fp8_workspace_bytes(const vptq_moe_desc *desc, int32_t T)
+{
+    const int rc = check_moe_desc(desc, T);
+    if (rc != VPTQ_OK) return rc;
+    return moe_fp8_workspace_bytes(desc->inner, desc->top_k, T);
+}
+
+int vptq_moe_fp8(const vptq_moe_desc *desc, const vptq_moe_ptrs *p, const void *x, int32_t T, void *out,
+                 void *workspace, size_t workspace_bytes, void *stream)
+{
+    const int rc = check_moe_desc(desc, T);
+    if (rc != VPTQ_OK) return rc;
+    if (p == nullptr) return VPTQ_E_NULL;
+    const void *all[9] = {p->router, p->gate, p->up, p->down, p->gate_scale, p->up_scale, p->down_scale, x, out};
+    for (int i = 0; i < 9; i++)
+        if (all[i] == nullptr) return VPTQ_E_NULL;
+    for (int i = 0; i < 9; i++)
+        if (!aligned16(all[i])) return VPTQ_E_ALIGN;
+    if (workspace == nullptr || (int64_t)workspace_bytes < moe_fp8_workspace_bytes(desc->inner, desc->top_k, T)) return VPTQ_E_WORKSPACE;
+    if ((reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return VPTQ_E_ALIGN;
+    MoeFp8 L;
+    L.hidden = desc->hidden; L.inner = desc->inner; L.experts = desc->n_experts; L.top = desc->top_k; L.T = T;
+    L.x_dtype = desc->x_dtype; L.out_dtype = desc->out_dtype; L.renormalize = (desc->flags & VPTQ_FLAG_MOE_RENORMALIZE) ? 1 : 0;
+    L.x = x; L.router = p->router; L.gate = p->gate; L.up = p->up; L.down = p->down;
+    L.gate_scale = p->gate_scale; L.up_scale = p->up_scale; L.down_scale = p->down_scale; L.out = out;
+    const cudaError_t e = launch_moe_fp8(L, workspace, reinterpret_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? VPTQ_OK : cuda_fail(e);
 }
 
 const char *vptq_status_string(int code)

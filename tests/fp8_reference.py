@@ -51,3 +51,27 @@ def random_weight(rows, cols, gen, device):
     q[:, :cols] = (torch.randn(rows, cols, generator=gen, device=device) * 90).clamp(-448, 448).to(torch.float8_e4m3fn)
     scale = (torch.rand(-(-rows // BLOCK), -(-cols // BLOCK), generator=gen, device=device) + 0.5) * 1e-3
     return q, scale
+
+
+def moe(x, router, gate, gate_scale, up, up_scale, down, down_scale, top_k, renormalize):
+    """A mixture-of-experts layer in FP64; the choices are those of the FP64 logits (ties: the lowest expert)."""
+    hidden, inner = x.shape[1], gate.shape[1]
+    logits = x.double() @ router.double().t()
+    p = torch.softmax(logits, dim=1)
+    out = torch.zeros(x.shape, dtype=torch.float64, device=x.device)
+    q, s = quantize(x, 1)
+    xv = q * expand(s, x.shape[0], hidden, 1)
+    for t in range(x.shape[0]):
+        chosen = torch.sort(logits[t], descending=True, stable=True).indices[:top_k].tolist()
+        total = sum(p[t, e] for e in chosen) if renormalize else 1.0
+        for e in chosen:
+            g = xv[t:t + 1] @ values(gate[e], gate_scale[e], hidden, 128).t()
+            u = xv[t:t + 1] @ values(up[e], up_scale[e], hidden, 128).t()
+            hq, hs = quantize(g / (1 + torch.exp(-g)) * u, 1)
+            out[t] += (p[t, e] / total * ((hq * expand(hs, 1, inner, 1)) @ values(down[e], down_scale[e], inner, 128).t()))[0]
+    return out
+
+
+def random_experts(experts, rows, cols, gen, device):
+    both = [random_weight(rows, cols, gen, device) for _ in range(experts)]
+    return torch.stack([q.view(torch.uint8) for q, _ in both]).view(torch.float8_e4m3fn), torch.stack([s for _, s in both])

@@ -109,3 +109,36 @@ def test_host_tensors_are_refused_before_any_call(b):
         b.vptq_linear_fp8(None, w, s)
     with pytest.raises(b.VptqError):
         b.vptq_fp8_quantize(x, 64)
+
+
+def test_moe_fp8_refusals(b):
+    f, p = b.lib.vptq_moe_fp8, 0x1000
+    names = [n for n, _ in b.MoePtrs._fields_]
+    ptrs = b.MoePtrs(*[p] * 7)
+    d = b.make_moe_desc(256, 128, 8, 2)
+    size = lambda d, T=1: b.lib.vptq_moe_fp8_workspace_bytes(C.byref(d), T)  # noqa: E731
+    call = lambda d, T=1, ptrs=ptrs, x=p, out=p, ws=p, n=1 << 30: f(C.byref(d), C.byref(ptrs), x, T, out, ws, n, None)  # noqa: E731
+    assert f(None, C.byref(ptrs), p, 1, p, p, 1 << 30, None) == b.E_NULL and f(C.byref(d), None, p, 1, p, p, 1 << 30, None) == b.E_NULL
+    assert call(d, x=None) == b.E_NULL and call(d, out=None) == b.E_NULL
+    assert call(d, x=p + 2) == b.E_ALIGN and call(d, out=p + 2) == b.E_ALIGN and call(d, ws=p + 16) == b.E_ALIGN
+    for i, name in enumerate(names):
+        for value, code in ((None, b.E_NULL), (p + 4, b.E_ALIGN)):
+            args = [p] * 7
+            args[i] = value
+            assert call(d, ptrs=b.MoePtrs(*args)) == code, name
+    need = size(d, 3)
+    assert need >= 3 * 2 * 128 * 4 and size(d, 4) > need
+    assert call(d, T=3, ws=None) == b.E_WORKSPACE and call(d, T=3, n=need - 1) == b.E_WORKSPACE
+    for T in (0, -1, b.MOE_MAX_TOKENS + 1):
+        assert call(d, T=T) == b.E_SHAPE and size(d, T) == b.E_SHAPE
+    for bad in ((0, 128, 8, 2), (256, 0, 8, 2), (256, 128, 0, 2), (256, 128, 8, 0), (256, 128, 8, 9), (256, 128, b.MOE_MAX_EXPERTS + 1, 2),
+                (256, 128, 64, b.MOE_MAX_TOP + 1), (1 << 24, 128, 64, 2), (256, 1 << 24, 64, 2)):
+        assert call(b.make_moe_desc(*bad)) == b.E_SHAPE, bad
+    assert call(b.make_moe_desc(256, 128, 8, 2, flags=b.FLAG_SCALE_BIAS)) == b.E_UNSUPPORTED
+    assert call(b.make_moe_desc(256, 128, 8, 2, x_dtype="fp32")) == b.E_UNSUPPORTED
+    bad = b.make_moe_desc(256, 128, 8, 2)
+    bad.out_dtype = b.DTYPE_E4M3
+    assert call(bad) == b.E_UNSUPPORTED
+    x = torch.zeros(1, 256, dtype=torch.float16)
+    with pytest.raises(AssertionError):
+        b.vptq_moe_fp8(x, x, *[x[None]] * 6, 2)
