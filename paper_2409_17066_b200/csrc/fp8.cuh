@@ -80,31 +80,43 @@ template <> struct Act<VPTQ_DTYPE_FP32> {
     static __device__ __forceinline__ float one(const void *p, long long i) { return reinterpret_cast<const float *>(p)[i]; }
 };
 
-// N consecutive values of a row, the first at column c of `cols` (zeros beyond); VEC: 16-byte loads (c and the row are aligned for
-// them, and the values beyond `cols` in the last of them belong to the row's next block or are not read: cols % (16 / bytes) == 0).
-template <int DT, bool VEC, int N>
-__device__ __forceinline__ void load_values(const void *row, int c, int cols, float (&v)[N])
+// Eight consecutive values of a row, as they lie in memory (16-byte loads: VEC) or one by one as FP32.
+template <int DT, bool VEC> struct Eight { float v[8]; };
+template <> struct Eight<VPTQ_DTYPE_FP16, true> { uint4 q; };
+template <> struct Eight<VPTQ_DTYPE_BF16, true> { uint4 q; };
+
+// ... the first at column c of `cols`, zeros beyond; VEC: c and the row are aligned for it and cols is a multiple of a load's values
+template <int DT, bool VEC>
+__device__ __forceinline__ Eight<DT, VEC> load_eight(const void *row, int c, int cols)
 {
+    Eight<DT, VEC> e;
     if constexpr (VEC && DT == VPTQ_DTYPE_FP32) {
 #pragma unroll
-        for (int i = 0; i < N; i += 4) {
+        for (int i = 0; i < 8; i += 4) {
             const float4 q = c + i < cols ? __ldg(reinterpret_cast<const float4 *>(reinterpret_cast<const float *>(row) + c + i)) : make_float4(0.f, 0.f, 0.f, 0.f);
-            v[i] = q.x; v[i + 1] = q.y; v[i + 2] = q.z; v[i + 3] = q.w;
+            e.v[i] = q.x; e.v[i + 1] = q.y; e.v[i + 2] = q.z; e.v[i + 3] = q.w;
         }
     } else if constexpr (VEC) {
+        e.q = c < cols ? __ldg(reinterpret_cast<const uint4 *>(reinterpret_cast<const uint16_t *>(row) + c)) : make_uint4(0, 0, 0, 0);
+    } else {
 #pragma unroll
-        for (int i = 0; i < N; i += 8) {
-            const uint4 q = c + i < cols ? __ldg(reinterpret_cast<const uint4 *>(reinterpret_cast<const uint16_t *>(row) + c + i)) : make_uint4(0, 0, 0, 0);
-            const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+        for (int i = 0; i < 8; i++) e.v[i] = c + i < cols ? Act<DT>::one(row, c + i) : 0.f;
+    }
+    return e;
+}
+template <int DT, bool VEC>
+__device__ __forceinline__ void values_of(const Eight<DT, VEC> &e, float (&v)[8])
+{
+    if constexpr (VEC && DT != VPTQ_DTYPE_FP32) {
+        const uint32_t w[4] = {e.q.x, e.q.y, e.q.z, e.q.w};
 #pragma unroll
-            for (int j = 0; j < 4; j++) {
-                const float2 f = Act<DT>::two(w[j]);
-                v[i + 2 * j] = f.x; v[i + 2 * j + 1] = f.y;
-            }
+        for (int j = 0; j < 4; j++) {
+            const float2 f = Act<DT>::two(w[j]);
+            v[2 * j] = f.x; v[2 * j + 1] = f.y;
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < N; i++) v[i] = c + i < cols ? Act<DT>::one(row, c + i) : 0.f;
+        for (int j = 0; j < 8; j++) v[j] = e.v[j];
     }
 }
 
@@ -126,6 +138,12 @@ __device__ __forceinline__ uint32_t magnitude(const float (&v)[N])
 #pragma unroll
     for (int i = 0; i < N; i++) m = max(m, __float_as_uint(v[i]) & 0x7FFFFFFFu);
     return m;
+}
+template <int DT, bool VEC>
+__device__ __forceinline__ uint32_t magnitude(const Eight<DT, VEC> &e)
+{
+    if constexpr (VEC && DT != VPTQ_DTYPE_FP32) return magnitude16<DT>(max16(max16(e.q.x, e.q.y), max16(e.q.z, e.q.w)));
+    else return magnitude<8>(e.v);
 }
 #endif
 

@@ -23,22 +23,23 @@ struct QuantizeParams {
     uint8_t *q;
     float *scale;
     int early;
+    long long step;            // rows form: blocks that all half warps take at a time, and the same as rows and column blocks
+    int step_rows, step_cols;
 };
 
-// eight values at column c of a row of q: pad columns (zeros) are written up to the row's end
-__device__ __forceinline__ void store_eight(uint8_t *row, long long pitch, int c, const float (&v)[8], float factor)
+// eight values at column c of a row of q; beyond `cols` zeros are written up to the row's end, whatever the factor
+template <int DT, bool VEC>
+__device__ __forceinline__ void store_eight(uint8_t *row, long long pitch, int c, int cols, const Eight<DT, VEC> &e, float factor)
 {
     if (c >= pitch) return;
+    float v[8];
+    values_of(e, v);
     uint2 o;
     o.x = fp8_quad(v[0] * factor, v[1] * factor, v[2] * factor, v[3] * factor);
     o.y = fp8_quad(v[4] * factor, v[5] * factor, v[6] * factor, v[7] * factor);
     *reinterpret_cast<uint2 *>(row + c) = o;
-}
-
-// (a value beyond the row's end is 0, and 0 * factor is not when the factor is infinite or NaN: the pad bytes are zeros all the same)
-__device__ __forceinline__ void clear_pad(uint8_t *row, long long pitch, int c, int cols)
-{
-    for (int i = max(c, cols); i < c + 8 && i < pitch; i++) row[i] = 0;
+    if (c + 8 > cols)
+        for (int i = max(c, cols); i < c + 8; i++) row[i] = 0;         // (0 * factor is no zero when the factor is a NaN)
 }
 
 template <int DT, bool VEC, int UNROLL>
@@ -47,39 +48,35 @@ quantize_rows_kernel(const __grid_constant__ QuantizeParams P)
 {
     if (P.early) pdl_launch_dependents();
     pdl_wait();
-    const long long n = (long long)P.rows * P.col_blocks;
-    const int lane = threadIdx.x & 15;
-    const long long first = ((long long)blockIdx.x * THREADS + threadIdx.x) >> 4, step = ((long long)gridDim.x * THREADS) >> 4;
+    // blocks of the matrix, rows after one another, are dealt out over the half warps; row and column block are counted on without divisions
+    const int lane = threadIdx.x & 15, half = (threadIdx.x >> 4) & 1;
+    const long long first = ((long long)blockIdx.x * THREADS + threadIdx.x) >> 4;
+    int row = (int)(first / P.col_blocks), cb = (int)(first % P.col_blocks);
     // (a warp's two halves run the same number of rounds: shuffles)
-    for (long long b0 = first; b0 - ((threadIdx.x >> 4) & 1) < n; b0 += step * UNROLL) {
-        float v[UNROLL][8];
+    const long long n = (long long)P.rows * P.col_blocks;
+    for (long long b0 = first - half; b0 < n; b0 += P.step * UNROLL) {
+        Eight<DT, VEC> e[UNROLL];
+        int rows[UNROLL], cols[UNROLL];
         uint32_t m[UNROLL];
 #pragma unroll
         for (int u = 0; u < UNROLL; u++) {
-            const long long b = b0 + u * step, row = b / P.col_blocks;
-            const int c = (int)(b % P.col_blocks) * FP8_BLOCK + lane * 8;
-            if (b < n) {
-                load_values<DT, VEC, 8>(reinterpret_cast<const uint8_t *>(P.x) + row * P.ld * Act<DT>::BYTES, c, P.cols, v[u]);
-            } else {
-#pragma unroll
-                for (int i = 0; i < 8; i++) v[u][i] = 0.f;
-            }
+            rows[u] = row; cols[u] = cb * FP8_BLOCK + lane * 8;
+            e[u] = load_eight<DT, VEC>(reinterpret_cast<const uint8_t *>(P.x) + (row < P.rows ? row : 0) * P.ld * Act<DT>::BYTES, row < P.rows ? cols[u] : P.cols, P.cols);
+            cb += P.step_cols; row += P.step_rows;
+            if (cb >= P.col_blocks) { cb -= P.col_blocks; row++; }
         }
 #pragma unroll
         for (int u = 0; u < UNROLL; u++) {
-            m[u] = magnitude<8>(v[u]);
+            m[u] = magnitude(e[u]);
 #pragma unroll
             for (int o = 8; o > 0; o >>= 1) m[u] = max(m[u], __shfl_xor_sync(0xffffffffu, m[u], o));
         }
 #pragma unroll
         for (int u = 0; u < UNROLL; u++) {
-            const long long b = b0 + u * step, row = b / P.col_blocks;
-            if (b >= n) continue;
-            const int c = (int)(b % P.col_blocks) * FP8_BLOCK + lane * 8;
+            if (rows[u] >= P.rows) continue;
             const Fp8Scale s = fp8_scale(__uint_as_float(m[u]));
-            store_eight(P.q + row * P.pitch, P.pitch, c, v[u], s.factor);
-            if (c + 8 > P.cols) clear_pad(P.q + row * P.pitch, P.pitch, c, P.cols);
-            if (lane == 0) P.scale[b] = s.scale;
+            store_eight(P.q + rows[u] * P.pitch, P.pitch, cols[u], P.cols, e[u], s.factor);
+            if (lane == 0) P.scale[(long long)rows[u] * P.col_blocks + cols[u] / FP8_BLOCK] = s.scale;
         }
     }
 }
@@ -93,20 +90,15 @@ quantize_blocks_kernel(const __grid_constant__ QuantizeParams P)
     const int lane = threadIdx.x & 15, r0 = threadIdx.x >> 4;
     const int cb = blockIdx.x % P.col_blocks, rb = blockIdx.x / P.col_blocks;
     const int c = cb * FP8_BLOCK + lane * 8;
-    float v[ROUNDS][8];
+    Eight<DT, VEC> v[ROUNDS];
 #pragma unroll
     for (int i = 0; i < ROUNDS; i++) {
         const long long row = (long long)rb * FP8_BLOCK + i * ROWS + r0;
-        if (row < P.rows) {
-            load_values<DT, VEC, 8>(reinterpret_cast<const uint8_t *>(P.x) + row * P.ld * Act<DT>::BYTES, c, P.cols, v[i]);
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; j++) v[i][j] = 0.f;
-        }
+        v[i] = load_eight<DT, VEC>(reinterpret_cast<const uint8_t *>(P.x) + (row < P.rows ? row : 0) * P.ld * Act<DT>::BYTES, row < P.rows ? c : P.cols, P.cols);
     }
     uint32_t m = 0;
 #pragma unroll
-    for (int i = 0; i < ROUNDS; i++) m = max(m, magnitude<8>(v[i]));
+    for (int i = 0; i < ROUNDS; i++) m = max(m, magnitude(v[i]));
     m = __reduce_max_sync(0xffffffffu, m);
     if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = m;
     __syncthreads();
@@ -118,9 +110,17 @@ quantize_blocks_kernel(const __grid_constant__ QuantizeParams P)
     for (int i = 0; i < ROUNDS; i++) {
         const long long row = (long long)rb * FP8_BLOCK + i * ROWS + r0;
         if (row >= P.rows) break;
-        store_eight(P.q + row * P.pitch, P.pitch, c, v[i], s.factor);
-        if (c + 8 > P.cols) clear_pad(P.q + row * P.pitch, P.pitch, c, P.cols);
+        store_eight(P.q + row * P.pitch, P.pitch, c, P.cols, v[i], s.factor);
     }
+}
+
+template <int DT, bool VEC, int UNROLL>
+cudaError_t launch_rows(QuantizeParams P, long long ctas, cudaStream_t st)
+{
+    P.step = ctas * (THREADS / 16);
+    P.step_rows = (int)(P.step / P.col_blocks);
+    P.step_cols = (int)(P.step % P.col_blocks);
+    return launch_dependent("fp8_quantize", quantize_rows_kernel<DT, VEC, UNROLL>, (int)ctas, THREADS, 0, st, P);
 }
 
 template <int DT, bool VEC>
@@ -135,9 +135,8 @@ cudaError_t launch(const QuantizeParams &P, int block_rows, cudaStream_t st)
     const long long n = (long long)P.rows * P.col_blocks, per_cta = THREADS / 16;
     const long long resident = (long long)device_sm_count() * 8;
     const long long ctas = (n + per_cta - 1) / per_cta;
-    if (ctas <= resident) return launch_dependent("fp8_quantize", quantize_rows_kernel<DT, VEC, 1>, (int)ctas, THREADS, 0, st, P);
-    const long long want = (ctas + 3) / 4;
-    return launch_dependent("fp8_quantize", quantize_rows_kernel<DT, VEC, 4>, (int)(want < resident ? want : resident), THREADS, 0, st, P);
+    if (ctas <= resident) return launch_rows<DT, VEC, 1>(P, ctas, st);
+    return launch_rows<DT, VEC, 4>(P, (ctas + 3) / 4 < resident ? (ctas + 3) / 4 : resident, st);
 }
 
 }  // namespace

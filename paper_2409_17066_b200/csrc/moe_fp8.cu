@@ -87,11 +87,11 @@ __device__ __forceinline__ void router(const MoeFp8 &L, float *logits, uint32_t 
 #pragma unroll 4
             for (int c = lane * 8; c < L.hidden; c += 256) {
                 float a[8], b[8];
-                load_values<DT, true, 8>(w, c, L.hidden, a);
+                values_of(load_eight<DT, true>(w, c, L.hidden), a);
 #pragma unroll
                 for (int j = 0; j < 4; j++) {
                     if (t0 + j >= L.T) break;
-                    load_values<DT, true, 8>(x[j], c, L.hidden, b);
+                    values_of(load_eight<DT, true>(x[j], c, L.hidden), b);
 #pragma unroll
                     for (int q = 0; q < 8; q++) sum[j] = __fmaf_rn(a[q], b[q], sum[j]);
                 }
