@@ -70,49 +70,85 @@ __device__ __forceinline__ void store_peer(float *at, uint32_t rank, float v)
     asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(a), "f"(v) : "memory");
 }
 
-// logits of this CTA's quarter of the experts, to all four CTAs: a warp an expert and up to four tokens at a time
-template <int DT, bool VEC>
-__device__ __forceinline__ void router(const MoeFp8 &L, float *logits, uint32_t rank, int warp, int lane)
+// One warp: the products of an expert's router row with N tokens over columns [c0, c1); `ahead` loads of each row in flight.
+template <int DT, bool VEC, int N>
+__device__ __forceinline__ void router_products(const uint8_t *w, const uint8_t *x, long long row_bytes, int last_token, int c0, int c1, int cols, int lane, float (&sum)[4])
 {
-    const int n = (L.experts + CLUSTER - 1) / CLUSTER, quads = (L.T + 3) / 4;
-    for (int i = warp; i < n * quads; i += WARPS) {
-        const int e = (int)rank + CLUSTER * (i / quads), t0 = i % quads * 4;
-        if (e >= L.experts) continue;                     // (whole warps)
-        const uint8_t *w = reinterpret_cast<const uint8_t *>(L.router) + (long long)e * L.hidden * 2;
-        const uint8_t *x[4];
+    const uint8_t *rows[N];
 #pragma unroll
-        for (int j = 0; j < 4; j++) x[j] = reinterpret_cast<const uint8_t *>(L.x) + (long long)min(t0 + j, L.T - 1) * L.hidden * 2;
-        float sum[4] = {};
-        if (VEC) {
-#pragma unroll 4
-            for (int c = lane * 8; c < L.hidden; c += 256) {
-                float a[8], b[8];
-                values_of(load_eight<DT, true>(w, c, L.hidden), a);
+    for (int j = 0; j < N; j++) rows[j] = x + min(j, last_token) * row_bytes;          // (sums of tokens that are not there are dropped)
+    if constexpr (VEC) {
+        constexpr int AHEAD = N == 1 ? 4 : 2;
+#pragma unroll 1
+        for (int c = c0 + lane * 8; c < c1; c += 256 * AHEAD) {
+            Eight<DT, true> a[AHEAD], b[AHEAD][N];
 #pragma unroll
-                for (int j = 0; j < 4; j++) {
-                    if (t0 + j >= L.T) break;
-                    values_of(load_eight<DT, true>(x[j], c, L.hidden), b);
+            for (int u = 0; u < AHEAD; u++) {
+                const int at = c + 256 * u < c1 ? c + 256 * u : cols;                  // (columns beyond the end read as zeros)
+                a[u] = load_eight<DT, true>(w, at, cols);
 #pragma unroll
-                    for (int q = 0; q < 8; q++) sum[j] = __fmaf_rn(a[q], b[q], sum[j]);
+                for (int j = 0; j < N; j++) b[u][j] = load_eight<DT, true>(rows[j], at, cols);
+            }
+#pragma unroll
+            for (int u = 0; u < AHEAD; u++) {
+                float f[8], v[8];
+                values_of(a[u], f);
+#pragma unroll
+                for (int j = 0; j < N; j++) {
+                    values_of(b[u][j], v);
+#pragma unroll
+                    for (int q = 0; q < 8; q++) sum[j] = __fmaf_rn(f[q], v[q], sum[j]);
                 }
             }
-        } else {
-            for (int c = lane; c < L.hidden; c += 32) {
-                const float a = Act<DT>::one(w, c);
+        }
+    } else {
+        for (int c = c0 + lane; c < c1; c += 32) {
+            const float a = Act<DT>::one(w, c);
+#pragma unroll
+            for (int j = 0; j < N; j++) sum[j] = __fmaf_rn(a, Act<DT>::one(rows[j], c), sum[j]);
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < N; j++)
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], o);
+}
+
+// logits of this CTA's quarter of the experts, to all four CTAs: an expert and up to four tokens are a task, a warp's or, with few of them,
+// shared by `parts` warps, a run of columns each
+template <int DT, bool VEC>
+__device__ __forceinline__ void router(const MoeFp8 &L, float *logits, float (*partial)[4], uint32_t rank, int warp, int lane)
+{
+    const int quads = (L.T + 3) / 4, tasks = (L.experts + CLUSTER - 1) / CLUSTER * quads;
+    int shift = 0;                                        // parts = 2^shift
+    while ((tasks << (shift + 1)) <= WARPS) shift++;
+    const int width = ((L.hidden + (1 << shift) - 1 >> shift) + 255) / 256 * 256, part = warp & ((1 << shift) - 1);
+    for (int task = warp >> shift; task < tasks; task += WARPS >> shift) {
+        const int e = (int)rank + CLUSTER * (task / quads), t0 = task % quads * 4;
+        float sum[4] = {};
+        if (e < L.experts) {
+            const uint8_t *w = reinterpret_cast<const uint8_t *>(L.router) + (long long)e * L.hidden * 2;
+            const uint8_t *x = reinterpret_cast<const uint8_t *>(L.x) + (long long)t0 * L.hidden * 2;
+            const int c0 = part * width, c1 = min(L.hidden, c0 + width);
+            if (L.T == 1) router_products<DT, VEC, 1>(w, x, 0, 0, c0, c1, L.hidden, lane, sum);
+            else router_products<DT, VEC, 4>(w, x, 2ll * L.hidden, L.T - 1 - t0, c0, c1, L.hidden, lane, sum);
+        }
+        if (shift > 0) {                                  // (a single round)
+            if (lane == 0) *reinterpret_cast<float4 *>(partial[warp]) = make_float4(sum[0], sum[1], sum[2], sum[3]);
+            asm volatile("bar.sync 2, %0;" ::"n"(THREADS) : "memory");
+            if (part == 0) {
 #pragma unroll
                 for (int j = 0; j < 4; j++)
-                    if (t0 + j < L.T) sum[j] = __fmaf_rn(a, Act<DT>::one(x[j], c), sum[j]);
+                    for (int q = 1; q < 1 << shift; q++) sum[j] += partial[warp + q][j];
             }
         }
-#pragma unroll
-        for (int j = 0; j < 4; j++)
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], o);
         // lane 4 j + r: token t0 + j to CTA r
         const int j = lane >> 2;
         const float v = j == 0 ? sum[0] : j == 1 ? sum[1] : j == 2 ? sum[2] : sum[3];
-        if (j < 4 && t0 + j < L.T) store_peer(logits + (t0 + j) * L.experts + e, (uint32_t)(lane & 3), v);
+        if (part == 0 && e < L.experts && j < 4 && t0 + j < L.T) store_peer(logits + (t0 + j) * L.experts + e, (uint32_t)(lane & 3), v);
     }
+    // (warps without a task in that round meet the others all the same)
+    if (shift > 0 && (warp >> shift) >= tasks) asm volatile("bar.sync 2, %0;" ::"n"(THREADS) : "memory");
 }
 
 // an order of FP32 values as unsigned integers
@@ -122,46 +158,51 @@ __device__ __forceinline__ uint32_t order_of(float v)
     return (b & 0x80000000u) ? ~b : b | 0x80000000u;
 }
 
-// a warp: token t's choices and their weights
+// a warp: token t's choices and their weights; EACH: experts of a lane
+template <int EACH>
 __device__ __forceinline__ void choose_experts(const MoeFp8 &L, const float *logits, int t, int lane, int16_t *chosen, float *weight)
 {
-    constexpr int MOST = MOE_MAX_EXPERTS / 32;
-    float v[MOST];
-    float top = -__int_as_float(0x7F800000), total = 0.f;
+    const float *mine = logits + t * L.experts;
+    uint32_t key[EACH];                                   // 0: no expert, or chosen already
+    float v[EACH], top = -__int_as_float(0x7F800000), total = 0.f;
 #pragma unroll
-    for (int i = 0; i < MOST; i++) {
+    for (int i = 0; i < EACH; i++) {
         const int e = lane + 32 * i;
-        v[i] = e < L.experts ? logits[t * L.experts + e] : 0.f;
-        if (e < L.experts) top = fmaxf(top, v[i]);
+        v[i] = e < L.experts ? mine[e] : -__int_as_float(0x7F800000);
+        key[i] = e < L.experts ? max(order_of(v[i]), 1u) : 0u;
+        top = fmaxf(top, v[i]);
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    uint32_t free_experts = 0;                            // of this lane's
 #pragma unroll
-    for (int i = 0; i < MOST; i++)
-        if (lane + 32 * i < L.experts) { total += expf(v[i] - top); free_experts |= 1u << i; }
+    for (int i = 0; i < EACH; i++) total += lane + 32 * i < L.experts ? expf(v[i] - top) : 0.f;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
-    float picked = 0.f, mine = 0.f;                       // sum of the chosen ones' p; lane j: choice j's
+    int choice = 0;                                       // lane j: choice j
+#pragma unroll 1
     for (int j = 0; j < L.top; j++) {
-        uint32_t best = 0;
-        int e = 0x7FFFFFFF;
+        uint32_t best = key[0];
 #pragma unroll
-        for (int i = 0; i < MOST; i++) {
-            const uint32_t o = order_of(v[i]);
-            if ((free_experts >> i & 1u) && (e == 0x7FFFFFFF || o > best)) { best = o; e = lane + 32 * i; }
-        }
-        const uint32_t most = __reduce_max_sync(0xffffffffu, e == 0x7FFFFFFF ? 0u : best);
-        const int winner = (int)__reduce_min_sync(0xffffffffu, (uint32_t)(e != 0x7FFFFFFF && best == most ? e : 0x7FFFFFFF));
-        float p = 0.f;
+        for (int i = 1; i < EACH; i++) best = max(best, key[i]);
+        const uint32_t most = __reduce_max_sync(0xffffffffu, best);
+        uint32_t e = 0x7FFFFFFFu;
 #pragma unroll
-        for (int i = 0; i < MOST; i++)
-            if (winner == lane + 32 * i) { p = expf(v[i] - top) / total; free_experts &= ~(1u << i); }
-        p = __shfl_sync(0xffffffffu, p, winner & 31);
-        picked += p;
-        if (lane == j) { mine = p; chosen[t * L.top + j] = (int16_t)winner; }
+        for (int i = EACH - 1; i >= 0; i--)
+            if (key[i] == most) e = (uint32_t)(lane + 32 * i);
+        const int winner = (int)__reduce_min_sync(0xffffffffu, e);
+#pragma unroll
+        for (int i = 0; i < EACH; i++)
+            if (winner == lane + 32 * i) key[i] = 0u;
+        if (lane == j) choice = winner;
     }
-    if (lane < L.top) weight[t * L.top + lane] = L.renormalize ? mine / picked : mine;
+    const float p = lane < L.top ? expf(mine[choice] - top) / total : 0.f;
+    float picked = p;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) picked += __shfl_xor_sync(0xffffffffu, picked, o);
+    if (lane < L.top) {
+        chosen[t * L.top + lane] = (int16_t)choice;
+        weight[t * L.top + lane] = L.renormalize ? p / picked : p;
+    }
 }
 
 // all threads: the entries, experts ascending, an expert's pairs ascending
@@ -197,10 +238,10 @@ __device__ __forceinline__ void list_entries(const MoeFp8 &L, const int16_t *cho
     __syncthreads();
 }
 
-// ---- shared memory: [ring: a stage a warp][sums][plan][choices][barriers]; the logits lie in the ring until that is used --------
+// ---- shared memory: [ring: a stage a warp][two sets of sums][plan][choices][barriers]; the logits lie in the ring until that is used --------
 constexpr int UP_STAGE = UP_GROUPS * GROUP_BYTES, UP_STRIDE = UP_GROUPS * GROUP + 4;
 constexpr int UP_PART = WARPS * TOKENS * UP_STRIDE * 4;
-constexpr int OFF_PART = WARPS * UP_STAGE, OFF_PLAN = OFF_PART + UP_PART, OFF_CHOSEN = OFF_PLAN + (int)sizeof(Plan),
+constexpr int OFF_PART = WARPS * UP_STAGE, OFF_PLAN = OFF_PART + 2 * UP_PART, OFF_CHOSEN = OFF_PLAN + (int)sizeof(Plan),
               OFF_UP_BARS = OFF_CHOSEN + MAX_ENTRIES * 2, UP_SMEM = OFF_UP_BARS + WARPS * 8 + WARPS * 4;
 static_assert(UP_SMEM <= 232448 && MOE_MAX_TOKENS * MOE_MAX_EXPERTS * 4 <= OFF_PART && sizeof(Plan) % 16 == 0, "");
 
@@ -226,10 +267,13 @@ moe_gate_up_kernel(const __grid_constant__ CUtensorMap map_gate, const __grid_co
     cluster_sync();                                       // every CTA of the cluster runs: its memory may be written
     pdl_launch_dependents();
     pdl_wait();
-    router<DT, VEC>(L, logits, rank, warp, lane);
+    router<DT, VEC>(L, logits, reinterpret_cast<float(*)[4]>(part), rank, warp, lane);
     __syncwarp();
     cluster_sync();
-    for (int t = warp; t < L.T; t += WARPS) choose_experts(L, logits, t, lane, chosen, plan->weight);
+    for (int t = warp; t < L.T; t += WARPS) {
+        if (L.experts <= 64) choose_experts<2>(L, logits, t, lane, chosen, plan->weight);
+        else choose_experts<MOE_MAX_EXPERTS / 32>(L, logits, t, lane, chosen, plan->weight);
+    }
     __syncthreads();
     list_entries(L, chosen, plan, warp_total);
     if (blockIdx.x == 0)                                  // for the second kernel
@@ -238,102 +282,98 @@ moe_gate_up_kernel(const __grid_constant__ CUtensorMap map_gate, const __grid_co
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");                   // the logits were written where the copies go
     __syncthreads();
 
-    // this CTA's units
-    const int per_entry = (L.inner + GROUP - 1) / GROUP, kbs = (L.hidden + FP8_BLOCK - 1) / FP8_BLOCK;
-    const long long all = (long long)plan->entries * per_entry;
-    const long long begin = all * blockIdx.x / gridDim.x, end = all * (blockIdx.x + 1) / gridDim.x;
+    // this CTA's units (fewer than 2^28 in all)
+    const int per_entry = (L.inner + GROUP - 1) / GROUP, kbs = (L.hidden + FP8_BLOCK - 1) / FP8_BLOCK, scale_rows = (L.inner + FP8_BLOCK - 1) / FP8_BLOCK;
+    const int all = plan->entries * per_entry, share = all / (int)gridDim.x, larger = all - share * (int)gridDim.x, b = (int)blockIdx.x;
     uint32_t gave_up = 0;
-    // a pass: up to UNITS of one entry; and the next one
-    struct Pass { int entry, unit, n; long long left; };
-    auto cut = [&](Pass &p) { p.n = (int)min((long long)min(UNITS, per_entry - p.unit), p.left); };
+    // a pass: up to UNITS of one entry
+    struct Pass { int entry, unit, n, left; };
+    auto cut = [&](Pass &p) { p.n = min(min(UNITS, per_entry - p.unit), p.left); };
     auto advance = [&](Pass &p) {
         p.unit += p.n;
         p.left -= p.n;
         if (p.unit == per_entry) { p.unit = 0; p.entry++; }
         cut(p);
     };
-    Pass now = {(int)(begin / per_entry), (int)(begin % per_entry), 0, end - begin};
+    const int begin = b * share + min(b, larger);
+    Pass now = {begin / per_entry, begin % per_entry, 0, share + (b < larger ? 1 : 0)};
     cut(now);
-    // this warp's loads, in order: blocks warp, warp + 16, ... of one pass after the other; always a box of UNITS units (rows that a pass does
-    // not have are read with it and dropped)
+    // the warp's blocks in order: blocks warp, warp + 16, ... of one pass after the other; `ahead` is the one behind the block at work: its
+    // tokens and scales are fetched while that is multiplied, its weights as soon as the stage has been read.  Always boxes of UNITS
+    // units (rows that a pass does not have are read with it and dropped).
     Pass ahead = now;
-    int load_kb = warp;
+    int ahead_kb = warp;
+    if (warp >= kbs) ahead.n = 0;
     auto load = [&]() {
         const int row = plan->expert[ahead.entry] * L.inner + ahead.unit * GROUP;
         mbar_expect_tx(bar, UP_STAGE);
-        tma_load_2d(stage, &map_gate, load_kb * FP8_BLOCK, row, bar);
-        tma_load_2d(stage + UP_STAGE / 2, &map_up, load_kb * FP8_BLOCK, row, bar);
+        tma_load_2d(stage, &map_gate, ahead_kb * FP8_BLOCK, row, bar);
+        tma_load_2d(stage + UP_STAGE / 2, &map_up, ahead_kb * FP8_BLOCK, row, bar);
     };
-    auto next_load = [&]() {
-        load_kb += WARPS;
-        if (load_kb >= kbs) { load_kb = warp; advance(ahead); }
-    };
-    if (warp >= kbs) ahead.n = 0;
-    if (ahead.n > 0) {
-        if (lane == 0) load();
-        next_load();
-    }
-
     const int g = lane >> 2, t = lane & 3;
+    TokenRaw<DT, VEC> x;
+    float ws = 0.f;                                       // lane r: scale of the stage's group r in the block
+    auto fetch = [&]() {
+        const bool any = ahead.n > 0;
+        const int entry = any ? ahead.entry : 0;
+        const uint8_t *x_row = any && g < plan->count[entry] ? reinterpret_cast<const uint8_t *>(L.x) + (long long)(plan->pair[entry][g] / L.top) * L.hidden * 2 : nullptr;
+        x = load_token<DT, VEC>(x_row, t, ahead_kb, L.hidden);
+        const int row_block = min((ahead.unit + (lane & 1)) / (FP8_BLOCK / GROUP), scale_rows - 1);
+        ws = any ? __ldg((lane & 2 ? L.up_scale : L.gate_scale) + ((long long)plan->expert[entry] * scale_rows + row_block) * kbs + ahead_kb) : 0.f;
+    };
+    auto next_block = [&]() {
+        ahead_kb += WARPS;
+        if (ahead_kb >= kbs) { ahead_kb = warp; advance(ahead); }
+    };
+    if (ahead.n > 0 && lane == 0) load();
+    fetch();
+
     const int row = (g >> 1) | ((g & 1) << 2);            // (see linear_fp8_decode.cu)
     const uint32_t at0 = (uint32_t)(row * FP8_BLOCK + ((t ^ row) << 4)), at1 = (uint32_t)(row * FP8_BLOCK + (((t + 4) ^ row) << 4));
-    const int iterations = warp < kbs ? (kbs - warp + WARPS - 1) / WARPS : 0, scale_rows = (L.inner + FP8_BLOCK - 1) / FP8_BLOCK;
-    uint32_t parity = 0;
-    bool first = true;
-    for (; now.n > 0; advance(now)) {
-        const int expert = plan->expert[now.entry], count = plan->count[now.entry];
-        const uint8_t *x_row = g < count ? reinterpret_cast<const uint8_t *>(L.x) + (long long)(plan->pair[now.entry][g] / L.top) * L.hidden * 2 : nullptr;
-        // (a pass's units lie in one 128-row block, or the second of them in the next)
-        const int b0 = now.unit / (FP8_BLOCK / GROUP), b1 = min((now.unit + 1) / (FP8_BLOCK / GROUP), scale_rows - 1);
-        const long long of_expert = (long long)expert * scale_rows;
-        // scales of the warp's blocks j, 8 of them at a time: lane 8 r + j holds group r's
-        const float *scales = (lane < 16 ? L.gate_scale : L.up_scale) + (of_expert + (lane & 8 ? b1 : b0)) * kbs + warp;
-        auto block_scales = [&](int i) { return i + (lane & 7) < iterations ? __ldg(scales + (i + (lane & 7)) * WARPS) : 0.f; };
-        float ws = block_scales(0);
-        TokenRaw<DT, VEC> x = load_token<DT, VEC>(iterations > 0 ? x_row : nullptr, t, warp, L.hidden);
+    const int iterations = warp < kbs ? (kbs - warp + WARPS - 1) / WARPS : 0;
+    uint32_t parity = 0, which = 0;
+    for (; now.n > 0; advance(now), which ^= 1u) {
         float acc[UP_GROUPS][1][4] = {};
 #pragma unroll 1
         for (int i = 0; i < iterations; i++) {
-            if ((i & 7) == 0 && i > 0) ws = block_scales(i);
-            const TokenFrag b[1] = {quantize_token<DT, VEC>(x, 0.f)};
-            const float2 s = scales_of_columns(b[0].scale, t);
-            x = load_token<DT, VEC>(i + 1 < iterations ? x_row : nullptr, t, warp + (i + 1) * WARPS, L.hidden);
+            const TokenFrag tokens[1] = {quantize_token<DT, VEC>(x, 0.f)};
+            const float2 s = scales_of_columns(tokens[0].scale, t);
+            float w[UP_GROUPS];
+#pragma unroll
+            for (int r = 0; r < UP_GROUPS; r++) w[r] = __shfl_sync(0xffffffffu, ws, r);
+            next_block();
+            fetch();
             mbar_wait_uniform(bar, parity, gave_up);
             parity ^= 1u;
 #pragma unroll
             for (int r0 = 0; r0 < UP_GROUPS; r0 += UNITS) {
                 WeightFrag a[UNITS];
-                float w[UNITS];
 #pragma unroll
                 for (int r = 0; r < UNITS; r++) {
                     const uint32_t box = stage + (r0 + r) * GROUP_BYTES;
                     a[r].q[0][0] = load_shared16(box + at0); a[r].q[1][0] = load_shared16(box + 8 * FP8_BLOCK + at0);
                     a[r].q[0][1] = load_shared16(box + at1); a[r].q[1][1] = load_shared16(box + 8 * FP8_BLOCK + at1);
-                    w[r] = __shfl_sync(0xffffffffu, ws, 8 * (r0 + r) + (i & 7));
                 }
-                block_products<UNITS, 1>(&acc[r0], a, b, [&](int r, int) { return make_float2(s.x * w[r], s.y * w[r]); });
+                block_products<UNITS, 1>(&acc[r0], a, tokens, [&](int r, int) { return make_float2(s.x * w[r0 + r], s.y * w[r0 + r]); });
             }
             __syncwarp();                                 // every lane has read the stage
-            if (ahead.n > 0 && !__any_sync(0xffffffffu, gave_up != 0)) {
-                if (lane == 0) load();
-                next_load();
-            }
+            if (ahead.n > 0 && !__any_sync(0xffffffffu, gave_up != 0) && lane == 0) load();
         }
-        if (!first) __syncthreads();                      // the last pass's sums have been read
-        first = false;
-        float *mine = part + warp * TOKENS * UP_STRIDE;
+        // (two sets of sums: one is read while the next pass's warps that are done write the other)
+        float *sums = part + which * (WARPS * TOKENS * UP_STRIDE), *mine = sums + warp * TOKENS * UP_STRIDE;
 #pragma unroll
         for (int r = 0; r < UP_GROUPS; r++)
 #pragma unroll
             for (int i = 0; i < 4; i++) mine[(2 * t + (i & 1)) * UP_STRIDE + r * GROUP + row + 8 * (i >> 1)] = gave_up ? __int_as_float(0x7FFFFFFF) : acc[r][0][i];
         __syncthreads();
-        for (int i = threadIdx.x; i < count * now.n * GROUP; i += THREADS) {
-            const int token = i / (now.n * GROUP), m = i % (now.n * GROUP), col = now.unit * GROUP + m;
+        const int n = now.n * GROUP, count = plan->count[now.entry];
+        for (int i = threadIdx.x; i < count * n; i += THREADS) {
+            const int token = i / n, m = i % n, col = now.unit * GROUP + m;
             float gate = 0.f, up = 0.f;
 #pragma unroll
             for (int w = 0; w < WARPS; w++) {
-                gate += part[(w * TOKENS + token) * UP_STRIDE + m];
-                up += part[(w * TOKENS + token) * UP_STRIDE + UNITS * GROUP + m];
+                gate += sums[(w * TOKENS + token) * UP_STRIDE + m];
+                up += sums[(w * TOKENS + token) * UP_STRIDE + UNITS * GROUP + m];
             }
             // (columns up to the row's end in the workspace are zeros)
             if (col < P.h_stride) P.h[(long long)plan->pair[now.entry][token] * P.h_stride + col] = col < L.inner ? gate / (1.f + expf(-gate)) * up : 0.f;
@@ -404,67 +444,78 @@ moe_down_kernel(const __grid_constant__ CUtensorMap map_down, const __grid_const
     const int row = (g >> 1) | ((g & 1) << 2);
     const uint32_t at0 = (uint32_t)(row * FP8_BLOCK + ((t ^ row) << 4)), at1 = (uint32_t)(row * FP8_BLOCK + (((t + 4) ^ row) << 4));
     uint32_t slot = 0, parity = 0;
-    At now = {0, 0, warp};
-    settle(now);
+    // the block at work, and the one behind it, whose h and scales are fetched while that is multiplied
+    struct Block { At at; int kb, end; };                 // a block of the run `at`, which ends at `end`
+    auto begin_run = [&](Block &b) {
+        settle(b.at);
+        b.kb = b.at.r << run_shift;
+        b.end = min(kbs, b.kb + run);
+    };
+    auto next_block = [&](Block &b) {
+        if (++b.kb == b.end) { b.at.r += WARPS; begin_run(b); }
+    };
+    Block now = {{0, 0, warp}, 0, 0};
+    begin_run(now);
+    Block next = now;
+    TokenRaw<VPTQ_DTYPE_FP32, true> x;
+    float ws = 0.f;                                       // lanes 0, 1: scales of the pass's two groups in the block
+    auto fetch = [&]() {
+        const bool any = next.at.pass < P.down_passes;
+        const int entry = any ? next.at.entry : 0, group = any ? pass_begin(next.at.pass) + (lane & 1) : 0;
+        x = load_token<VPTQ_DTYPE_FP32, true>(any && g < plan->count[entry] ? P.h + (long long)plan->pair[entry][g] * P.h_stride : nullptr, t, next.kb, P.h_stride);
+        ws = any ? __ldg(L.down_scale + ((long long)plan->expert[entry] * scale_rows + min(group / (FP8_BLOCK / GROUP), scale_rows - 1)) * kbs + next.kb) : 0.f;
+    };
+    fetch();
     for (int p = 0; p < P.down_passes; p++) {
         const int g0 = pass_begin(p), n_groups = pass_begin(p + 1) - g0;
-        const int b0 = g0 / (FP8_BLOCK / GROUP), b1 = min((g0 + 1) / (FP8_BLOCK / GROUP), scale_rows - 1);
         for (int i = lane; i < down_slot_floats(L.T, P.down_groups); i += 32) mine[i] = 0.f;
         __syncwarp();
-        while (now.pass == p) {
-            // this warp's runs of one entry
-            const int entry = now.entry, n = plan->count[entry];
-            const long long of_expert = (long long)plan->expert[entry] * scale_rows;
-            const float *ws0 = L.down_scale + (of_expert + b0) * kbs, *ws1 = L.down_scale + (of_expert + b1) * kbs;
-            const float *h_row = g < n ? P.h + (long long)plan->pair[entry][g] * P.h_stride : nullptr;
-            float acc[DOWN_GROUPS][1][4] = {};
-            while (now.pass == p && now.entry == entry) {
-                const int kb0 = now.r << run_shift, kb1 = min(kbs, kb0 + run);
-                TokenRaw<VPTQ_DTYPE_FP32, true> x = load_token<VPTQ_DTYPE_FP32, true>(h_row, t, kb0, P.h_stride);
-                float w0 = __ldg(ws0 + kb0), w1 = __ldg(ws1 + kb0);
-                for (int kb = kb0; kb < kb1; kb++) {
-                    const TokenFrag b[1] = {quantize_token<VPTQ_DTYPE_FP32, true>(x, 0.f)};
-                    const float2 s = scales_of_columns(b[0].scale, t);
-                    const float c0 = w0, c1 = w1;
-                    if (kb + 1 < kb1) {
-                        x = load_token<VPTQ_DTYPE_FP32, true>(h_row, t, kb + 1, P.h_stride);
-                        w0 = __ldg(ws0 + kb + 1);
-                        w1 = __ldg(ws1 + kb + 1);
-                    }
-                    if (kb == kb0) mbar_wait_uniform(bars + 8 * slot, parity, gave_up);
-                    WeightFrag a[DOWN_GROUPS];
+        float acc[DOWN_GROUPS][1][4] = {};
+#pragma unroll 1
+        while (now.at.pass == p) {
+            const TokenFrag tokens[1] = {quantize_token<VPTQ_DTYPE_FP32, true>(x, 0.f)};
+            const float2 s = scales_of_columns(tokens[0].scale, t);
+            const float w0 = __shfl_sync(0xffffffffu, ws, 0), w1 = __shfl_sync(0xffffffffu, ws, 1);
+            next_block(next);
+            fetch();
+            const int in_run = now.kb - (now.at.r << run_shift), entry = now.at.entry;
+            if (in_run == 0) mbar_wait_uniform(bars + 8 * slot, parity, gave_up);
+            WeightFrag a[DOWN_GROUPS];
 #pragma unroll
-                    for (int r = 0; r < DOWN_GROUPS; r++) {
-                        // (one group: the other's operands are whatever lies behind, dropped)
-                        const uint32_t box = ring + slot * stage_bytes + (uint32_t)((kb - kb0) * block_bytes + r * GROUP_BYTES);
-                        a[r].q[0][0] = load_shared16(box + at0); a[r].q[1][0] = load_shared16(box + 8 * FP8_BLOCK + at0);
-                        a[r].q[0][1] = load_shared16(box + at1); a[r].q[1][1] = load_shared16(box + 8 * FP8_BLOCK + at1);
-                    }
-                    block_products<DOWN_GROUPS, 1>(acc, a, b, [&](int r, int) { return r == 0 ? make_float2(s.x * c0, s.y * c0) : make_float2(s.x * c1, s.y * c1); });
-                }
+            for (int r = 0; r < DOWN_GROUPS; r++) {
+                // (one group: the other's operands are whatever lies behind, dropped)
+                const uint32_t box = ring + slot * stage_bytes + (uint32_t)(in_run * block_bytes + r * GROUP_BYTES);
+                a[r].q[0][0] = load_shared16(box + at0); a[r].q[1][0] = load_shared16(box + 8 * FP8_BLOCK + at0);
+                a[r].q[0][1] = load_shared16(box + at1); a[r].q[1][1] = load_shared16(box + 8 * FP8_BLOCK + at1);
+            }
+            block_products<DOWN_GROUPS, 1>(acc, a, tokens, [&](int r, int) { return r == 0 ? make_float2(s.x * w0, s.y * w0) : make_float2(s.x * w1, s.y * w1); });
+            if (now.kb == now.end - 1) {
                 __syncwarp();                             // every lane has read the stage
-                if (ahead.pass < P.down_passes && !__any_sync(0xffffffffu, gave_up != 0)) {
-                    if (lane == 0) load(slot);
+                if (ahead.pass < P.down_passes) {
+                    if (!__any_sync(0xffffffffu, gave_up != 0) && lane == 0) load(slot);
                     ahead.r += WARPS;
                     settle(ahead);
                 }
                 if (++slot == (uint32_t)stages) { slot = 0; parity ^= 1u; }
-                now.r += WARPS;
-                settle(now);
             }
-            // each (row, token) of the entry is one lane's: an expert has a token once
+            now = next;
+            if (now.at.pass != p || now.at.entry != entry) {
+                // the entry's sums; each (row, token) is one lane's: an expert has a token once
+                const int n = plan->count[entry];
 #pragma unroll
-            for (int r = 0; r < DOWN_GROUPS; r++)
+                for (int r = 0; r < DOWN_GROUPS; r++)
 #pragma unroll
-                for (int i = 0; i < 4; i++) {
-                    const int j = 2 * t + (i & 1);
-                    if (r < n_groups && j < n) {
-                        const int pair = plan->pair[entry][j];
-                        float *to = mine + pair / L.top * stride + r * GROUP + row + 8 * (i >> 1);
-                        *to = __fmaf_rn(plan->weight[pair], gave_up ? __int_as_float(0x7FFFFFFF) : acc[r][0][i], *to);
+                    for (int i = 0; i < 4; i++) {
+                        const int j = 2 * t + (i & 1);
+                        if (r < n_groups && j < n) {
+                            const int pair = plan->pair[entry][j];
+                            float *to = mine + pair / L.top * stride + r * GROUP + row + 8 * (i >> 1);
+                            *to = __fmaf_rn(plan->weight[pair], gave_up ? __int_as_float(0x7FFFFFFF) : acc[r][0][i], *to);
+                        }
+                        acc[r][0][i] = 0.f;
                     }
-                }
-            __syncwarp();
+                __syncwarp();
+            }
         }
         __syncthreads();
         const int rows = n_groups * GROUP, m0 = g0 * GROUP;
