@@ -27,21 +27,6 @@ struct QuantizeParams {
     int step_rows, step_cols;
 };
 
-// eight values at column c of a row of q; beyond `cols` zeros are written up to the row's end, whatever the factor
-template <int DT, bool VEC>
-__device__ __forceinline__ void store_eight(uint8_t *row, long long pitch, int c, int cols, const Eight<DT, VEC> &e, float factor)
-{
-    if (c >= pitch) return;
-    float v[8];
-    values_of(e, v);
-    uint2 o;
-    o.x = fp8_quad(v[0] * factor, v[1] * factor, v[2] * factor, v[3] * factor);
-    o.y = fp8_quad(v[4] * factor, v[5] * factor, v[6] * factor, v[7] * factor);
-    *reinterpret_cast<uint2 *>(row + c) = o;
-    if (c + 8 > cols)
-        for (int i = max(c, cols); i < c + 8; i++) row[i] = 0;         // (0 * factor is no zero when the factor is a NaN)
-}
-
 template <int DT, bool VEC, int UNROLL>
 __global__ void __launch_bounds__(THREADS)
 quantize_rows_kernel(const __grid_constant__ QuantizeParams P)

@@ -2,16 +2,17 @@
 //   logits = x Wr^T, p = softmax(logits), the k largest logits of a token (equal ones: the lowest expert) with weights p, or p divided
 //   by the chosen ones' sum;  h = silu(x Wg^T) * (x Wu^T) per token and choice;  out = sum over the choices of weight * (h Wd^T).
 //
-// moe_gate_up_kernel: clusters of four CTAs compute all logits, a quarter each, exchange them, and every CTA makes the choices and the
-// list of experts in use by itself: no wait for another cluster and no launch for the router.  Then the units (16 gate and the 16 up
-// rows of an expert in use) are dealt out over all CTAs; a warp takes every sixteenth 128-column block of up to two units at a time
-// into a stage of its own (as in linear_fp8_decode.cu), multiplies it with up to 8 of the expert's tokens (fp8_mma.cuh), and
-// the warps' sums meet in shared memory, where h is formed (FP32, to the workspace).
-// moe_down_kernel: a CTA owns 16 or 32 rows of the result; its warps share the blocks of all the experts in use, quantizing h on the way;
-// per expert a warp adds weight * sums to a slot of its own for each token, and the slots are added in warp order.  No atomics: a result
-// does not depend on timing.
-// Bound by HBM: the weights of the experts in use, each once (once for every 8 of its tokens), and for one token of small experts by
-// the way through router, two launches and two reductions.
+// moe_gate_up_kernel: clusters of four CTAs quantize x and compute all logits, a quarter each, and every CTA makes the choices and the
+// list of experts in use by itself: no wait for another cluster and no launch for the router.  Then 128 columns of h of an expert in
+// use at a time are a cluster's, 32 gate and 32 up rows a CTA's: a warp takes every sixteenth 128-column block of them into a stage of
+// its own (as in linear_fp8_decode.cu), multiplies it with up to 8 of the expert's tokens (fp8_mma.cuh), the warps' sums meet in shared
+// memory, and the four CTAs exchange the largest magnitude of their 32 columns, so that h leaves as e4m3 with its scale.
+// moe_down_kernel: a CTA owns 16 or 32 rows of the result; its warps share the blocks of all the experts in use; per expert a warp adds
+// weight * sums to a slot of its own for each token, and the slots are added in warp order.  No atomics: a result does not depend on
+// timing.
+// Bound by HBM: the weights of the experts in use, each once (once for every 8 of its tokens); for one token of small experts by the
+// way through router, two launches and two reductions.  Quantizing x and h where they are multiplied cost 250 instructions a block,
+// more than everything else in the loops together.
 // Every wait is bounded; a warp whose wait gives up leaves NaN.
 #include "fp8_mma.cuh"
 #include "moe_fp8.cuh"
@@ -45,12 +46,25 @@ struct Plan {
 
 struct Params {
     MoeFp8 L;
-    Plan *plan;            // in the workspace
-    float *h;              // [T * top][h_stride]
-    int h_stride;
+    Plan *plan;            // in the workspace, as are:
+    uint8_t *hq;           // h: [T * top][hq_pitch] e4m3 and [T * top][ceil(inner / 128)] scales
+    float *hs;
+    uint8_t *xq;           // x, a copy for every cluster: [T][xq_pitch] e4m3 and [T][ceil(hidden / 128)] scales
+    float *xs;
+    int hq_pitch, xq_pitch;
     int down_groups;       // groups of a pass of the down kernel
     int down_passes, down_run_shift;
 };
+
+// a lane's share of one token's e4m3 values in one block, written by this kernel's cluster or by the kernel before; row: null for zeros
+__device__ __forceinline__ TokenRaw<VPTQ_DTYPE_E4M3, true> load_e4m3(const uint8_t *row, int t, int kb, int pitch)
+{
+    TokenRaw<VPTQ_DTYPE_E4M3, true> r;
+    const int c0 = kb * FP8_BLOCK + 16 * t;
+#pragma unroll
+    for (int c = 0; c < 2; c++) r.q[c] = row != nullptr && c0 + 64 * c < pitch ? __ldcg(reinterpret_cast<const uint4 *>(row + c0 + 64 * c)) : make_uint4(0, 0, 0, 0);
+    return r;
+}
 
 __device__ __forceinline__ uint4 load_shared16(uint32_t a)
 {
@@ -68,6 +82,35 @@ __device__ __forceinline__ void store_peer(float *at, uint32_t rank, float v)
     uint32_t a;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_addr(at)), "r"(rank));
     asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(a), "f"(v) : "memory");
+}
+
+// this cluster's copy of x in e4m3: a half warp a block, as in fp8_quantize.cu
+template <int DT, bool VEC>
+__device__ __forceinline__ void quantize_tokens(const MoeFp8 &L, uint8_t *xq, float *xs, int pitch, uint32_t rank)
+{
+    const int kbs = (L.hidden + FP8_BLOCK - 1) / FP8_BLOCK, lane = threadIdx.x & 15, half = (threadIdx.x >> 4) & 1;
+    for (int b0 = ((int)rank * THREADS + (int)threadIdx.x >> 4) - half; b0 < L.T * kbs; b0 += CLUSTER * THREADS / 16) {      // (whole warps)
+        const int block = b0 + half, token = block / kbs, kb = block % kbs, c = kb * FP8_BLOCK + lane * 8;
+        const bool in = token < L.T;
+        const Eight<DT, VEC> v = load_eight<DT, VEC>(reinterpret_cast<const uint8_t *>(L.x) + (long long)(in ? token : 0) * L.hidden * 2, in ? c : L.hidden, L.hidden);
+        uint32_t m = magnitude(v);
+#pragma unroll
+        for (int o = 8; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+        const Fp8Scale s = fp8_scale(__uint_as_float(m));
+        if (in) {
+            store_eight(xq + (long long)token * pitch, pitch, c, L.hidden, v, s.factor);
+            if (lane == 0) xs[block] = s.scale;
+        }
+    }
+}
+
+// ... counted on a barrier of the same CTA when it has arrived
+__device__ __forceinline__ void store_peer_async(float *at, uint32_t bar, uint32_t rank, float v)
+{
+    uint32_t a, b;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_addr(at)), "r"(rank));
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(b) : "r"(bar), "r"(rank));
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.b32 [%0], %1, [%2];" ::"r"(a), "r"(__float_as_uint(v)), "r"(b) : "memory");
 }
 
 // One warp: the products of an expert's router row with N tokens over columns [c0, c1); `ahead` loads of each row in flight.
@@ -211,6 +254,7 @@ __device__ __forceinline__ void list_entries(const MoeFp8 &L, const int16_t *cho
     const int e = threadIdx.x, warp = e >> 5, lane = e & 31, pairs = L.T * L.top;
     int count = 0;
     if (e < L.experts)
+#pragma unroll 8
         for (int p = 0; p < pairs; p++) count += chosen[p] == e ? 1 : 0;
     const int entries = (count + TOKENS - 1) / TOKENS;
     int before = entries;                                 // inclusive sum over the warp, then over the warps
@@ -222,6 +266,7 @@ __device__ __forceinline__ void list_entries(const MoeFp8 &L, const int16_t *cho
     if (lane == 31) warp_total[warp] = before;
     __syncthreads();
     int all = 0;
+#pragma unroll
     for (int w = 0; w < WARPS; w++) {
         if (w < warp) before += warp_total[w];
         all += warp_total[w];
@@ -242,23 +287,26 @@ __device__ __forceinline__ void list_entries(const MoeFp8 &L, const int16_t *cho
 constexpr int UP_STAGE = UP_GROUPS * GROUP_BYTES, UP_STRIDE = UP_GROUPS * GROUP + 4;
 constexpr int UP_PART = WARPS * TOKENS * UP_STRIDE * 4;
 constexpr int OFF_PART = WARPS * UP_STAGE, OFF_PLAN = OFF_PART + 2 * UP_PART, OFF_CHOSEN = OFF_PLAN + (int)sizeof(Plan),
-              OFF_UP_BARS = OFF_CHOSEN + MAX_ENTRIES * 2, UP_SMEM = OFF_UP_BARS + WARPS * 8 + WARPS * 4;
-static_assert(UP_SMEM <= 232448 && MOE_MAX_TOKENS * MOE_MAX_EXPERTS * 4 <= OFF_PART && sizeof(Plan) % 16 == 0, "");
+              OFF_UP_BARS = OFF_CHOSEN + MAX_ENTRIES * 2, UP_SMEM = OFF_UP_BARS + (WARPS + 2) * 8 + WARPS * 4;
+static_assert(UP_SMEM + 1024 <= 232448 && MOE_MAX_TOKENS * MOE_MAX_EXPERTS * 4 <= OFF_PART && sizeof(Plan) % 16 == 0, "");
 
 template <int DT, bool VEC>
 __global__ void __launch_bounds__(THREADS, 1)
 moe_gate_up_kernel(const __grid_constant__ CUtensorMap map_gate, const __grid_constant__ CUtensorMap map_up, const __grid_constant__ Params P)
 {
     extern __shared__ __align__(1024) uint8_t sm[];
+    __shared__ float peaks[2][TOKENS][CLUSTER];           // largest magnitudes of the four CTAs' columns of h
     const MoeFp8 &L = P.L;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     float *logits = reinterpret_cast<float *>(sm), *part = reinterpret_cast<float *>(sm + OFF_PART);
     Plan *plan = reinterpret_cast<Plan *>(sm + OFF_PLAN);
     int16_t *chosen = reinterpret_cast<int16_t *>(sm + OFF_CHOSEN);
-    int *warp_total = reinterpret_cast<int *>(sm + OFF_UP_BARS + WARPS * 8);
+    int *warp_total = reinterpret_cast<int *>(sm + OFF_UP_BARS + (WARPS + 2) * 8);
+    const uint32_t peak_bars = smem_addr(sm + OFF_UP_BARS) + 8 * WARPS;            // two: the peaks of a pass are complete
     const uint32_t bar = smem_addr(sm + OFF_UP_BARS) + 8 * warp, stage = smem_addr(sm) + warp * UP_STAGE;
     if (lane == 0) {
         mbar_init(bar, 1);
+        if (warp < 2) mbar_init(peak_bars + 8 * warp, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     uint32_t rank;
@@ -267,6 +315,10 @@ moe_gate_up_kernel(const __grid_constant__ CUtensorMap map_gate, const __grid_co
     cluster_sync();                                       // every CTA of the cluster runs: its memory may be written
     pdl_launch_dependents();
     pdl_wait();
+    const int kbs = (L.hidden + FP8_BLOCK - 1) / FP8_BLOCK, cluster = (int)blockIdx.x / CLUSTER, clusters = (int)gridDim.x / CLUSTER;
+    uint8_t *xq = P.xq + (long long)cluster * L.T * P.xq_pitch;
+    float *xs = P.xs + (long long)cluster * L.T * kbs;
+    quantize_tokens<DT, VEC>(L, xq, xs, P.xq_pitch, rank);
     router<DT, VEC>(L, logits, reinterpret_cast<float(*)[4]>(part), rank, warp, lane);
     __syncwarp();
     cluster_sync();
@@ -282,65 +334,59 @@ moe_gate_up_kernel(const __grid_constant__ CUtensorMap map_gate, const __grid_co
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");                   // the logits were written where the copies go
     __syncthreads();
 
-    // this CTA's units (fewer than 2^28 in all)
-    const int per_entry = (L.inner + GROUP - 1) / GROUP, kbs = (L.hidden + FP8_BLOCK - 1) / FP8_BLOCK, scale_rows = (L.inner + FP8_BLOCK - 1) / FP8_BLOCK;
-    const int all = plan->entries * per_entry, share = all / (int)gridDim.x, larger = all - share * (int)gridDim.x, b = (int)blockIdx.x;
+    // this cluster's passes: 128 columns of h of an entry each (fewer than 2^25 in all); this CTA's two units of a pass
+    const int per_entry = (L.inner + FP8_BLOCK - 1) / FP8_BLOCK;
+    const int all = plan->entries * per_entry, share = all / clusters, larger = all - share * clusters, begin = cluster * share + min(cluster, larger);
+    const int passes = share + (cluster < larger ? 1 : 0);
     uint32_t gave_up = 0;
-    // a pass: up to UNITS of one entry
-    struct Pass { int entry, unit, n, left; };
-    auto cut = [&](Pass &p) { p.n = min(min(UNITS, per_entry - p.unit), p.left); };
+    struct Pass { int entry, block, left; };
     auto advance = [&](Pass &p) {
-        p.unit += p.n;
-        p.left -= p.n;
-        if (p.unit == per_entry) { p.unit = 0; p.entry++; }
-        cut(p);
+        p.left--;
+        if (++p.block == per_entry) { p.block = 0; p.entry++; }
     };
-    const int begin = b * share + min(b, larger);
-    Pass now = {begin / per_entry, begin % per_entry, 0, share + (b < larger ? 1 : 0)};
-    cut(now);
+    Pass now = {begin / per_entry, begin % per_entry, passes};
     // the warp's blocks in order: blocks warp, warp + 16, ... of one pass after the other; `ahead` is the one behind the block at work: its
-    // tokens and scales are fetched while that is multiplied, its weights as soon as the stage has been read.  Always boxes of UNITS
-    // units (rows that a pass does not have are read with it and dropped).
+    // tokens and scales are fetched while that is multiplied, its weights as soon as the stage has been read.  (Rows beyond the
+    // expert's are read with the boxes and dropped.)
     Pass ahead = now;
     int ahead_kb = warp;
-    if (warp >= kbs) ahead.n = 0;
+    if (warp >= kbs) ahead.left = 0;
     auto load = [&]() {
-        const int row = plan->expert[ahead.entry] * L.inner + ahead.unit * GROUP;
+        const int row = plan->expert[ahead.entry] * L.inner + ahead.block * FP8_BLOCK + (int)rank * (UNITS * GROUP);
         mbar_expect_tx(bar, UP_STAGE);
         tma_load_2d(stage, &map_gate, ahead_kb * FP8_BLOCK, row, bar);
         tma_load_2d(stage + UP_STAGE / 2, &map_up, ahead_kb * FP8_BLOCK, row, bar);
     };
     const int g = lane >> 2, t = lane & 3;
-    TokenRaw<DT, VEC> x;
-    float ws = 0.f;                                       // lane r: scale of the stage's group r in the block
+    TokenRaw<VPTQ_DTYPE_E4M3, true> x;
+    float x_scale = 0.f, ws = 0.f;                        // ws: lane 0 the gate's scale of the block, lane 1 the up's
     auto fetch = [&]() {
-        const bool any = ahead.n > 0;
+        const bool any = ahead.left > 0;
         const int entry = any ? ahead.entry : 0;
-        const uint8_t *x_row = any && g < plan->count[entry] ? reinterpret_cast<const uint8_t *>(L.x) + (long long)(plan->pair[entry][g] / L.top) * L.hidden * 2 : nullptr;
-        x = load_token<DT, VEC>(x_row, t, ahead_kb, L.hidden);
-        const int row_block = min((ahead.unit + (lane & 1)) / (FP8_BLOCK / GROUP), scale_rows - 1);
-        ws = any ? __ldg((lane & 2 ? L.up_scale : L.gate_scale) + ((long long)plan->expert[entry] * scale_rows + row_block) * kbs + ahead_kb) : 0.f;
+        const bool mine = any && g < plan->count[entry];
+        const int token = mine ? plan->pair[entry][g] / L.top : 0;
+        x = load_e4m3(mine ? xq + (long long)token * P.xq_pitch : nullptr, t, ahead_kb, P.xq_pitch);
+        x_scale = mine ? __ldcg(xs + token * kbs + ahead_kb) : 0.f;
+        ws = any ? __ldg((lane & 1 ? L.up_scale : L.gate_scale) + ((long long)plan->expert[entry] * per_entry + ahead.block) * kbs + ahead_kb) : 0.f;
     };
     auto next_block = [&]() {
         ahead_kb += WARPS;
         if (ahead_kb >= kbs) { ahead_kb = warp; advance(ahead); }
     };
-    if (ahead.n > 0 && lane == 0) load();
+    if (ahead.left > 0 && lane == 0) load();
     fetch();
 
     const int row = (g >> 1) | ((g & 1) << 2);            // (see linear_fp8_decode.cu)
     const uint32_t at0 = (uint32_t)(row * FP8_BLOCK + ((t ^ row) << 4)), at1 = (uint32_t)(row * FP8_BLOCK + (((t + 4) ^ row) << 4));
     const int iterations = warp < kbs ? (kbs - warp + WARPS - 1) / WARPS : 0;
-    uint32_t parity = 0, which = 0;
-    for (; now.n > 0; advance(now), which ^= 1u) {
+    uint32_t parity = 0, which = 0, peak_parity = 0;
+    for (; now.left > 0; advance(now), peak_parity ^= which, which ^= 1u) {
         float acc[UP_GROUPS][1][4] = {};
 #pragma unroll 1
         for (int i = 0; i < iterations; i++) {
-            const TokenFrag tokens[1] = {quantize_token<DT, VEC>(x, 0.f)};
+            const TokenFrag tokens[1] = {quantize_token<VPTQ_DTYPE_E4M3, true>(x, x_scale)};
             const float2 s = scales_of_columns(tokens[0].scale, t);
-            float w[UP_GROUPS];
-#pragma unroll
-            for (int r = 0; r < UP_GROUPS; r++) w[r] = __shfl_sync(0xffffffffu, ws, r);
+            const float w0 = __shfl_sync(0xffffffffu, ws, 0), w1 = __shfl_sync(0xffffffffu, ws, 1);
             next_block();
             fetch();
             mbar_wait_uniform(bar, parity, gave_up);
@@ -354,29 +400,44 @@ moe_gate_up_kernel(const __grid_constant__ CUtensorMap map_gate, const __grid_co
                     a[r].q[0][0] = load_shared16(box + at0); a[r].q[1][0] = load_shared16(box + 8 * FP8_BLOCK + at0);
                     a[r].q[0][1] = load_shared16(box + at1); a[r].q[1][1] = load_shared16(box + 8 * FP8_BLOCK + at1);
                 }
-                block_products<UNITS, 1>(&acc[r0], a, tokens, [&](int r, int) { return make_float2(s.x * w[r0 + r], s.y * w[r0 + r]); });
+                const float w = r0 == 0 ? w0 : w1;
+                block_products<UNITS, 1>(&acc[r0], a, tokens, [&](int, int) { return make_float2(s.x * w, s.y * w); });
             }
             __syncwarp();                                 // every lane has read the stage
-            if (ahead.n > 0 && !__any_sync(0xffffffffu, gave_up != 0) && lane == 0) load();
+            if (ahead.left > 0 && !__any_sync(0xffffffffu, gave_up != 0) && lane == 0) load();
         }
-        // (two sets of sums: one is read while the next pass's warps that are done write the other)
+        // (two sets of sums, and of magnitudes: one is read while the next pass's warps that are done write the other.  A CTA two passes ahead has
+        // had this one's magnitudes of the pass between, which leave behind the __syncthreads that every reader of this pass's comes to.)
         float *sums = part + which * (WARPS * TOKENS * UP_STRIDE), *mine = sums + warp * TOKENS * UP_STRIDE;
 #pragma unroll
         for (int r = 0; r < UP_GROUPS; r++)
 #pragma unroll
             for (int i = 0; i < 4; i++) mine[(2 * t + (i & 1)) * UP_STRIDE + r * GROUP + row + 8 * (i >> 1)] = gave_up ? __int_as_float(0x7FFFFFFF) : acc[r][0][i];
         __syncthreads();
-        const int n = now.n * GROUP, count = plan->count[now.entry];
-        for (int i = threadIdx.x; i < count * n; i += THREADS) {
-            const int token = i / n, m = i % n, col = now.unit * GROUP + m;
+        if (threadIdx.x == 0) mbar_expect_tx(peak_bars + 8 * which, (uint32_t)plan->count[now.entry] * CLUSTER * 4);
+        // a warp a token, a lane a column
+        const bool has = warp < plan->count[now.entry];
+        const int col = now.block * FP8_BLOCK + (int)rank * (UNITS * GROUP) + lane;
+        float h = 0.f;
+        if (has) {
             float gate = 0.f, up = 0.f;
 #pragma unroll
             for (int w = 0; w < WARPS; w++) {
-                gate += sums[(w * TOKENS + token) * UP_STRIDE + m];
-                up += sums[(w * TOKENS + token) * UP_STRIDE + UNITS * GROUP + m];
+                gate += sums[(w * TOKENS + warp) * UP_STRIDE + lane];
+                up += sums[(w * TOKENS + warp) * UP_STRIDE + UNITS * GROUP + lane];
             }
-            // (columns up to the row's end in the workspace are zeros)
-            if (col < P.h_stride) P.h[(long long)plan->pair[now.entry][token] * P.h_stride + col] = col < L.inner ? gate / (1.f + expf(-gate)) * up : 0.f;
+            if (col < L.inner) h = gate / (1.f + expf(-gate)) * up;
+            uint32_t most = __reduce_max_sync(0xffffffffu, __float_as_uint(h) & 0x7FFFFFFFu);
+            if (lane < CLUSTER) store_peer_async(&peaks[which][warp][rank], peak_bars + 8 * which, (uint32_t)lane, __uint_as_float(most));
+            __syncwarp();
+            mbar_wait_uniform(peak_bars + 8 * which, peak_parity, gave_up);
+            most = 0;
+#pragma unroll
+            for (int r = 0; r < CLUSTER; r++) most = max(most, __float_as_uint(peaks[which][warp][r]));
+            const Fp8Scale s = fp8_scale(__uint_as_float(most));
+            const int pair = plan->pair[now.entry][warp];
+            if (col < P.hq_pitch) P.hq[(long long)pair * P.hq_pitch + col] = col < L.inner ? (uint8_t)fp8_pair(h * s.factor, 0.f) : (uint8_t)0;
+            if (rank == 0 && lane == 0) P.hs[(long long)pair * per_entry + now.block] = s.scale;
         }
     }
     if (gave_up) {                                        // copies in flight get a bounded time to land before the CTA exits
@@ -457,12 +518,15 @@ moe_down_kernel(const __grid_constant__ CUtensorMap map_down, const __grid_const
     Block now = {{0, 0, warp}, 0, 0};
     begin_run(now);
     Block next = now;
-    TokenRaw<VPTQ_DTYPE_FP32, true> x;
-    float ws = 0.f;                                       // lanes 0, 1: scales of the pass's two groups in the block
+    TokenRaw<VPTQ_DTYPE_E4M3, true> x;
+    float x_scale = 0.f, ws = 0.f;                        // ws: lanes 0, 1: scales of the pass's two groups in the block
     auto fetch = [&]() {
         const bool any = next.at.pass < P.down_passes;
         const int entry = any ? next.at.entry : 0, group = any ? pass_begin(next.at.pass) + (lane & 1) : 0;
-        x = load_token<VPTQ_DTYPE_FP32, true>(any && g < plan->count[entry] ? P.h + (long long)plan->pair[entry][g] * P.h_stride : nullptr, t, next.kb, P.h_stride);
+        const bool mine = any && g < plan->count[entry];
+        const int pair = mine ? plan->pair[entry][g] : 0;
+        x = load_e4m3(mine ? P.hq + (long long)pair * P.hq_pitch : nullptr, t, next.kb, P.hq_pitch);
+        x_scale = mine ? __ldcg(P.hs + (long long)pair * kbs + next.kb) : 0.f;
         ws = any ? __ldg(L.down_scale + ((long long)plan->expert[entry] * scale_rows + min(group / (FP8_BLOCK / GROUP), scale_rows - 1)) * kbs + next.kb) : 0.f;
     };
     fetch();
@@ -473,7 +537,7 @@ moe_down_kernel(const __grid_constant__ CUtensorMap map_down, const __grid_const
         float acc[DOWN_GROUPS][1][4] = {};
 #pragma unroll 1
         while (now.at.pass == p) {
-            const TokenFrag tokens[1] = {quantize_token<VPTQ_DTYPE_FP32, true>(x, 0.f)};
+            const TokenFrag tokens[1] = {quantize_token<VPTQ_DTYPE_E4M3, true>(x, x_scale)};
             const float2 s = scales_of_columns(tokens[0].scale, t);
             const float w0 = __shfl_sync(0xffffffffu, ws, 0), w1 = __shfl_sync(0xffffffffu, ws, 1);
             next_block(next);
@@ -535,20 +599,35 @@ moe_down_kernel(const __grid_constant__ CUtensorMap map_down, const __grid_const
     }
 }
 
-int h_stride_of(int inner) { return (inner + 3) / 4 * 4; }
-long long plan_bytes() { return ((long long)sizeof(Plan) + 255) / 256 * 256; }
+// workspace: plan, h and its scales, a copy of x and its scales for every cluster
+struct Workspace { long long hq, hs, xq, xs, bytes; };
+Workspace workspace_of(int hidden, int inner, int top, int T)
+{
+    auto up = [](long long v) { return (v + 255) / 256 * 256; };
+    const long long clusters = device_sm_count() / CLUSTER > 0 ? device_sm_count() / CLUSTER : 1, pairs = (long long)T * top;
+    Workspace w;
+    w.hq = up((long long)sizeof(Plan));
+    w.hs = up(w.hq + pairs * fp8_row_bytes(inner));
+    w.xq = up(w.hs + 4 * pairs * ceil_div(inner, FP8_BLOCK));
+    w.xs = up(w.xq + clusters * T * fp8_row_bytes(hidden));
+    w.bytes = up(w.xs + 4 * clusters * T * ceil_div(hidden, FP8_BLOCK));
+    return w;
+}
 
 }  // namespace
 
-long long moe_fp8_workspace_bytes(int inner, int top, int T) { return plan_bytes() + 4ll * T * top * h_stride_of(inner); }
+long long moe_fp8_workspace_bytes(int hidden, int inner, int top, int T) { return workspace_of(hidden, inner, top, T).bytes; }
 
 cudaError_t launch_moe_fp8(const MoeFp8 &L, void *ws, cudaStream_t st)
 {
+    const Workspace w = workspace_of(L.hidden, L.inner, L.top, L.T);
+    uint8_t *w8 = reinterpret_cast<uint8_t *>(ws);
     Params P;
     P.L = L;
-    P.plan = reinterpret_cast<Plan *>(ws);
-    P.h = reinterpret_cast<float *>(reinterpret_cast<uint8_t *>(ws) + plan_bytes());
-    P.h_stride = h_stride_of(L.inner);
+    P.plan = reinterpret_cast<Plan *>(w8);
+    P.hq = w8 + w.hq; P.hs = reinterpret_cast<float *>(w8 + w.hs);
+    P.xq = w8 + w.xq; P.xs = reinterpret_cast<float *>(w8 + w.xs);
+    P.hq_pitch = (int)fp8_row_bytes(L.inner); P.xq_pitch = (int)fp8_row_bytes(L.hidden);
     const int sms = device_sm_count();
     const long long pitch_h = fp8_row_bytes(L.hidden), pitch_i = fp8_row_bytes(L.inner);
     const int down_all = ceil_div(L.hidden, GROUP), down_grid = down_all < sms ? down_all : sms, most = ceil_div(down_all, down_grid);
@@ -572,8 +651,9 @@ cudaError_t launch_moe_fp8(const MoeFp8 &L, void *ws, cudaStream_t st)
                                              : (vec ? moe_gate_up_kernel<VPTQ_DTYPE_FP16, true> : moe_gate_up_kernel<VPTQ_DTYPE_FP16, false>);
     cudaError_t e = allow_dynamic_smem(reinterpret_cast<const void *>(kern), UP_SMEM);
     if (e != cudaSuccess) return e;
-    const int clusters = max_resident_clusters(reinterpret_cast<const void *>(kern), CLUSTER, THREADS, UP_SMEM);
+    int clusters = max_resident_clusters(reinterpret_cast<const void *>(kern), CLUSTER, THREADS, UP_SMEM);
     if (clusters < 1) return cudaErrorNotSupported;
+    if (clusters > sms / CLUSTER && sms >= CLUSTER) clusters = sms / CLUSTER;      // (the workspace has no more copies)
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(CLUSTER * clusters));
     cfg.blockDim = dim3(THREADS);

@@ -15,7 +15,7 @@ struct MoeFp8 {
     void *out;                                            // [T][hidden]
 };
 
-long long moe_fp8_workspace_bytes(int inner, int top, int T);
+long long moe_fp8_workspace_bytes(int hidden, int inner, int top, int T);
 cudaError_t launch_moe_fp8(const MoeFp8 &L, void *ws, cudaStream_t st);
 
 }  // namespace vptq

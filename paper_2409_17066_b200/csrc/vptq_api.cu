@@ -654,7 +654,7 @@ int64_t vptq_moe_fp8_workspace_bytes(const vptq_moe_desc *desc, int32_t T)
 {
     const int rc = check_moe_desc(desc, T);
     if (rc != VPTQ_OK) return rc;
-    return moe_fp8_workspace_bytes(desc->inner, desc->top_k, T);
+    return moe_fp8_workspace_bytes(desc->hidden, desc->inner, desc->top_k, T);
 }
 
 int vptq_moe_fp8(const vptq_moe_desc *desc, const vptq_moe_ptrs *p, const void *x, int32_t T, void *out,
@@ -668,7 +668,7 @@ int vptq_moe_fp8(const vptq_moe_desc *desc, const vptq_moe_ptrs *p, const void *
         if (all[i] == nullptr) return VPTQ_E_NULL;
     for (int i = 0; i < 9; i++)
         if (!aligned16(all[i])) return VPTQ_E_ALIGN;
-    if (workspace == nullptr || (int64_t)workspace_bytes < moe_fp8_workspace_bytes(desc->inner, desc->top_k, T)) return VPTQ_E_WORKSPACE;
+    if (workspace == nullptr || (int64_t)workspace_bytes < moe_fp8_workspace_bytes(desc->hidden, desc->inner, desc->top_k, T)) return VPTQ_E_WORKSPACE;
     if ((reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return VPTQ_E_ALIGN;
     MoeFp8 L;
     L.hidden = desc->hidden; L.inner = desc->inner; L.experts = desc->n_experts; L.top = desc->top_k; L.T = T;
