@@ -2,18 +2,25 @@
 // bit (FP32, three separately rounded operations, then FP16), quantized by the rule of fp8_quantize.cu, without the FP16 matrix in
 // global memory.
 //
-// A CTA makes one 128 x 128 block: its threads look up the (vector row, column) pairs that meet the block, ITEMS at a time so that
-// as many table reads are in flight, and leave the FP16 values in shared memory; the block's maximum and the rounding follow.
+// A CTA makes a 128 x 128 block at a time: its threads look up the (vector row, column) pairs that meet the block, ITEMS at a time so
+// that as many table reads are in flight, and leave the FP16 values in shared memory; the block's maximum and the rounding follow.
 // A vector row that crosses a block's edge is looked up by both blocks (v = 8 never does; v = 6: 23 rows instead of 21.3).
+// TABLES: main and residual table of a layer with one group are staged in shared memory as 16-byte rows, and two CTAs an SM go through
+// the blocks; out of L1 every 4-byte piece of a 12-byte row is a wavefront of its own for each lane (11008 x 4096 with v = 6: 97 us).
+// A table in L2 (1 MiB) is bound by its random reads, one a clock and SM.
 #include "fp8.cuh"
+#include "index_words.cuh"
+
+#include <type_traits>
 
 namespace vptq {
 
 namespace {
 
-constexpr int THREADS = 256;
-constexpr int COL_LANES = THREADS / FP8_BLOCK;            // vector rows of a block taken at a time
-constexpr int ITEMS = 4;
+// threads of a CTA, and pairs that a thread looks up at a time: out of L2 more CTAs (8192 x 28672: 314 us; 512 threads 367), out of shared
+// memory more threads to hide their arithmetic behind one another's (11008 x 4096, v = 6: 81 us; 256 threads 108)
+template <bool TABLES> constexpr int threads() { return TABLES ? 512 : 256; }
+template <bool TABLES> constexpr int items() { return TABLES ? 2 : 4; }
 constexpr int TILE_STRIDE = FP8_BLOCK + 8;                // halves; 16-byte rows, half warps read them without conflicts
 
 struct DequantFp8Params {
@@ -22,15 +29,16 @@ struct DequantFp8Params {
     float *scale;
     const int *inverse;       // stored column of every input feature (-1: none names it), or null
     long long pitch;
-    int col_blocks;
+    int col_blocks, blocks;
 };
+constexpr int TABLES_MAX = (115712 - 1024 - FP8_BLOCK * TILE_STRIDE * 2) / 16;         // entries of both tables, two CTAs an SM
 
 // V = 0: any length, component by component
 template <int V> struct Row { uint32_t w[V > 0 ? V / 2 : 1]; };
 template <int V>
 __device__ __forceinline__ Row<V> table_row(const __half *__restrict__ tab, long long e)
 {
-    Row<V> r;
+    Row<V> r = {};
     if constexpr (V == 8) {
         const uint4 q = __ldg(reinterpret_cast<const uint4 *>(tab) + e);
         r.w[0] = q.x; r.w[1] = q.y; r.w[2] = q.z; r.w[3] = q.w;
@@ -62,21 +70,20 @@ __device__ __forceinline__ float finish(float t, bool has_scale, float s, float 
     return has_scale ? __fadd_rn(__fmul_rn(t, s), b) : t;              // never contracted to an FMA
 }
 
-template <int V>
-__global__ void __launch_bounds__(THREADS)
-dequant_fp8_kernel(const __grid_constant__ DequantFp8Params P)
+template <int V, bool TABLES>
+__device__ __forceinline__ void restore_block(const DequantFp8Params &P, int index, __half (*tile)[TILE_STRIDE], uint32_t *part, const uint4 *tables)
 {
-    __shared__ __align__(16) __half tile[FP8_BLOCK][TILE_STRIDE];
-    __shared__ uint32_t part[THREADS / 32];
+    constexpr int THREADS = threads<TABLES>(), ITEMS = items<TABLES>();
+    constexpr int COL_LANES = THREADS / FP8_BLOCK;        // vector rows of a block taken at a time
     const LayerView &L = P.L;
-    const int cb = blockIdx.x % P.col_blocks, rb = blockIdx.x / P.col_blocks;
+    const int cb = index % P.col_blocks, rb = index / P.col_blocks;
     const int m0 = rb * FP8_BLOCK, m1 = min(L.M, m0 + FP8_BLOCK);
     const int v = V > 0 ? V : L.v;
     {
         const int c = threadIdx.x % FP8_BLOCK, sub = threadIdx.x / FP8_BLOCK;
         const int f = cb * FP8_BLOCK + c;                                 // input feature
         const int n = f >= L.N ? -1 : P.inverse ? __ldg(P.inverse + f) : f;      // stored column
-        float sc = 1.f, bi = 0.f;
+        float sc = 1.f, bi = -0.f;                                        // without them t * 1 + (-0) = t, whatever t and its sign
         if (n >= 0 && L.has_scale && !L.scale_rows) { sc = __half2float(__ldg(L.scale + n)); bi = __half2float(__ldg(L.bias + n)); }
         auto put = [&](int m, float t) {
             float s = sc, b = bi;
@@ -86,11 +93,22 @@ dequant_fp8_kernel(const __grid_constant__ DequantFp8Params P)
         if (n < 0) {
             for (int m = m0 + sub; m < m1; m += COL_LANES) tile[m - m0][c] = __float2half_rn(0.f);
         } else if (n < L.n_out) {
-            for (int r = m0 / L.v0 + sub; r * L.v0 < m1; r += COL_LANES) {
-                const int i0 = clamp_index(load_index(L.s0.ptr + (long long)r * L.s0.stride, n, L.s0.bits), L.k0);
+            // (few columns, but a wait for every read of each would hold up the whole block: eight indices, then their rows)
+            const int r1 = (m1 + L.v0 - 1) / L.v0;
+            for (int r0 = m0 / L.v0 + sub; r0 < r1; r0 += COL_LANES * 8) {
+                int i0[8];
+#pragma unroll
+                for (int i = 0; i < 8; i++)
+                    i0[i] = clamp_index(load_index(L.s0.ptr + (long long)min(r0 + i * COL_LANES, r1 - 1) * L.s0.stride, n, L.s0.bits), L.k0);
                 for (int j = 0; j < L.v0; j++) {
-                    const int m = r * L.v0 + j;
-                    if (m >= m0 && m < m1) put(m, __half2float(__ldg(L.c0 + (long long)i0 * L.v0 + j)));
+                    float t[8];
+#pragma unroll
+                    for (int i = 0; i < 8; i++) t[i] = __half2float(__ldg(L.c0 + (long long)i0[i] * L.v0 + j));
+#pragma unroll
+                    for (int i = 0; i < 8; i++) {
+                        const int r = r0 + i * COL_LANES, m = r * L.v0 + j;
+                        if (r < r1 && m >= m0 && m < m1) put(m, t[i]);
+                    }
                 }
             }
         } else {
@@ -108,13 +126,45 @@ dequant_fp8_kernel(const __grid_constant__ DequantFp8Params P)
                 }
 #pragma unroll
                 for (int i = 0; i < ITEMS; i++) {
-                    w1[i] = table_row<V>(L.c1, e1[i]);
-                    if (res) w2[i] = table_row<V>(L.c2, e2[i]);
+                    if constexpr (TABLES) {
+                        const uint4 q = tables[e1[i]], p = tables[res ? L.k1 + e2[i] : 0];
+                        const uint32_t a[4] = {q.x, q.y, q.z, q.w}, b[4] = {p.x, p.y, p.z, p.w};
+#pragma unroll
+                        for (int k = 0; k < V / 2; k++) { w1[i].w[k] = a[k]; w2[i].w[k] = b[k]; }
+                    } else {
+                        w1[i] = table_row<V>(L.c1, e1[i]);
+                        if (res) w2[i] = table_row<V>(L.c2, e2[i]);
+                    }
                 }
 #pragma unroll
                 for (int i = 0; i < ITEMS; i++) {
                     const int r = r0 + i * COL_LANES;
                     if (r >= r1) break;
+                    if constexpr (V > 0) {
+                        // scale per column: two values at a time, without checks where the block has the whole vector (a value at a time with
+                        // all checks took three times the instructions)
+                        if (!L.scale_rows) {
+                            const int first = r * V - m0;
+                            __half *dst = &tile[0][c] + first * TILE_STRIDE;
+                            auto pairs = [&](auto whole) {
+#pragma unroll
+                                for (int k = 0; k < V / 2; k++) {
+                                    float2 y = __half22float2(*reinterpret_cast<const __half2 *>(&w1[i].w[k]));
+                                    if (res) {
+                                        const float2 z = __half22float2(*reinterpret_cast<const __half2 *>(&w2[i].w[k]));
+                                        y.x = __fadd_rn(y.x, z.x);
+                                        y.y = __fadd_rn(y.y, z.y);
+                                    }
+                                    const __half2 o = __floats2half2_rn(__fadd_rn(__fmul_rn(y.x, sc), bi), __fadd_rn(__fmul_rn(y.y, sc), bi));
+                                    if (decltype(whole)::value || (unsigned)(first + 2 * k) < (unsigned)(m1 - m0)) dst[2 * k * TILE_STRIDE] = __low2half(o);
+                                    if (decltype(whole)::value || (unsigned)(first + 2 * k + 1) < (unsigned)(m1 - m0)) dst[(2 * k + 1) * TILE_STRIDE] = __high2half(o);
+                                }
+                            };
+                            if (first >= 0 && r * V + V <= m1) pairs(std::true_type());
+                            else pairs(std::false_type());
+                            continue;
+                        }
+                    }
                     auto one = [&](int j) {
                         const int m = r * v + j;
                         if (m < m0 || m >= m1) return;
@@ -150,7 +200,7 @@ dequant_fp8_kernel(const __grid_constant__ DequantFp8Params P)
 #pragma unroll
     for (int i = 0; i < THREADS / 32; i++) most = max(most, part[i]);
     const Fp8Scale s = fp8_scale(__half2float(__ushort_as_half((unsigned short)most)));
-    if (threadIdx.x == 0) P.scale[blockIdx.x] = s.scale;
+    if (threadIdx.x == 0) P.scale[index] = s.scale;
     if (c >= P.pitch) return;
 #pragma unroll
     for (int i = 0; i < ROUNDS; i++) {
@@ -168,6 +218,45 @@ dequant_fp8_kernel(const __grid_constant__ DequantFp8Params P)
         if (c + 8 > L.N)
             for (int j = max(0, L.N - c); j < 8; j++) dst[j] = 0;         // pad bytes are zeros, whatever the factor
     }
+}
+
+template <int V, bool TABLES>
+__global__ void __launch_bounds__(threads<TABLES>(), TABLES ? 2 : 4)
+dequant_fp8_kernel(const __grid_constant__ DequantFp8Params P)
+{
+    constexpr int THREADS = threads<TABLES>();
+    __shared__ __align__(16) __half tile[FP8_BLOCK][TILE_STRIDE];
+    __shared__ uint32_t part[THREADS / 32];
+    extern __shared__ __align__(16) uint4 tables[];
+    if constexpr (TABLES) {
+        for (int i = threadIdx.x; i < P.L.k1 + P.L.k2; i += THREADS)
+            tables[i] = i < P.L.k1 ? load_centroid_row(P.L.c1, i, V) : load_centroid_row(P.L.c2, i - P.L.k1, V);
+        __syncthreads();
+        for (int b = blockIdx.x; b < P.blocks; b += gridDim.x) {
+            restore_block<V, true>(P, b, tile, part, tables);
+            __syncthreads();
+        }
+    } else {
+        restore_block<V, false>(P, blockIdx.x, tile, part, nullptr);
+    }
+}
+
+template <int V>
+cudaError_t restore(const DequantFp8Params &P, cudaStream_t st)
+{
+    if constexpr (V == 6 || V == 8) {
+        // staging pays when a CTA reads more rows out of the tables than they have
+        const int grid = 2 * device_sm_count(), entries = P.L.k1 + P.L.k2;
+        if (P.L.G == 1 && P.L.Nc > 0 && entries <= TABLES_MAX && (long long)P.L.R * P.L.Nc / grid > entries) {
+            auto kern = dequant_fp8_kernel<V, true>;
+            const cudaError_t e = allow_dynamic_smem(reinterpret_cast<const void *>(kern), 16ull * TABLES_MAX);
+            if (e != cudaSuccess) return e;
+            kern<<<P.blocks < grid ? P.blocks : grid, threads<true>(), 16ull * entries, st>>>(P);
+            return cudaGetLastError();
+        }
+    }
+    dequant_fp8_kernel<V, false><<<P.blocks, threads<false>(), 0, st>>>(P);
+    return cudaGetLastError();
 }
 
 // stored column order -> the stored column of every feature; a list that is no permutation: the largest column that names it, -1 none
@@ -193,14 +282,13 @@ cudaError_t launch_dequant_fp8(const LayerView &L, uint8_t *q, float *scale, int
         if ((e = cudaGetLastError()) != cudaSuccess) return e;
         P.inverse = inverse;
     }
-    const unsigned blocks = (unsigned)((long long)ceil_div(L.M, FP8_BLOCK) * P.col_blocks);
+    P.blocks = (int)((long long)ceil_div(L.M, FP8_BLOCK) * P.col_blocks);
     switch (L.v) {
-    case 8: dequant_fp8_kernel<8><<<blocks, THREADS, 0, st>>>(P); break;
-    case 6: dequant_fp8_kernel<6><<<blocks, THREADS, 0, st>>>(P); break;
-    case 12: dequant_fp8_kernel<12><<<blocks, THREADS, 0, st>>>(P); break;
-    default: dequant_fp8_kernel<0><<<blocks, THREADS, 0, st>>>(P);
+    case 8: return restore<8>(P, st);
+    case 6: return restore<6>(P, st);
+    case 12: return restore<12>(P, st);
+    default: return restore<0>(P, st);
     }
-    return cudaGetLastError();
 }
 
 }  // namespace vptq
