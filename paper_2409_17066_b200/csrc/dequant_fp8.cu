@@ -2,25 +2,29 @@
 // bit (FP32, three separately rounded operations, then FP16), quantized by the rule of fp8_quantize.cu, without the FP16 matrix in
 // global memory.
 //
-// A CTA makes a 128 x 128 block at a time: its threads look up the (vector row, column) pairs that meet the block, ITEMS at a time so
-// that as many table reads are in flight, and leave the FP16 values in shared memory; the block's maximum and the rounding follow.
+// A CTA makes a 128 x 128 block at a time and leaves its FP16 values in shared memory; the block's maximum and the rounding follow.
+// A thread takes four adjacent columns of a vector row: their indices are one window of packed words, their values leave as 8-byte
+// stores (one column to a thread: 8192 x 28672 322 us instead of 255; eight to a thread spill: 335). Columns that do not lie so, under
+// a permutation, beside the outliers, at other index widths, are looked up one to a thread, ITEMS vector rows at a time so that as many
+// table reads are in flight.
 // A vector row that crosses a block's edge is looked up by both blocks (v = 8 never does; v = 6: 23 rows instead of 21.3).
 // TABLES: main and residual table of a layer with one group are staged in shared memory as 16-byte rows, and two CTAs an SM go through
-// the blocks; out of L1 every 4-byte piece of a 12-byte row is a wavefront of its own for each lane (11008 x 4096 with v = 6: 97 us).
-// A table in L2 (1 MiB) is bound by its random reads, one a clock and SM.
+// the blocks; out of L1 every 4-byte piece of a 12-byte row is a wavefront of its own for each lane (11008 x 4096 with v = 6: 97 us
+// instead of 75).
+// A table in L2 (1 MiB) is bound by its random reads, one a clock and SM: 4096 x 4096 17.8 us; a small table by the arithmetic.
 #include "fp8.cuh"
 #include "index_words.cuh"
-
-#include <type_traits>
+#include "restore_words.cuh"
 
 namespace vptq {
 
 namespace {
 
-// threads of a CTA, and pairs that a thread looks up at a time: out of L2 more CTAs (8192 x 28672: 314 us; 512 threads 367), out of shared
-// memory more threads to hide their arithmetic behind one another's (11008 x 4096, v = 6: 81 us; 256 threads 108)
+// threads of a CTA, and pairs that a thread looks up at a time: out of L2 more CTAs, out of shared memory more threads to hide their
+// arithmetic behind one another's (one column to a thread: 8192 x 28672 314 us, 512 threads 367; 11008 x 4096, v = 6, 81, 256 threads 108)
 template <bool TABLES> constexpr int threads() { return TABLES ? 512 : 256; }
 template <bool TABLES> constexpr int items() { return TABLES ? 2 : 4; }
+constexpr int CPL = 4;                                   // adjacent columns that a thread restores together
 constexpr int TILE_STRIDE = FP8_BLOCK + 8;                // halves; 16-byte rows, half warps read them without conflicts
 
 struct DequantFp8Params {
@@ -33,29 +37,9 @@ struct DequantFp8Params {
 };
 constexpr int TABLES_MAX = (115712 - 1024 - FP8_BLOCK * TILE_STRIDE * 2) / 16;         // entries of both tables, two CTAs an SM
 
-// V = 0: any length, component by component
-template <int V> struct Row { uint32_t w[V > 0 ? V / 2 : 1]; };
+// component j of a table row: out of its words, or (V = 0: any length) out of the table
 template <int V>
-__device__ __forceinline__ Row<V> table_row(const __half *__restrict__ tab, long long e)
-{
-    Row<V> r = {};
-    if constexpr (V == 8) {
-        const uint4 q = __ldg(reinterpret_cast<const uint4 *>(tab) + e);
-        r.w[0] = q.x; r.w[1] = q.y; r.w[2] = q.z; r.w[3] = q.w;
-    } else if constexpr (V % 4 == 0 && V > 0) {
-#pragma unroll
-        for (int i = 0; i < V / 4; i++) {
-            const uint2 q = __ldg(reinterpret_cast<const uint2 *>(tab) + e * (V / 4) + i);
-            r.w[2 * i] = q.x; r.w[2 * i + 1] = q.y;
-        }
-    } else if constexpr (V > 0) {
-#pragma unroll
-        for (int i = 0; i < V / 2; i++) r.w[i] = __ldg(reinterpret_cast<const uint32_t *>(tab) + e * (V / 2) + i);
-    }
-    return r;
-}
-template <int V>
-__device__ __forceinline__ float component(const Row<V> &r, const __half *__restrict__ tab, long long e, int v, int j)
+__device__ __forceinline__ float component(const RowWords<V> &r, const __half *__restrict__ tab, long long e, int v, int j)
 {
     if constexpr (V > 0) {
         const uint32_t w = r.w[j / 2];
@@ -79,9 +63,77 @@ __device__ __forceinline__ void restore_block(const DequantFp8Params &P, int ind
     const int cb = index % P.col_blocks, rb = index / P.col_blocks;
     const int m0 = rb * FP8_BLOCK, m1 = min(L.M, m0 + FP8_BLOCK);
     const int v = V > 0 ? V : L.v;
-    {
+    // columns [fast0, fast1) of the block are restored several adjacent ones to a thread, the others one to a thread
+    int fast0 = 0, fast1 = 0;
+    if constexpr (V > 0) {
+        const int b1 = L.s1.bits, b2 = L.k2 > 0 ? L.s2.bits : 8;
+        if (P.inverse == nullptr && !L.scale_rows && (b1 == 8 || b1 == 12 || b1 == 16) && (b2 == 8 || b2 == 12 || b2 == 16)) {
+            fast0 = min(FP8_BLOCK, (max(0, L.n_out - cb * FP8_BLOCK) + CPL - 1) / CPL * CPL);
+            fast1 = min(FP8_BLOCK, (L.N - cb * FP8_BLOCK) / CPL * CPL);
+        }
+        const int per_row = (fast1 - fast0) / CPL, first = m0 / V, rows = (m1 + V - 1) / V - first;
+        const bool res = L.k2 > 0;
+        for (int task = threadIdx.x; per_row > 0 && task < rows * per_row; task += THREADS) {
+            const int r = first + task / per_row, c = fast0 + task % per_row * CPL, n = cb * FP8_BLOCK + c, col = n - L.n_out;
+            const unsigned bit1 = (unsigned)col * (unsigned)b1, bit2 = (unsigned)col * (unsigned)b2;
+            const IndexWindow<CPL> q1 = load_window<CPL>(L.s1.ptr + (long long)r * L.s1.stride, bit1, (unsigned)(L.s1.stride >> 2));
+            IndexWindow<CPL> q2 = {};
+            if (res) q2 = load_window<CPL>(L.s2.ptr + (long long)r * L.s2.stride, bit2, (unsigned)(L.s2.stride >> 2));
+            int i1[CPL], i2[CPL];
+            decode_window<CPL>(q1, bit1 & 31u, b1, L.k1, i1);
+            decode_window<CPL>(q2, bit2 & 31u, b2, res ? L.k2 : 1, i2);
+            RowWords<V> w1[CPL], w2[CPL];
+#pragma unroll
+            for (int k = 0; k < CPL; k++) {
+                if constexpr (TABLES) {
+                    const uint4 a = tables[i1[k]], b = tables[res ? L.k1 + i2[k] : 0];
+                    const uint32_t wa[4] = {a.x, a.y, a.z, a.w}, wb[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+                    for (int j = 0; j < V / 2; j++) { w1[k].w[j] = wa[j]; w2[k].w[j] = wb[j]; }
+                } else {
+                    const long long group = L.G > 1 ? (col + k) / L.cpg : 0;
+                    w1[k] = row_from_global<V>(L.c1, group * L.k1 + i1[k]);
+                    if (res) w2[k] = row_from_global<V>(L.c2, group * L.k2 + i2[k]);
+                }
+            }
+            // scale and bias of the columns; without them t * 1 + (-0) = t, whatever t and its sign
+            float sc[CPL], bi[CPL];
+#pragma unroll
+            for (int k = 0; k < CPL; k += 2) {
+                float2 fs = make_float2(1.f, 1.f), fb = make_float2(-0.f, -0.f);
+                if (L.has_scale) {
+                    fs = __half22float2(__ldg(reinterpret_cast<const __half2 *>(L.scale + n + k)));
+                    fb = __half22float2(__ldg(reinterpret_cast<const __half2 *>(L.bias + n + k)));
+                }
+                sc[k] = fs.x; sc[k + 1] = fs.y; bi[k] = fb.x; bi[k + 1] = fb.y;
+            }
+            const int at = r * V - m0;
+            __half *dst = &tile[0][c] + at * TILE_STRIDE;
+#pragma unroll
+            for (int j = 0; j < V / 2; j++) {
+                float2 y[CPL];                                            // components 2j, 2j + 1 of the thread's columns
+#pragma unroll
+                for (int k = 0; k < CPL; k++) {
+                    y[k] = __half22float2(*reinterpret_cast<const __half2 *>(&w1[k].w[j]));
+                    if (res) y[k] = add_half2(y[k], w2[k].w[j]);
+                    y[k].x = __fadd_rn(__fmul_rn(y[k].x, sc[k]), bi[k]);
+                    y[k].y = __fadd_rn(__fmul_rn(y[k].y, sc[k]), bi[k]);
+                }
+#pragma unroll
+                for (int h = 0; h < 2; h++) {
+                    __align__(8) __half2 o[CPL / 2];
+#pragma unroll
+                    for (int k = 0; k < CPL; k += 2) o[k / 2] = __floats2half2_rn(h ? y[k].y : y[k].x, h ? y[k + 1].y : y[k + 1].x);
+                    if ((unsigned)(at + 2 * j + h) < (unsigned)(m1 - m0))
+                        *reinterpret_cast<uint2 *>(dst + (2 * j + h) * TILE_STRIDE) = *reinterpret_cast<const uint2 *>(o);
+                }
+            }
+        }
+    }
+    if (fast0 > 0 || fast1 < FP8_BLOCK) {
         const int c = threadIdx.x % FP8_BLOCK, sub = threadIdx.x / FP8_BLOCK;
         const int f = cb * FP8_BLOCK + c;                                 // input feature
+        const bool done = c >= fast0 && c < fast1;
         const int n = f >= L.N ? -1 : P.inverse ? __ldg(P.inverse + f) : f;      // stored column
         float sc = 1.f, bi = -0.f;                                        // without them t * 1 + (-0) = t, whatever t and its sign
         if (n >= 0 && L.has_scale && !L.scale_rows) { sc = __half2float(__ldg(L.scale + n)); bi = __half2float(__ldg(L.bias + n)); }
@@ -90,7 +142,8 @@ __device__ __forceinline__ void restore_block(const DequantFp8Params &P, int ind
             if (L.has_scale && L.scale_rows) { s = __half2float(__ldg(L.scale + m)); b = __half2float(__ldg(L.bias + m)); }
             tile[m - m0][c] = __float2half_rn(finish(t, L.has_scale, s, b));
         };
-        if (n < 0) {
+        if (done) {
+        } else if (n < 0) {
             for (int m = m0 + sub; m < m1; m += COL_LANES) tile[m - m0][c] = __float2half_rn(0.f);
         } else if (n < L.n_out) {
             // (few columns, but a wait for every read of each would hold up the whole block: eight indices, then their rows)
@@ -117,7 +170,7 @@ __device__ __forceinline__ void restore_block(const DequantFp8Params &P, int ind
             const int r1 = (m1 + v - 1) / v;                              // (m1 <= M: rows that exist)
             for (int r0 = m0 / v + sub; r0 < r1; r0 += COL_LANES * ITEMS) {
                 long long e1[ITEMS], e2[ITEMS];
-                Row<V> w1[ITEMS], w2[ITEMS];
+                RowWords<V> w1[ITEMS], w2[ITEMS];
 #pragma unroll
                 for (int i = 0; i < ITEMS; i++) {
                     const int r = min(r0 + i * COL_LANES, r1 - 1);
@@ -131,40 +184,15 @@ __device__ __forceinline__ void restore_block(const DequantFp8Params &P, int ind
                         const uint32_t a[4] = {q.x, q.y, q.z, q.w}, b[4] = {p.x, p.y, p.z, p.w};
 #pragma unroll
                         for (int k = 0; k < V / 2; k++) { w1[i].w[k] = a[k]; w2[i].w[k] = b[k]; }
-                    } else {
-                        w1[i] = table_row<V>(L.c1, e1[i]);
-                        if (res) w2[i] = table_row<V>(L.c2, e2[i]);
+                    } else if constexpr (V > 0) {
+                        w1[i] = row_from_global<V>(L.c1, e1[i]);
+                        if (res) w2[i] = row_from_global<V>(L.c2, e2[i]);
                     }
                 }
 #pragma unroll
                 for (int i = 0; i < ITEMS; i++) {
                     const int r = r0 + i * COL_LANES;
                     if (r >= r1) break;
-                    if constexpr (V > 0) {
-                        // scale per column: two values at a time, without checks where the block has the whole vector (a value at a time with
-                        // all checks took three times the instructions)
-                        if (!L.scale_rows) {
-                            const int first = r * V - m0;
-                            __half *dst = &tile[0][c] + first * TILE_STRIDE;
-                            auto pairs = [&](auto whole) {
-#pragma unroll
-                                for (int k = 0; k < V / 2; k++) {
-                                    float2 y = __half22float2(*reinterpret_cast<const __half2 *>(&w1[i].w[k]));
-                                    if (res) {
-                                        const float2 z = __half22float2(*reinterpret_cast<const __half2 *>(&w2[i].w[k]));
-                                        y.x = __fadd_rn(y.x, z.x);
-                                        y.y = __fadd_rn(y.y, z.y);
-                                    }
-                                    const __half2 o = __floats2half2_rn(__fadd_rn(__fmul_rn(y.x, sc), bi), __fadd_rn(__fmul_rn(y.y, sc), bi));
-                                    if (decltype(whole)::value || (unsigned)(first + 2 * k) < (unsigned)(m1 - m0)) dst[2 * k * TILE_STRIDE] = __low2half(o);
-                                    if (decltype(whole)::value || (unsigned)(first + 2 * k + 1) < (unsigned)(m1 - m0)) dst[(2 * k + 1) * TILE_STRIDE] = __high2half(o);
-                                }
-                            };
-                            if (first >= 0 && r * V + V <= m1) pairs(std::true_type());
-                            else pairs(std::false_type());
-                            continue;
-                        }
-                    }
                     auto one = [&](int j) {
                         const int m = r * v + j;
                         if (m < m0 || m >= m1) return;
@@ -221,7 +249,7 @@ __device__ __forceinline__ void restore_block(const DequantFp8Params &P, int ind
 }
 
 template <int V, bool TABLES>
-__global__ void __launch_bounds__(threads<TABLES>(), TABLES ? 2 : 4)
+__global__ void __launch_bounds__(threads<TABLES>(), TABLES ? 2 : V > 8 ? 3 : 4)
 dequant_fp8_kernel(const __grid_constant__ DequantFp8Params P)
 {
     constexpr int THREADS = threads<TABLES>();
