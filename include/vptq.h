@@ -448,13 +448,13 @@ int vptq_kmeans_update(const void *W, int32_t M, int32_t N, int32_t v, const int
  *
  * vptq_fp8_quantize: x [rows][cols] of x_dtype (FP16, BF16 or FP32), its rows `ld` values apart (ld >= cols; any alignment of a
  *   value of the type), to q and scale (16-byte aligned, q packed at the pitch above).  block_rows is 1 or 128, else VPTQ_E_SHAPE.
- *   rows = 0 does nothing. */
+ *   rows = 0 does nothing; rows and cols are at most 2^30, else VPTQ_E_SHAPE (M, N and B of the calls below too). */
 int64_t vptq_fp8_row_bytes(int32_t n_cols);
 int vptq_fp8_quantize(const void *x, int32_t x_dtype, int32_t n_rows, int32_t n_cols, int64_t ld, int32_t block_rows,
                       uint8_t *q, float *scale, void *stream);
 /* A vector-quantized layer as an e4m3 weight: the FP16 values of vptq_dequant, bit for bit, quantized by the rule with
  * block_rows = 128; the FP16 matrix is not written anywhere.  q [M][pitch(N)], scale [ceil(M / 128)][ceil(N / 128)].  Layers with a
- * stored column order (VPTQ_FLAG_COL_PERM) need vptq_dequant_fp8_workspace_bytes() bytes of workspace, others none. */
+ * stored column order (VPTQ_FLAG_COL_PERM) need vptq_dequant_fp8_workspace_bytes() bytes of workspace, others none.  N < 2^28, else VPTQ_E_SHAPE. */
 int64_t vptq_dequant_fp8_workspace_bytes(const vptq_layer_desc *desc);
 int vptq_dequant_fp8(const vptq_layer_desc *desc, const vptq_layer_ptrs *p, uint8_t *q, float *scale,
                      void *workspace, size_t workspace_bytes, void *stream);

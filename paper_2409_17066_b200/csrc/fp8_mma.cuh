@@ -22,7 +22,6 @@ struct WeightFrag { uint4 q[2][2]; };
 template <int DT, bool VEC> struct TokenRaw { float v[32]; };                         // (value by value)
 template <> struct TokenRaw<VPTQ_DTYPE_FP16, true> { uint4 q[4]; };
 template <> struct TokenRaw<VPTQ_DTYPE_BF16, true> { uint4 q[4]; };
-template <> struct TokenRaw<VPTQ_DTYPE_FP32, true> { float4 q[8]; };
 template <bool VEC> struct TokenRaw<VPTQ_DTYPE_E4M3, VEC> { uint4 q[2]; };
 
 // ... and as MMA operands with the block's scale
@@ -43,12 +42,6 @@ __device__ __forceinline__ TokenRaw<DT, VEC> load_token(const void *row, int t, 
         for (int i = 0; i < 32; i++) {
             const int c = c0 + 64 * (i >> 4) + (i & 15);
             r.v[i] = row != nullptr && c < cols ? Act<DT>::one(row, c) : 0.f;
-        }
-    } else if constexpr (DT == VPTQ_DTYPE_FP32) {
-#pragma unroll
-        for (int i = 0; i < 8; i++) {
-            const int c = c0 + 64 * (i >> 2) + 4 * (i & 3);
-            r.q[i] = row != nullptr && c < cols ? __ldcg(reinterpret_cast<const float4 *>(reinterpret_cast<const float *>(row) + c)) : make_float4(0.f, 0.f, 0.f, 0.f);
         }
     } else {
 #pragma unroll
@@ -75,9 +68,6 @@ __device__ __forceinline__ TokenFrag quantize_token(const TokenRaw<DT, VEC> &r, 
         if constexpr (!VEC) {
 #pragma unroll
             for (int i = 0; i < 32; i++) v[i] = r.v[i];
-        } else if constexpr (DT == VPTQ_DTYPE_FP32) {
-#pragma unroll
-            for (int i = 0; i < 8; i++) { v[4 * i] = r.q[i].x; v[4 * i + 1] = r.q[i].y; v[4 * i + 2] = r.q[i].z; v[4 * i + 3] = r.q[i].w; }
         } else {
 #pragma unroll
             for (int i = 0; i < 4; i++) {
@@ -90,7 +80,7 @@ __device__ __forceinline__ TokenFrag quantize_token(const TokenRaw<DT, VEC> &r, 
             }
         }
         uint32_t m;
-        if constexpr (VEC && DT != VPTQ_DTYPE_FP32) {
+        if constexpr (VEC) {
             uint32_t w[4];
 #pragma unroll
             for (int i = 0; i < 4; i++) w[i] = max16(max16(r.q[i].x, r.q[i].y), max16(r.q[i].z, r.q[i].w));

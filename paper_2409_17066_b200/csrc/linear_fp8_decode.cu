@@ -2,16 +2,17 @@
 //
 // Persistent CTAs, one per SM, own consecutive groups of 16 output rows and take up to PASS of them (a pass) through all columns.  Each of
 // the 8 or 16 warps takes every eighth (sixteenth) run of 128-column blocks and feeds itself: a ring of stages in shared memory, a stage one run of the
-// pass's rows in one TMA box (128-byte swizzle), refilled as soon as it has been read.  A TMA instruction costs about 100 clocks of an
-// SM whatever it brings, so a run is as many blocks as make 8 KB (one where rows are no multiple of 128 bytes), and the activations,
-// which no other warp of the CTA needs, come straight from global memory, two blocks ahead.  (A ring for the whole CTA filled by a warp
-// of its own took 11.0 us for 4096 x 4096, stages with the activations in boxes of their own 6.5.)  The scales are fetched for 32 (the
+// pass's rows in one TMA box (128-byte swizzle), refilled as soon as it has been read.  A run is as many blocks as make 8 KB (one where
+// rows are no multiple of 128 bytes): fewer copies and waits (4096 x 4096, one token in 16 bits, 6.8 us; a block at a time 7.2).  The
+// activations, which no other warp of the CTA needs, come straight from global memory, two blocks ahead.  (A ring for the whole CTA
+// filled by a warp of its own took 11.0 us.)  The scales are fetched for 32 (the
 // weight's) or 4 blocks (the tokens') at a time, one to a lane.
 // The warp multiplies (fp8_mma.cuh) and keeps FP32 sums of all the pass's rows.  16-bit activations are quantized on the way, by the
 // same rule as vptq_fp8_quantize: the four lanes that hold a token's block find its maximum with two shuffles, and all the pass's rows
 // share that work.  At the end of a pass the warps' sums meet in shared memory and are added in warp order: a result does not depend on
 // timing.
-// Bound by HBM: M * N bytes.
+// Large weights are bound by HBM, M * N bytes (28672 x 8192 40.3 us, 5.8 TB/s); small ones by what a warp does for a block, one step
+// after the other: 1000 to 1900 clocks.
 // Every wait is bounded; a warp whose wait gives up leaves NaN.
 #include "fp8_mma.cuh"
 #include "tcgen05_ptx.cuh"
@@ -85,17 +86,18 @@ linear_fp8_decode_kernel(const __grid_constant__ CUtensorMap map_full, const __g
             load_groups = pass_begin(load_pass + 1) - pass_begin(load_pass);
         }
     };
-    // (the weights are no preceding kernel's output: the first stages come in while that still runs)
     if (lane == 0) {
         for (uint32_t s = 0; s < stages; s++) mbar_init(bars + 8 * s, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    pdl_launch_dependents();
+    // (weight, scales and activations may all be the preceding kernel's output; weights ahead of the wait would save 0.2 us of a call)
+    pdl_wait();
     for (uint32_t s = 0; s < stages && load_pass < passes; s++) {
         if (lane == 0) load(s);
         next_load();
     }
     __syncwarp();
-    pdl_launch_dependents();
     uint32_t gave_up = 0;
 
     const int g = lane >> 2, t = lane & 3;
@@ -115,7 +117,6 @@ linear_fp8_decode_kernel(const __grid_constant__ CUtensorMap map_full, const __g
         const int mine = (runs - warp + WARPS - 1) / WARPS;                    // runs; the last one of all may be short
         iterations = mine * run - ((warp + (mine - 1) * WARPS) == runs - 1 ? runs * run - kbs : 0);
     }
-    pdl_wait();                                           // the activations may be the preceding kernel's
     uint32_t slot = 0, parity = 0;
     for (int p = 0; p < passes; p++) {
         const int g0 = pass_begin(p), n_groups = pass_begin(p + 1) - g0;

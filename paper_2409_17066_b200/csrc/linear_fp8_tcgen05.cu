@@ -333,28 +333,18 @@ linear_fp8_tcgen05_kernel(const __grid_constant__ CUtensorMap map_x, const __gri
         if (warp == 0) {
             // ---- loads: this CTA's tokens, and its part of the tile's features; the bytes of a pair count on rank 0's barrier ----
             uint32_t it = 0;
-            // the first stages' weights are no one's output: they may come in while the preceding kernel still runs
-            uint32_t early = 0;
             const uint32_t full0 = PAIR > 1 ? address_in(bar_full(0), 0) : bar_full(0);
             const int n_part = t_rank * (TN / PAIR);
-            if (first < P.tiles)
-                for (int kb = kb0; kb < kb1 && early < ST; kb++, early++)
-                    if (elect_one()) {
-                        if (t_rank == 0) mbar_expect_tx(bar_full(early), PAIR * SB);
-                        tma_load<PAIR>(base + early * SB + X_BYTES, &map_w, kb * FP8_BLOCK, first / P.tiles_t * TN + n_part, full0 + 8 * early);
-                    }
-            pdl_wait();
+            pdl_wait();                                                        // (weight and activations may be the preceding kernel's)
             for (int tile = first; tile < P.tiles; tile += step) {
                 const int t0 = (tile % P.tiles_t * PAIR + t_rank) * TM, n0 = tile / P.tiles_t * TN + n_part;
                 for (int kb = kb0; kb < kb1; kb++, it++) {
                     const uint32_t s = it % ST;
-                    if (it >= early) mbar_wait_uniform(bar_empty(s), ((it / ST) & 1) ^ 1u, gave_up);
+                    mbar_wait_uniform(bar_empty(s), ((it / ST) & 1) ^ 1u, gave_up);
                     if (gave_up) break;
                     if (elect_one()) {
-                        if (it >= early) {
-                            if (t_rank == 0) mbar_expect_tx(bar_full(s), PAIR * SB);
-                            tma_load<PAIR>(base + s * SB + X_BYTES, &map_w, kb * FP8_BLOCK, n0, full0 + 8 * s);
-                        }
+                        if (t_rank == 0) mbar_expect_tx(bar_full(s), PAIR * SB);
+                        tma_load<PAIR>(base + s * SB + X_BYTES, &map_w, kb * FP8_BLOCK, n0, full0 + 8 * s);
                         tma_load<PAIR>(base + s * SB, &map_x, kb * FP8_BLOCK, t0, full0 + 8 * s);
                     }
                     __syncwarp();

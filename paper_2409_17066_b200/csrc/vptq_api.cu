@@ -550,7 +550,7 @@ int64_t vptq_fp8_row_bytes(int32_t n_cols)
 int vptq_fp8_quantize(const void *x, int32_t x_dtype, int32_t n_rows, int32_t n_cols, int64_t ld, int32_t block_rows,
                       uint8_t *q, float *scale, void *stream)
 {
-    if (n_rows < 0 || n_cols <= 0 || n_cols > FP8_MAX_SIZE || ld < n_cols || (block_rows != 1 && block_rows != FP8_BLOCK)) return VPTQ_E_SHAPE;
+    if (n_rows < 0 || n_rows > FP8_MAX_SIZE || n_cols <= 0 || n_cols > FP8_MAX_SIZE || ld < n_cols || (block_rows != 1 && block_rows != FP8_BLOCK)) return VPTQ_E_SHAPE;
     if (x_dtype != VPTQ_DTYPE_FP16 && x_dtype != VPTQ_DTYPE_BF16 && x_dtype != VPTQ_DTYPE_FP32) return VPTQ_E_UNSUPPORTED;
     if (n_rows == 0) return VPTQ_OK;
     if (x == nullptr || q == nullptr || scale == nullptr) return VPTQ_E_NULL;
@@ -574,7 +574,7 @@ int vptq_dequant_fp8(const vptq_layer_desc *desc, const vptq_layer_ptrs *p, uint
     if (rc != VPTQ_OK) return rc;
     rc = check_ptrs(desc, p);
     if (rc != VPTQ_OK) return rc;
-    if (desc->M > FP8_MAX_SIZE || desc->N > FP8_MAX_SIZE) return VPTQ_E_SHAPE;
+    if (desc->M > FP8_MAX_SIZE || desc->N >= 1 << 28) return VPTQ_E_SHAPE;               // (an index's bit in its row is counted in 32 bits)
     if (q == nullptr || scale == nullptr) return VPTQ_E_NULL;
     if (!aligned16(q) || !aligned16(scale)) return VPTQ_E_ALIGN;
     const int64_t need = vptq_dequant_fp8_workspace_bytes(desc);

@@ -67,6 +67,16 @@ def test_dequant_fp8_refusals(b):
     assert f(C.byref(perm), C.byref(pp), p, p, p + 16, need, None) == b.E_ALIGN
 
 
+def test_sizes_beyond_the_counters_are_refused(b):
+    p = 0x1000
+    assert b.lib.vptq_fp8_quantize(p, 0, 2 ** 31 - 1, 1, 1, 1, p, p, None) == b.E_SHAPE
+    assert b.lib.vptq_fp8_quantize(p, 0, 1, 2 ** 30 + 1, 2 ** 31, 1, p, p, None) == b.E_SHAPE
+    # (an index's bit in its row is counted in 32 bits)
+    ptrs = b.LayerPtrs(p, p, None, None, None, None, p, p)
+    wide = b.make_desc(8, 2 ** 28, 8, 65536)
+    assert b.lib.vptq_dequant_fp8(C.byref(wide), C.byref(ptrs), p, p, None, 0, None) == b.E_SHAPE
+
+
 def test_linear_fp8_refusals(b):
     f, p = b.lib.vptq_linear_fp8, 0x1000
     d = b.make_fp8_desc(64, 64, "e4m3", "fp16")

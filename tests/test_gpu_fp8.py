@@ -108,6 +108,19 @@ def test_dequant_fp8_is_the_quantized_restored_weight(b, spec):
     check_quantized(q, scale, W, 128)
 
 
+# (large enough that the tables are staged in shared memory; index widths of 8, 12 and 16 bits and others, columns that start and end
+# inside a block, rows that cross its edge)
+STAGED = [synth.LayerSpec("f_s8", 1000, 1100, v=8, k1=256), synth.LayerSpec("f_s8_res", 1003, 1101, v=8, k1=256, k2=256), synth.LayerSpec("f_s6_out", 1000, 1102, v=6, k1=256, k2=64, n_out=33, v0=4, k0=16),
+          synth.LayerSpec("f_s6_12", 4100, 2006, v=6, k1=4096, n_out=130, v0=2, k0=64), synth.LayerSpec("f_s8_perm", 1000, 1100, v=8, k1=256, k2=16, permuted=True),
+          synth.LayerSpec("f_l2_16", 500, 1030, v=8, k1=65536, k2=256, n_out=5, v0=8, k0=256), synth.LayerSpec("f_l2_groups", 500, 1024, v=8, k1=4096, n_groups=4)]
+
+
+@pytest.mark.parametrize("spec", STAGED, ids=lambda s: s.name)
+def test_dequant_fp8_of_larger_layers(b, spec):
+    dl = b.DeviceLayer(synth.make_layer(spec, 0, 3, 1))
+    check_quantized(*dl.dequant_fp8(), dl.dequant(), 128)
+
+
 def test_dequant_fp8_scale_per_row(b):
     spec = synth.LayerSpec("f_scale_rows", 200, 200, v=8, k1=256, n_out=5, v0=4, k0=16)
     d = synth.make_layer(spec, 0, 3, 1)
@@ -267,6 +280,71 @@ def test_other_streams_and_replayed_graphs(b, B):
         two.replay()
         torch.cuda.synchronize()
         assert same(a, want) and same(c, want) and same(e, want)
+
+
+@pytest.mark.parametrize("B", [1, 8, 16, 300])
+def test_weights_written_just_before(b, B):
+    M, N = 1100, 1024
+    g = gen(10)
+    x = torch.randn(B, N, generator=g, device="cuda").half()
+    Ws = [(torch.randn(M, N, generator=g, device="cuda") * (i + 1)).half() for i in range(6)]
+    want = []
+    for W in Ws:
+        q, s = b.vptq_fp8_quantize(W, 128)
+        torch.cuda.synchronize()
+        want.append(b.vptq_linear_fp8(x, q, s, out_dtype="fp32"))
+        torch.cuda.synchronize()
+    def all_of_them():
+        got, q, s = [], None, None
+        for W in Ws:
+            del q, s                                 # the next ones take their place
+            q, s = b.vptq_fp8_quantize(W, 128)
+            got.append(b.vptq_linear_fp8(x, q, s, out_dtype="fp32"))
+        return got
+    assert all(same(a, w) for a, w in zip(all_of_them(), want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = all_of_them()
+    for _ in range(3):
+        for a in got:
+            a.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(same(a, w) for a, w in zip(got, want))
+
+
+def test_one_row_of_activations_as_a_weight(b):
+    # one row's scales have the same shape either way: what the quantizer has just written may be the weight
+    g = gen(11)
+    x = torch.randn(4, 4096, generator=g, device="cuda").half()
+    rows = [torch.randn(1, 4096, generator=g, device="cuda").half() for _ in range(4)]
+    want = []
+    for r in rows:
+        q, s = b.vptq_fp8_quantize(r)
+        torch.cuda.synchronize()
+        want.append(b.vptq_linear_fp8(x, q, s))
+        torch.cuda.synchronize()
+    q = s = None
+    for r, w in zip(rows, want):
+        del q, s
+        q, s = b.vptq_fp8_quantize(r)
+        assert same(b.vptq_linear_fp8(x, q, s), w)
+
+
+@pytest.mark.parametrize("B", [2, 16, 77, 300])
+def test_two_calls_at_once(b, B):
+    w, ws, x, _, _ = operands(4096, 4096, B, "bf16", 12)
+    other = (x * 0.5).contiguous()
+    want, want_other = b.vptq_linear_fp8(x, w, ws), b.vptq_linear_fp8(other, w, ws)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(8):
+        for i, t in enumerate((x, other)):
+            with torch.cuda.stream(streams[i]):
+                got[i].append(b.vptq_linear_fp8(t, w, ws))
+    torch.cuda.synchronize()
+    assert all(same(y, want) for y in got[0]) and all(same(y, want_other) for y in got[1])
 
 
 def test_a_layer_restored_once_runs_its_prompts(b):

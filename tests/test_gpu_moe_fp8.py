@@ -122,6 +122,40 @@ def test_streams_and_replayed_graphs(b):
         assert torch.equal(first, one) and torch.equal(second, two)
 
 
+def test_the_most_tokens_experts_and_choices(b):
+    args = layer(136, 48, 256, 32, "bf16", 10)
+    close(b.vptq_moe_fp8(*args, 16, out=torch.empty(32, 136, device="cuda")), ref.moe(*args, 16, True))
+
+
+@pytest.mark.parametrize("T", [1, 8, 32])
+def test_two_calls_at_once(b, T):
+    args = layer(1024, 512, 32, T, "bf16", 11)
+    other = (args[0] * 0.5, *args[1:])
+    want, want_other = b.vptq_moe_fp8(*args, 4), b.vptq_moe_fp8(*other, 4)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(8):
+        for i, a in enumerate((args, other)):
+            with torch.cuda.stream(streams[i]):
+                got[i].append(b.vptq_moe_fp8(*a, 4))
+    torch.cuda.synchronize()
+    assert all(torch.equal(y, want) for y in got[0]) and all(torch.equal(y, want_other) for y in got[1])
+
+
+def test_experts_and_router_written_just_before(b):
+    layers = [layer(512, 384, 8, 3, "fp16", 20 + i) for i in range(4)]
+    want = []
+    for a in layers:
+        want.append(b.vptq_moe_fp8(*a, 2))
+        torch.cuda.synchronize()
+    room = [torch.empty_like(t) for t in layers[0]]
+    for a, w in zip(layers, want):
+        for to, t in zip(room, a):
+            to.view(torch.uint8).copy_(t.view(torch.uint8))
+        assert torch.equal(b.vptq_moe_fp8(*room, 2), w)
+
+
 def test_a_layers_experts_made_by_the_quantizer(b):
     """The operators together: experts quantized block by block when they are loaded, the layer for single tokens, and the same experts'
     projections through vptq_linear_fp8 for a prompt."""
