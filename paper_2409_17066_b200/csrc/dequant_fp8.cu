@@ -4,13 +4,14 @@
 //
 // A CTA makes a 128 x 128 block at a time and leaves its FP16 values in shared memory; the block's maximum and the rounding follow.
 // A thread takes four adjacent columns of a vector row: their indices are one window of packed words, their values leave as 8-byte
-// stores (one column to a thread: 8192 x 28672 322 us instead of 255; eight to a thread spill: 335). Columns that do not lie so, under
+// stores (one column to a thread: 8192 x 28672 322 us instead of 253; eight to a thread spill: 335). Columns that do not lie so, under
 // a permutation, beside the outliers, at other index widths, are looked up one to a thread, ITEMS vector rows at a time so that as many
 // table reads are in flight.
 // A vector row that crosses a block's edge is looked up by both blocks (v = 8 never does; v = 6: 23 rows instead of 21.3).
 // TABLES: main and residual table of a layer with one group are staged in shared memory as 16-byte rows, and two CTAs an SM go through
 // the blocks; out of L1 every 4-byte piece of a 12-byte row is a wavefront of its own for each lane (11008 x 4096 with v = 6: 97 us
-// instead of 75).
+// instead of 75).  Blocks are dealt out column of blocks by column, so that those with outliers, which take twice as long, come first and to
+// CTAs of their own (row by row some CTAs had three of them: 75 us instead of 62).
 // A table in L2 (1 MiB) is bound by its random reads, one a clock and SM: 4096 x 4096 17.8 us; a small table by the arithmetic.
 #include "fp8.cuh"
 #include "index_words.cuh"
@@ -33,7 +34,7 @@ struct DequantFp8Params {
     float *scale;
     const int *inverse;       // stored column of every input feature (-1: none names it), or null
     long long pitch;
-    int col_blocks, blocks;
+    int row_blocks, col_blocks, blocks;
 };
 constexpr int TABLES_MAX = (115712 - 1024 - FP8_BLOCK * TILE_STRIDE * 2) / 16;         // entries of both tables, two CTAs an SM
 
@@ -60,7 +61,7 @@ __device__ __forceinline__ void restore_block(const DequantFp8Params &P, int ind
     constexpr int THREADS = threads<TABLES>(), ITEMS = items<TABLES>();
     constexpr int COL_LANES = THREADS / FP8_BLOCK;        // vector rows of a block taken at a time
     const LayerView &L = P.L;
-    const int cb = index % P.col_blocks, rb = index / P.col_blocks;
+    const int rb = index % P.row_blocks, cb = index / P.row_blocks;
     const int m0 = rb * FP8_BLOCK, m1 = min(L.M, m0 + FP8_BLOCK);
     const int v = V > 0 ? V : L.v;
     // columns [fast0, fast1) of the block are restored several adjacent ones to a thread, the others one to a thread
@@ -71,11 +72,21 @@ __device__ __forceinline__ void restore_block(const DequantFp8Params &P, int ind
             fast0 = min(FP8_BLOCK, (max(0, L.n_out - cb * FP8_BLOCK) + CPL - 1) / CPL * CPL);
             fast1 = min(FP8_BLOCK, (L.N - cb * FP8_BLOCK) / CPL * CPL);
         }
-        const int per_row = (fast1 - fast0) / CPL, first = m0 / V, rows = (m1 + V - 1) / V - first;
+        const int c = (threadIdx.x & 31) * CPL, n = cb * FP8_BLOCK + c, col = n - L.n_out, r1 = (m1 + V - 1) / V;
         const bool res = L.k2 > 0;
-        for (int task = threadIdx.x; per_row > 0 && task < rows * per_row; task += THREADS) {
-            const int r = first + task / per_row, c = fast0 + task % per_row * CPL, n = cb * FP8_BLOCK + c, col = n - L.n_out;
-            const unsigned bit1 = (unsigned)col * (unsigned)b1, bit2 = (unsigned)col * (unsigned)b2;
+        const unsigned bit1 = (unsigned)col * (unsigned)b1, bit2 = (unsigned)col * (unsigned)b2;
+        // scale and bias of the columns; without them t * 1 + (-0) = t, whatever t and its sign
+        float sc[CPL], bi[CPL];
+#pragma unroll
+        for (int k = 0; k < CPL; k += 2) {
+            float2 fs = make_float2(1.f, 1.f), fb = make_float2(-0.f, -0.f);
+            if (L.has_scale && c >= fast0 && c < fast1) {
+                fs = __half22float2(__ldg(reinterpret_cast<const __half2 *>(L.scale + n + k)));
+                fb = __half22float2(__ldg(reinterpret_cast<const __half2 *>(L.bias + n + k)));
+            }
+            sc[k] = fs.x; sc[k + 1] = fs.y; bi[k] = fb.x; bi[k + 1] = fb.y;
+        }
+        for (int r = c >= fast0 && c < fast1 ? m0 / V + (int)(threadIdx.x >> 5) : r1; r < r1; r += THREADS / 32) {
             const IndexWindow<CPL> q1 = load_window<CPL>(L.s1.ptr + (long long)r * L.s1.stride, bit1, (unsigned)(L.s1.stride >> 2));
             IndexWindow<CPL> q2 = {};
             if (res) q2 = load_window<CPL>(L.s2.ptr + (long long)r * L.s2.stride, bit2, (unsigned)(L.s2.stride >> 2));
@@ -95,17 +106,6 @@ __device__ __forceinline__ void restore_block(const DequantFp8Params &P, int ind
                     w1[k] = row_from_global<V>(L.c1, group * L.k1 + i1[k]);
                     if (res) w2[k] = row_from_global<V>(L.c2, group * L.k2 + i2[k]);
                 }
-            }
-            // scale and bias of the columns; without them t * 1 + (-0) = t, whatever t and its sign
-            float sc[CPL], bi[CPL];
-#pragma unroll
-            for (int k = 0; k < CPL; k += 2) {
-                float2 fs = make_float2(1.f, 1.f), fb = make_float2(-0.f, -0.f);
-                if (L.has_scale) {
-                    fs = __half22float2(__ldg(reinterpret_cast<const __half2 *>(L.scale + n + k)));
-                    fb = __half22float2(__ldg(reinterpret_cast<const __half2 *>(L.bias + n + k)));
-                }
-                sc[k] = fs.x; sc[k + 1] = fs.y; bi[k] = fb.x; bi[k + 1] = fb.y;
             }
             const int at = r * V - m0;
             __half *dst = &tile[0][c] + at * TILE_STRIDE;
@@ -228,7 +228,7 @@ __device__ __forceinline__ void restore_block(const DequantFp8Params &P, int ind
 #pragma unroll
     for (int i = 0; i < THREADS / 32; i++) most = max(most, part[i]);
     const Fp8Scale s = fp8_scale(__half2float(__ushort_as_half((unsigned short)most)));
-    if (threadIdx.x == 0) P.scale[index] = s.scale;
+    if (threadIdx.x == 0) P.scale[(long long)rb * P.col_blocks + cb] = s.scale;
     if (c >= P.pitch) return;
 #pragma unroll
     for (int i = 0; i < ROUNDS; i++) {
@@ -260,7 +260,11 @@ dequant_fp8_kernel(const __grid_constant__ DequantFp8Params P)
         for (int i = threadIdx.x; i < P.L.k1 + P.L.k2; i += THREADS)
             tables[i] = i < P.L.k1 ? load_centroid_row(P.L.c1, i, V) : load_centroid_row(P.L.c2, i - P.L.k1, V);
         __syncthreads();
-        for (int b = blockIdx.x; b < P.blocks; b += gridDim.x) {
+        // (the first blocks may hold outliers, and take longer: the blocks left over for the last round go to other CTAs)
+        const int rounds = P.blocks / (int)gridDim.x;
+        for (int i = 0; i <= rounds; i++) {
+            const int b = i * (int)gridDim.x + (int)(i < rounds ? blockIdx.x : gridDim.x - 1 - blockIdx.x);
+            if (b >= P.blocks) break;
             restore_block<V, true>(P, b, tile, part, tables);
             __syncthreads();
         }
@@ -310,7 +314,8 @@ cudaError_t launch_dequant_fp8(const LayerView &L, uint8_t *q, float *scale, int
         if ((e = cudaGetLastError()) != cudaSuccess) return e;
         P.inverse = inverse;
     }
-    P.blocks = (int)((long long)ceil_div(L.M, FP8_BLOCK) * P.col_blocks);
+    P.row_blocks = ceil_div(L.M, FP8_BLOCK);
+    P.blocks = (int)((long long)P.row_blocks * P.col_blocks);
     switch (L.v) {
     case 8: return restore<8>(P, st);
     case 6: return restore<6>(P, st);

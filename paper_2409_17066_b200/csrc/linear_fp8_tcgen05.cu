@@ -1,4 +1,4 @@
-// out = x W^T for more than 16 tokens over an e4m3 weight with 128 x 128 block scales, on the tensor cores.
+// out = x W^T for more than 8 tokens over an e4m3 weight with 128 x 128 block scales, on the tensor cores.
 //
 // D[token][feature] per block of 128 columns is one group of four tcgen05.mma (kind::f8f6f4, 128 tokens x TN features x 32 columns
 // each) into a TMEM buffer of its own; the block's two scales differ from the next block's, so the sum over blocks is formed in
