@@ -6,7 +6,8 @@
 // 16-byte load of 16-bit values, an 8-byte store); the block's maximum is four shuffles.  A half warp has UNROLL blocks in flight.
 // blocks form (weights, a scale per 128 x 128): a CTA takes a block, 16 lanes a row of it, the values stay in registers between the
 // maximum and the rounding: one pass over the matrix.
-// Both are bound by HBM: 2 or 4 bytes read and one written a value.
+// 2 or 4 bytes read and one written a value: the blocks form is bound by HBM (28672 x 8192 from 16 bits 101 to 114 us), the rows form by its
+// instructions, issue slots 63 % busy (4096 x 8192 from 16 bits 25.3 us, 4.0 TB/s).
 #include "fp8.cuh"
 
 namespace vptq {

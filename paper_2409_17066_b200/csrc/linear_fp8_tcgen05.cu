@@ -11,6 +11,9 @@
 // CTAs are persistent over tiles, tokens fastest, so that those that run together share weight tiles in L2.
 // Few tiles: SPLIT CTAs of a cluster share a tile's columns, leave their sums in shared memory, and each adds up its share of the
 // tile's rows in rank order: one launch, no scratch, and a result that does not depend on timing.
+// Bound by the two L2-side and issue-side halves of a block, operand tiles at 50 to 55 bytes a clock and SM and the sums' fmas, which overlap only
+// partly: 8192 x 28672 at 2048 tokens 467 us sustained, 2060 TFLOP/s; 8192 x 8192 at 2048 120 us, 103 without the loads, 106 without the fmas.
+// Few tokens: HBM (28672 x 8192 at 16 tokens 44.5 us, 5.3 TB/s).
 // Every wait is bounded; one that gives up sets the status word of the workspace.
 #include "fp8.cuh"
 #include "fp8_tcgen05.cuh"
