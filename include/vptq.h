@@ -464,6 +464,8 @@ int vptq_dequant_fp8(const vptq_layer_desc *desc, const vptq_layer_ptrs *p, uint
  *   x_dtype VPTQ_DTYPE_E4M3: x [B][pitch(N)] with x_scale [B][ceil(N / 128)] (block_rows = 1)
  *           VPTQ_DTYPE_FP16 / _BF16: x [B][N], quantized inside the call by the rule (x_scale is not read): the same operands, and
  *           so the same result, as vptq_fp8_quantize followed by the call above
+ *   every pointer is 16-byte aligned, the scales' too (VPTQ_E_ALIGN): of a stack of scale matrices whose sizes are no multiples of four
+ *   values, a part is copied by the caller (the Python functions do that)
  *   out_dtype FP16, BF16 or FP32;  flags: VPTQ_FLAG_CONCURRENT and VPTQ_FLAG_DETERMINISTIC are accepted and change nothing (no CTA
  *           waits for another launch's, every sum has a fixed order).
  * At most 8 tokens take the kernel "fp8_decode" (no workspace), more "fp8_tcgen05" (vptq_linear_fp8_path), whose workspace, 256-byte

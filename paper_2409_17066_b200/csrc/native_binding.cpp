@@ -5,6 +5,7 @@
 // attribute look-ups, ctypes conversions and torch.cuda.current_stream().
 #include <Python.h>
 
+#include <ATen/ops/clone.h>
 #include <ATen/ops/empty.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
@@ -255,6 +256,13 @@ int32_t code_of(at::ScalarType t)
     return t == at::kHalf ? VPTQ_DTYPE_FP16 : t == at::kBFloat16 ? VPTQ_DTYPE_BF16 : t == at::kFloat ? VPTQ_DTYPE_FP32 : t == at::kFloat8_e4m3fn ? VPTQ_DTYPE_E4M3 : -1;
 }
 
+// Scales as the C ABI takes them, on a 16-byte boundary.  Part of a stack of them (an expert's, some tokens') starts at any multiple of
+// four bytes: that part is copied, on the current stream.
+at::Tensor aligned(const at::Tensor &scale)
+{
+    return (reinterpret_cast<uintptr_t>(scale.data_ptr()) & 15u) == 0 ? scale : scale.detach().clone();
+}
+
 constexpr int64_t MAX_INT = 0x7FFFFFFF;
 
 // fp8_quantize(x, block_rows) -> (q, scale)
@@ -345,10 +353,11 @@ PyObject *py_linear_fp8(PyObject *, PyObject *const *a, Py_ssize_t n)
             ws = own.data_ptr();
             ws_bytes = (size_t)need;
         }
+        const at::Tensor w_scale = aligned(*ws_t), x_scale = xs ? aligned(*xs) : at::Tensor();
         int rc;
         Py_BEGIN_ALLOW_THREADS
-        rc = vptq_linear_fp8(&d, x->data_ptr(), xs ? static_cast<const float *>(xs->data_ptr()) : nullptr, (int32_t)B,
-                             static_cast<const uint8_t *>(w->data_ptr()), static_cast<const float *>(ws_t->data_ptr()), result.data_ptr(), ws, ws_bytes,
+        rc = vptq_linear_fp8(&d, x->data_ptr(), xs ? static_cast<const float *>(x_scale.data_ptr()) : nullptr, (int32_t)B,
+                             static_cast<const uint8_t *>(w->data_ptr()), static_cast<const float *>(w_scale.data_ptr()), result.data_ptr(), ws, ws_bytes,
                              current_stream());
         Py_END_ALLOW_THREADS
         if (rc != VPTQ_OK) return fail(rc);
@@ -391,10 +400,11 @@ PyObject *py_moe_fp8(PyObject *, PyObject *const *a, Py_ssize_t n)
     if (!workspace_of(a[11], &ws, &ws_bytes)) return nullptr;
     const int64_t need = vptq_moe_fp8_workspace_bytes(&d, (int32_t)T);
     if (need < 0) return fail((int)need);
-    const vptq_moe_ptrs p = {router.data_ptr(), static_cast<const uint8_t *>(gate.data_ptr()), static_cast<const uint8_t *>(t[4]->data_ptr()),
-                             static_cast<const uint8_t *>(t[6]->data_ptr()), static_cast<const float *>(t[3]->data_ptr()),
-                             static_cast<const float *>(t[5]->data_ptr()), static_cast<const float *>(t[7]->data_ptr())};
     return guarded([&]() -> PyObject * {
+        const at::Tensor gate_scale = aligned(*t[3]), up_scale = aligned(*t[5]), down_scale = aligned(*t[7]);
+        const vptq_moe_ptrs p = {router.data_ptr(), static_cast<const uint8_t *>(gate.data_ptr()), static_cast<const uint8_t *>(t[4]->data_ptr()),
+                                 static_cast<const uint8_t *>(t[6]->data_ptr()), static_cast<const float *>(gate_scale.data_ptr()),
+                                 static_cast<const float *>(up_scale.data_ptr()), static_cast<const float *>(down_scale.data_ptr())};
         at::Tensor own, result = out ? *out : at::empty({T, hidden}, x.options());
         if (ws == nullptr) {
             own = at::empty({need}, x.options().dtype(at::kByte));

@@ -1,0 +1,67 @@
+"""Calls of the 8-bit floating point operators that a program makes beside the plain ones: slices of stacked operands."""
+import pytest
+import torch
+
+import fp8_reference as ref
+from test_gpu_fp8 import same
+from test_gpu_moe_fp8 import layer
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def b():
+    from paper_2409_17066_b200 import build as vbuild
+    vbuild.build()
+    from paper_2409_17066_b200 import binding
+    return binding
+
+
+# ---- scales that start at any multiple of four bytes ---------------------------------------------------
+
+@pytest.mark.parametrize("B", [3, 40])
+def test_every_expert_of_a_stack_takes_a_prompt(b, B):
+    g = torch.Generator(device="cuda").manual_seed(1)
+    w, s = ref.random_experts(4, 256, 384, g, "cuda")                  # 2 x 3 scales an expert: 24 bytes from one to the next
+    x = torch.randn(B, 384, generator=g, device="cuda").half()
+    for e in range(4):
+        assert s[e].data_ptr() % 16 == 8 * (e % 2)
+        assert same(b.vptq_linear_fp8(x, w[e], s[e]), b.vptq_linear_fp8(x, w[e], s[e].clone()))
+
+
+@pytest.mark.parametrize("B", [3, 40])
+def test_some_tokens_of_a_quantized_batch(b, B):
+    g = torch.Generator(device="cuda").manual_seed(2)
+    w, s = ref.random_weight(130, 384, g, "cuda")
+    q, qs = b.vptq_fp8_quantize(torch.randn(B + 3, 384, generator=g, device="cuda"))
+    for t in range(1, 4):
+        assert qs[t:].data_ptr() % 16 != 0
+        got = b.vptq_linear_fp8(q[t:t + B], w, s, x_scale=qs[t:t + B], out_dtype="fp32")
+        want = b.vptq_linear_fp8(q[t:t + B].clone(), w, s, x_scale=qs[t:t + B].clone(), out_dtype="fp32")
+        assert same(got, want)
+
+
+def test_layers_of_a_stack_of_experts(b):
+    one, two = (layer(256, 384, 3, 2, "bf16", 30 + i) for i in range(2))
+    both = [torch.stack([p.view(torch.uint8), q.view(torch.uint8)]).view(p.dtype) if p.dtype == torch.float8_e4m3fn else torch.stack([p, q])
+            for p, q in zip(one, two)]
+    assert any(t[1].data_ptr() % 16 for t in both[3::2])
+    for i, a in enumerate((one, two)):
+        assert same(b.vptq_moe_fp8(*[t[i] for t in both], 2), b.vptq_moe_fp8(*a, 2))
+
+
+def test_slices_of_scales_in_a_replayed_graph(b):
+    g = torch.Generator(device="cuda").manual_seed(3)
+    w, s = ref.random_experts(2, 256, 384, g, "cuda")
+    x = torch.randn(20, 384, generator=g, device="cuda").half()
+    b.vptq_linear_fp8(x, w[1], s[1].clone())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y = b.vptq_linear_fp8(x, w[1], s[1])
+    s.mul_(1.5)                                                        # what a replay reads is what the scales hold then
+    want = b.vptq_linear_fp8(x, w[1], s[1].clone())
+    for _ in range(2):
+        y.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert same(y, want)
