@@ -344,10 +344,11 @@ PyObject *py_linear_fp8(PyObject *, PyObject *const *a, Py_ssize_t n)
     void *ws;
     size_t ws_bytes;
     if (!workspace_of(a[6], &ws, &ws_bytes)) return nullptr;
-    const int64_t need = vptq_linear_fp8_workspace_bytes(&d, (int32_t)B);
+    const int64_t need = vptq_linear_fp8_workspace_bytes(&d, B > 0 ? (int32_t)B : 1);
     if (need < 0) return fail((int)need);
     return guarded([&]() -> PyObject * {
         at::Tensor own, result = out ? *out : at::empty({B, M}, x->options().dtype(dtype_of(d.out_dtype)));
+        if (B == 0) return out ? Py_NewRef(a[5]) : THPVariable_Wrap(result);           // no tokens: nothing to do
         if (need > 0 && ws == nullptr) {
             own = at::empty({need}, x->options().dtype(at::kByte));
             ws = own.data_ptr();
@@ -398,14 +399,15 @@ PyObject *py_moe_fp8(PyObject *, PyObject *const *a, Py_ssize_t n)
     void *ws;
     size_t ws_bytes;
     if (!workspace_of(a[11], &ws, &ws_bytes)) return nullptr;
-    const int64_t need = vptq_moe_fp8_workspace_bytes(&d, (int32_t)T);
+    const int64_t need = vptq_moe_fp8_workspace_bytes(&d, T > 0 ? (int32_t)T : 1);
     if (need < 0) return fail((int)need);
     return guarded([&]() -> PyObject * {
+        at::Tensor own, result = out ? *out : at::empty({T, hidden}, x.options());
+        if (T == 0) return out ? Py_NewRef(a[10]) : THPVariable_Wrap(result);
         const at::Tensor gate_scale = aligned(*t[3]), up_scale = aligned(*t[5]), down_scale = aligned(*t[7]);
         const vptq_moe_ptrs p = {router.data_ptr(), static_cast<const uint8_t *>(gate.data_ptr()), static_cast<const uint8_t *>(t[4]->data_ptr()),
                                  static_cast<const uint8_t *>(t[6]->data_ptr()), static_cast<const float *>(gate_scale.data_ptr()),
                                  static_cast<const float *>(up_scale.data_ptr()), static_cast<const float *>(down_scale.data_ptr())};
-        at::Tensor own, result = out ? *out : at::empty({T, hidden}, x.options());
         if (ws == nullptr) {
             own = at::empty({need}, x.options().dtype(at::kByte));
             ws = own.data_ptr();

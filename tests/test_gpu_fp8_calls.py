@@ -1,4 +1,4 @@
-"""Calls of the 8-bit floating point operators that a program makes beside the plain ones: slices of stacked operands."""
+"""Calls of the 8-bit floating point operators that a program makes beside the plain ones: slices of stacked operands, empty batches."""
 import pytest
 import torch
 
@@ -65,3 +65,32 @@ def test_slices_of_scales_in_a_replayed_graph(b):
         graph.replay()
         torch.cuda.synchronize()
         assert same(y, want)
+
+
+# ---- empty batches ---------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("x_type", ["fp16", "bf16", "e4m3"])
+def test_an_empty_batch_through_the_operators(b, x_type):
+    g = torch.Generator(device="cuda").manual_seed(4)
+    w, s = ref.random_weight(130, 256, g, "cuda")
+    x, xs = torch.empty(0, 256, device="cuda", dtype=torch.bfloat16 if x_type == "bf16" else torch.float16), None
+    if x_type == "e4m3":
+        x, xs = b.vptq_fp8_quantize(x)
+    y = b.vptq_linear_fp8(x, w, s, x_scale=xs)
+    assert tuple(y.shape) == (0, 130) and y.dtype == (torch.float16 if x_type == "fp16" else torch.bfloat16)
+    out = torch.empty(0, 130, device="cuda")
+    assert b.vptq_linear_fp8(x, w, s, x_scale=xs, out=out) is out
+    with pytest.raises(AssertionError):
+        b.vptq_linear_fp8(x, w, s, x_scale=xs, out=torch.empty(0, 131, device="cuda"))
+    with pytest.raises(b.VptqError):                                   # what else is refused still is
+        b.vptq_linear_fp8(torch.empty(0, 256, device="cuda"), w, s)
+
+
+def test_an_empty_batch_through_the_experts(b):
+    args = layer(256, 128, 4, 2, "fp16", 5)
+    y = b.vptq_moe_fp8(args[0][:0], *args[1:], 2)
+    assert tuple(y.shape) == (0, 256) and y.dtype == torch.float16
+    out = torch.empty(0, 256, device="cuda")
+    assert b.vptq_moe_fp8(args[0][:0], *args[1:], 2, out=out) is out
+    with pytest.raises(b.VptqError):
+        b.vptq_moe_fp8(args[0][:0], *args[1:], 5)
