@@ -443,8 +443,8 @@ def vptq_linear_fp8(x: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, x_s
     """out [B][M] = x * W^T over an e4m3 weight w [M][pitch], w_scale [ceil(M / 128)][ceil(N / 128)].  x is fp16 or bf16 [B][N]
     (quantized inside the call) or e4m3 [B][pitch] with x_scale [B][ceil(N / 128)].  out_dtype "fp16", "bf16" or "fp32" (default:
     that of `out`, else of x, else "bf16").  Contiguous tensors of one device, the current one; scales that do not start on a 16-byte
-    boundary, as parts of a stack may, are copied; no tokens (B = 0) make an empty result.  A workspace is only taken from the caller to
-    read its status word afterwards (vptq_workspace_status); without one the call allocates its own."""
+    boundary, as parts of a stack may, are copied; no tokens (B = 0) make an empty result.  A workspace
+    (contiguous, of that device) is only taken from the caller to read its status word afterwards (vptq_workspace_status); without one the call allocates its own."""
     return _native.linear_fp8(x, w, w_scale, x_scale, None if out_dtype is None else _DT[out_dtype], out, workspace)
 
 

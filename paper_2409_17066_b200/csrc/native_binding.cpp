@@ -215,6 +215,15 @@ PyObject *py_dequant(PyObject *, PyObject *const *a, Py_ssize_t n)
 bool on_current_device(const at::Tensor &t) { return t.is_cuda() && t.get_device() == c10::cuda::current_device(); }
 bool plain(const at::Tensor &t) { return on_current_device(t) && t.is_contiguous(); }
 
+// workspace argument: a contiguous tensor of the current device (its bytes are written) or None
+bool room_of(PyObject *o, void **p, size_t *bytes)
+{
+    if (!workspace_of(o, p, bytes)) return false;
+    if (o == Py_None || plain(THPVariable_Unpack(o))) return true;
+    assertion("workspace: a contiguous tensor of the current device");
+    return false;
+}
+
 // runs a call that may throw (torch's allocator) and turns what it throws into a Python error
 template <typename F>
 PyObject *guarded(F f)
@@ -296,7 +305,7 @@ PyObject *py_dequant_fp8(PyObject *, PyObject *const *a, Py_ssize_t n)
     const vptq_layer_ptrs *p = d ? struct_of<vptq_layer_ptrs>(a[1]) : nullptr;
     void *ws = nullptr;
     size_t ws_bytes = 0;
-    if (!p || !workspace_of(a[2], &ws, &ws_bytes)) return nullptr;
+    if (!p || !room_of(a[2], &ws, &ws_bytes)) return nullptr;
     const int64_t need = vptq_dequant_fp8_workspace_bytes(d);
     if (need < 0) return fail((int)need);
     return guarded([&]() -> PyObject * {
@@ -343,7 +352,7 @@ PyObject *py_linear_fp8(PyObject *, PyObject *const *a, Py_ssize_t n)
         return assertion("out [B][M], contiguous, of the type asked for");
     void *ws;
     size_t ws_bytes;
-    if (!workspace_of(a[6], &ws, &ws_bytes)) return nullptr;
+    if (!room_of(a[6], &ws, &ws_bytes)) return nullptr;
     const int64_t need = vptq_linear_fp8_workspace_bytes(&d, B > 0 ? (int32_t)B : 1);
     if (need < 0) return fail((int)need);
     return guarded([&]() -> PyObject * {
@@ -398,7 +407,7 @@ PyObject *py_moe_fp8(PyObject *, PyObject *const *a, Py_ssize_t n)
     if (out && (!plain(*out) || out->dim() != 2 || out->size(0) != T || out->size(1) != hidden)) return assertion("out [T][hidden], contiguous");
     void *ws;
     size_t ws_bytes;
-    if (!workspace_of(a[11], &ws, &ws_bytes)) return nullptr;
+    if (!room_of(a[11], &ws, &ws_bytes)) return nullptr;
     const int64_t need = vptq_moe_fp8_workspace_bytes(&d, T > 0 ? (int32_t)T : 1);
     if (need < 0) return fail((int)need);
     return guarded([&]() -> PyObject * {

@@ -1,4 +1,5 @@
-"""Calls of the 8-bit floating point operators that a program makes beside the plain ones: slices of stacked operands, empty batches."""
+"""Calls of the 8-bit floating point operators that a program makes beside the plain ones: slices of stacked operands, empty batches,
+workspaces."""
 import pytest
 import torch
 
@@ -94,3 +95,19 @@ def test_an_empty_batch_through_the_experts(b):
     assert b.vptq_moe_fp8(args[0][:0], *args[1:], 2, out=out) is out
     with pytest.raises(b.VptqError):
         b.vptq_moe_fp8(args[0][:0], *args[1:], 5)
+
+
+# ---- a workspace that the kernels cannot write ---------------------------------------------------------------
+
+def test_a_workspace_elsewhere_is_refused(b):
+    g = torch.Generator(device="cuda").manual_seed(7)
+    w, s = ref.random_weight(130, 256, g, "cuda")
+    x = torch.randn(20, 256, generator=g, device="cuda").half()
+    args = layer(256, 128, 4, 2, "fp16", 8)
+    spread = torch.zeros(1 << 21, 2, dtype=torch.uint8, device="cuda")[:, 0]              # every other byte: not all of it is the workspace's
+    for room in (torch.zeros(1 << 22, dtype=torch.uint8), spread):
+        with pytest.raises(AssertionError, match="workspace"):
+            b.vptq_linear_fp8(x, w, s, workspace=room)
+        with pytest.raises(AssertionError, match="workspace"):
+            b.vptq_moe_fp8(*args, 2, workspace=room)
+    assert not spread.any()
