@@ -426,7 +426,8 @@ def vptq_fp8_quantize(x: torch.Tensor, block_rows: int = 1):
 
 
 def vptq_dequant_fp8(desc: LayerDesc, ptrs: LayerPtrs, workspace: Optional[torch.Tensor] = None):
-    """(q, scale) of a vector-quantized layer, as vptq_fp8_quantize(W, 128) of its restored FP16 weight gives them."""
+    """(q, scale) of a vector-quantized layer, as vptq_fp8_quantize(W, 128) of its restored FP16 weight gives them.  The layer is in the
+    memory of the current device, where the result is made."""
     return _native.dequant_fp8(desc, ptrs, workspace)
 
 

@@ -5,6 +5,7 @@
 // attribute look-ups, ctypes conversions and torch.cuda.current_stream().
 #include <Python.h>
 
+#include <ATen/detail/CUDAHooksInterface.h>
 #include <ATen/ops/clone.h>
 #include <ATen/ops/empty.h>
 #include <c10/cuda/CUDAFunctions.h>
@@ -224,6 +225,16 @@ bool room_of(PyObject *o, void **p, size_t *bytes)
     return false;
 }
 
+// whether an address that came without a tensor is memory of the current device
+bool address_on_current_device(const void *p)
+{
+    try {
+        return at::detail::getCUDAHooks().getDeviceFromPtr(const_cast<void *>(p)).index() == c10::cuda::current_device();
+    } catch (const std::exception &) {                                           // (host memory, or no device)
+        return false;
+    }
+}
+
 // runs a call that may throw (torch's allocator) and turns what it throws into a Python error
 template <typename F>
 PyObject *guarded(F f)
@@ -308,6 +319,8 @@ PyObject *py_dequant_fp8(PyObject *, PyObject *const *a, Py_ssize_t n)
     if (!p || !room_of(a[2], &ws, &ws_bytes)) return nullptr;
     const int64_t need = vptq_dequant_fp8_workspace_bytes(d);
     if (need < 0) return fail((int)need);
+    for (const void *stream : {p->packed_idx, p->outlier_idx})                   // (a pointer that is missing is the C ABI's to refuse)
+        if (stream && !address_on_current_device(stream)) return assertion("a layer in the current device's memory");
     return guarded([&]() -> PyObject * {
         const at::TensorOptions options = at::TensorOptions().device(at::kCUDA, c10::cuda::current_device());
         const Fp8Tensors r = empty_fp8(d->M, d->N, 128, options);

@@ -22,3 +22,15 @@ def test_a_workspace_in_host_memory_is_refused(b):
     need = b.lib.vptq_dequant_fp8_workspace_bytes(C.byref(desc))
     with pytest.raises(AssertionError, match="workspace"):
         b.vptq_dequant_fp8(desc, ptrs, torch.zeros(need, dtype=torch.uint8))
+
+
+def test_a_layer_elsewhere_is_refused(b):
+    # (its addresses are nothing that the current device's kernels may read)
+    desc = b.make_desc(64, 64, 8, 256)
+    streams = [torch.zeros(1 << 14, dtype=torch.uint8) for _ in range(4)]
+    idx, table, scale, bias = (t.data_ptr() for t in streams)
+    with pytest.raises(AssertionError, match="current device"):
+        b.vptq_dequant_fp8(desc, b.LayerPtrs(idx, table, None, None, None, None, scale, bias))
+    out = b.make_desc(64, 64, 8, 256, 0, 64, 8, 16)
+    with pytest.raises(AssertionError, match="current device"):
+        b.vptq_dequant_fp8(out, b.LayerPtrs(None, None, None, None, idx, table, scale, bias))

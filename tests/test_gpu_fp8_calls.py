@@ -1,5 +1,5 @@
 """Calls of the 8-bit floating point operators that a program makes beside the plain ones: slices of stacked operands, empty batches,
-workspaces."""
+workspaces and layers in other memory."""
 import pytest
 import torch
 
@@ -111,3 +111,14 @@ def test_a_workspace_elsewhere_is_refused(b):
         with pytest.raises(AssertionError, match="workspace"):
             b.vptq_moe_fp8(*args, 2, workspace=room)
     assert not spread.any()
+
+
+def test_a_layer_in_host_memory_is_refused(b):
+    desc = b.make_desc(64, 64, 8, 256)
+    streams = [torch.zeros(1 << 14, dtype=torch.uint8) for _ in range(4)]
+    idx, table, scale, bias = (t.data_ptr() for t in streams)
+    with pytest.raises(AssertionError, match="current device"):
+        b.vptq_dequant_fp8(desc, b.LayerPtrs(idx, table, None, None, None, None, scale, bias))
+    streams = [t.cuda() for t in streams]                              # the same layer where it belongs: zeros, with one scale
+    q, s = b.vptq_dequant_fp8(desc, b.LayerPtrs(streams[0].data_ptr(), streams[1].data_ptr(), None, None, None, None, streams[2].data_ptr(), streams[3].data_ptr()))
+    assert q.device == s.device == streams[0].device and not q.view(torch.uint8).any()
