@@ -195,10 +195,10 @@ __device__ __forceinline__ void router(const MoeFp8 &L, float *logits, float (*p
     if (shift > 0 && (warp >> shift) >= tasks) asm volatile("bar.sync 2, %0;" ::"n"(THREADS) : "memory");
 }
 
-// an order of FP32 values as unsigned integers
+// an order of FP32 values as unsigned integers; both zeros are equal
 __device__ __forceinline__ uint32_t order_of(float v)
 {
-    const uint32_t b = __float_as_uint(v);
+    const uint32_t b = __float_as_uint(__fadd_rn(v, 0.f));            // (-0 + 0 = 0)
     return (b & 0x80000000u) ? ~b : b | 0x80000000u;
 }
 

@@ -1,5 +1,5 @@
 """Calls of the 8-bit floating point operators that a program makes beside the plain ones: slices of stacked operands, empty batches,
-workspaces and layers in other memory."""
+workspaces and layers in other memory, logits that are zeros of both signs."""
 import pytest
 import torch
 
@@ -122,3 +122,18 @@ def test_a_layer_in_host_memory_is_refused(b):
     streams = [t.cuda() for t in streams]                              # the same layer where it belongs: zeros, with one scale
     q, s = b.vptq_dequant_fp8(desc, b.LayerPtrs(streams[0].data_ptr(), streams[1].data_ptr(), None, None, None, None, streams[2].data_ptr(), streams[3].data_ptr()))
     assert q.device == s.device == streams[0].device and not q.view(torch.uint8).any()
+
+
+# ---- zeros of both signs are equal logits -------------------------------------------------------------------
+
+def test_logits_that_vanish_go_to_the_lowest_experts(b):
+    # products of 1e-60 are zeros in FP32, below zero for the first experts and above for the others: all logits are equal
+    args = layer(1024, 128, 40, 1, "bf16", 6)
+    args[0].fill_(1e-30)
+    args[3].mul_(1e30), args[5].mul_(1e30)                             # (the experts' results are ordinary values all the same)
+    args[1].fill_(1e-30)
+    args[1][:7] = -1e-30
+    got = b.vptq_moe_fp8(*args, 3, False, out=torch.empty(1, 1024, device="cuda"))
+    args[1].zero_()
+    want = b.vptq_moe_fp8(*args, 3, False, out=torch.empty(1, 1024, device="cuda"))
+    assert want.any() and same(got, want)
