@@ -36,6 +36,7 @@ struct DecodeParams {
     int passes;                // of every CTA
     int stage_groups, stages;  // groups that a stage holds (the largest pass of any CTA), stages of a warp
     int run_shift;             // log2 of a stage's blocks
+    unsigned long long wait_limit;
 };
 
 __device__ __forceinline__ uint4 load_shared16(uint32_t a)
@@ -148,7 +149,7 @@ linear_fp8_decode_kernel(const __grid_constant__ CUtensorMap map_full, const __g
             x = x_next;
             fetch(x_next);
             const uint32_t stage = ring + slot * stage_bytes + (uint32_t)(in_run * n_groups * GROUP_BYTES);
-            if (in_run == 0) mbar_wait_uniform(bars + 8 * slot, parity, gave_up);
+            if (in_run == 0) mbar_wait_within(bars + 8 * slot, parity, D.wait_limit, gave_up);
             // (groups that the pass does not have are multiplied with whatever lies behind its own, and dropped)
 #pragma unroll
             for (int r0 = 0; r0 < PASS; r0 += BATCH) {
@@ -178,11 +179,12 @@ linear_fp8_decode_kernel(const __grid_constant__ CUtensorMap map_full, const __g
         // the warps' sums, in warp order
         if (p > 0) asm volatile("bar.sync 1, %0;" ::"n"(32 * WARPS) : "memory");       // the last pass's have been read
         float *mine = part + warp * 8 * stride;
+        const bool lost = __any_sync(0xffffffffu, gave_up != 0);      // (every lane's sums hold products of all lanes' operands)
 #pragma unroll
         for (int r = 0; r < PASS; r++) {
             if (r >= n_groups) break;
 #pragma unroll
-            for (int i = 0; i < 4; i++) mine[(2 * t + (i & 1)) * stride + r * GROUP + row + 8 * (i >> 1)] = gave_up ? __int_as_float(0x7FFFFFFF) : acc[r][0][i];
+            for (int i = 0; i < 4; i++) mine[(2 * t + (i & 1)) * stride + r * GROUP + row + 8 * (i >> 1)] = lost ? __int_as_float(0x7FFFFFFF) : acc[r][0][i];
         }
         asm volatile("bar.sync 1, %0;" ::"n"(32 * WARPS) : "memory");
         const int rows = n_groups * GROUP, m0 = g0 * GROUP;
@@ -195,10 +197,7 @@ linear_fp8_decode_kernel(const __grid_constant__ CUtensorMap map_full, const __g
             store_out(P.out, (long long)token * P.M + m0 + m, sum, P.out_dtype);
         }
     }
-    if (gave_up) {                                        // copies in flight get a bounded time to land before the CTA exits
-        const long long c0 = clock64();
-        while (clock64() - c0 < 20000000ll) {}
-    }
+    if (gave_up) let_copies_land();
 }
 
 template <int DT, bool VEC, int PASS, bool RUNS, int WARPS>
@@ -211,6 +210,7 @@ cudaError_t run(const Fp8Linear &P, cudaStream_t st)
     D.L = P;
     D.passes = ceil_div(most, PASS);
     D.stage_groups = ceil_div(most, D.passes);
+    D.wait_limit = wait_limit();
     D.run_shift = 0;                                      // up to 8 KB, but something to do for every warp first
     if (RUNS)
         while ((2 << D.run_shift) * D.stage_groups <= 4 && ceil_div(kbs, 2 << D.run_shift) >= WARPS) D.run_shift++;

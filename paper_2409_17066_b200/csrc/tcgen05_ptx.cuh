@@ -86,6 +86,41 @@ __device__ __forceinline__ void mbar_wait_uniform(uint32_t bar, uint32_t parity,
                  : "+r"(gave_up) : "r"(bar), "r"(parity), "n"(WAIT_LIMIT_CYCLES) : "memory");
 }
 
+// The same with a limit in clocks, and its own order of steps: one poll that does not block, then the limit before every poll that may, so
+// that a limit of a few clocks (wait_limit) ends the first wait that is not satisfied already.  A lane's `gave_up` is its own: the warp votes.
+__device__ __forceinline__ void mbar_wait_within(uint32_t bar, uint32_t parity, unsigned long long limit, uint32_t &gave_up)
+{
+    asm volatile("{\n\t.reg .pred p, q;\n\t.reg .u64 t0, t1;\n\t"
+                 "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+                 "@p bra DONE;\n\t"
+                 "mov.u64 t0, %%clock64;\n\t"
+                 "AGAIN:\n\t"
+                 "mov.u64 t1, %%clock64;\n\t"
+                 "sub.u64 t1, t1, t0;\n\t"
+                 "setp.ge.u64 q, t1, %3;\n\t"
+                 "setp.ne.or.u32 q, %0, 0, q;\n\t"
+                 "@q bra LOST;\n\t"
+                 "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+                 "@p bra DONE;\n\t"
+                 "bra AGAIN;\n\t"
+                 "LOST:\n\t"
+                 "mov.u32 %0, 1;\n\t"
+                 "DONE:\n\t}"
+                 : "+r"(gave_up) : "r"(bar), "r"(parity), "l"(limit) : "memory");
+}
+// limit for kernels launched now: about two seconds, or what vptq_debug_set_wait_limit asked for
+inline unsigned long long wait_limit()
+{
+    const unsigned long long limit = debug_wait_limit();
+    return limit ? limit : WAIT_LIMIT_CYCLES;
+}
+// At the end of a CTA in which a wait gave up: copies and MMAs that are still under way get ten milliseconds before its memory goes.
+__device__ __forceinline__ void let_copies_land()
+{
+    const long long c0 = clock64();
+    while (clock64() - c0 < 20000000ll) {}
+}
+
 // linear bulk copy global -> shared memory (16-byte aligned addresses, size a multiple of 16)
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar)
 {

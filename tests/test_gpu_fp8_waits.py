@@ -1,0 +1,51 @@
+"""Device-side waits of the 8-bit floating point kernels that run out: every result is right or a NaN, and the next call is right."""
+import pytest
+import torch
+
+import fp8_reference as ref
+from test_gpu_fp8 import same
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def b():
+    from paper_2409_17066_b200 import build as vbuild
+    vbuild.build()
+    from paper_2409_17066_b200 import binding
+    return binding
+
+
+def with_short_waits(b, call):
+    """call() while the first wait that is not satisfied already is abandoned."""
+    torch.cuda.synchronize()
+    try:
+        b.lib.vptq_debug_set_wait_limit(1)
+        y = call()
+        torch.cuda.synchronize()
+    finally:
+        b.lib.vptq_debug_set_wait_limit(0)
+    return y
+
+
+def right_or_nan(y, clean, some=True):
+    lost = torch.isnan(y)
+    assert ((y == clean) | lost).all() and (lost.any() or not some), float(lost.float().mean())
+
+
+# (235 MB: far more than is on its way when a warp looks for its first blocks.  Rows of FP16 values that are no multiple of 16 bytes are read
+# one value at a time, for longer than the weights take: no wait need run out there.)
+@pytest.mark.parametrize("x_type", ["fp16", "e4m3"])
+@pytest.mark.parametrize("M,N,B", [(28672, 8192, 1), (28000, 8190, 8), (4736, 49152, 3)])
+def test_few_tokens(b, M, N, B, x_type):
+    g = torch.Generator(device="cuda").manual_seed(M + B)
+    w, s = ref.random_weight(M, N, g, "cuda")
+    x, xs = torch.randn(B, N, generator=g, device="cuda").half(), None
+    if x_type == "e4m3":
+        x, xs = b.vptq_fp8_quantize(x)
+    call = lambda: b.vptq_linear_fp8(x, w, s, x_scale=xs, out_dtype="fp32")  # noqa: E731
+    clean = call()
+    assert torch.isfinite(clean).all()
+    for _ in range(2):
+        right_or_nan(with_short_waits(b, call), clean, some=x_type == "e4m3" or N % 8 == 0)
+        assert same(call(), clean)
