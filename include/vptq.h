@@ -537,8 +537,8 @@ int vptq_linear_fused_has_status(const vptq_layer_desc *descs, int32_t n_layers,
  * two seconds; this sets the limit, in SM clock cycles, for the kernels launched afterwards by any thread
  * (0 restores the default).  With a limit of a few cycles a healthy kernel abandons its first wait that is
  * not already satisfied, reports VPTQ_E_TIMEOUT in its status word, leaves no copy in flight and returns;
- * the context stays usable.  Honoured by the path "decode_bucket_fma" and by "fp8_decode" (vptq_linear_fp8), which
- * leaves NaN in the results instead of a status.  Process-wide; not for production. */
+ * the context stays usable.  Honoured by the path "decode_bucket_fma", and by "fp8_decode" (vptq_linear_fp8) and
+ * vptq_moe_fp8, which leave NaN in the results instead of a status.  Process-wide; not for production. */
 void vptq_debug_set_wait_limit(uint64_t cycles);
 /* 1 when the kernels of vptq_linear / vptq_linear_fused for these arguments let one CTA wait for a flag that another CTA of
  * the same grid raises, 0 when no CTA waits for another, negative VPTQ_E_* on bad arguments.  Only the tensor-core kernel

@@ -55,6 +55,7 @@ struct Params {
     int hq_pitch, xq_pitch;
     int down_groups;       // groups of a pass of the down kernel
     int down_passes, down_run_shift;
+    unsigned long long wait_limit;
 };
 
 // a lane's share of one token's e4m3 values in one block, written by this kernel's cluster or by the kernel before; row: null for zeros
@@ -390,7 +391,7 @@ moe_gate_up_kernel(const __grid_constant__ CUtensorMap map_gate, const __grid_co
             const float w0 = __shfl_sync(0xffffffffu, ws, 0), w1 = __shfl_sync(0xffffffffu, ws, 1);
             next_block();
             fetch();
-            mbar_wait_uniform(bar, parity, gave_up);
+            mbar_wait_within(bar, parity, P.wait_limit, gave_up);
             parity ^= 1u;
 #pragma unroll
             for (int r0 = 0; r0 < UP_GROUPS; r0 += UNITS) {
@@ -408,14 +409,17 @@ moe_gate_up_kernel(const __grid_constant__ CUtensorMap map_gate, const __grid_co
             if (ahead.left > 0 && !__any_sync(0xffffffffu, gave_up != 0) && lane == 0) load();
         }
         // (two sets of sums, and of magnitudes: one is read while the next pass's warps that are done write the other.  A CTA two passes ahead has
-        // had this one's magnitudes of the pass between, which leave behind the __syncthreads that every reader of this pass's comes to.)
+        // had this one's magnitudes of the pass between, which leave behind the barrier that every reader of this pass's comes to.)
         float *sums = part + which * (WARPS * TOKENS * UP_STRIDE), *mine = sums + warp * TOKENS * UP_STRIDE;
 #pragma unroll
         for (int r = 0; r < UP_GROUPS; r++)
 #pragma unroll
-            for (int i = 0; i < 4; i++) mine[(2 * t + (i & 1)) * UP_STRIDE + r * GROUP + row + 8 * (i >> 1)] = gave_up ? __int_as_float(0x7FFFFFFF) : acc[r][0][i];
-        __syncthreads();
-        if (threadIdx.x == 0) mbar_expect_tx(peak_bars + 8 * which, (uint32_t)plan->count[now.entry] * CLUSTER * 4);
+            for (int i = 0; i < 4; i++) mine[(2 * t + (i & 1)) * UP_STRIDE + r * GROUP + row + 8 * (i >> 1)] = acc[r][0][i];
+        // A wait of any warp that gave up, here or in a pass before, ends this CTA's part: from here on its columns of h are NaN and it sends no
+        // magnitudes, so that its peers' waits run out as well.  (One that went on sending would be passes ahead of those that wait for it.)
+        const bool lost = __syncthreads_or(gave_up != 0);
+        if (lost) gave_up = 1;
+        if (threadIdx.x == 0 && !lost) mbar_expect_tx(peak_bars + 8 * which, (uint32_t)plan->count[now.entry] * CLUSTER * 4);
         // a warp a token, a lane a column
         const bool has = warp < plan->count[now.entry];
         const int col = now.block * FP8_BLOCK + (int)rank * (UNITS * GROUP) + lane;
@@ -429,21 +433,29 @@ moe_gate_up_kernel(const __grid_constant__ CUtensorMap map_gate, const __grid_co
             }
             if (col < L.inner) h = gate / (1.f + expf(-gate)) * up;
             uint32_t most = __reduce_max_sync(0xffffffffu, __float_as_uint(h) & 0x7FFFFFFFu);
-            if (lane < CLUSTER) store_peer_async(&peaks[which][warp][rank], peak_bars + 8 * which, (uint32_t)lane, __uint_as_float(most));
-            __syncwarp();
-            mbar_wait_uniform(peak_bars + 8 * which, peak_parity, gave_up);
+            if (!lost) {
+                if (lane < CLUSTER) store_peer_async(&peaks[which][warp][rank], peak_bars + 8 * which, (uint32_t)lane, __uint_as_float(most));
+                __syncwarp();
+                mbar_wait_within(peak_bars + 8 * which, peak_parity, P.wait_limit, gave_up);
+            }
             most = 0;
 #pragma unroll
             for (int r = 0; r < CLUSTER; r++) most = max(most, __float_as_uint(peaks[which][warp][r]));
+            // (its columns and, from rank 0, the block's scale)
+            if (__any_sync(0xffffffffu, gave_up != 0)) { h = __int_as_float(0x7FFFFFFF); most = 0x7FFFFFFFu; }
             const Fp8Scale s = fp8_scale(__uint_as_float(most));
             const int pair = plan->pair[now.entry][warp];
             if (col < P.hq_pitch) P.hq[(long long)pair * P.hq_pitch + col] = col < L.inner ? (uint8_t)fp8_pair(h * s.factor, 0.f) : (uint8_t)0;
             if (rank == 0 && lane == 0) P.hs[(long long)pair * per_entry + now.block] = s.scale;
         }
     }
-    if (gave_up) {                                        // copies in flight get a bounded time to land before the CTA exits
-        const long long c0 = clock64();
-        while (clock64() - c0 < 20000000ll) {}
+    // A CTA whose waits gave up did not see all of its peers' magnitudes arrive: it stays until all have sent theirs.  (The others have had the
+    // last pass's from all four.)
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    if (__any_sync(0xffffffffu, gave_up != 0)) {
+        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+        let_copies_land();
     }
 }
 
@@ -544,7 +556,7 @@ moe_down_kernel(const __grid_constant__ CUtensorMap map_down, const __grid_const
             next_block(next);
             fetch();
             const int in_run = now.kb - (now.at.r << run_shift), entry = now.at.entry;
-            if (in_run == 0) mbar_wait_uniform(bars + 8 * slot, parity, gave_up);
+            if (in_run == 0) mbar_wait_within(bars + 8 * slot, parity, P.wait_limit, gave_up);
             WeightFrag a[DOWN_GROUPS];
 #pragma unroll
             for (int r = 0; r < DOWN_GROUPS; r++) {
@@ -567,6 +579,7 @@ moe_down_kernel(const __grid_constant__ CUtensorMap map_down, const __grid_const
             if (now.at.pass != p || now.at.entry != entry) {
                 // the entry's sums; each (row, token) is one lane's: an expert has a token once
                 const int n = plan->count[entry];
+                const bool lost = __any_sync(0xffffffffu, gave_up != 0);
 #pragma unroll
                 for (int r = 0; r < DOWN_GROUPS; r++)
 #pragma unroll
@@ -575,7 +588,7 @@ moe_down_kernel(const __grid_constant__ CUtensorMap map_down, const __grid_const
                         if (r < n_groups && j < n) {
                             const int pair = plan->pair[entry][j];
                             float *to = mine + pair / L.top * stride + r * GROUP + row + 8 * (i >> 1);
-                            *to = __fmaf_rn(plan->weight[pair], gave_up ? __int_as_float(0x7FFFFFFF) : acc[r][0][i], *to);
+                            *to = __fmaf_rn(plan->weight[pair], lost ? __int_as_float(0x7FFFFFFF) : acc[r][0][i], *to);
                         }
                         acc[r][0][i] = 0.f;
                     }
@@ -594,10 +607,7 @@ moe_down_kernel(const __grid_constant__ CUtensorMap map_down, const __grid_const
         }
         __syncthreads();
     }
-    if (gave_up) {
-        const long long c0 = clock64();
-        while (clock64() - c0 < 20000000ll) {}
-    }
+    if (gave_up) let_copies_land();
 }
 
 // workspace: plan, h and its scales, a copy of x and its scales for every cluster
@@ -629,6 +639,7 @@ cudaError_t launch_moe_fp8(const MoeFp8 &L, void *ws, cudaStream_t st)
     P.hq = w8 + w.hq; P.hs = reinterpret_cast<float *>(w8 + w.hs);
     P.xq = w8 + w.xq; P.xs = reinterpret_cast<float *>(w8 + w.xs);
     P.hq_pitch = (int)fp8_row_bytes(L.inner); P.xq_pitch = (int)fp8_row_bytes(L.hidden);
+    P.wait_limit = wait_limit();
     const int sms = device_sm_count();
     const long long pitch_h = fp8_row_bytes(L.hidden), pitch_i = fp8_row_bytes(L.inner);
     const int down_all = ceil_div(L.hidden, GROUP), down_grid = down_all < sms ? down_all : sms, most = ceil_div(down_all, down_grid);

@@ -4,6 +4,7 @@ import torch
 
 import fp8_reference as ref
 from test_gpu_fp8 import same
+from test_gpu_moe_fp8 import layer
 
 pytestmark = pytest.mark.gpu
 
@@ -48,4 +49,15 @@ def test_few_tokens(b, M, N, B, x_type):
     assert torch.isfinite(clean).all()
     for _ in range(2):
         right_or_nan(with_short_waits(b, call), clean, some=x_type == "e4m3" or N % 8 == 0)
+        assert same(call(), clean)
+
+
+@pytest.mark.parametrize("hidden,inner,experts,top,T", [(2048, 8192, 8, 2, 8), (2048, 1024, 64, 8, 1), (4096, 3000, 6, 3, 29), (1000, 4000, 12, 6, 4)])
+def test_experts(b, hidden, inner, experts, top, T):
+    args = layer(hidden, inner, experts, T, "bf16", hidden + T)
+    call = lambda: b.vptq_moe_fp8(*args, top, out=torch.empty(T, hidden, device="cuda"))  # noqa: E731
+    clean = call()
+    assert torch.isfinite(clean).all()
+    for _ in range(2):
+        right_or_nan(with_short_waits(b, call), clean)
         assert same(call(), clean)
