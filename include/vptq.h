@@ -470,8 +470,8 @@ int vptq_dequant_fp8(const vptq_layer_desc *desc, const vptq_layer_ptrs *p, uint
  *           waits for another launch's, every sum has a fixed order).
  * At most 8 tokens take the kernel "fp8_decode" (no workspace), more "fp8_tcgen05" (vptq_linear_fp8_path), whose workspace, 256-byte
  * aligned, starts with a status word (vptq_workspace_status); its contents on entry are irrelevant, calls that may overlap must not
- * share one.  All device-side waits are bounded: one that gives up leaves VPTQ_E_TIMEOUT in the status word, or NaN in the results of
- * "fp8_decode". */
+ * share one.  All device-side waits are bounded: one that gives up leaves NaN in the results that it concerns and, with "fp8_tcgen05",
+ * VPTQ_E_TIMEOUT in the status word. */
 typedef struct vptq_fp8_desc {
     int32_t M, N;        /* out_features, in_features */
     int32_t x_dtype;     /* VPTQ_DTYPE_E4M3, _FP16 or _BF16 */
@@ -519,9 +519,9 @@ int vptq_moe_fp8(const vptq_moe_desc *desc, const vptq_moe_ptrs *p, const void *
 
 const char *vptq_status_string(int code);
 const char *vptq_last_cuda_error(void);
-/* Three kernels — the batched tensor-core kernel and the one over prepared images, behind vptq_linear and
- * vptq_linear_fused, and "assign_tcgen05" behind vptq_assign — keep an int32 status word at byte 0 of their workspace;
- * vptq_linear_has_status() and vptq_linear_fused_has_status() tell for which calls.  After any other call the workspace holds
+/* Four kernels — the batched tensor-core kernel and the one over prepared images, behind vptq_linear and
+ * vptq_linear_fused, "assign_tcgen05" behind vptq_assign, and "fp8_tcgen05" behind vptq_linear_fp8 — keep an int32 status word at
+ * byte 0 of their workspace; vptq_linear_has_status() and vptq_linear_fused_has_status() tell for which calls of the first two.  After any other call the workspace holds
  * no status and this call has no meaning.  It synchronises `stream`, reads the word and returns VPTQ_E_TIMEOUT if a
  * bounded device-side wait gave up during the call (the output is then invalid; the context stays
  * usable), VPTQ_E_UNSUPPORTED if the prepared-image kernel refused its image, else VPTQ_OK.  A null
@@ -537,8 +537,8 @@ int vptq_linear_fused_has_status(const vptq_layer_desc *descs, int32_t n_layers,
  * two seconds; this sets the limit, in SM clock cycles, for the kernels launched afterwards by any thread
  * (0 restores the default).  With a limit of a few cycles a healthy kernel abandons its first wait that is
  * not already satisfied, reports VPTQ_E_TIMEOUT in its status word, leaves no copy in flight and returns;
- * the context stays usable.  Honoured by the path "decode_bucket_fma", and by "fp8_decode" (vptq_linear_fp8) and
- * vptq_moe_fp8, which leave NaN in the results instead of a status.  Process-wide; not for production. */
+ * the context stays usable.  Honoured by the path "decode_bucket_fma", by vptq_linear_fp8 and by
+ * vptq_moe_fp8; "fp8_decode" and vptq_moe_fp8 have no status word and leave NaN in the results.  Process-wide; not for production. */
 void vptq_debug_set_wait_limit(uint64_t cycles);
 /* 1 when the kernels of vptq_linear / vptq_linear_fused for these arguments let one CTA wait for a flag that another CTA of
  * the same grid raises, 0 when no CTA waits for another, negative VPTQ_E_* on bad arguments.  Only the tensor-core kernel

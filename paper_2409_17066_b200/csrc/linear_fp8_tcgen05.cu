@@ -14,7 +14,8 @@
 // Bound by the two L2-side and issue-side halves of a block, operand tiles at 50 to 55 bytes a clock and SM and the sums' fmas, which overlap only
 // partly: 8192 x 28672 at 2048 tokens 467 us sustained, 2060 TFLOP/s; 8192 x 8192 at 2048 120 us, 103 without the loads, 106 without the fmas.
 // Few tokens: HBM (28672 x 8192 at 16 tokens 44.5 us, 5.3 TB/s).
-// Every wait is bounded; one that gives up sets the status word of the workspace.
+// Every wait is bounded.  A warp whose wait gives up stops: it loads, multiplies or hands on nothing more, so that the waits that depend
+// on it run out too and no sum is made of what has not arrived.  The results of warps that gave up are NaN, and the workspace's status word is set.
 #include "fp8.cuh"
 #include "fp8_tcgen05.cuh"
 #include "tcgen05_ptx.cuh"
@@ -56,6 +57,7 @@ struct Params {
     int out_dtype;
     int tma_out;           // rows of `out` are 16-byte aligned: stored by TMA
     int *status;
+    unsigned long long wait_limit;
 };
 
 // `bar` is a shared::cluster address; of a pair, that of either CTA
@@ -151,6 +153,16 @@ __device__ __forceinline__ float4 load_peer(uint32_t addr, uint32_t rank)
     asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(address_in(addr, rank)) : "memory");
     return v;
 }
+__device__ __forceinline__ uint32_t load_peer_word(uint32_t addr, uint32_t rank)
+{
+    uint32_t v;
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(address_in(addr, rank)) : "memory");
+    return v;
+}
+__device__ __forceinline__ void store_peer_word(uint32_t addr, uint32_t rank, uint32_t v)
+{
+    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(address_in(addr, rank)), "r"(v) : "memory");
+}
 __device__ __forceinline__ uint32_t pair16(float a, float b, int dtype)
 {
     if (dtype == VPTQ_DTYPE_FP16) {
@@ -165,6 +177,7 @@ __device__ __forceinline__ uint32_t pair16(float a, float b, int dtype)
 struct Sums {
     uint32_t tmem, staging;
     uint8_t *staging_p, *sm;
+    uint32_t lost_at;                      // shared memory: not 0 when a wait of the CTA's other warps gave up
     const float *scales;                   // two buffers of SCALE_BYTES
     uint32_t acc_full, acc_empty, scale_full, scale_empty;      // barriers, the first of two each
     int first, step, kb0, kb1;             // tiles and columns
@@ -173,6 +186,20 @@ struct Sums {
 
 // where token `row`'s scale lies in a buffer's line of TM: lines are written by 16 lanes at a time, one line each, and read along
 __device__ __forceinline__ int scale_slot(int line, int row) { return line * TM + (row ^ (2 * line)); }
+
+__device__ __forceinline__ uint32_t load_word(uint32_t addr)
+{
+    uint32_t v;
+    asm volatile("ld.volatile.shared.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+    return v;
+}
+
+// NaN to `rows` x `cols` values of the result; thread `i` of n
+__device__ __forceinline__ void store_nan(const Params &P, int row, int rows, int col, int cols, int i, int n)
+{
+    for (int r = 0; r < rows; r++)
+        for (int c = i; c < cols; c += n) store_out(P.out, (long long)(row + r) * P.M + col + c, __int_as_float(0x7FFFFFFF), P.out_dtype);
+}
 
 // Sums of half a tile's features, from c_first on, of the 32 tokens of lane quarter q.
 template <int TN, int SPLIT, int PAIR>
@@ -191,15 +218,15 @@ __device__ __forceinline__ void accumulate(const CUtensorMap &map_out, const Par
         for (int kb = S.kb0; kb < S.kb1; kb++, it++) {
             const uint32_t buf = it & 1, taddr = S.tmem + buf * 256;
             const int line = (kb - S.kb0) % SCALE_KBS;
-            if (line == 0) mbar_wait_uniform(S.scale_full + 8 * (group & 1), (group >> 1) & 1, gave_up);
+            if (line == 0) mbar_wait_within(S.scale_full + 8 * (group & 1), (group >> 1) & 1, P.wait_limit, gave_up);
             const float *scales = S.scales + (group & 1) * (SCALE_BYTES / 4), *ws = scales + SCALE_KBS * TM + 4 * line + block;
             const float xs = scales[scale_slot(line, 32 * q + lane)], s0 = xs * ws[0], s1 = xs * ws[1];
             if (line == SCALE_KBS - 1 || kb == S.kb1 - 1) {
                 __syncwarp();
-                if (lane == 0) mbar_arrive(S.scale_empty + 8 * (group & 1));
+                if (lane == 0 && !gave_up) mbar_arrive(S.scale_empty + 8 * (group & 1));
                 group++;
             }
-            mbar_wait_uniform(S.acc_full + 8 * buf, (it >> 1) & 1, gave_up);
+            mbar_wait_blocking(S.acc_full + 8 * buf, (it >> 1) & 1, P.wait_limit, gave_up);
             tc_fence_after();
             uint32_t d[2][16];
             tmem_start16(taddr, d[0]);
@@ -211,7 +238,7 @@ __device__ __forceinline__ void accumulate(const CUtensorMap &map_out, const Par
                     // everything read: the buffer is the MMA warp's again
                     tc_fence_before();
                     __syncwarp();
-                    if (lane == 0) {
+                    if (lane == 0 && !gave_up) {
                         if (PAIR == 2) arrive_in_cluster(S.acc_empty + 8 * buf);
                         else mbar_arrive(S.acc_empty + 8 * buf);
                     }
@@ -281,6 +308,14 @@ __device__ __forceinline__ void accumulate(const CUtensorMap &map_out, const Par
                     __syncwarp();
                 }
             }
+            // A lane that gave up went on without handing anything on; the warp's sums are no good whichever lane it was.  (NaN is written over them:
+            // put into the registers of the sums, or into the values on their way out, it cost 20 us of 8192 x 28672 at 2048 tokens.)
+            if (__any_sync(0xffffffffu, (gave_up | load_word(S.lost_at)) != 0)) {
+                if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+                __syncwarp();
+                const int rows = min(32, P.B - t0 - 32 * q), cols = min(COUNT, P.M - n0 - c_first);
+                store_nan(P, t0 + 32 * q, rows, n0 + c_first, cols, lane, 32);
+            }
         }
     }
     if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
@@ -293,7 +328,7 @@ linear_fp8_tcgen05_kernel(const __grid_constant__ CUtensorMap map_x, const __gri
 {
     constexpr int ST = stages<TN, PAIR>(), SB = stage_bytes<TN, PAIR>();
     extern __shared__ __align__(1024) uint8_t sm[];
-    __shared__ uint32_t tmem_slot;
+    __shared__ uint32_t tmem_slot, lost;                  // lost: a wait of this CTA gave up (of a pair: of either)
     const uint32_t base = smem_addr(sm), staging0 = base + ST * SB, bars = staging0 + FIXED_BYTES - BARRIERS;
     float *scales = reinterpret_cast<float *>(sm + ST * SB + ACC_WARPS * STAGING);
     auto bar_full = [&](int s) { return bars + 8u * s; };
@@ -305,6 +340,7 @@ linear_fp8_tcgen05_kernel(const __grid_constant__ CUtensorMap map_x, const __gri
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
     if (threadIdx.x == 0) {
+        lost = 0;
         for (int s = 0; s < ST; s++) { mbar_init(bar_full(s), 1); mbar_init(bar_empty(s), 1); }
         for (int b = 0; b < 2; b++) { mbar_init(bar_acc_full(b), 1); mbar_init(bar_acc_empty(b), PAIR * ACC_WARPS); mbar_init(bar_scale_full(b), SCALE_WARPS); mbar_init(bar_scale_empty(b), ACC_WARPS); }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -329,7 +365,15 @@ linear_fp8_tcgen05_kernel(const __grid_constant__ CUtensorMap map_x, const __gri
     const int rank = SPLIT * PAIR > 1 ? (int)cluster_rank() : 0, t_rank = PAIR > 1 ? rank : 0;
     const int first = (int)blockIdx.x / (SPLIT * PAIR), step = SPLIT > 1 ? P.tiles : (int)gridDim.x / PAIR;
     const int kb0 = SPLIT > 1 ? (int)((long long)P.kbs * rank / SPLIT) : 0, kb1 = SPLIT > 1 ? (int)((long long)P.kbs * (rank + 1) / SPLIT) : P.kbs;
+    const uint32_t lost_at = smem_addr(&lost);
     uint32_t gave_up = 0;
+    auto report = [&]() {                                 // (at the end of a role: to both CTAs of a pair, which leave together)
+        if (__any_sync(0xffffffffu, gave_up != 0) && lane == 0) {
+            if (PAIR == 2) { store_peer_word(lost_at, 0, 1); store_peer_word(lost_at, 1, 1); }
+            else *reinterpret_cast<volatile uint32_t *>(&lost) = 1;
+        }
+        __syncwarp();
+    };
 
     if (warp < ACC_WARP0) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(FEW_REGS));
@@ -343,34 +387,28 @@ linear_fp8_tcgen05_kernel(const __grid_constant__ CUtensorMap map_x, const __gri
                 const int t0 = (tile % P.tiles_t * PAIR + t_rank) * TM, n0 = tile / P.tiles_t * TN + n_part;
                 for (int kb = kb0; kb < kb1; kb++, it++) {
                     const uint32_t s = it % ST;
-                    mbar_wait_uniform(bar_empty(s), ((it / ST) & 1) ^ 1u, gave_up);
-                    if (gave_up) break;
-                    if (elect_one()) {
+                    mbar_wait_flagged(bar_empty(s), ((it / ST) & 1) ^ 1u, P.wait_limit, lost_at, gave_up);
+                    if (elect_one() && !gave_up) {
                         if (t_rank == 0) mbar_expect_tx(bar_full(s), PAIR * SB);
                         tma_load<PAIR>(base + s * SB + X_BYTES, &map_w, kb * FP8_BLOCK, n0, full0 + 8 * s);
                         tma_load<PAIR>(base + s * SB, &map_x, kb * FP8_BLOCK, t0, full0 + 8 * s);
                     }
                     __syncwarp();
                 }
-                if (gave_up) break;
-            }
-            // copies still in flight (only after a wait that ran out) get a bounded time to land before the CTA exits
-            if (gave_up) {
-                const long long c0 = clock64();
-                while (clock64() - c0 < 20000000ll) {}
             }
         } else if (warp == 1) {
             // ---- MMAs: e4m3 x e4m3 -> FP32, both K-major; of a pair, rank 0's over the memory of both ----
             constexpr uint32_t IDESC = (1u << 4) | ((uint32_t)(TN >> 3) << 17) | ((uint32_t)(PAIR * TM >> 4) << 24);
             const uint64_t a0 = make_smem_desc(base, 16, 1024, LAYOUT_SW128), b0 = make_smem_desc(base + X_BYTES, 16, 1024, LAYOUT_SW128);
             uint32_t it = 0;
+            pdl_wait();                                                        // (a wait's time does not begin before the preceding kernel has ended)
             for (int tile = first; tile < P.tiles && t_rank == 0; tile += step)
                 for (int kb = kb0; kb < kb1; kb++, it++) {
                     const uint32_t s = it % ST, buf = it & 1;
-                    mbar_wait_uniform(bar_full(s), (it / ST) & 1, gave_up);
-                    mbar_wait_uniform(bar_acc_empty(buf), ((it >> 1) & 1) ^ 1u, gave_up);
+                    mbar_wait_flagged(bar_full(s), (it / ST) & 1, P.wait_limit, lost_at, gave_up);
+                    mbar_wait_flagged(bar_acc_empty(buf), ((it >> 1) & 1) ^ 1u, P.wait_limit, lost_at, gave_up);
                     tc_fence_after();
-                    if (elect_one()) {
+                    if (elect_one() && !gave_up) {
                         const uint64_t at = (uint64_t)((s * SB) >> 4);
 #pragma unroll
                         for (int k = 0; k < FP8_BLOCK / 32; k++) mma_f8<PAIR>(tmem + buf * 256, a0 + at + 2 * k, b0 + at + 2 * k, IDESC, k > 0);
@@ -388,7 +426,10 @@ linear_fp8_tcgen05_kernel(const __grid_constant__ CUtensorMap map_x, const __gri
                 const int t0 = (tile % P.tiles_t * PAIR + t_rank) * TM, n0 = tile / P.tiles_t * TN, rows = min(TM, P.B - t0);
                 for (int kb = kb0; kb < kb1; kb += SCALE_KBS, group++) {
                     float *buf = scales + (group & 1) * (SCALE_BYTES / 4);
-                    mbar_wait_uniform(bar_scale_empty(group & 1), ((group >> 1) & 1) ^ 1u, gave_up);
+                    mbar_wait_flagged(bar_scale_empty(group & 1), ((group >> 1) & 1) ^ 1u, P.wait_limit, lost_at, gave_up);
+                    // (Scales of a wait that gave up go into a buffer that may be in use: whoever reads them finds `lost` at the tile's end.  A way
+                    // out of the loop here, or conditional stores, would keep the loads from being under way early and together: 8192 x 28672 at
+                    // 2048 tokens 485 us, 522 and 590.)
                     const bool in = kb + line < kb1;
                     const float *src = P.x_scale + (long long)t0 * P.kbs + kb + line;
 #pragma unroll 8
@@ -401,12 +442,12 @@ linear_fp8_tcgen05_kernel(const __grid_constant__ CUtensorMap map_x, const __gri
                             buf[SCALE_KBS * TM + 4 * line + j + odd] = in ? __ldg(P.w_scale + (long long)block * P.kbs + kb + line) : 0.f;
                         }
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(bar_scale_full(group & 1));
+                    if (lane == 0 && !gave_up) mbar_arrive(bar_scale_full(group & 1));
                 }
             }
         }
+        report();
         if constexpr (SPLIT > 1) {
-            __syncwarp();
             cluster_sync();
             cluster_sync();
         }
@@ -416,12 +457,15 @@ linear_fp8_tcgen05_kernel(const __grid_constant__ CUtensorMap map_x, const __gri
         const int w = warp - ACC_WARP0, q = warp & 3, share = w >> 2;          // TMEM lane quarter this warp may read, its part of the features
         pdl_wait();                                                            // (the result, and the status word, may be the preceding kernel's)
         if (blockIdx.x == 0 && threadIdx.x == 32 * ACC_WARP0) *P.status = 0;
-        const Sums S = {tmem + ((uint32_t)(32 * q) << 16) + share * (TN / 2), staging0 + w * STAGING, sm + ST * SB + w * STAGING, sm, scales,
+        const Sums S = {tmem + ((uint32_t)(32 * q) << 16) + share * (TN / 2), staging0 + w * STAGING, sm + ST * SB + w * STAGING, sm, lost_at, scales,
                         bar_acc_full(0), PAIR > 1 ? address_in(bar_acc_empty(0), 0) : bar_acc_empty(0), bar_scale_full(0), bar_scale_empty(0), first, step, kb0, kb1, t_rank};
         accumulate<TN, SPLIT, PAIR>(map_out, P, S, share * (TN / 2), q, lane, gave_up);
+        report();
         if constexpr (SPLIT > 1) {
-            __syncwarp();
             cluster_sync();
+            uint32_t peers_lost[SPLIT];                                        // (looked at below: no wait for it here)
+#pragma unroll
+            for (int r = 0; r < SPLIT; r++) peers_lost[r] = load_peer_word(lost_at, (uint32_t)r);
             // rows of the tile that are tokens, dealt out over the ranks; four features a thread, the ranks' sums added in order
             const int t0 = first % P.tiles_t * TM, n0 = first / P.tiles_t * TN;
             const int rows = min(TM, P.B - t0), r0 = rows * rank / SPLIT, r1 = rows * (rank + 1) / SPLIT;
@@ -445,19 +489,27 @@ linear_fp8_tcgen05_kernel(const __grid_constant__ CUtensorMap map_x, const __gri
                         if (col + k < P.M) store_out(P.out, o + k, e[k], P.out_dtype);
                 }
             }
+            uint32_t any_lost = 0;
+#pragma unroll
+            for (int r = 0; r < SPLIT; r++) any_lost |= peers_lost[r];
+            if (any_lost) {                                                    // (the same for every thread)
+                asm volatile("bar.sync 1, %0;" ::"n"(32 * ACC_WARPS) : "memory");
+                store_nan(P, t0 + r0, r1 - r0, n0, min(TN, P.M - n0), threadIdx.x - 32 * ACC_WARP0, 32 * ACC_WARPS);
+            }
             __syncwarp();
             cluster_sync();                                                    // a peer may still read this CTA's sums
         }
     }
     // (what the warps run together from here on has to do with the registers that the first four kept)
-    if (__any_sync(0xffffffffu, gave_up != 0) && lane == 0) {
-        pdl_wait();
-        atomicExch(P.status, VPTQ_E_TIMEOUT);
-    }
-    __syncwarp();
     tc_fence_before();
     __syncthreads();
     if constexpr (PAIR == 2) cluster_sync();              // neither CTA leaves while the other's MMAs, copies or arrivals need it
+    if (*reinterpret_cast<volatile uint32_t *>(&lost)) {
+        let_copies_land();
+        if (threadIdx.x == 0) atomicExch(P.status, VPTQ_E_TIMEOUT);            // (long after the word was cleared)
+        __syncthreads();
+        if constexpr (PAIR == 2) cluster_sync();
+    }
     if (warp == 1) {
         tc_fence_after();
         if constexpr (PAIR == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
@@ -560,6 +612,7 @@ cudaError_t launch_linear_fp8_tcgen05(const Fp8Linear &L, int *status, cudaStrea
     Params P;
     P.M = L.M; P.B = L.B; P.kbs = ceil_div(L.N, FP8_BLOCK);
     P.x_scale = L.x_scale; P.w_scale = L.w_scale; P.out = L.out; P.out_dtype = L.out_dtype; P.status = status;
+    P.wait_limit = wait_limit();
     P.tiles_t = P.tiles = P.tma_out = 0;
     const Choice c = choose(L.M, L.B, P.kbs);
     if (c.pair == 2) switch (c.tn) {

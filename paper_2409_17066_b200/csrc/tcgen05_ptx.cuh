@@ -86,33 +86,77 @@ __device__ __forceinline__ void mbar_wait_uniform(uint32_t bar, uint32_t parity,
                  : "+r"(gave_up) : "r"(bar), "r"(parity), "n"(WAIT_LIMIT_CYCLES) : "memory");
 }
 
-// The same with a limit in clocks, and its own order of steps: one poll that does not block, then the limit before every poll that may, so
-// that a limit of a few clocks (wait_limit) ends the first wait that is not satisfied already.  A lane's `gave_up` is its own: the warp votes.
-__device__ __forceinline__ void mbar_wait_within(uint32_t bar, uint32_t parity, unsigned long long limit, uint32_t &gave_up)
-{
-    asm volatile("{\n\t.reg .pred p, q;\n\t.reg .u64 t0, t1;\n\t"
-                 "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-                 "@p bra DONE;\n\t"
-                 "mov.u64 t0, %%clock64;\n\t"
-                 "AGAIN:\n\t"
-                 "mov.u64 t1, %%clock64;\n\t"
-                 "sub.u64 t1, t1, t0;\n\t"
-                 "setp.ge.u64 q, t1, %3;\n\t"
-                 "setp.ne.or.u32 q, %0, 0, q;\n\t"
-                 "@q bra LOST;\n\t"
-                 "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-                 "@p bra DONE;\n\t"
-                 "bra AGAIN;\n\t"
-                 "LOST:\n\t"
-                 "mov.u32 %0, 1;\n\t"
-                 "DONE:\n\t}"
-                 : "+r"(gave_up) : "r"(bar), "r"(parity), "l"(limit) : "memory");
-}
 // limit for kernels launched now: about two seconds, or what vptq_debug_set_wait_limit asked for
 inline unsigned long long wait_limit()
 {
     const unsigned long long limit = debug_wait_limit();
     return limit ? limit : WAIT_LIMIT_CYCLES;
+}
+// mbar_wait_uniform with such a limit.  A blocking poll lasts longer than any wait of a healthy kernel: a short limit goes without.  A lane's
+// `gave_up` is its own.
+__device__ __forceinline__ void mbar_wait_within(uint32_t bar, uint32_t parity, unsigned long long limit, uint32_t &gave_up)
+{
+    asm volatile("{\n\t.reg .pred p, q;\n\t.reg .u64 t0, t1;\n\t"
+                 "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+                 "@p bra DONE;\n\t"
+                 "setp.ge.u64 q, %3, 65536;\n\t"
+                 "@q mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+                 "@p bra DONE;\n\t"
+                 "mov.u64 t0, %%clock64;\n\t"
+                 "AGAIN:\n\t"
+                 "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+                 "@p bra DONE;\n\t"
+                 "mov.u64 t1, %%clock64;\n\t"
+                 "sub.u64 t1, t1, t0;\n\t"
+                 "setp.lt.u64 q, t1, %3;\n\t"
+                 "setp.eq.and.u32 q, %0, 0, q;\n\t"
+                 "@q bra AGAIN;\n\t"
+                 "mov.u32 %0, 1;\n\t"
+                 "DONE:\n\t}"
+                 : "+r"(gave_up) : "r"(bar), "r"(parity), "l"(limit) : "memory");
+}
+// ... which also sets the word at `flag` in shared memory, for the CTA's other warps, before this lane does anything more
+__device__ __forceinline__ void mbar_wait_flagged(uint32_t bar, uint32_t parity, unsigned long long limit, uint32_t flag, uint32_t &gave_up)
+{
+    asm volatile("{\n\t.reg .pred p, q;\n\t.reg .u64 t0, t1;\n\t"
+                 "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+                 "@p bra DONE;\n\t"
+                 "setp.ge.u64 q, %3, 65536;\n\t"
+                 "@q mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+                 "@p bra DONE;\n\t"
+                 "mov.u64 t0, %%clock64;\n\t"
+                 "AGAIN:\n\t"
+                 "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+                 "@p bra DONE;\n\t"
+                 "mov.u64 t1, %%clock64;\n\t"
+                 "sub.u64 t1, t1, t0;\n\t"
+                 "setp.lt.u64 q, t1, %3;\n\t"
+                 "setp.eq.and.u32 q, %0, 0, q;\n\t"
+                 "@q bra AGAIN;\n\t"
+                 "mov.u32 %0, 1;\n\t"
+                 "st.volatile.shared.u32 [%4], %0;\n\t"
+                 "fence.acq_rel.cta;\n\t"
+                 "DONE:\n\t}"
+                 : "+r"(gave_up) : "r"(bar), "r"(parity), "l"(limit), "r"(flag) : "memory");
+}
+// ... in the innermost loop of a kernel whose other waits end with a short limit: every poll blocks (the clock is looked at between them)
+__device__ __forceinline__ void mbar_wait_blocking(uint32_t bar, uint32_t parity, unsigned long long limit, uint32_t &gave_up)
+{
+    asm volatile("{\n\t.reg .pred p, q;\n\t.reg .u64 t0, t1;\n\t"
+                 "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+                 "@p bra DONE;\n\t"
+                 "mov.u64 t0, %%clock64;\n\t"
+                 "AGAIN:\n\t"
+                 "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+                 "@p bra DONE;\n\t"
+                 "mov.u64 t1, %%clock64;\n\t"
+                 "sub.u64 t1, t1, t0;\n\t"
+                 "setp.lt.u64 q, t1, %3;\n\t"
+                 "setp.eq.and.u32 q, %0, 0, q;\n\t"
+                 "@q bra AGAIN;\n\t"
+                 "mov.u32 %0, 1;\n\t"
+                 "DONE:\n\t}"
+                 : "+r"(gave_up) : "r"(bar), "r"(parity), "l"(limit) : "memory");
 }
 // At the end of a CTA in which a wait gave up: copies and MMAs that are still under way get ten milliseconds before its memory goes.
 __device__ __forceinline__ void let_copies_land()
