@@ -647,7 +647,7 @@ cudaError_t launch_moe_fp8(const MoeFp8 &L, void *ws, cudaStream_t st)
     P.down_passes = ceil_div(most, DOWN_GROUPS);
     P.down_groups = ceil_div(most, P.down_passes);
     P.down_run_shift = 0;
-    if (L.inner % FP8_BLOCK == 0 && P.down_groups * 2 <= 4 && (long long)down_kbs * L.top >= 2 * WARPS) P.down_run_shift = 1;
+    if (L.inner % FP8_BLOCK == 0 && (long long)down_kbs * L.top >= 2 * WARPS) P.down_run_shift = 1;
     CUtensorMap gate, up, down;
     const long long rows_i = (long long)L.experts * L.inner, rows_h = (long long)L.experts * L.hidden;
     if (!encode_tensor_map(&gate, CU_TENSOR_MAP_DATA_TYPE_UINT8, L.gate, pitch_h, rows_i, pitch_h, 0, 0, FP8_BLOCK, UNITS * GROUP, 1, CU_TENSOR_MAP_SWIZZLE_128B) ||
