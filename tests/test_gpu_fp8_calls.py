@@ -1,9 +1,11 @@
 """Calls of the 8-bit floating point operators that a program makes beside the plain ones: slices of stacked operands, empty batches,
-workspaces and layers in other memory, logits that are zeros of both signs."""
+workspaces and layers in other memory, logits that are zeros of both signs,
+restores in a graph."""
 import pytest
 import torch
 
 import fp8_reference as ref
+from paper_2409_17066_b200 import synth
 from test_gpu_fp8 import same
 from test_gpu_moe_fp8 import layer
 
@@ -137,3 +139,22 @@ def test_logits_that_vanish_go_to_the_lowest_experts(b):
     args[1].zero_()
     want = b.vptq_moe_fp8(*args, 3, False, out=torch.empty(1, 1024, device="cuda"))
     assert want.any() and same(got, want)
+
+
+# ---- restores in a graph -------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("permuted", [False, True])
+def test_a_restore_in_a_replayed_graph(b, permuted):
+    spec = synth.LayerSpec("f_graph", 1000, 1100, v=8, k1=256, k2=16, permuted=permuted)
+    dl = b.DeviceLayer(synth.make_layer(spec, 0, 3, 1))
+    dl.dequant_fp8()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        q, s = dl.dequant_fp8()
+    dl.c1.mul_(0.75)                                                   # what a replay restores is the layer as it is then
+    want, want_scale = dl.dequant_fp8()
+    for _ in range(2):
+        q.view(torch.uint8).zero_(), s.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert same(q, want) and same(s, want_scale)
