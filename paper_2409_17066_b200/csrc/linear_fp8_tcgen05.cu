@@ -218,7 +218,7 @@ __device__ __forceinline__ void accumulate(const CUtensorMap &map_out, const Par
         for (int kb = S.kb0; kb < S.kb1; kb++, it++) {
             const uint32_t buf = it & 1, taddr = S.tmem + buf * 256;
             const int line = (kb - S.kb0) % SCALE_KBS;
-            if (line == 0) mbar_wait_within(S.scale_full + 8 * (group & 1), (group >> 1) & 1, P.wait_limit, gave_up);
+            if (line == 0) mbar_wait_or_flag(S.scale_full + 8 * (group & 1), (group >> 1) & 1, S.lost_at, gave_up);
             const float *scales = S.scales + (group & 1) * (SCALE_BYTES / 4), *ws = scales + SCALE_KBS * TM + 4 * line + block;
             const float xs = scales[scale_slot(line, 32 * q + lane)], s0 = xs * ws[0], s1 = xs * ws[1];
             if (line == SCALE_KBS - 1 || kb == S.kb1 - 1) {
@@ -226,7 +226,7 @@ __device__ __forceinline__ void accumulate(const CUtensorMap &map_out, const Par
                 if (lane == 0 && !gave_up) mbar_arrive(S.scale_empty + 8 * (group & 1));
                 group++;
             }
-            mbar_wait_blocking(S.acc_full + 8 * buf, (it >> 1) & 1, P.wait_limit, gave_up);
+            mbar_wait_or_flag(S.acc_full + 8 * buf, (it >> 1) & 1, S.lost_at, gave_up);
             tc_fence_after();
             uint32_t d[2][16];
             tmem_start16(taddr, d[0]);
@@ -310,7 +310,7 @@ __device__ __forceinline__ void accumulate(const CUtensorMap &map_out, const Par
             }
             // A lane that gave up went on without handing anything on; the warp's sums are no good whichever lane it was.  (NaN is written over them:
             // put into the registers of the sums, or into the values on their way out, it cost 20 us of 8192 x 28672 at 2048 tokens.)
-            if (__any_sync(0xffffffffu, (gave_up | load_word(S.lost_at)) != 0)) {
+            if (__any_sync(0xffffffffu, load_word(S.lost_at) != 0)) {
                 if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
                 __syncwarp();
                 const int rows = min(32, P.B - t0 - 32 * q), cols = min(COUNT, P.M - n0 - c_first);
@@ -387,7 +387,7 @@ linear_fp8_tcgen05_kernel(const __grid_constant__ CUtensorMap map_x, const __gri
                 const int t0 = (tile % P.tiles_t * PAIR + t_rank) * TM, n0 = tile / P.tiles_t * TN + n_part;
                 for (int kb = kb0; kb < kb1; kb++, it++) {
                     const uint32_t s = it % ST;
-                    mbar_wait_flagged(bar_empty(s), ((it / ST) & 1) ^ 1u, P.wait_limit, lost_at, gave_up);
+                    mbar_wait_or_flag(bar_empty(s), ((it / ST) & 1) ^ 1u, lost_at, gave_up);
                     if (elect_one() && !gave_up) {
                         if (t_rank == 0) mbar_expect_tx(bar_full(s), PAIR * SB);
                         tma_load<PAIR>(base + s * SB + X_BYTES, &map_w, kb * FP8_BLOCK, n0, full0 + 8 * s);
@@ -406,7 +406,7 @@ linear_fp8_tcgen05_kernel(const __grid_constant__ CUtensorMap map_x, const __gri
                 for (int kb = kb0; kb < kb1; kb++, it++) {
                     const uint32_t s = it % ST, buf = it & 1;
                     mbar_wait_flagged(bar_full(s), (it / ST) & 1, P.wait_limit, lost_at, gave_up);
-                    mbar_wait_flagged(bar_acc_empty(buf), ((it >> 1) & 1) ^ 1u, P.wait_limit, lost_at, gave_up);
+                    mbar_wait_or_flag(bar_acc_empty(buf), ((it >> 1) & 1) ^ 1u, lost_at, gave_up);
                     tc_fence_after();
                     if (elect_one() && !gave_up) {
                         const uint64_t at = (uint64_t)((s * SB) >> 4);
@@ -426,7 +426,7 @@ linear_fp8_tcgen05_kernel(const __grid_constant__ CUtensorMap map_x, const __gri
                 const int t0 = (tile % P.tiles_t * PAIR + t_rank) * TM, n0 = tile / P.tiles_t * TN, rows = min(TM, P.B - t0);
                 for (int kb = kb0; kb < kb1; kb += SCALE_KBS, group++) {
                     float *buf = scales + (group & 1) * (SCALE_BYTES / 4);
-                    mbar_wait_flagged(bar_scale_empty(group & 1), ((group >> 1) & 1) ^ 1u, P.wait_limit, lost_at, gave_up);
+                    mbar_wait_or_flag(bar_scale_empty(group & 1), ((group >> 1) & 1) ^ 1u, lost_at, gave_up);
                     // (Scales of a wait that gave up go into a buffer that may be in use: whoever reads them finds `lost` at the tile's end.  A way
                     // out of the loop here, or conditional stores, would keep the loads from being under way early and together: 8192 x 28672 at
                     // 2048 tokens 485 us, 522 and 590.)
@@ -463,9 +463,7 @@ linear_fp8_tcgen05_kernel(const __grid_constant__ CUtensorMap map_x, const __gri
         report();
         if constexpr (SPLIT > 1) {
             cluster_sync();
-            uint32_t peers_lost[SPLIT];                                        // (looked at below: no wait for it here)
-#pragma unroll
-            for (int r = 0; r < SPLIT; r++) peers_lost[r] = load_peer_word(lost_at, (uint32_t)r);
+            const uint32_t peer_lost = lane < SPLIT ? load_peer_word(lost_at, (uint32_t)lane) : 0u;       // (looked at below: no wait for it here)
             // rows of the tile that are tokens, dealt out over the ranks; four features a thread, the ranks' sums added in order
             const int t0 = first % P.tiles_t * TM, n0 = first / P.tiles_t * TN;
             const int rows = min(TM, P.B - t0), r0 = rows * rank / SPLIT, r1 = rows * (rank + 1) / SPLIT;
@@ -489,10 +487,8 @@ linear_fp8_tcgen05_kernel(const __grid_constant__ CUtensorMap map_x, const __gri
                         if (col + k < P.M) store_out(P.out, o + k, e[k], P.out_dtype);
                 }
             }
-            uint32_t any_lost = 0;
-#pragma unroll
-            for (int r = 0; r < SPLIT; r++) any_lost |= peers_lost[r];
-            if (any_lost) {                                                    // (the same for every thread)
+            __syncwarp();
+            if (__any_sync(0xffffffffu, peer_lost != 0)) {                     // (the same for every warp)
                 asm volatile("bar.sync 1, %0;" ::"n"(32 * ACC_WARPS) : "memory");
                 store_nan(P, t0 + r0, r1 - r0, n0, min(TN, P.M - n0), threadIdx.x - 32 * ACC_WARP0, 32 * ACC_WARPS);
             }

@@ -139,24 +139,27 @@ __device__ __forceinline__ void mbar_wait_flagged(uint32_t bar, uint32_t parity,
                  "DONE:\n\t}"
                  : "+r"(gave_up) : "r"(bar), "r"(parity), "l"(limit), "r"(flag) : "memory");
 }
-// ... in the innermost loop of a kernel whose other waits end with a short limit: every poll blocks (the clock is looked at between them)
-__device__ __forceinline__ void mbar_wait_blocking(uint32_t bar, uint32_t parity, unsigned long long limit, uint32_t &gave_up)
+// The same flag, for waits that depend on one of those: no limit of their own but the two seconds, and an end as soon as the flag is set.
+__device__ __forceinline__ void mbar_wait_or_flag(uint32_t bar, uint32_t parity, uint32_t flag, uint32_t &gave_up)
 {
-    asm volatile("{\n\t.reg .pred p, q;\n\t.reg .u64 t0, t1;\n\t"
+    asm volatile("{\n\t.reg .pred p, q;\n\t.reg .u64 t0, t1;\n\t.reg .u32 f;\n\t"
                  "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
                  "@p bra DONE;\n\t"
                  "mov.u64 t0, %%clock64;\n\t"
                  "AGAIN:\n\t"
                  "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
                  "@p bra DONE;\n\t"
+                 "ld.volatile.shared.u32 f, [%3];\n\t"
                  "mov.u64 t1, %%clock64;\n\t"
                  "sub.u64 t1, t1, t0;\n\t"
-                 "setp.lt.u64 q, t1, %3;\n\t"
-                 "setp.eq.and.u32 q, %0, 0, q;\n\t"
+                 "setp.lt.u64 q, t1, %4;\n\t"
+                 "setp.eq.and.u32 q, f, 0, q;\n\t"
                  "@q bra AGAIN;\n\t"
                  "mov.u32 %0, 1;\n\t"
+                 "st.volatile.shared.u32 [%3], %0;\n\t"
+                 "fence.acq_rel.cta;\n\t"
                  "DONE:\n\t}"
-                 : "+r"(gave_up) : "r"(bar), "r"(parity), "l"(limit) : "memory");
+                 : "+r"(gave_up) : "r"(bar), "r"(parity), "r"(flag), "n"(WAIT_LIMIT_CYCLES) : "memory");
 }
 // At the end of a CTA in which a wait gave up: copies and MMAs that are still under way get ten milliseconds before its memory goes.
 __device__ __forceinline__ void let_copies_land()
