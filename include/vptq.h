@@ -459,8 +459,8 @@ int64_t vptq_dequant_fp8_workspace_bytes(const vptq_layer_desc *desc);
 int vptq_dequant_fp8(const vptq_layer_desc *desc, const vptq_layer_ptrs *p, uint8_t *q, float *scale,
                      void *workspace, size_t workspace_bytes, void *stream);
 
-/* out[B][M] = x[B][N] * W^T over an e4m3 weight (block_rows = 128): FP32 sums of exact products, a block's sum multiplied by its two
- * scales, the result rounded once to out_dtype.
+/* out[B][M] = x[B][N] * W^T over an e4m3 weight (block_rows = 128): FP32 sums of exact products, a block's sum multiplied by the FP32
+ * product of its two scales, the result rounded once to out_dtype.
  *   x_dtype VPTQ_DTYPE_E4M3: x [B][pitch(N)] with x_scale [B][ceil(N / 128)] (block_rows = 1)
  *           VPTQ_DTYPE_FP16 / _BF16: x [B][N], quantized inside the call by the rule (x_scale is not read): the same operands, and
  *           so the same result, as vptq_fp8_quantize followed by the call above

@@ -4,7 +4,7 @@
 //
 // A CTA makes a 128 x 128 block at a time and leaves its FP16 values in shared memory; the block's maximum and the rounding follow.
 // A thread takes four adjacent columns of a vector row: their indices are one window of packed words, their values leave as 8-byte
-// stores (one column to a thread: 8192 x 28672 322 us instead of 253; eight to a thread spill: 335). Columns that do not lie so, under
+// stores (one column to a thread: 8192 x 28672 with 65536 + 256 entries 322 us instead of 254; eight to a thread spill: 335). Columns that do not lie so, under
 // a permutation, beside the outliers, at other index widths, are looked up one to a thread, ITEMS vector rows at a time so that as many
 // table reads are in flight.
 // A vector row that crosses a block's edge is looked up by both blocks (v = 8 never does; v = 6: 23 rows instead of 21.3).
@@ -12,7 +12,9 @@
 // the blocks; out of L1 every 4-byte piece of a 12-byte row is a wavefront of its own for each lane (11008 x 4096 with v = 6: 97 us
 // instead of 75).  Blocks are dealt out column of blocks by column, so that those with outliers, which take twice as long, come first and to
 // CTAs of their own (row by row some CTAs had three of them: 75 us instead of 62).
-// A table in L2 (1 MiB) is bound by its random reads, one a clock and SM: 4096 x 4096 17.8 us; a small table by the arithmetic.
+// A table in L2 (1 MiB) makes a random read a vector, one a clock and SM; what it takes beyond them are dependent reads, indices and then
+// rows, with one block at a time a CTA (4096 x 4096 17.8 us, of which the reads are 8).  A small table is bound by the arithmetic (8192 x 28672
+// with 256 entries 201 us).
 #include "fp8.cuh"
 #include "index_words.cuh"
 #include "restore_words.cuh"

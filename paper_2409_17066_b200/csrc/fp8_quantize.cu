@@ -6,8 +6,10 @@
 // 16-byte load of 16-bit values, an 8-byte store); the block's maximum is four shuffles.  A half warp has UNROLL blocks in flight.
 // blocks form (weights, a scale per 128 x 128): a CTA takes a block, 16 lanes a row of it, the values stay in registers between the
 // maximum and the rounding: one pass over the matrix.
-// 2 or 4 bytes read and one written a value: the blocks form is bound by HBM (28672 x 8192 from 16 bits 101 to 114 us), the rows form by its
-// instructions, issue slots 63 % busy (4096 x 8192 from 16 bits 25.3 us, 4.0 TB/s).
+// 2 or 4 bytes read and one written a value: the blocks form is bound by HBM (28672 x 8192 from 16 bits 114 to 116 us, 6.1 TB/s; from FP32
+// 168, 7.0 TB/s, four of five bytes of it read), the rows form by neither HBM nor its issue slots (63 % busy) alone: for eight values a lane it does
+// four shuffles and both divisions, and four CTAs an SM have room for their registers (4096 x 8192 from 16 bits 25.3 us, 4.0 TB/s; from FP32
+// 30.8, 5.4 TB/s).
 #include "fp8.cuh"
 
 namespace vptq {
@@ -117,7 +119,7 @@ cudaError_t launch(const QuantizeParams &P, int block_rows, cudaStream_t st)
         quantize_blocks_kernel<DT, VEC><<<(unsigned)blocks, THREADS, 0, st>>>(P);
         return cudaGetLastError();
     }
-    // small calls: a block of values per half warp; large ones: four in flight, and CTAs that stay
+    // small calls: a block of values per half warp; large ones: four in flight, on eight CTAs an SM, of which four (FP32: three) run at a time
     const long long n = (long long)P.rows * P.col_blocks, per_cta = THREADS / 16;
     const long long resident = (long long)device_sm_count() * 8;
     const long long ctas = (n + per_cta - 1) / per_cta;

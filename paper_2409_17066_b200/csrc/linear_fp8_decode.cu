@@ -11,9 +11,9 @@
 // same rule as vptq_fp8_quantize: the four lanes that hold a token's block find its maximum with two shuffles, and all the pass's rows
 // share that work.  At the end of a pass the warps' sums meet in shared memory and are added in warp order: a result does not depend on
 // timing.
-// Large weights are bound by HBM, M * N bytes (28672 x 8192 40.3 us, 5.8 TB/s); small ones by what a warp does for a block, one step
+// Large weights are bound by HBM, M * N bytes (28672 x 8192 40.4 us, 5.8 TB/s); small ones by what a warp does for a block, one step
 // after the other: 1000 to 1900 clocks.
-// Every wait is bounded; a warp whose wait gives up leaves NaN.
+// Every wait is bounded; a warp whose wait gives up leaves NaN from there on.
 #include "fp8_mma.cuh"
 #include "tcgen05_ptx.cuh"
 #include "tma_2d.cuh"

@@ -12,8 +12,8 @@
 // Few tiles: SPLIT CTAs of a cluster share a tile's columns, leave their sums in shared memory, and each adds up its share of the
 // tile's rows in rank order: one launch, no scratch, and a result that does not depend on timing.
 // Bound by the two L2-side and issue-side halves of a block, operand tiles at 50 to 55 bytes a clock and SM and the sums' fmas, which overlap only
-// partly: 8192 x 28672 at 2048 tokens 467 us sustained, 2060 TFLOP/s; 8192 x 8192 at 2048 120 us, 103 without the loads, 106 without the fmas.
-// Few tokens: HBM (28672 x 8192 at 16 tokens 44.5 us, 5.3 TB/s).
+// partly: 8192 x 28672 at 2048 tokens 475 us sustained, 2030 TFLOP/s; 8192 x 8192 at 2048 121 us (103 without the loads, 106 without the fmas).
+// Few tokens: HBM (28672 x 8192 at 16 tokens 46 us, 5.1 TB/s).
 // Every wait is bounded.  A warp whose wait gives up stops: it loads, multiplies or hands on nothing more, so that the waits that depend
 // on it run out too and no sum is made of what has not arrived.  The results of warps that gave up are NaN, and the workspace's status word is set.
 #include "fp8.cuh"
