@@ -11,7 +11,7 @@
 // weight * sums to a slot of its own for each token, and the slots are added in warp order.  No atomics: a result does not depend on
 // timing.
 // Bound by HBM: the weights of the experts in use, each once (once for every 8 of its tokens; 2 of 8 experts of 4096 -> 14336 for 8 tokens:
-// 224 to 253 us from one box to another, 5.7 and 5.4 TB/s in the two kernels); for one token of small experts (8 of 64 of 2048 -> 1024: 27 us) by the way through
+// 224 to 253 us from one device to another, 5.7 and 5.4 TB/s in the two kernels); for one token of small experts (8 of 64 of 2048 -> 1024: 27 us) by the way through
 // router, two launches and two reductions.  Quantizing x and h where they are multiplied cost 250 instructions a block,
 // more than everything else in the loops together.
 // Every wait is bounded; a CTA of the first kernel, or a warp of the second, whose wait gives up leaves NaN from there on.
