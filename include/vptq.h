@@ -59,6 +59,7 @@ extern "C" {
 #define VPTQ_DTYPE_BF16 1
 #define VPTQ_DTYPE_FP32 2
 #define VPTQ_DTYPE_E4M3 3   /* 8-bit floating point (vptq_fp8_* and vptq_linear_fp8 only)              */
+#define VPTQ_DTYPE_E2M1 4   /* 4-bit floating point (vptq_fp4_*, vptq_linear_fp4 and caches only)            */
 
 #define VPTQ_FLAG_SCALE_BIAS   1  /* scale and bias are present                                     */
 #define VPTQ_FLAG_SCALE_ROWS   2  /* scale/bias are per OUTPUT row ([M]) instead of per input column */
@@ -515,12 +516,99 @@ int64_t vptq_moe_fp8_workspace_bytes(const vptq_moe_desc *desc, int32_t T);
 int vptq_moe_fp8(const vptq_moe_desc *desc, const vptq_moe_ptrs *p, const void *x, int32_t T, void *out,
                  void *workspace, size_t workspace_bytes, void *stream);
 
+/* ---- 4-bit floating point: operands with a power of two for 32 columns, and the product over them ---- */
+
+/* The paper has no counterpart.  B200's tensor cores take e2m1 operands at four times the FP16 rate and multiply by their blocks' powers of
+ * two themselves; a layer that is restored once to this format takes 17/32 of a byte a weight.
+ *
+ * An e2m1 matrix is [rows][pitch] bytes, pitch = vptq_fp4_row_bytes(cols) = 16 * ceil(cols / 32), two columns a byte, the lower column in the low
+ * half; codes of columns that the matrix does not have are zero.  A code is a sign (bit 3) and a magnitude (bits 0..2: 0, 0.5, 1, 1.5, 2, 3, 4, 6).
+ * Every 32 columns of a row have a scale byte b, which stands for 2^(b - 127), or for NaN if it is 255; value = e2m1 * scale.
+ * The scale bytes lie in tiles of 128 rows and 4 blocks, [ceil(rows / 128)][ceil(cols / 128)][32][16] (vptq_fp4_scale_bytes): that of row r
+ * and block k = column / 32 is at [r / 128][k / 4][r % 32][(r % 128) / 32 * 4 + k % 4].  Bytes of rows and blocks that the matrix does not have are zero.
+ * The rule of the quantization: a = max |x| over the block lies in [3.5, 7) * 2^e for one e; b = e + 127, but at least 0, and 0 for a = 0;
+ * code = round(x / 2^(b - 127)), to the nearest value, ties to the even code.  (Magnitudes between 6 and 7 times the scale become 6, which is nearest.)
+ * A block with an infinity or a NaN gets the byte 255, and every value of it reads as NaN.
+ *
+ * vptq_fp4_quantize: x [rows][cols] of x_dtype (FP16, BF16 or FP32), its rows `ld` values apart (ld >= cols; any alignment of a value of
+ *   the type), to q and scale (16-byte aligned).  rows = 0 does nothing; rows and cols are at most 2^30, else VPTQ_E_SHAPE (M, N and B of the calls
+ *   below too).
+ * vptq_fp4_values: such a matrix back to out [rows][cols], packed, of out_dtype (FP16, BF16 or FP32; FP16 rounds and overflows as a conversion
+ *   does, the others hold every value that the quantization makes). */
+int64_t vptq_fp4_row_bytes(int32_t n_cols);
+int64_t vptq_fp4_scale_bytes(int32_t n_rows, int32_t n_cols);
+int vptq_fp4_quantize(const void *x, int32_t x_dtype, int32_t n_rows, int32_t n_cols, int64_t ld, uint8_t *q, uint8_t *scale, void *stream);
+int vptq_fp4_values(const uint8_t *q, const uint8_t *scale, int32_t n_rows, int32_t n_cols, int32_t out_dtype, void *out, void *stream);
+/* A vector-quantized layer as an e2m1 weight: the FP16 values of vptq_dequant, bit for bit, quantized by the rule; the FP16 matrix is not
+ * written anywhere.  q [M][pitch(N)], scale vptq_fp4_scale_bytes(M, N).  Workspace and limits as in vptq_dequant_fp8
+ * (vptq_dequant_fp8_workspace_bytes). */
+int vptq_dequant_fp4(const vptq_layer_desc *desc, const vptq_layer_ptrs *p, uint8_t *q, uint8_t *scale,
+                     void *workspace, size_t workspace_bytes, void *stream);
+
+/* out[B][M] = x[B][N] * W^T over an e2m1 weight: FP32 sums, the result rounded once to out_dtype.
+ *   x_dtype VPTQ_DTYPE_E2M1: x [B][pitch(N)] with x_scale (tiles of its B rows)
+ *           VPTQ_DTYPE_FP16 / _BF16: x [B][N], quantized inside the call by the rule (x_scale is not read): the same operands, and
+ *           so the same result, as vptq_fp4_quantize followed by the call above
+ *   every pointer is 16-byte aligned (VPTQ_E_ALIGN), but for x of 16 bits: any alignment of a value;  out_dtype FP16, BF16 or FP32
+ *   flags: VPTQ_FLAG_CONCURRENT and VPTQ_FLAG_DETERMINISTIC are accepted and change nothing (no CTA waits for another launch's, every
+ *           sum has a fixed order).
+ * The workspace, 256-byte aligned, starts with a status word (vptq_workspace_status); its contents on entry are irrelevant, calls that may
+ * overlap must not share one.  All device-side waits are bounded: one that gives up leaves NaN in the results that it concerns and
+ * VPTQ_E_TIMEOUT in the status word. */
+typedef struct vptq_fp4_desc {
+    int32_t M, N;        /* out_features, in_features */
+    int32_t x_dtype;     /* VPTQ_DTYPE_E2M1, _FP16 or _BF16 */
+    int32_t out_dtype;   /* VPTQ_DTYPE_FP16, _BF16 or _FP32 */
+    int32_t flags;       /* VPTQ_FLAG_CONCURRENT, VPTQ_FLAG_DETERMINISTIC or 0 */
+} vptq_fp4_desc;
+int64_t vptq_linear_fp4_workspace_bytes(const vptq_fp4_desc *desc, int32_t B);
+int vptq_linear_fp4(const vptq_fp4_desc *desc, const void *x, const uint8_t *x_scale, int32_t B,
+                    const uint8_t *w, const uint8_t *w_scale, void *out,
+                    void *workspace, size_t workspace_bytes, void *stream);
+const char *vptq_linear_fp4_path(const vptq_fp4_desc *desc, int32_t B);
+int vptq_linear_fp4_launches(const vptq_fp4_desc *desc, int32_t B);
+
+/* ---- caches of keys and values in 8 or 4 bits --------------------------------------- */
+
+/* Pages of page_size tokens: k and v [n_pages][n_heads][page_size][row], row = vptq_cache_row_bytes bytes, and beside them k_scale and v_scale
+ * [n_pages][n_heads][page_size][vptq_cache_row_scales].  A row (a token's key or value of one head, head_dim columns) is
+ *   cache_dtype VPTQ_DTYPE_E4M3: a row of vptq_fp8_quantize with block_rows = 1: ceil(head_dim / 16) * 16 bytes, FP32 scales
+ *   cache_dtype VPTQ_DTYPE_E2M1: a row of vptq_fp4_quantize: ceil(head_dim / 32) * 16 bytes, scale bytes in the order of the blocks
+ * A call is about n_tokens tokens of n_seqs sequences, one after the other: tokens cu[s] .. cu[s+1] - 1 belong to sequence s (cu has
+ * n_seqs + 1 entries, ascending), and token cu[s] + i of the call is token start[s] + i of the sequence, in place (start[s] + i) % page_size of page
+ * table[s][(start[s] + i) / page_size] (table [n_seqs][table_width]; entries that no token needs may be anything).
+ *   vptq_cache_write: k and v [n_tokens][n_heads][head_dim] of x_dtype (FP16, BF16 or FP32) into the cache; a token's heads and the tokens are any
+ *     distances apart (strides in values, not negative), a head's columns are adjacent; any alignment of a value
+ *   vptq_cache_read: those tokens' keys and values into k and v, packed, rounded once to x_dtype
+ * Tokens in no sequence (before cu[0], from cu[n_seqs] on) are left out: nothing is written for them.  A token whose position is negative or
+ * beyond the table, or whose page is not in [0, n_pages), is not written, and reads as zeros.  Two tokens of one write that have the same
+ * place (a page that two sequences share) leave it with codes and scales of either.
+ * Codes are 16-byte aligned, FP32 scales and the int32 arrays 4-byte aligned.  n_heads, page_size and n_pages are positive, head_dim is 1 to
+ * VPTQ_CACHE_MAX_DIM, n_heads at most 65536, the others at most 2^30, else VPTQ_E_SHAPE; no tokens or no sequences: nothing is done. */
+#define VPTQ_CACHE_MAX_DIM 4096
+typedef struct vptq_cache_desc {
+    int32_t n_heads, head_dim, page_size, n_pages;
+    int32_t n_seqs, table_width;
+    int32_t cache_dtype; /* VPTQ_DTYPE_E4M3 or _E2M1 */
+    int32_t x_dtype;     /* VPTQ_DTYPE_FP16, _BF16 or _FP32 */
+} vptq_cache_desc;
+typedef struct vptq_cache_ptrs {
+    uint8_t *k, *v;
+    void    *k_scale, *v_scale;
+    const int32_t *table, *start, *cu;
+} vptq_cache_ptrs;
+int64_t vptq_cache_row_bytes(int32_t head_dim, int32_t cache_dtype);
+int64_t vptq_cache_row_scales(int32_t head_dim, int32_t cache_dtype);
+int vptq_cache_write(const vptq_cache_desc *desc, const vptq_cache_ptrs *p, const void *k, const void *v, int32_t n_tokens,
+                     int64_t k_token_stride, int64_t k_head_stride, int64_t v_token_stride, int64_t v_head_stride, void *stream);
+int vptq_cache_read(const vptq_cache_desc *desc, const vptq_cache_ptrs *p, void *k, void *v, int32_t n_tokens, void *stream);
+
 /* ---- diagnostics ------------------------------------------------------------------ */
 
 const char *vptq_status_string(int code);
 const char *vptq_last_cuda_error(void);
-/* Four kernels — the batched tensor-core kernel and the one over prepared images, behind vptq_linear and
- * vptq_linear_fused, "assign_tcgen05" behind vptq_assign, and "fp8_tcgen05" behind vptq_linear_fp8 — keep an int32 status word at
+/* Five kernels — the batched tensor-core kernel and the one over prepared images, behind vptq_linear and
+ * vptq_linear_fused, "assign_tcgen05" behind vptq_assign, "fp8_tcgen05" behind vptq_linear_fp8 and "fp4_tcgen05" behind vptq_linear_fp4 — keep an int32 status word at
  * byte 0 of their workspace; vptq_linear_has_status() and vptq_linear_fused_has_status() tell for which calls of the first two.  After any other call the workspace holds
  * no status and this call has no meaning.  It synchronises `stream`, reads the word and returns VPTQ_E_TIMEOUT if a
  * bounded device-side wait gave up during the call (the output is then invalid; the context stays
@@ -537,7 +625,7 @@ int vptq_linear_fused_has_status(const vptq_layer_desc *descs, int32_t n_layers,
  * two seconds; this sets the limit, in SM clock cycles, for the kernels launched afterwards by any thread
  * (0 restores the default).  With a limit of a few cycles a healthy kernel abandons its first wait that is
  * not already satisfied, reports VPTQ_E_TIMEOUT in its status word, leaves no copy in flight and returns;
- * the context stays usable.  Honoured by the path "decode_bucket_fma", by vptq_linear_fp8 and by
+ * the context stays usable.  Honoured by the path "decode_bucket_fma", by vptq_linear_fp8, vptq_linear_fp4 and
  * vptq_moe_fp8; "fp8_decode" and vptq_moe_fp8 have no status word and leave NaN in the results.  Process-wide; not for production. */
 void vptq_debug_set_wait_limit(uint64_t cycles);
 /* 1 when the kernels of vptq_linear / vptq_linear_fused for these arguments let one CTA wait for a flag that another CTA of

@@ -32,12 +32,13 @@ OK = 0
 E_NULL, E_SHAPE, E_ALIGN, E_UNSUPPORTED, E_WORKSPACE, E_INDEX_RANGE, E_CUDA, E_TIMEOUT = range(-1, -9, -1)
 E_SCRATCH_LIMIT = -9
 NOALLOC_SCRATCH_BYTES = 1 << 20
-DTYPE_FP16, DTYPE_BF16, DTYPE_FP32, DTYPE_E4M3 = 0, 1, 2, 3
+DTYPE_FP16, DTYPE_BF16, DTYPE_FP32, DTYPE_E4M3, DTYPE_E2M1 = 0, 1, 2, 3, 4
 FLAG_SCALE_BIAS, FLAG_SCALE_ROWS, FLAG_FORCE_GENERIC, FLAG_COL_PERM, FLAG_PREPARED = 1, 2, 4, 8, 16
 FLAG_CONCURRENT = 32
 FLAG_DETERMINISTIC = 64
 FLAG_MOE_RENORMALIZE = 128
 MOE_MAX_TOKENS, MOE_MAX_EXPERTS, MOE_MAX_TOP = 32, 256, 16
+CACHE_MAX_DIM = 4096
 
 _DT = {"fp16": DTYPE_FP16, "bf16": DTYPE_BF16, "fp32": DTYPE_FP32}
 _TORCH_DT = {DTYPE_FP16: torch.float16, DTYPE_BF16: torch.bfloat16, DTYPE_FP32: torch.float32}
@@ -63,6 +64,23 @@ class LayerPtrs(C.Structure):
 class Fp8Desc(C.Structure):
     """vptq_fp8_desc"""
     _fields_ = [("M", C.c_int32), ("N", C.c_int32), ("x_dtype", C.c_int32), ("out_dtype", C.c_int32), ("flags", C.c_int32)]
+
+
+class Fp4Desc(C.Structure):
+    """vptq_fp4_desc"""
+    _fields_ = [("M", C.c_int32), ("N", C.c_int32), ("x_dtype", C.c_int32), ("out_dtype", C.c_int32), ("flags", C.c_int32)]
+
+
+class CacheDesc(C.Structure):
+    """vptq_cache_desc"""
+    _fields_ = [("n_heads", C.c_int32), ("head_dim", C.c_int32), ("page_size", C.c_int32), ("n_pages", C.c_int32), ("n_seqs", C.c_int32),
+                ("table_width", C.c_int32), ("cache_dtype", C.c_int32), ("x_dtype", C.c_int32)]
+
+
+class CachePtrs(C.Structure):
+    """vptq_cache_ptrs"""
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p), ("table", C.c_void_p),
+                ("start", C.c_void_p), ("cu", C.c_void_p)]
 
 
 class MoeDesc(C.Structure):
@@ -129,6 +147,22 @@ EXPORTS = {
     "vptq_moe_fp8_workspace_bytes": (C.c_int64, [C.POINTER(MoeDesc), C.c_int32]),
     "vptq_moe_fp8": (C.c_int, [C.POINTER(MoeDesc), C.POINTER(MoePtrs), C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_size_t,
                                C.c_void_p]),
+    "vptq_fp4_row_bytes": (C.c_int64, [C.c_int32]),
+    "vptq_fp4_scale_bytes": (C.c_int64, [C.c_int32, C.c_int32]),
+    "vptq_fp4_quantize": (C.c_int, [C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "vptq_fp4_values": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p]),
+    "vptq_dequant_fp4": (C.c_int, [C.POINTER(LayerDesc), C.POINTER(LayerPtrs), C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t,
+                                   C.c_void_p]),
+    "vptq_linear_fp4_workspace_bytes": (C.c_int64, [C.POINTER(Fp4Desc), C.c_int32]),
+    "vptq_linear_fp4": (C.c_int, [C.POINTER(Fp4Desc), C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p,
+                                  C.c_void_p, C.c_size_t, C.c_void_p]),
+    "vptq_linear_fp4_path": (C.c_char_p, [C.POINTER(Fp4Desc), C.c_int32]),
+    "vptq_linear_fp4_launches": (C.c_int, [C.POINTER(Fp4Desc), C.c_int32]),
+    "vptq_cache_row_bytes": (C.c_int64, [C.c_int32, C.c_int32]),
+    "vptq_cache_row_scales": (C.c_int64, [C.c_int32, C.c_int32]),
+    "vptq_cache_write": (C.c_int, [C.POINTER(CacheDesc), C.POINTER(CachePtrs), C.c_void_p, C.c_void_p, C.c_int32, C.c_int64, C.c_int64,
+                                   C.c_int64, C.c_int64, C.c_void_p]),
+    "vptq_cache_read": (C.c_int, [C.POINTER(CacheDesc), C.POINTER(CachePtrs), C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p]),
     "vptq_status_string": (C.c_char_p, [C.c_int]),
     "vptq_last_cuda_error": (C.c_char_p, []),
     "vptq_workspace_status": (C.c_int, [C.c_void_p, C.c_void_p]),
@@ -478,6 +512,101 @@ def vptq_moe_fp8(x: torch.Tensor, router: torch.Tensor, gate: torch.Tensor, gate
     return _native.moe_fp8(x, router, gate, gate_scale, up, up_scale, down, down_scale, top_k, renormalize, out, workspace)
 
 
+# ---- 4-bit floating point ----------------------------------------------------------------
+
+def vptq_fp4_row_bytes(n_cols: int) -> int:
+    return lib.vptq_fp4_row_bytes(n_cols)
+
+
+def vptq_fp4_scale_bytes(n_rows: int, n_cols: int) -> int:
+    return lib.vptq_fp4_scale_bytes(n_rows, n_cols)
+
+
+def make_fp4_desc(M, N, x_dtype="fp16", out_dtype="fp16", flags=0) -> Fp4Desc:
+    return Fp4Desc(M, N, DTYPE_E2M1 if x_dtype == "e2m1" else _DT[x_dtype], _DT[out_dtype], flags)
+
+
+def vptq_fp4_quantize(x: torch.Tensor):
+    """(q, scale) of x [rows][cols] (fp16, bf16 or fp32; the columns adjacent, any distance between rows): q uint8 [rows][16 * ceil(cols / 32)],
+    two e2m1 codes a byte, scale uint8 [ceil(rows / 128)][ceil(cols / 128)][32][16], a power of two for every 32 columns of a row."""
+    return _native.fp4_quantize(x)
+
+
+def vptq_fp4_values(q: torch.Tensor, scale: torch.Tensor, cols: int, out_dtype: Optional[str] = None,
+                    out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The values [rows][cols] of an e2m1 matrix (q, scale); out_dtype "fp16", "bf16" or "fp32" (default: that of `out`, else "bf16")."""
+    return _native.fp4_values(q, scale, cols, None if out_dtype is None else _DT[out_dtype], out)
+
+
+def vptq_dequant_fp4(desc: LayerDesc, ptrs: LayerPtrs, workspace: Optional[torch.Tensor] = None):
+    """(q, scale) of a vector-quantized layer, as vptq_fp4_quantize(W) of its restored FP16 weight gives them.  The layer is in the memory
+    of the current device, where the result is made."""
+    return _native.dequant_fp4(desc, ptrs, workspace)
+
+
+def vptq_linear_fp4_workspace_bytes(desc: Fp4Desc, B: int) -> int:
+    n = lib.vptq_linear_fp4_workspace_bytes(C.byref(desc), B)
+    if n < 0:
+        raise VptqError(int(n))
+    return n
+
+
+def vptq_linear_fp4(x: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, x_scale: Optional[torch.Tensor] = None,
+                    out_dtype: Optional[str] = None, out: Optional[torch.Tensor] = None,
+                    workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """out [B][M] = x * W^T over an e2m1 weight w [M][pitch] and its scales w_scale.  x is fp16 or bf16 [B][N] (quantized inside the call)
+    or e2m1 (uint8) [B][pitch] with x_scale.  out_dtype "fp16", "bf16" or "fp32" (default: that of `out`, else of x, else "bf16").
+    Contiguous tensors of one device, the current one; no tokens (B = 0) make an empty result.  A workspace (contiguous, of that device)
+    is only taken from the caller to read its status word afterwards (vptq_workspace_status); without one the call allocates its own."""
+    return _native.linear_fp4(x, w, w_scale, x_scale, None if out_dtype is None else _DT[out_dtype], out, workspace)
+
+
+def vptq_linear_fp4_path(desc: Fp4Desc, B: int) -> str:
+    return lib.vptq_linear_fp4_path(C.byref(desc), B).decode()
+
+
+def vptq_linear_fp4_launches(desc: Fp4Desc, B: int) -> int:
+    return lib.vptq_linear_fp4_launches(C.byref(desc), B)
+
+
+# ---- caches of keys and values in 8 or 4 bits ----------------------------------------------
+
+def vptq_cache_row_bytes(head_dim: int, cache_dtype: str) -> int:
+    return lib.vptq_cache_row_bytes(head_dim, {"e4m3": DTYPE_E4M3, "e2m1": DTYPE_E2M1}[cache_dtype])
+
+
+def vptq_cache_row_scales(head_dim: int, cache_dtype: str) -> int:
+    return lib.vptq_cache_row_scales(head_dim, {"e4m3": DTYPE_E4M3, "e2m1": DTYPE_E2M1}[cache_dtype])
+
+
+def make_cache(n_pages: int, page_size: int, n_heads: int, head_dim: int, cache_dtype: str = "e4m3", device="cuda"):
+    """(k_cache, k_scale, v_cache, v_scale), all zeros: the cache that vptq_cache_write and vptq_cache_read take.  Codes are float8_e4m3fn or, two to
+    a byte, uint8; scales fp32 (128 columns) or uint8 (powers of two, 32 columns)."""
+    shape = (n_pages, n_heads, page_size)
+    row, scales = vptq_cache_row_bytes(head_dim, cache_dtype), vptq_cache_row_scales(head_dim, cache_dtype)
+    if row < 0:
+        raise VptqError(int(row))
+    codes, scale = (torch.float8_e4m3fn, torch.float32) if cache_dtype == "e4m3" else (torch.uint8, torch.uint8)
+    return tuple(torch.zeros((*shape, n), dtype=t, device=device) for n, t in ((row, codes), (scales, scale)) * 2)
+
+
+def vptq_cache_write(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, k_scale: torch.Tensor, v_cache: torch.Tensor,
+                     v_scale: torch.Tensor, table: torch.Tensor, start: torch.Tensor, cu: torch.Tensor) -> None:
+    """k and v [tokens][heads][dim] (fp16, bf16 or fp32; a head's columns adjacent, heads and tokens any distance apart) into the pages of
+    the cache: tokens cu[s] .. cu[s + 1] - 1 are those of sequence s from its token start[s] on, in the pages table[s].  table [sequences][width],
+    start [sequences], cu [sequences + 1], int32.  Pages outside the cache are left out; see vptq.h."""
+    return _native.cache_write(k, v, k_cache, k_scale, v_cache, v_scale, table, start, cu)
+
+
+def vptq_cache_read(k_cache: torch.Tensor, k_scale: torch.Tensor, v_cache: torch.Tensor, v_scale: torch.Tensor, table: torch.Tensor,
+                    start: torch.Tensor, cu: torch.Tensor, n_tokens: int, head_dim: int, out_dtype: Optional[str] = None,
+                    k: Optional[torch.Tensor] = None, v: Optional[torch.Tensor] = None):
+    """(k, v) [n_tokens][heads][head_dim] of those tokens out of the cache; out_dtype "fp16", "bf16" or "fp32" (default: that of k and v, else
+    "bf16").  Rows of tokens in no sequence (from cu[-1] on) are left as they are; in tensors that the call makes they are undefined."""
+    return _native.cache_read(k_cache, k_scale, v_cache, v_scale, table, start, cu, n_tokens, head_dim,
+                              None if out_dtype is None else _DT[out_dtype], k, v)
+
+
 # ---- a quantized layer resident on the device ------------------------------------------
 
 class DeviceLayer:
@@ -580,6 +709,10 @@ class DeviceLayer:
     def dequant_fp8(self):
         """(q, scale): the restored weight in e4m3 with 128 x 128 block scales, an operand of vptq_linear_fp8."""
         return vptq_dequant_fp8(self.desc, self.ptrs)
+
+    def dequant_fp4(self):
+        """(q, scale): the restored weight in e2m1 with a power of two for every 32 columns, an operand of vptq_linear_fp4."""
+        return vptq_dequant_fp4(self.desc, self.ptrs)
 
     def linear(self, x: torch.Tensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         y = _native.layer_linear(self.desc, self.ptrs, self._ws, x, out)

@@ -15,7 +15,8 @@
 // A table in L2 (1 MiB) makes a random read a vector, one a clock and SM; what it takes beyond them are dependent reads, indices and then
 // rows, with one block at a time a CTA (4096 x 4096 17.8 us, of which the reads are 8).  A small table is bound by the arithmetic (8192 x 28672
 // with 256 entries 201 us).
-#include "fp8.cuh"
+// E2M1: the same to e2m1 with a power of two for every 32 columns of a row (fp4.cuh): only what follows the FP16 values differs.
+#include "fp4.cuh"
 #include "index_words.cuh"
 #include "restore_words.cuh"
 
@@ -33,7 +34,8 @@ constexpr int TILE_STRIDE = FP8_BLOCK + 8;                // halves; 16-byte row
 struct DequantFp8Params {
     LayerView L;
     uint8_t *q;
-    float *scale;
+    float *scale;             // e4m3
+    uint8_t *tiles;           // e2m1: its scales
     const int *inverse;       // stored column of every input feature (-1: none names it), or null
     long long pitch;
     int row_blocks, col_blocks, blocks;
@@ -57,7 +59,7 @@ __device__ __forceinline__ float finish(float t, bool has_scale, float s, float 
     return has_scale ? __fadd_rn(__fmul_rn(t, s), b) : t;              // never contracted to an FMA
 }
 
-template <int V, bool TABLES>
+template <int V, bool TABLES, bool E2M1>
 __device__ __forceinline__ void restore_block(const DequantFp8Params &P, int index, __half (*tile)[TILE_STRIDE], uint32_t *part, const uint4 *tables)
 {
     constexpr int THREADS = threads<TABLES>(), ITEMS = items<TABLES>();
@@ -216,6 +218,23 @@ __device__ __forceinline__ void restore_block(const DequantFp8Params &P, int ind
     // 16 lanes a row, eight columns a lane (rows beyond M were not written: left out)
     constexpr int ROWS = THREADS / 16, ROUNDS = FP8_BLOCK / ROWS;
     const int lane = threadIdx.x & 15, sub = threadIdx.x >> 4, c = cb * FP8_BLOCK + lane * 8;
+    if constexpr (E2M1) {
+        // four lanes are a block; the scales of 128 x 128 values are one tile, whose rows beyond M hold zeros
+        uint8_t *scales = P.tiles + ((long long)rb * P.col_blocks + cb) * FP4_TILE_BYTES;
+#pragma unroll
+        for (int i = 0; i < ROUNDS; i++) {
+            const int row = i * ROWS + sub;
+            const bool in = m0 + row < m1;
+            Eight<VPTQ_DTYPE_FP16, true> e;
+            e.q = in && c < L.N ? *reinterpret_cast<const uint4 *>(&tile[row][lane * 8]) : make_uint4(0, 0, 0, 0);
+            const uint32_t b = fp4_block_scale(magnitude(e));
+            float v[8];
+            values_of(e, v);
+            if (in && c / 2 < P.pitch) *reinterpret_cast<uint32_t *>(P.q + (long long)(m0 + row) * P.pitch + c / 2) = fp4_codes(v, b, L.N - c);
+            if ((lane & 3) == 0) scales[fp4_scale_at(row, lane >> 2)] = (uint8_t)b;
+        }
+        return;
+    }
     uint4 w[ROUNDS];
     uint32_t most = 0;
 #pragma unroll
@@ -250,7 +269,7 @@ __device__ __forceinline__ void restore_block(const DequantFp8Params &P, int ind
     }
 }
 
-template <int V, bool TABLES>
+template <int V, bool TABLES, bool E2M1>
 __global__ void __launch_bounds__(threads<TABLES>(), TABLES ? 2 : V > 8 ? 3 : 4)
 dequant_fp8_kernel(const __grid_constant__ DequantFp8Params P)
 {
@@ -267,29 +286,29 @@ dequant_fp8_kernel(const __grid_constant__ DequantFp8Params P)
         for (int i = 0; i <= rounds; i++) {
             const int b = i * (int)gridDim.x + (int)(i < rounds ? blockIdx.x : gridDim.x - 1 - blockIdx.x);
             if (b >= P.blocks) break;
-            restore_block<V, true>(P, b, tile, part, tables);
+            restore_block<V, true, E2M1>(P, b, tile, part, tables);
             __syncthreads();
         }
     } else {
-        restore_block<V, false>(P, blockIdx.x, tile, part, nullptr);
+        restore_block<V, false, E2M1>(P, blockIdx.x, tile, part, nullptr);
     }
 }
 
-template <int V>
+template <int V, bool E2M1>
 cudaError_t restore(const DequantFp8Params &P, cudaStream_t st)
 {
     if constexpr (V == 6 || V == 8) {
         // staging pays when a CTA reads more rows out of the tables than they have
         const int grid = 2 * device_sm_count(), entries = P.L.k1 + P.L.k2;
         if (P.L.G == 1 && P.L.Nc > 0 && entries <= TABLES_MAX && (long long)P.L.R * P.L.Nc / grid > entries) {
-            auto kern = dequant_fp8_kernel<V, true>;
+            auto kern = dequant_fp8_kernel<V, true, E2M1>;
             const cudaError_t e = allow_dynamic_smem(reinterpret_cast<const void *>(kern), 16ull * TABLES_MAX);
             if (e != cudaSuccess) return e;
             kern<<<P.blocks < grid ? P.blocks : grid, threads<true>(), 16ull * entries, st>>>(P);
             return cudaGetLastError();
         }
     }
-    dequant_fp8_kernel<V, false><<<P.blocks, threads<false>(), 0, st>>>(P);
+    dequant_fp8_kernel<V, false, E2M1><<<P.blocks, threads<false>(), 0, st>>>(P);
     return cudaGetLastError();
 }
 
@@ -301,13 +320,11 @@ inverse_order_kernel(LayerView L, int *inverse)
     if (j < L.N) atomicMax(inverse + in_col(L, j), j);
 }
 
-}  // namespace
-
-cudaError_t launch_dequant_fp8(const LayerView &L, uint8_t *q, float *scale, int *inverse, cudaStream_t st)
+template <bool E2M1>
+cudaError_t launch(DequantFp8Params &P, int *inverse, cudaStream_t st)
 {
-    DequantFp8Params P;
-    P.L = L; P.q = q; P.scale = scale; P.inverse = nullptr;
-    P.pitch = fp8_row_bytes(L.N);
+    const LayerView &L = P.L;
+    P.inverse = nullptr;
     P.col_blocks = ceil_div(L.N, FP8_BLOCK);
     if (L.perm != nullptr) {
         cudaError_t e = cudaMemsetAsync(inverse, 0xFF, 4ull * L.N, st);
@@ -319,11 +336,30 @@ cudaError_t launch_dequant_fp8(const LayerView &L, uint8_t *q, float *scale, int
     P.row_blocks = ceil_div(L.M, FP8_BLOCK);
     P.blocks = (int)((long long)P.row_blocks * P.col_blocks);
     switch (L.v) {
-    case 8: return restore<8>(P, st);
-    case 6: return restore<6>(P, st);
-    case 12: return restore<12>(P, st);
-    default: return restore<0>(P, st);
+    case 8: return restore<8, E2M1>(P, st);
+    case 6: return restore<6, E2M1>(P, st);
+    case 12: return restore<12, E2M1>(P, st);
+    default: return restore<0, E2M1>(P, st);
     }
+}
+
+}  // namespace
+
+cudaError_t launch_dequant_fp8(const LayerView &L, uint8_t *q, float *scale, int *inverse, cudaStream_t st)
+{
+    DequantFp8Params P;
+    P.L = L; P.q = q; P.scale = scale; P.tiles = nullptr;
+    P.pitch = fp8_row_bytes(L.N);
+    return launch<false>(P, inverse, st);
+}
+
+cudaError_t launch_dequant_fp4(const LayerView &L, uint8_t *q, uint8_t *scale, int *inverse, cudaStream_t st)
+{
+    static_assert(FP4_TILE_ROWS == FP8_BLOCK && FP4_TILE_COLS == FP8_BLOCK, "a CTA's block is a tile of scales");
+    DequantFp8Params P;
+    P.L = L; P.q = q; P.scale = nullptr; P.tiles = scale;
+    P.pitch = fp4_row_bytes(L.N);
+    return launch<true>(P, inverse, st);
 }
 
 }  // namespace vptq

@@ -1,0 +1,42 @@
+// vptq_linear_fp4: which kernels a call takes.
+#include "fp4.cuh"
+#include "fp4_tcgen05.cuh"
+
+namespace vptq {
+
+namespace {
+
+// workspace of the tensor-core kernel: the status word, then the activations' scales and e2m1 codes
+struct Workspace { long long scales, values, bytes; };
+Workspace workspace_of(int N, int B, int x_dtype)
+{
+    Workspace w = {256, 256, 256};
+    if (x_dtype != VPTQ_DTYPE_E2M1) {
+        w.values = w.scales + (fp4_scale_bytes(B, N) + 255) / 256 * 256;
+        w.bytes = w.values + B * fp4_row_bytes(N);
+    }
+    return w;
+}
+
+}  // namespace
+
+long long linear_fp4_workspace_bytes(int N, int B, int x_dtype) { return workspace_of(N, B, x_dtype).bytes; }
+int linear_fp4_launches(int, int x_dtype) { return x_dtype != VPTQ_DTYPE_E2M1 ? 2 : 1; }
+const char *linear_fp4_path(int) { return "fp4_tcgen05"; }
+
+cudaError_t launch_linear_fp4(const Fp4Linear &P, void *ws, cudaStream_t st)
+{
+    uint8_t *w8 = reinterpret_cast<uint8_t *>(ws);
+    Fp4Linear Q = P;
+    if (P.x_dtype != VPTQ_DTYPE_E2M1) {
+        const Workspace w = workspace_of(P.N, P.B, P.x_dtype);
+        const cudaError_t e = launch_fp4_quantize(P.x, P.x_dtype, P.B, P.N, P.N, w8 + w.values, w8 + w.scales, true, st);
+        if (e != cudaSuccess) return e;
+        Q.x = w8 + w.values;
+        Q.x_scale = w8 + w.scales;
+        Q.x_dtype = VPTQ_DTYPE_E2M1;
+    }
+    return launch_linear_fp4_tcgen05(Q, reinterpret_cast<int *>(ws), st);
+}
+
+}  // namespace vptq

@@ -18,8 +18,7 @@
 // on it run out too and no sum is made of what has not arrived.  The results of warps that gave up are NaN, and the workspace's status word is set.
 #include "fp8.cuh"
 #include "fp8_tcgen05.cuh"
-#include "tcgen05_ptx.cuh"
-#include "tma_2d.cuh"
+#include "tcgen05_pair.cuh"
 
 namespace vptq {
 
@@ -60,21 +59,6 @@ struct Params {
     unsigned long long wait_limit;
 };
 
-// `bar` is a shared::cluster address; of a pair, that of either CTA
-template <int PAIR>
-__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar)
-{
-    if constexpr (PAIR == 2)
-        asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
-                     ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
-    else
-        tma_load_2d(dst, map, x, y, bar);
-}
-__device__ __forceinline__ void tma_store(const CUtensorMap *map, uint32_t src, int x, int y)
-{
-    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];"
-                 ::"l"(map), "r"(src), "r"(x), "r"(y) : "memory");
-}
 template <int PAIR>
 __device__ __forceinline__ void mma_f8(uint32_t d_tmem, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
 {
@@ -87,91 +71,8 @@ __device__ __forceinline__ void mma_f8(uint32_t d_tmem, uint64_t a, uint64_t b, 
                      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
                      ::"r"(d_tmem), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
 }
-// arrive on the barrier (of a pair: at that place in both CTAs) once all MMAs issued so far have completed
-template <int PAIR>
-__device__ __forceinline__ void commit(uint32_t bar)
-{
-    if constexpr (PAIR == 2)
-        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)3) : "memory");
-    else
-        umma_commit(bar);
-}
-__device__ __forceinline__ uint32_t address_in(uint32_t addr, uint32_t rank)
-{
-    uint32_t at;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(addr), "r"(rank));
-    return at;
-}
-// arrive on a barrier of this cluster (shared::cluster address)
-__device__ __forceinline__ void arrive_in_cluster(uint32_t bar)
-{
-    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
-}
-// 16 consecutive FP32 accumulator columns of this lane's row: started here, read after tmem_wait16 of the same registers
-__device__ __forceinline__ void tmem_start16(uint32_t taddr, uint32_t (&r)[16])
-{
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
-                   "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-                 : "r"(taddr));
-}
-__device__ __forceinline__ void tmem_wait16(uint32_t (&r)[16])
-{
-    asm volatile("tcgen05.wait::ld.sync.aligned;"
-                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
-                   "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
-                 :: "memory");
-}
-__device__ __forceinline__ uint64_t pack2(uint32_t lo, uint32_t hi)
-{
-    uint64_t r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(lo), "r"(hi));
-    return r;
-}
-__device__ __forceinline__ float2 unpack2(uint64_t v)
-{
-    uint32_t lo, hi;
-    asm("mov.b64 {%0, %1}, %2;" : "=r"(lo), "=r"(hi) : "l"(v));
-    return make_float2(__uint_as_float(lo), __uint_as_float(hi));
-}
-__device__ __forceinline__ void fma2(uint64_t &acc, uint64_t a, uint64_t b) { asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(acc) : "l"(a), "l"(b)); }
 
-__device__ __forceinline__ uint32_t cluster_rank()
-{
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
-}
-__device__ __forceinline__ void cluster_sync()
-{
-    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-__device__ __forceinline__ float4 load_peer(uint32_t addr, uint32_t rank)
-{
-    float4 v;
-    asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(address_in(addr, rank)) : "memory");
-    return v;
-}
-__device__ __forceinline__ uint32_t load_peer_word(uint32_t addr, uint32_t rank)
-{
-    uint32_t v;
-    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(address_in(addr, rank)) : "memory");
-    return v;
-}
-__device__ __forceinline__ void store_peer_word(uint32_t addr, uint32_t rank, uint32_t v)
-{
-    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(address_in(addr, rank)), "r"(v) : "memory");
-}
-__device__ __forceinline__ uint32_t pair16(float a, float b, int dtype)
-{
-    if (dtype == VPTQ_DTYPE_FP16) {
-        const __half2 h = __floats2half2_rn(a, b);
-        return *reinterpret_cast<const uint32_t *>(&h);
-    }
-    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
-    return *reinterpret_cast<const uint32_t *>(&h);
-}
+__device__ __forceinline__ void fma2(uint64_t &acc, uint64_t a, uint64_t b) { asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(acc) : "l"(a), "l"(b)); }
 
 // What the accumulating warps need of a CTA.
 struct Sums {
@@ -186,13 +87,6 @@ struct Sums {
 
 // where token `row`'s scale lies in a buffer's line of TM: lines are written by 16 lanes at a time, one line each, and read along
 __device__ __forceinline__ int scale_slot(int line, int row) { return line * TM + (row ^ (2 * line)); }
-
-__device__ __forceinline__ uint32_t load_word(uint32_t addr)
-{
-    uint32_t v;
-    asm volatile("ld.volatile.shared.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
-    return v;
-}
 
 // NaN to `rows` x `cols` values of the result; thread `i` of n
 __device__ __forceinline__ void store_nan(const Params &P, int row, int rows, int col, int cols, int i, int n)
@@ -346,13 +240,7 @@ linear_fp8_tcgen05_kernel(const __grid_constant__ CUtensorMap map_x, const __gri
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) {
-        if constexpr (PAIR == 2) {
-            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&tmem_slot)), "r"(512) : "memory");
-            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
-        } else {
-            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&tmem_slot)), "r"(512) : "memory");
-            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-        }
+        tmem_alloc_all<PAIR>(smem_addr(&tmem_slot));
     }
     tc_fence_before();
     __syncthreads();
@@ -508,8 +396,7 @@ linear_fp8_tcgen05_kernel(const __grid_constant__ CUtensorMap map_x, const __gri
     }
     if (warp == 1) {
         tc_fence_after();
-        if constexpr (PAIR == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
-        else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+        tmem_free_all<PAIR>(tmem);
     }
 }
 

@@ -308,10 +308,10 @@ PyObject *py_fp8_quantize(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
-// dequant_fp8(desc, ptrs, workspace or None) -> (q, scale)
-PyObject *py_dequant_fp8(PyObject *, PyObject *const *a, Py_ssize_t n)
+// desc, ptrs, workspace or None -> (q, scale) of a layer restored to a narrow format: `empty` makes the two, `restore` is the C ABI's call
+template <typename Empty, typename Restore>
+PyObject *restored(PyObject *const *a, Empty empty, Restore restore)
 {
-    if (n != 3) { PyErr_SetString(PyExc_TypeError, "dequant_fp8 takes 3 arguments"); return nullptr; }
     const vptq_layer_desc *d = struct_of<vptq_layer_desc>(a[0]);
     const vptq_layer_ptrs *p = d ? struct_of<vptq_layer_ptrs>(a[1]) : nullptr;
     void *ws = nullptr;
@@ -323,7 +323,7 @@ PyObject *py_dequant_fp8(PyObject *, PyObject *const *a, Py_ssize_t n)
         if (stream && !address_on_current_device(stream)) return assertion("a layer in the current device's memory");
     return guarded([&]() -> PyObject * {
         const at::TensorOptions options = at::TensorOptions().device(at::kCUDA, c10::cuda::current_device());
-        const Fp8Tensors r = empty_fp8(d->M, d->N, 128, options);
+        const auto r = empty(d, options);
         at::Tensor own;
         if (need > 0 && ws == nullptr) {
             own = at::empty({need}, options.dtype(at::kByte));
@@ -332,10 +332,20 @@ PyObject *py_dequant_fp8(PyObject *, PyObject *const *a, Py_ssize_t n)
         }
         int rc;
         Py_BEGIN_ALLOW_THREADS
-        rc = vptq_dequant_fp8(d, p, static_cast<uint8_t *>(r.q.data_ptr()), static_cast<float *>(r.scale.data_ptr()), ws, ws_bytes, current_stream());
+        rc = restore(d, p, r.q.data_ptr(), r.scale.data_ptr(), ws, ws_bytes);
         Py_END_ALLOW_THREADS
         return rc != VPTQ_OK ? fail(rc) : pair_of(r.q, r.scale);
     });
+}
+
+// dequant_fp8(desc, ptrs, workspace or None) -> (q, scale)
+PyObject *py_dequant_fp8(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (n != 3) { PyErr_SetString(PyExc_TypeError, "dequant_fp8 takes 3 arguments"); return nullptr; }
+    return restored(a, [](const vptq_layer_desc *d, const at::TensorOptions &options) { return empty_fp8(d->M, d->N, 128, options); },
+                    [](const vptq_layer_desc *d, const vptq_layer_ptrs *p, void *q, void *scale, void *ws, size_t ws_bytes) {
+                        return vptq_dequant_fp8(d, p, static_cast<uint8_t *>(q), static_cast<float *>(scale), ws, ws_bytes, current_stream());
+                    });
 }
 
 // linear_fp8(x, w, w_scale, x_scale or None, out dtype or None, out or None, workspace or None) -> out
@@ -445,6 +455,225 @@ PyObject *py_moe_fp8(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
+// ---- 4-bit floating point ---------------------------------------------------------------------------------------------------
+
+int64_t fp4_pitch(int64_t cols) { return (cols + 31) / 32 * 16; }
+
+// tensors of an e2m1 matrix: [rows][pitch] and its tiles of scales
+struct Fp4Tensors { at::Tensor q, scale; };
+Fp4Tensors empty_fp4(int64_t rows, int64_t cols, const at::TensorOptions &options)
+{
+    return {at::empty({rows, fp4_pitch(cols)}, options.dtype(at::kByte)), at::empty({(rows + 127) / 128, (cols + 127) / 128, 32, 16}, options.dtype(at::kByte))};
+}
+
+// [rows][pitch] e2m1 codes with tiles of scales
+bool is_fp4(const at::Tensor &q, const at::Tensor &scale, int64_t rows, int64_t cols)
+{
+    return plain(q) && plain(scale) && q.scalar_type() == at::kByte && scale.scalar_type() == at::kByte && q.dim() == 2 && scale.dim() == 4 &&
+           q.size(0) == rows && q.size(1) == fp4_pitch(cols) && scale.size(0) == (rows + 127) / 128 && scale.size(1) == (cols + 127) / 128 &&
+           scale.size(2) == 32 && scale.size(3) == 16;
+}
+
+// a type argument: a code, or None (then `otherwise`); false with a Python error
+bool dtype_argument(PyObject *o, int32_t otherwise, int32_t *code)
+{
+    *code = otherwise;
+    if (o == Py_None) return true;
+    *code = (int32_t)PyLong_AsLong(o);
+    return !PyErr_Occurred();
+}
+
+// fp4_quantize(x) -> (q, scale)
+PyObject *py_fp4_quantize(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (n != 1) { PyErr_SetString(PyExc_TypeError, "fp4_quantize takes 1 argument"); return nullptr; }
+    const at::Tensor *x = tensor_of(a[0]);
+    if (!x) return nullptr;
+    if (!on_current_device(*x)) return assertion("a CUDA tensor of the current device");
+    if (x->dim() != 2 || x->size(1) < 1 || x->size(0) > MAX_INT || x->size(1) > MAX_INT) return assertion("x [rows][cols]");
+    const int64_t rows = x->size(0), cols = x->size(1), ld = rows > 1 ? x->stride(0) : cols;
+    if ((cols > 1 && x->stride(1) != 1) || ld < cols) return assertion("a row's columns next to each other, rows apart");
+    return guarded([&]() -> PyObject * {
+        const Fp4Tensors r = empty_fp4(rows, cols, x->options());
+        int rc;
+        Py_BEGIN_ALLOW_THREADS
+        rc = vptq_fp4_quantize(x->data_ptr(), code_of(x->scalar_type()), (int32_t)rows, (int32_t)cols, ld, static_cast<uint8_t *>(r.q.data_ptr()),
+                               static_cast<uint8_t *>(r.scale.data_ptr()), current_stream());
+        Py_END_ALLOW_THREADS
+        return rc != VPTQ_OK ? fail(rc) : pair_of(r.q, r.scale);
+    });
+}
+
+// fp4_values(q, scale, cols, out dtype or None, out or None) -> out
+PyObject *py_fp4_values(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (n != 5) { PyErr_SetString(PyExc_TypeError, "fp4_values takes 5 arguments"); return nullptr; }
+    const at::Tensor *q = tensor_of(a[0]), *scale = q ? tensor_of(a[1]) : nullptr, *out = nullptr;
+    const long cols = scale ? PyLong_AsLong(a[2]) : -1;
+    int32_t dtype;
+    if (!scale || (cols == -1 && PyErr_Occurred()) || (a[4] != Py_None && !(out = tensor_of(a[4])))) return nullptr;
+    if (!dtype_argument(a[3], out ? code_of(out->scalar_type()) : VPTQ_DTYPE_BF16, &dtype)) return nullptr;
+    if (cols < 1 || cols > MAX_INT || q->dim() != 2 || q->size(0) > MAX_INT) return fail(VPTQ_E_SHAPE);
+    const int64_t rows = q->size(0);
+    if (!is_fp4(*q, *scale, rows, cols)) return assertion("q uint8 [rows][16 * ceil(cols / 32)] with scales uint8 [ceil(rows / 128)][ceil(cols / 128)][32][16]");
+    if (out && (!plain(*out) || out->dim() != 2 || out->size(0) != rows || out->size(1) != cols || code_of(out->scalar_type()) != dtype))
+        return assertion("out [rows][cols], contiguous, of the type asked for");
+    return guarded([&]() -> PyObject * {
+        at::Tensor result = out ? *out : at::empty({rows, cols}, q->options().dtype(dtype_of(dtype)));
+        int rc;
+        Py_BEGIN_ALLOW_THREADS
+        rc = vptq_fp4_values(static_cast<const uint8_t *>(q->data_ptr()), static_cast<const uint8_t *>(scale->data_ptr()), (int32_t)rows, (int32_t)cols, dtype,
+                             result.data_ptr(), current_stream());
+        Py_END_ALLOW_THREADS
+        if (rc != VPTQ_OK) return fail(rc);
+        return out ? Py_NewRef(a[4]) : THPVariable_Wrap(result);
+    });
+}
+
+// dequant_fp4(desc, ptrs, workspace or None) -> (q, scale)
+PyObject *py_dequant_fp4(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (n != 3) { PyErr_SetString(PyExc_TypeError, "dequant_fp4 takes 3 arguments"); return nullptr; }
+    return restored(a, [](const vptq_layer_desc *d, const at::TensorOptions &options) { return empty_fp4(d->M, d->N, options); },
+                    [](const vptq_layer_desc *d, const vptq_layer_ptrs *p, void *q, void *scale, void *ws, size_t ws_bytes) {
+                        return vptq_dequant_fp4(d, p, static_cast<uint8_t *>(q), static_cast<uint8_t *>(scale), ws, ws_bytes, current_stream());
+                    });
+}
+
+// linear_fp4(x, w, w_scale, x_scale or None, out dtype or None, out or None, workspace or None) -> out
+PyObject *py_linear_fp4(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (n != 7) { PyErr_SetString(PyExc_TypeError, "linear_fp4 takes 7 arguments"); return nullptr; }
+    const at::Tensor *x = tensor_of(a[0]), *w = x ? tensor_of(a[1]) : nullptr, *w_scale = w ? tensor_of(a[2]) : nullptr;
+    const at::Tensor *x_scale = nullptr, *out = nullptr;
+    if (!w_scale || (a[3] != Py_None && !(x_scale = tensor_of(a[3]))) || (a[5] != Py_None && !(out = tensor_of(a[5])))) return nullptr;
+    const bool e2m1 = x->scalar_type() == at::kByte;
+    vptq_fp4_desc d = {};
+    d.x_dtype = e2m1 ? VPTQ_DTYPE_E2M1 : code_of(x->scalar_type());
+    if (x->dim() != 2 || w->dim() != 2 || !plain(*x) || x->size(0) > MAX_INT || x->size(1) > MAX_INT / 2 || w->size(0) > MAX_INT)
+        return assertion("x [B][N] and w [M][pitch], contiguous tensors of the current device");
+    const int64_t B = x->size(0), N = e2m1 ? 2 * x->size(1) : x->size(1), M = w->size(0);
+    if (!is_fp4(*w, *w_scale, M, N)) return assertion("w uint8 [M][16 * ceil(N / 32)] with scales uint8 [ceil(M / 128)][ceil(N / 128)][32][16]");
+    if (e2m1 != (x_scale != nullptr)) return assertion("x_scale comes with e2m1 activations, and with no others");
+    if (e2m1 && !is_fp4(*x, *x_scale, B, N)) return assertion("x uint8 [B][pitch] with scales uint8 [ceil(B / 128)][ceil(N / 128)][32][16]");
+    d.M = (int32_t)M; d.N = (int32_t)N;
+    if (!dtype_argument(a[4], out ? code_of(out->scalar_type()) : e2m1 ? VPTQ_DTYPE_BF16 : d.x_dtype, &d.out_dtype)) return nullptr;
+    if (out && (!plain(*out) || out->dim() != 2 || out->size(0) != B || out->size(1) != M || code_of(out->scalar_type()) != d.out_dtype))
+        return assertion("out [B][M], contiguous, of the type asked for");
+    void *ws;
+    size_t ws_bytes;
+    if (!room_of(a[6], &ws, &ws_bytes)) return nullptr;
+    const int64_t need = vptq_linear_fp4_workspace_bytes(&d, B > 0 ? (int32_t)B : 1);
+    if (need < 0) return fail((int)need);
+    return guarded([&]() -> PyObject * {
+        at::Tensor own, result = out ? *out : at::empty({B, M}, x->options().dtype(dtype_of(d.out_dtype)));
+        if (B == 0) return out ? Py_NewRef(a[5]) : THPVariable_Wrap(result);           // no tokens: nothing to do
+        if (need > 0 && ws == nullptr) {
+            own = at::empty({need}, x->options().dtype(at::kByte));
+            ws = own.data_ptr();
+            ws_bytes = (size_t)need;
+        }
+        int rc;
+        Py_BEGIN_ALLOW_THREADS
+        rc = vptq_linear_fp4(&d, x->data_ptr(), x_scale ? static_cast<const uint8_t *>(x_scale->data_ptr()) : nullptr, (int32_t)B,
+                             static_cast<const uint8_t *>(w->data_ptr()), static_cast<const uint8_t *>(w_scale->data_ptr()), result.data_ptr(), ws, ws_bytes,
+                             current_stream());
+        Py_END_ALLOW_THREADS
+        if (rc != VPTQ_OK) return fail(rc);
+        return out ? Py_NewRef(a[5]) : THPVariable_Wrap(result);
+    });
+}
+
+// ---- caches of keys and values ----------------------------------------------------------------------------------------------
+
+// The cache's four tensors and the three of its sequences, a[0..6], checked against one another and a row's columns; false with a Python error.
+bool cache_of(PyObject *const *a, int64_t heads, int64_t dim, vptq_cache_desc *d, vptq_cache_ptrs *p)
+{
+    const at::Tensor *t[7];
+    for (int i = 0; i < 7; i++)
+        if (!(t[i] = tensor_of(a[i]))) return false;
+    const at::Tensor &k = *t[0], &k_scale = *t[1], &v = *t[2], &v_scale = *t[3], &table = *t[4], &start = *t[5], &cu = *t[6];
+    for (int i = 0; i < 7; i++)
+        if (!plain(*t[i])) { assertion("contiguous tensors of the current device"); return false; }
+    const bool e4m3 = k.scalar_type() == at::kFloat8_e4m3fn;
+    if ((!e4m3 && k.scalar_type() != at::kByte) || v.scalar_type() != k.scalar_type() || k_scale.scalar_type() != (e4m3 ? at::kFloat : at::kByte) ||
+        v_scale.scalar_type() != k_scale.scalar_type()) {
+        assertion("codes float8_e4m3fn with FP32 scales, or uint8 with uint8 scales");
+        return false;
+    }
+    if (dim < 1 || dim > VPTQ_CACHE_MAX_DIM || k.dim() != 4 || k_scale.dim() != 4) { fail(VPTQ_E_SHAPE); return false; }
+    d->cache_dtype = e4m3 ? VPTQ_DTYPE_E4M3 : VPTQ_DTYPE_E2M1;
+    if (k.sizes() != v.sizes() || k_scale.sizes() != v_scale.sizes() || k.sizes().slice(0, 3) != k_scale.sizes().slice(0, 3) || (heads >= 0 && k.size(1) != heads) ||
+        k.size(3) != vptq_cache_row_bytes((int32_t)dim, d->cache_dtype) || k_scale.size(3) != vptq_cache_row_scales((int32_t)dim, d->cache_dtype)) {
+        assertion("codes [pages][heads][page][row bytes] and scales [pages][heads][page][row scales], keys' and values' alike, for this head size");
+        return false;
+    }
+    if (table.scalar_type() != at::kInt || start.scalar_type() != at::kInt || cu.scalar_type() != at::kInt || table.dim() != 2 || start.dim() != 1 || cu.dim() != 1 ||
+        start.size(0) != table.size(0) || cu.size(0) != table.size(0) + 1) {
+        assertion("table [sequences][width], start [sequences], cu [sequences + 1], int32");
+        return false;
+    }
+    for (const int64_t n : {k.size(0), k.size(1), k.size(2), table.size(0), table.size(1)})
+        if (n > MAX_INT) { fail(VPTQ_E_SHAPE); return false; }
+    d->n_pages = (int32_t)k.size(0); d->n_heads = (int32_t)k.size(1); d->page_size = (int32_t)k.size(2); d->head_dim = (int32_t)dim;
+    d->n_seqs = (int32_t)table.size(0); d->table_width = (int32_t)table.size(1);
+    *p = {static_cast<uint8_t *>(k.data_ptr()), static_cast<uint8_t *>(v.data_ptr()), k_scale.data_ptr(), v_scale.data_ptr(), static_cast<const int32_t *>(table.data_ptr()),
+          static_cast<const int32_t *>(start.data_ptr()), static_cast<const int32_t *>(cu.data_ptr())};
+    return true;
+}
+
+// cache_write(k, v, k_cache, k_scale, v_cache, v_scale, table, start, cu)
+PyObject *py_cache_write(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (n != 9) { PyErr_SetString(PyExc_TypeError, "cache_write takes 9 arguments"); return nullptr; }
+    const at::Tensor *k = tensor_of(a[0]), *v = k ? tensor_of(a[1]) : nullptr;
+    if (!v) return nullptr;
+    if (!on_current_device(*k) || !on_current_device(*v)) return assertion("CUDA tensors of the current device");
+    if (k->dim() != 3 || k->sizes() != v->sizes() || k->scalar_type() != v->scalar_type() || (k->size(2) > 1 && (k->stride(2) != 1 || v->stride(2) != 1)))
+        return assertion("k and v [tokens][heads][dim] of one type, a head's columns next to each other");
+    if (k->size(0) > MAX_INT) return fail(VPTQ_E_SHAPE);
+    vptq_cache_desc d = {};
+    vptq_cache_ptrs p;
+    if (!cache_of(a + 2, k->size(1), k->size(2), &d, &p)) return nullptr;
+    d.x_dtype = code_of(k->scalar_type());
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = vptq_cache_write(&d, &p, k->data_ptr(), v->data_ptr(), (int32_t)k->size(0), k->stride(0), k->stride(1), v->stride(0), v->stride(1), current_stream());
+    Py_END_ALLOW_THREADS
+    if (rc != VPTQ_OK) return fail(rc);
+    Py_RETURN_NONE;
+}
+
+// cache_read(k_cache, k_scale, v_cache, v_scale, table, start, cu, n_tokens, head_dim, out dtype or None, k or None, v or None) -> (k, v)
+PyObject *py_cache_read(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (n != 12) { PyErr_SetString(PyExc_TypeError, "cache_read takes 12 arguments"); return nullptr; }
+    const long tokens = PyLong_AsLong(a[7]);
+    if (tokens == -1 && PyErr_Occurred()) return nullptr;
+    const long dim = PyLong_AsLong(a[8]);
+    if (dim == -1 && PyErr_Occurred()) return nullptr;
+    const at::Tensor *k = nullptr, *v = nullptr;
+    if ((a[10] != Py_None && !(k = tensor_of(a[10]))) || (a[11] != Py_None && !(v = tensor_of(a[11])))) return nullptr;
+    vptq_cache_desc d = {};
+    vptq_cache_ptrs p;
+    if (!cache_of(a, -1, dim, &d, &p)) return nullptr;
+    if (tokens < 0 || tokens > MAX_INT) return fail(VPTQ_E_SHAPE);
+    const at::Tensor *given = k ? k : v;
+    if (!dtype_argument(a[9], given ? code_of(given->scalar_type()) : VPTQ_DTYPE_BF16, &d.x_dtype)) return nullptr;
+    for (const at::Tensor *t : {k, v})
+        if (t && (!plain(*t) || t->dim() != 3 || t->size(0) != tokens || t->size(1) != d.n_heads || t->size(2) != dim || code_of(t->scalar_type()) != d.x_dtype))
+            return assertion("k and v [tokens][heads][dim], contiguous, of the type asked for");
+    return guarded([&]() -> PyObject * {
+        const at::TensorOptions options = THPVariable_Unpack(a[0]).options().dtype(dtype_of(d.x_dtype));
+        at::Tensor k_out = k ? *k : at::empty({tokens, d.n_heads, dim}, options), v_out = v ? *v : at::empty({tokens, d.n_heads, dim}, options);
+        int rc;
+        Py_BEGIN_ALLOW_THREADS
+        rc = vptq_cache_read(&d, &p, k_out.data_ptr(), v_out.data_ptr(), (int32_t)tokens, current_stream());
+        Py_END_ALLOW_THREADS
+        return rc != VPTQ_OK ? fail(rc) : pair_of(k_out, v_out);
+    });
+}
+
 PyObject *py_set_error_class(PyObject *, PyObject *cls)
 {
     Py_INCREF(cls);
@@ -461,6 +690,12 @@ PyMethodDef methods[] = {
     {"dequant_fp8", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_dequant_fp8)), METH_FASTCALL, "vptq_dequant_fp8 on torch tensors"},
     {"linear_fp8", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_linear_fp8)), METH_FASTCALL, "vptq_linear_fp8 on torch tensors"},
     {"moe_fp8", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_moe_fp8)), METH_FASTCALL, "vptq_moe_fp8 on torch tensors"},
+    {"fp4_quantize", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_fp4_quantize)), METH_FASTCALL, "vptq_fp4_quantize on torch tensors"},
+    {"fp4_values", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_fp4_values)), METH_FASTCALL, "vptq_fp4_values on torch tensors"},
+    {"dequant_fp4", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_dequant_fp4)), METH_FASTCALL, "vptq_dequant_fp4 on torch tensors"},
+    {"linear_fp4", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_linear_fp4)), METH_FASTCALL, "vptq_linear_fp4 on torch tensors"},
+    {"cache_write", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_cache_write)), METH_FASTCALL, "vptq_cache_write on torch tensors"},
+    {"cache_read", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_cache_read)), METH_FASTCALL, "vptq_cache_read on torch tensors"},
     {"set_error_class", py_set_error_class, METH_O, "exception raised for VPTQ_E_* codes"},
     {nullptr, nullptr, 0, nullptr}};
 

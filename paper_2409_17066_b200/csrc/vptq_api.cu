@@ -11,6 +11,8 @@
 #include "prepared.cuh"
 #include "fp8.cuh"
 #include "moe_fp8.cuh"
+#include "fp4.cuh"
+#include "kv_cache.cuh"
 
 #include <vector>
 
@@ -567,8 +569,8 @@ int64_t vptq_dequant_fp8_workspace_bytes(const vptq_layer_desc *desc)
     return (desc->flags & VPTQ_FLAG_COL_PERM) ? (4ll * desc->N + 255) / 256 * 256 : 0;
 }
 
-int vptq_dequant_fp8(const vptq_layer_desc *desc, const vptq_layer_ptrs *p, uint8_t *q, float *scale,
-                     void *workspace, size_t workspace_bytes, void *stream)
+// what a restore to a narrow format asks of its layer, its two outputs and the workspace
+static int check_restore(const vptq_layer_desc *desc, const vptq_layer_ptrs *p, const void *q, const void *scale, const void *workspace, size_t workspace_bytes)
 {
     int rc = check_desc(desc);
     if (rc != VPTQ_OK) return rc;
@@ -582,6 +584,14 @@ int vptq_dequant_fp8(const vptq_layer_desc *desc, const vptq_layer_ptrs *p, uint
         if (workspace == nullptr || (int64_t)workspace_bytes < need) return VPTQ_E_WORKSPACE;
         if ((reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return VPTQ_E_ALIGN;
     }
+    return VPTQ_OK;
+}
+
+int vptq_dequant_fp8(const vptq_layer_desc *desc, const vptq_layer_ptrs *p, uint8_t *q, float *scale,
+                     void *workspace, size_t workspace_bytes, void *stream)
+{
+    const int rc = check_restore(desc, p, q, scale, workspace, workspace_bytes);
+    if (rc != VPTQ_OK) return rc;
     const LayerView L = make_view(desc, p);
     const cudaError_t e = launch_dequant_fp8(L, q, scale, reinterpret_cast<int *>(workspace), reinterpret_cast<cudaStream_t>(stream));
     return e == cudaSuccess ? VPTQ_OK : cuda_fail(e);
@@ -676,6 +686,169 @@ int vptq_moe_fp8(const vptq_moe_desc *desc, const vptq_moe_ptrs *p, const void *
     L.x = x; L.router = p->router; L.gate = p->gate; L.up = p->up; L.down = p->down;
     L.gate_scale = p->gate_scale; L.up_scale = p->up_scale; L.down_scale = p->down_scale; L.out = out;
     const cudaError_t e = launch_moe_fp8(L, workspace, reinterpret_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? VPTQ_OK : cuda_fail(e);
+}
+
+int64_t vptq_fp4_row_bytes(int32_t n_cols)
+{
+    if (n_cols < 0) return VPTQ_E_SHAPE;
+    return fp4_row_bytes(n_cols);
+}
+
+int64_t vptq_fp4_scale_bytes(int32_t n_rows, int32_t n_cols)
+{
+    if (n_rows < 0 || n_cols < 0) return VPTQ_E_SHAPE;
+    return fp4_scale_bytes(n_rows, n_cols);
+}
+
+int vptq_fp4_quantize(const void *x, int32_t x_dtype, int32_t n_rows, int32_t n_cols, int64_t ld, uint8_t *q, uint8_t *scale, void *stream)
+{
+    if (n_rows < 0 || n_rows > FP8_MAX_SIZE || n_cols <= 0 || n_cols > FP8_MAX_SIZE || ld < n_cols) return VPTQ_E_SHAPE;
+    if (x_dtype != VPTQ_DTYPE_FP16 && x_dtype != VPTQ_DTYPE_BF16 && x_dtype != VPTQ_DTYPE_FP32) return VPTQ_E_UNSUPPORTED;
+    if (n_rows == 0) return VPTQ_OK;
+    if (x == nullptr || q == nullptr || scale == nullptr) return VPTQ_E_NULL;
+    if (!aligned16(q) || !aligned16(scale) || (reinterpret_cast<uintptr_t>(x) & (x_dtype == VPTQ_DTYPE_FP32 ? 3u : 1u))) return VPTQ_E_ALIGN;
+    const cudaError_t e = launch_fp4_quantize(x, x_dtype, n_rows, n_cols, ld, q, scale, false, reinterpret_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? VPTQ_OK : cuda_fail(e);
+}
+
+int vptq_fp4_values(const uint8_t *q, const uint8_t *scale, int32_t n_rows, int32_t n_cols, int32_t out_dtype, void *out, void *stream)
+{
+    if (n_rows < 0 || n_rows > FP8_MAX_SIZE || n_cols <= 0 || n_cols > FP8_MAX_SIZE) return VPTQ_E_SHAPE;
+    if (out_dtype != VPTQ_DTYPE_FP16 && out_dtype != VPTQ_DTYPE_BF16 && out_dtype != VPTQ_DTYPE_FP32) return VPTQ_E_UNSUPPORTED;
+    if (n_rows == 0) return VPTQ_OK;
+    if (q == nullptr || scale == nullptr || out == nullptr) return VPTQ_E_NULL;
+    if (!aligned16(q) || !aligned16(scale) || !aligned16(out)) return VPTQ_E_ALIGN;
+    const cudaError_t e = launch_fp4_values(q, scale, n_rows, n_cols, out_dtype, out, reinterpret_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? VPTQ_OK : cuda_fail(e);
+}
+
+int vptq_dequant_fp4(const vptq_layer_desc *desc, const vptq_layer_ptrs *p, uint8_t *q, uint8_t *scale,
+                     void *workspace, size_t workspace_bytes, void *stream)
+{
+    const int rc = check_restore(desc, p, q, scale, workspace, workspace_bytes);
+    if (rc != VPTQ_OK) return rc;
+    const LayerView L = make_view(desc, p);
+    const cudaError_t e = launch_dequant_fp4(L, q, scale, reinterpret_cast<int *>(workspace), reinterpret_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? VPTQ_OK : cuda_fail(e);
+}
+
+static int check_fp4_desc(const vptq_fp4_desc *d, int32_t B)
+{
+    if (d == nullptr) return VPTQ_E_NULL;
+    if (d->M <= 0 || d->N <= 0 || B <= 0 || d->M > FP8_MAX_SIZE || d->N > FP8_MAX_SIZE || B > FP8_MAX_SIZE) return VPTQ_E_SHAPE;
+    if (d->x_dtype != VPTQ_DTYPE_E2M1 && d->x_dtype != VPTQ_DTYPE_FP16 && d->x_dtype != VPTQ_DTYPE_BF16) return VPTQ_E_UNSUPPORTED;
+    if (d->out_dtype != VPTQ_DTYPE_FP16 && d->out_dtype != VPTQ_DTYPE_BF16 && d->out_dtype != VPTQ_DTYPE_FP32) return VPTQ_E_UNSUPPORTED;
+    if (d->flags & ~(VPTQ_FLAG_CONCURRENT | VPTQ_FLAG_DETERMINISTIC)) return VPTQ_E_UNSUPPORTED;
+    return VPTQ_OK;
+}
+
+int64_t vptq_linear_fp4_workspace_bytes(const vptq_fp4_desc *desc, int32_t B)
+{
+    const int rc = check_fp4_desc(desc, B);
+    if (rc != VPTQ_OK) return rc;
+    return linear_fp4_workspace_bytes(desc->N, B, desc->x_dtype);
+}
+
+int vptq_linear_fp4(const vptq_fp4_desc *desc, const void *x, const uint8_t *x_scale, int32_t B,
+                    const uint8_t *w, const uint8_t *w_scale, void *out,
+                    void *workspace, size_t workspace_bytes, void *stream)
+{
+    const int rc = check_fp4_desc(desc, B);
+    if (rc != VPTQ_OK) return rc;
+    const bool e2m1 = desc->x_dtype == VPTQ_DTYPE_E2M1;
+    if (x == nullptr || w == nullptr || w_scale == nullptr || out == nullptr || (e2m1 && x_scale == nullptr)) return VPTQ_E_NULL;
+    if ((reinterpret_cast<uintptr_t>(x) & (e2m1 ? 15u : 1u)) || !aligned16(w) || !aligned16(w_scale) || !aligned16(out) || (e2m1 && !aligned16(x_scale))) return VPTQ_E_ALIGN;
+    const long long need = linear_fp4_workspace_bytes(desc->N, B, desc->x_dtype);
+    if (workspace == nullptr || (long long)workspace_bytes < need) return VPTQ_E_WORKSPACE;
+    if ((reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return VPTQ_E_ALIGN;
+    Fp4Linear P;
+    P.M = desc->M; P.N = desc->N; P.B = B; P.x_dtype = desc->x_dtype; P.out_dtype = desc->out_dtype;
+    P.x = x; P.x_scale = e2m1 ? x_scale : nullptr; P.w = w; P.w_scale = w_scale; P.out = out;
+    const cudaError_t e = launch_linear_fp4(P, workspace, reinterpret_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? VPTQ_OK : cuda_fail(e);
+}
+
+const char *vptq_linear_fp4_path(const vptq_fp4_desc *desc, int32_t B)
+{
+    if (check_fp4_desc(desc, B) != VPTQ_OK) return "invalid";
+    return linear_fp4_path(B);
+}
+
+int vptq_linear_fp4_launches(const vptq_fp4_desc *desc, int32_t B)
+{
+    const int rc = check_fp4_desc(desc, B);
+    if (rc != VPTQ_OK) return rc;
+    return linear_fp4_launches(B, desc->x_dtype);
+}
+
+int64_t vptq_cache_row_bytes(int32_t head_dim, int32_t cache_dtype)
+{
+    if (head_dim <= 0 || head_dim > VPTQ_CACHE_MAX_DIM) return VPTQ_E_SHAPE;
+    if (cache_dtype != VPTQ_DTYPE_E4M3 && cache_dtype != VPTQ_DTYPE_E2M1) return VPTQ_E_UNSUPPORTED;
+    return cache_dtype == VPTQ_DTYPE_E4M3 ? fp8_row_bytes(head_dim) : fp4_row_bytes(head_dim);
+}
+
+int64_t vptq_cache_row_scales(int32_t head_dim, int32_t cache_dtype)
+{
+    const int64_t rc = vptq_cache_row_bytes(head_dim, cache_dtype);
+    if (rc < 0) return rc;
+    return ceil_div(head_dim, cache_dtype == VPTQ_DTYPE_E4M3 ? FP8_BLOCK : FP4_BLOCK);
+}
+
+// the arguments that writing and reading share, as the kernels see them
+static int make_cache(const vptq_cache_desc *d, const vptq_cache_ptrs *p, const void *k, const void *v, int32_t n_tokens, KvCache *C)
+{
+    if (d == nullptr) return VPTQ_E_NULL;
+    if (d->n_heads <= 0 || d->n_heads > 65536 || d->head_dim <= 0 || d->head_dim > VPTQ_CACHE_MAX_DIM || d->page_size <= 0 || d->page_size > FP8_MAX_SIZE ||
+        d->n_pages <= 0 || d->n_pages > FP8_MAX_SIZE || d->n_seqs < 0 || d->n_seqs > FP8_MAX_SIZE || d->table_width < 0 || d->table_width > FP8_MAX_SIZE ||
+        n_tokens < 0 || n_tokens > FP8_MAX_SIZE)
+        return VPTQ_E_SHAPE;
+    if (d->cache_dtype != VPTQ_DTYPE_E4M3 && d->cache_dtype != VPTQ_DTYPE_E2M1) return VPTQ_E_UNSUPPORTED;
+    if (d->x_dtype != VPTQ_DTYPE_FP16 && d->x_dtype != VPTQ_DTYPE_BF16 && d->x_dtype != VPTQ_DTYPE_FP32) return VPTQ_E_UNSUPPORTED;
+    C->tokens = d->n_seqs == 0 ? 0 : n_tokens;
+    if (C->tokens == 0) return VPTQ_OK;
+    if (p == nullptr || p->k == nullptr || p->v == nullptr || p->k_scale == nullptr || p->v_scale == nullptr || (p->table == nullptr && d->table_width > 0) ||
+        p->start == nullptr || p->cu == nullptr || k == nullptr || v == nullptr)
+        return VPTQ_E_NULL;
+    C->e2m1 = d->cache_dtype == VPTQ_DTYPE_E2M1 ? 1 : 0;
+    const uintptr_t value = d->x_dtype == VPTQ_DTYPE_FP32 ? 3u : 1u, scale = C->e2m1 ? 0u : 3u;
+    if (!aligned16(p->k) || !aligned16(p->v) || ((reinterpret_cast<uintptr_t>(p->k_scale) | reinterpret_cast<uintptr_t>(p->v_scale)) & scale) ||
+        ((reinterpret_cast<uintptr_t>(p->table) | reinterpret_cast<uintptr_t>(p->start) | reinterpret_cast<uintptr_t>(p->cu)) & 3u) ||
+        ((reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v)) & value))
+        return VPTQ_E_ALIGN;
+    C->heads = d->n_heads; C->dim = d->head_dim; C->page = d->page_size; C->pages = d->n_pages;
+    C->seqs = d->n_seqs; C->width = d->table_width; C->x_dtype = d->x_dtype;
+    C->q[0] = p->k; C->q[1] = p->v; C->scale[0] = p->k_scale; C->scale[1] = p->v_scale;
+    C->table = p->table; C->start = p->start; C->cu = p->cu;
+    C->x[0] = const_cast<void *>(k); C->x[1] = const_cast<void *>(v);
+    return VPTQ_OK;
+}
+
+int vptq_cache_write(const vptq_cache_desc *desc, const vptq_cache_ptrs *p, const void *k, const void *v, int32_t n_tokens,
+                     int64_t k_token_stride, int64_t k_head_stride, int64_t v_token_stride, int64_t v_head_stride, void *stream)
+{
+    KvCache C;
+    const int rc = make_cache(desc, p, k, v, n_tokens, &C);
+    if (rc != VPTQ_OK) return rc;
+    if (k_token_stride < 0 || k_head_stride < 0 || v_token_stride < 0 || v_head_stride < 0) return VPTQ_E_SHAPE;
+    if (C.tokens == 0) return VPTQ_OK;
+    C.token_stride[0] = k_token_stride; C.token_stride[1] = v_token_stride;
+    C.head_stride[0] = k_head_stride; C.head_stride[1] = v_head_stride;
+    const cudaError_t e = launch_cache_write(C, reinterpret_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? VPTQ_OK : cuda_fail(e);
+}
+
+int vptq_cache_read(const vptq_cache_desc *desc, const vptq_cache_ptrs *p, void *k, void *v, int32_t n_tokens, void *stream)
+{
+    KvCache C;
+    const int rc = make_cache(desc, p, k, v, n_tokens, &C);
+    if (rc != VPTQ_OK || C.tokens == 0) return rc;
+    for (int i = 0; i < 2; i++) {
+        C.head_stride[i] = C.dim;
+        C.token_stride[i] = (long long)C.heads * C.dim;
+    }
+    const cudaError_t e = launch_cache_read(C, reinterpret_cast<cudaStream_t>(stream));
     return e == cudaSuccess ? VPTQ_OK : cuda_fail(e);
 }
 
