@@ -584,7 +584,7 @@ int vptq_linear_fp4_launches(const vptq_fp4_desc *desc, int32_t B);
  * beyond the table, or whose page is not in [0, n_pages), is not written, and reads as zeros.  Two tokens of one write that have the same
  * place (a page that two sequences share) leave it with codes and scales of either.
  * Codes are 16-byte aligned, FP32 scales and the int32 arrays 4-byte aligned.  n_heads, page_size and n_pages are positive, head_dim is 1 to
- * VPTQ_CACHE_MAX_DIM, n_heads at most 65536, the others at most 2^30, else VPTQ_E_SHAPE; no tokens or no sequences: nothing is done. */
+ * VPTQ_CACHE_MAX_DIM, n_heads at most 4096, the others at most 2^30, else VPTQ_E_SHAPE; no tokens or no sequences: nothing is done. */
 #define VPTQ_CACHE_MAX_DIM 4096
 typedef struct vptq_cache_desc {
     int32_t n_heads, head_dim, page_size, n_pages;

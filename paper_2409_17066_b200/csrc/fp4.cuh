@@ -57,6 +57,12 @@ __device__ __forceinline__ float fp4_scale_value(uint32_t b)
     return __uint_as_float(b == 255u ? 0x7FFFFFFFu : b == 0u ? 0x00400000u : b << 23);
 }
 
+// (a * f, b * f), two products in one instruction
+__device__ __forceinline__ void times2(float &x, float &y, float a, float b, float f)
+{
+    asm("{\n\t.reg .b64 v, s;\n\tmov.b64 v, {%2, %3};\n\tmov.b64 s, {%4, %4};\n\tmul.rn.f32x2 v, v, s;\n\tmov.b64 {%0, %1}, v;\n\t}" : "=f"(x), "=f"(y) : "f"(a), "f"(b), "f"(f));
+}
+
 // Eight values to codes, nearest, ties to even, at most 6; v[0] in the lowest four bits.
 __device__ __forceinline__ uint32_t fp4_eight(const float (&v)[8])
 {
@@ -82,6 +88,36 @@ __device__ __forceinline__ void fp4_values8(uint32_t q, float (&v)[8])
     }
 }
 
+// Sixteen consecutive values of a row, as two times eight; zeros beyond `cols`.
+template <int DT, bool VEC> struct Sixteen { Eight<DT, VEC> h[2]; };
+template <int DT, bool VEC>
+__device__ __forceinline__ Sixteen<DT, VEC> load_sixteen(const void *row, int c, int cols)
+{
+    return {{load_eight<DT, VEC>(row, c, cols), load_eight<DT, VEC>(row, c + 8, cols)}};
+}
+// the larger magnitudes of two words of packed 16-bit values, whose signs are cleared
+__device__ __forceinline__ uint32_t larger2(uint32_t a, uint32_t b)
+{
+    asm("max.u16x2 %0, %0, %1;" : "+r"(a) : "r"(b));
+    return a;
+}
+// their largest magnitude, as bits of an FP32 value in which NaN > infinity > every number
+template <int DT, bool VEC>
+__device__ __forceinline__ uint32_t magnitude(const Sixteen<DT, VEC> &e)
+{
+    if constexpr (VEC && DT != VPTQ_DTYPE_FP32) {
+        const uint32_t w[8] = {e.h[0].q.x, e.h[0].q.y, e.h[0].q.z, e.h[0].q.w, e.h[1].q.x, e.h[1].q.y, e.h[1].q.z, e.h[1].q.w};
+        uint32_t m = w[0] & 0x7FFF7FFFu;
+#pragma unroll
+        for (int i = 1; i < 8; i++) m = larger2(m, w[i] & 0x7FFF7FFFu);
+        return magnitude16<DT>(m);
+    } else {
+        return max(magnitude<8>(e.h[0].v), magnitude<8>(e.h[1].v));
+    }
+}
+// Two adjacent lanes hold a block's 32 values: its scale byte.
+__device__ __forceinline__ uint32_t fp4_pair_scale(uint32_t m) { return fp4_scale_byte(max(m, __shfl_xor_sync(0xffffffffu, m, 1))); }
+
 // Four adjacent lanes hold a block's 32 values: its scale byte, from each lane's largest magnitude (as bits).
 __device__ __forceinline__ uint32_t fp4_block_scale(uint32_t m)
 {
@@ -97,8 +133,47 @@ __device__ __forceinline__ uint32_t fp4_codes(const float (&v)[8], uint32_t b, i
     const float f = fp4_factor(b);
     float t[8];
 #pragma unroll
-    for (int i = 0; i < 8; i++) t[i] = v[i] * f;
+    for (int i = 0; i < 8; i += 2) times2(t[i], t[i + 1], v[i], v[i + 1], f);
     return fp4_eight(t);
+}
+
+// codes of sixteen values, of which the first `n` exist
+template <int DT, bool VEC>
+__device__ __forceinline__ uint2 fp4_codes16(const Sixteen<DT, VEC> &e, uint32_t b, int n)
+{
+    float lo[8], hi[8];
+    values_of(e.h[0], lo);
+    values_of(e.h[1], hi);
+    return make_uint2(fp4_codes(lo, b, n), fp4_codes(hi, b, n - 8));
+}
+
+// values of eight codes times their scale
+__device__ __forceinline__ void fp4_scaled8(uint32_t q, float s, float (&v)[8])
+{
+    fp4_values8(q, v);
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) times2(v[i], v[i + 1], v[i], v[i + 1], s);
+}
+
+// eight FP32 values as four words of 16-bit ones
+template <int DT>
+__device__ __forceinline__ void pack16(const float (&v)[8], uint32_t (&w)[4])
+{
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        if constexpr (DT == VPTQ_DTYPE_FP16) {
+            const __half2 h = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
+            w[i] = *reinterpret_cast<const uint32_t *>(&h);
+        } else {
+            const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+            w[i] = *reinterpret_cast<const uint32_t *>(&h);
+        }
+    }
+}
+// 32 bytes on a boundary of 32
+__device__ __forceinline__ void store32(void *p, const uint32_t (&a)[4], const uint32_t (&b)[4])
+{
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]), "r"(b[2]), "r"(b[3]) : "memory");
 }
 
 // eight values to `out` at column c of a row of `cols` values; VEC: the row starts on 16 bytes and cols is a multiple of a store's values
@@ -112,21 +187,36 @@ __device__ __forceinline__ void store_values8(void *row, int c, int cols, const 
         if (c + 4 < cols) __stcs(p + 1, make_float4(v[4], v[5], v[6], v[7]));
     } else if constexpr (VEC) {
         uint32_t w[4];
-#pragma unroll
-        for (int i = 0; i < 4; i++) {
-            if constexpr (DT == VPTQ_DTYPE_FP16) {
-                const __half2 h = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
-                w[i] = *reinterpret_cast<const uint32_t *>(&h);
-            } else {
-                const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-                w[i] = *reinterpret_cast<const uint32_t *>(&h);
-            }
-        }
+        pack16<DT>(v, w);
         __stcs(reinterpret_cast<uint4 *>(reinterpret_cast<uint16_t *>(row) + c), make_uint4(w[0], w[1], w[2], w[3]));
     } else {
 #pragma unroll
         for (int i = 0; i < 8; i++)
             if (c + i < cols) store_out(row, c + i, v[i], DT);
+    }
+}
+// Sixteen values to `out` at column c of a row of `cols` values.  wide: the row starts on 32 bytes and cols is a multiple of 16.
+template <int DT, bool VEC>
+__device__ __forceinline__ void store_values16(void *row, int c, int cols, bool wide, const float (&lo)[8], const float (&hi)[8])
+{
+    if (VEC && wide) {
+        if constexpr (DT == VPTQ_DTYPE_FP32) {
+#pragma unroll
+            for (int i = 0; i < 2; i++) {
+                uint32_t a[4], b[4];
+#pragma unroll
+                for (int k = 0; k < 4; k++) { a[k] = __float_as_uint(i ? hi[k] : lo[k]); b[k] = __float_as_uint(i ? hi[4 + k] : lo[4 + k]); }
+                store32(reinterpret_cast<float *>(row) + c + 8 * i, a, b);
+            }
+        } else {
+            uint32_t a[4], b[4];
+            pack16<DT>(lo, a);
+            pack16<DT>(hi, b);
+            store32(reinterpret_cast<uint16_t *>(row) + c, a, b);
+        }
+    } else {
+        store_values8<DT, VEC>(row, c, cols, lo);
+        store_values8<DT, VEC>(row, c + 8, cols, hi);
     }
 }
 #endif

@@ -39,10 +39,7 @@ fp4_values_kernel(const __grid_constant__ ValuesParams P)
         const int row = row0 + u * (THREADS / 16);
         if (row >= P.rows) break;
         float v[8];
-        fp4_values8(q[u], v);
-        const float s = fp4_scale_value(b[u]);
-#pragma unroll
-        for (int i = 0; i < 8; i++) v[i] *= s;
+        fp4_scaled8(q[u], fp4_scale_value(b[u]), v);
         store_values8<DT, VEC>(reinterpret_cast<uint8_t *>(P.out) + (long long)row * P.cols * (DT == VPTQ_DTYPE_FP32 ? 4 : 2), c, P.cols, v);
     }
 }

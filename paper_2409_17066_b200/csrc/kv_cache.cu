@@ -1,42 +1,38 @@
 // Keys and values of tokens into the pages of a quantized cache, and out of them.
 //
-// A row (token, keys or values, head) is dealt with in pieces of 128 columns by 16 lanes, eight adjacent columns each (rows of at most 64
-// columns by 8 lanes): a 16-byte load of 16-bit values, 8 (e4m3) or 4 bytes (e2m1) of codes.  Its scale is two shuffles (e2m1) or four
+// A row (token, keys or values, head) is dealt with in pieces of 128 columns by 8 lanes, sixteen adjacent columns each (rows of at most 64
+// columns by 4 lanes): 32 bytes of 16-bit values, 16 (e4m3) or 8 bytes (e2m1) of codes.  Its scale is one shuffle (e2m1) or three
 // (e4m3), by the rules of the matrices (fp8.cuh, fp4.cuh).
-// All pieces of a warp belong to one token, whose place every warp looks up for itself: the token's sequence by a search of 32 places at a
-// time (two rounds for 1024 sequences), then its page.  When writing, the values are on their way to the registers meanwhile.
+// A CTA takes some tokens: a thread looks up the place of each (a binary search for its sequence, then its page) and leaves it in shared
+// memory, and every thread goes through its tokens with one and the same piece of a row, so that what changes from token to token is three
+// addresses.  Up to four tokens' reads are in flight a thread; when writing, the first four before the places are known.
 // Nothing outside the cache is touched whatever the tables say: tokens without a sequence, positions beyond the table and pages that the
 // cache does not have are not written; read, they give zeros (tokens without a sequence: nothing).
-// Bound by HBM where there are many tokens, by the latency of three dependent reads (sequences, start, page) where there are few.
+// Bound by HBM where there are many tokens, by the latency of dependent reads (sequences, start, page, codes) where there are few.
 #include "kv_cache.cuh"
 
 namespace vptq {
 
 namespace {
 
-constexpr int THREADS = 256, WARPS = THREADS / 32;
+constexpr int THREADS = 256;
 
 struct CacheParams {
     KvCache C;
     long long row_bytes, scales;               // of a row in the cache
     int chunks, units;                         // pieces of a row, and of a token (keys and values of all heads)
-    int warps;                                 // warps that share a token
+    int width, groups;                         // pieces of a token that a CTA takes, and tokens that it takes side by side
+    int wide;                                  // rows to be read lie on 32 bytes, in pieces of 32 bytes
 };
 
-// Place of token t: the cache row of head 0, -1 when it has none, -2 when it is in no sequence.  For a whole warp.
+// Place of token t: the cache row of head 0, -1 when it has none, -2 when it is in no sequence.
 __device__ __forceinline__ long long find_row(const KvCache &C, int t)
 {
-    // the last sequence that does not begin behind t (the first entry of a group of `stride` that its lanes look at stands for all)
-    const int lane = threadIdx.x & 31;
-    int lo = 0, n = C.seqs;
-    while (true) {
-        const int stride = (n + 31) / 32, i = lane * stride;
-        const bool before = i < n && __ldg(C.cu + lo + i) <= t;
-        const int count = __popc(__ballot_sync(0xffffffffu, before));
-        if (count == 0) return -2;
-        lo += (count - 1) * stride;
-        if (stride == 1) break;
-        n = min(stride, n - (count - 1) * stride);
+    int lo = 0, n = C.seqs;                    // the last sequence that does not begin behind t is in [lo, lo + n)
+    while (n > 1) {
+        const int half = n / 2;
+        if (__ldg(C.cu + lo + half) <= t) { lo += half; n -= half; }
+        else n = half;
     }
     const int begin = __ldg(C.cu + lo), end = __ldg(C.cu + lo + 1), start = __ldg(C.start + lo);
     if (t < begin || t >= end) return -2;
@@ -48,60 +44,88 @@ __device__ __forceinline__ long long find_row(const KvCache &C, int t)
     return (long long)page * C.heads * C.page + token % C.page;
 }
 
-// Piece `unit` of a token: which of keys and values, which head, which columns.
-struct Piece { int kv, head, c; };
-__device__ __forceinline__ Piece piece_of(const CacheParams &P, int unit, int c0)
+// What a thread works on: keys or values, a head, its first column of sixteen, and the tokens first, first + groups, ... of the CTA's.
+struct Piece { int kv, head, c, first; bool any; };
+template <int LANES>
+__device__ __forceinline__ Piece piece_of(const CacheParams &P)
 {
+    const int slot = threadIdx.x / LANES, group = slot / P.width, unit = blockIdx.y * P.width + slot - group * P.width;
     const int row = unit / P.chunks, kv = row >= P.C.heads ? 1 : 0;
-    return {kv, row - kv * P.C.heads, (unit - row * P.chunks) * FP8_BLOCK + c0};
+    return {kv, row - kv * P.C.heads, (unit - row * P.chunks) * FP8_BLOCK + (int)(threadIdx.x % LANES) * 16, group, group < P.groups && unit < P.units};
 }
 
-template <int DT, bool VEC, bool E2M1, int LANES, int ROUNDS>
+constexpr int BATCH = 4;                       // tokens of a thread whose reads are in flight together
+
+// e4m3 codes of sixteen values, of which the first `n` exist (the others are zeros, whatever the factor)
+template <int DT, bool VEC>
+__device__ __forceinline__ uint4 e4m3_codes16(const Sixteen<DT, VEC> &e, float f, int n)
+{
+    uint32_t w[4];
+#pragma unroll
+    for (int h = 0; h < 2; h++) {
+        float v[8], t[8];
+        values_of(e.h[h], v);
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) times2(t[i], t[i + 1], v[i], v[i + 1], f);
+        w[2 * h] = fp8_quad(t[0], t[1], t[2], t[3]);
+        w[2 * h + 1] = fp8_quad(t[4], t[5], t[6], t[7]);
+    }
+    if (n < 16)
+#pragma unroll
+        for (int i = 0; i < 4; i++) w[i] = n >= 4 * i + 4 ? w[i] : n <= 4 * i ? 0u : w[i] & ((1u << (8 * (n - 4 * i))) - 1u);
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// N tokens a thread
+template <int DT, bool VEC, bool E2M1, int LANES, int N>
 __global__ void __launch_bounds__(THREADS)
 cache_write_kernel(const __grid_constant__ CacheParams P)
 {
-    constexpr int PER_WARP = 32 / LANES;
+    constexpr int TOGETHER = N < BATCH ? N : BATCH;
+    __shared__ long long place[THREADS];
     const KvCache &C = P.C;
     pdl_wait();
-    const long long w = (long long)blockIdx.x * WARPS + (threadIdx.x >> 5);
-    const int t = (int)(w / P.warps), lane = threadIdx.x & (LANES - 1);
-    if (t >= C.tokens) return;
-    const int unit0 = (int)(w % P.warps) * ROUNDS * PER_WARP + (int)(threadIdx.x & 31) / LANES;
-    Eight<DT, VEC> e[ROUNDS];
+    const int tokens = N * P.groups, t0 = (int)blockIdx.x * tokens, lane = threadIdx.x % LANES;
+    const Piece p = piece_of<LANES>(P);
+    const long long step = P.groups * C.token_stride[p.kv] * Act<DT>::BYTES;
+    const uint8_t *x = reinterpret_cast<const uint8_t *>(C.x[p.kv]) + ((t0 + p.first) * C.token_stride[p.kv] + p.head * C.head_stride[p.kv]) * Act<DT>::BYTES;
+    uint8_t *q = C.q[p.kv] + (E2M1 ? p.c / 2 : p.c), *scale = reinterpret_cast<uint8_t *>(C.scale[p.kv]);
+    const long long head_rows = (long long)p.head * C.page;
+#pragma unroll 1
+    for (int k = 0; k < N; k += TOGETHER) {
+        Sixteen<DT, VEC> e[TOGETHER];
 #pragma unroll
-    for (int i = 0; i < ROUNDS; i++) {
-        const int unit = unit0 + i * PER_WARP;
-        const Piece p = piece_of(P, unit < P.units ? unit : 0, lane * 8);
-        const long long at = t * C.token_stride[p.kv] + p.head * C.head_stride[p.kv];
-        e[i] = load_eight<DT, VEC>(reinterpret_cast<const uint8_t *>(C.x[p.kv]) + at * Act<DT>::BYTES, unit < P.units ? p.c : C.dim, C.dim);
-    }
-    const long long row0 = find_row(C, t);
-    if (row0 < 0) return;
+        for (int i = 0; i < TOGETHER; i++) {
+            const int t = p.first + (k + i) * P.groups;
+            e[i] = load_sixteen<DT, VEC>(x, p.any && t0 + t < C.tokens ? p.c : C.dim, C.dim);
+            x += step;
+        }
+        if (k == 0) {
+            if (threadIdx.x < tokens) place[threadIdx.x] = t0 + (int)threadIdx.x < C.tokens ? find_row(C, t0 + threadIdx.x) : -2;
+            __syncthreads();
+        }
 #pragma unroll
-    for (int i = 0; i < ROUNDS; i++) {
-        const int unit = unit0 + i * PER_WARP;
-        const Piece p = piece_of(P, unit < P.units ? unit : 0, lane * 8);
-        const long long row = row0 + (long long)p.head * C.page;
-        uint32_t m = magnitude(e[i]);
-        if constexpr (E2M1) {
-            const uint32_t b = fp4_block_scale(m);
-            if (unit >= P.units || p.c / 2 >= P.row_bytes) continue;
-            float v[8];
-            values_of(e[i], v);
-            *reinterpret_cast<uint32_t *>(C.q[p.kv] + row * P.row_bytes + p.c / 2) = fp4_codes(v, b, C.dim - p.c);
-            if ((lane & 3) == 0) reinterpret_cast<uint8_t *>(C.scale[p.kv])[row * P.scales + p.c / FP4_BLOCK] = (uint8_t)b;
-        } else {
+        for (int i = 0; i < TOGETHER; i++) {
+            uint32_t m = magnitude(e[i]);
+            const long long at = p.any ? place[p.first + (k + i) * P.groups] : -1, row = at + head_rows;
+            if constexpr (E2M1) {
+                const uint32_t b = fp4_pair_scale(m);
+                if (at < 0 || p.c / 2 >= P.row_bytes) continue;
+                *reinterpret_cast<uint2 *>(q + row * P.row_bytes) = fp4_codes16(e[i], b, C.dim - p.c);
+                if ((lane & 1) == 0) scale[row * P.scales + p.c / FP4_BLOCK] = (uint8_t)b;
+            } else {
 #pragma unroll
-            for (int o = LANES / 2; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
-            if (unit >= P.units) continue;
-            const Fp8Scale s = fp8_scale(__uint_as_float(m));
-            store_eight(C.q[p.kv] + row * P.row_bytes, P.row_bytes, p.c, C.dim, e[i], s.factor);
-            if (lane == 0) reinterpret_cast<float *>(C.scale[p.kv])[row * P.scales + p.c / FP8_BLOCK] = s.scale;
+                for (int o = LANES / 2; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+                if (at < 0) continue;
+                const Fp8Scale s = fp8_scale(__uint_as_float(m));
+                if (p.c < P.row_bytes) *reinterpret_cast<uint4 *>(q + row * P.row_bytes) = e4m3_codes16(e[i], s.factor, C.dim - p.c);
+                if (lane == 0) reinterpret_cast<float *>(scale)[row * P.scales + p.c / FP8_BLOCK] = s.scale;
+            }
         }
     }
 }
 
-__device__ __forceinline__ void e4m3_values8(uint2 q, float (&v)[8])
+__device__ __forceinline__ void e4m3_scaled8(uint2 q, float s, float (&v)[8])
 {
     uint32_t h[4];
     asm("{\n\t.reg .b16 a, b, c, d;\n\tmov.b32 {a, b}, %4;\n\tmov.b32 {c, d}, %5;\n\t"
@@ -110,80 +134,100 @@ __device__ __forceinline__ void e4m3_values8(uint2 q, float (&v)[8])
 #pragma unroll
     for (int i = 0; i < 4; i++) {
         const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&h[i]));
-        v[2 * i] = f.x; v[2 * i + 1] = f.y;
+        times2(v[2 * i], v[2 * i + 1], f.x, f.y, s);
     }
 }
 
-template <int DT, bool VEC, bool E2M1, int LANES, int ROUNDS>
+template <int DT, bool VEC, bool E2M1, int LANES, int N>
 __global__ void __launch_bounds__(THREADS)
 cache_read_kernel(const __grid_constant__ CacheParams P)
 {
-    constexpr int PER_WARP = 32 / LANES;
+    constexpr int TOGETHER = N < BATCH ? N : BATCH, BYTES = DT == VPTQ_DTYPE_FP32 ? 4 : 2;
+    __shared__ long long place[THREADS];
     const KvCache &C = P.C;
     pdl_wait();
-    const long long w = (long long)blockIdx.x * WARPS + (threadIdx.x >> 5);
-    const int t = (int)(w / P.warps), lane = threadIdx.x & (LANES - 1);
-    if (t >= C.tokens) return;
-    const int unit0 = (int)(w % P.warps) * ROUNDS * PER_WARP + (int)(threadIdx.x & 31) / LANES;
-    const long long row0 = find_row(C, t);
-    if (row0 == -2) return;
-    uint2 q[ROUNDS];
-    float s[ROUNDS];
+    const int tokens = N * P.groups, t0 = (int)blockIdx.x * tokens;
+    if (threadIdx.x < tokens) place[threadIdx.x] = t0 + (int)threadIdx.x < C.tokens ? find_row(C, t0 + threadIdx.x) : -2;
+    const Piece p = piece_of<LANES>(P);
+    const long long step = P.groups * C.token_stride[p.kv] * BYTES;
+    uint8_t *x = reinterpret_cast<uint8_t *>(C.x[p.kv]) + ((t0 + p.first) * C.token_stride[p.kv] + p.head * C.head_stride[p.kv]) * BYTES;
+    const long long head_rows = (long long)p.head * C.page;
+    const uint8_t *q = C.q[p.kv] + head_rows * P.row_bytes + (E2M1 ? p.c / 2 : p.c);
+    const uint8_t *scale = reinterpret_cast<const uint8_t *>(C.scale[p.kv]) + (head_rows * P.scales + p.c / (E2M1 ? FP4_BLOCK : FP8_BLOCK)) * (E2M1 ? 1 : 4);
+    __syncthreads();
+    if (!p.any || p.c >= C.dim) return;
+#pragma unroll 1
+    for (int k = 0; k < N; k += TOGETHER) {
+        uint4 codes[TOGETHER];
+        float s[TOGETHER];
+        bool in[TOGETHER];
 #pragma unroll
-    for (int i = 0; i < ROUNDS; i++) {
-        const int unit = unit0 + i * PER_WARP;
-        q[i] = make_uint2(0, 0);
-        s[i] = 0.f;
-        if (row0 < 0 || unit >= P.units) continue;
-        const Piece p = piece_of(P, unit, lane * 8);
-        if (p.c >= C.dim) continue;
-        const long long row = row0 + (long long)p.head * C.page;
-        if constexpr (E2M1) {
-            q[i].x = __ldcs(reinterpret_cast<const uint32_t *>(C.q[p.kv] + row * P.row_bytes + p.c / 2));
-            s[i] = fp4_scale_value(__ldg(reinterpret_cast<const uint8_t *>(C.scale[p.kv]) + row * P.scales + p.c / FP4_BLOCK));
-        } else {
-            q[i] = __ldcs(reinterpret_cast<const uint2 *>(C.q[p.kv] + row * P.row_bytes + p.c));
-            s[i] = __ldg(reinterpret_cast<const float *>(C.scale[p.kv]) + row * P.scales + p.c / FP8_BLOCK);
+        for (int i = 0; i < TOGETHER; i++) {
+            const long long row = place[p.first + (k + i) * P.groups];
+            in[i] = row != -2;
+            codes[i] = make_uint4(0, 0, 0, 0);
+            s[i] = 0.f;
+            if (row < 0) continue;
+            if constexpr (E2M1) {
+                const uint2 w = __ldcs(reinterpret_cast<const uint2 *>(q + row * P.row_bytes));
+                codes[i].x = w.x; codes[i].y = w.y;
+                s[i] = fp4_scale_value(__ldg(scale + row * P.scales));
+            } else {
+                codes[i] = __ldcs(reinterpret_cast<const uint4 *>(q + row * P.row_bytes));
+                s[i] = __ldg(reinterpret_cast<const float *>(scale) + row * P.scales);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < TOGETHER; i++) {
+            float lo[8], hi[8];
+            if constexpr (E2M1) {
+                fp4_scaled8(codes[i].x, s[i], lo);
+                fp4_scaled8(codes[i].y, s[i], hi);
+            } else {
+                e4m3_scaled8(make_uint2(codes[i].x, codes[i].y), s[i], lo);
+                e4m3_scaled8(make_uint2(codes[i].z, codes[i].w), s[i], hi);
+            }
+            if (in[i]) store_values16<DT, VEC>(x, p.c, C.dim, P.wide, lo, hi);
+            x += step;
         }
     }
-#pragma unroll
-    for (int i = 0; i < ROUNDS; i++) {
-        const int unit = unit0 + i * PER_WARP;
-        if (unit >= P.units) break;
-        const Piece p = piece_of(P, unit, lane * 8);
-        float v[8];
-        if constexpr (E2M1) fp4_values8(q[i].x, v);
-        else e4m3_values8(q[i], v);
-#pragma unroll
-        for (int k = 0; k < 8; k++) v[k] *= s[i];
-        const long long at = t * C.token_stride[p.kv] + p.head * C.head_stride[p.kv];
-        store_values8<DT, VEC>(reinterpret_cast<uint8_t *>(C.x[p.kv]) + at * (DT == VPTQ_DTYPE_FP32 ? 4 : 2), p.c, C.dim, v);
-    }
 }
 
-template <int DT, bool VEC, bool E2M1, int LANES, int ROUNDS>
-cudaError_t launch(CacheParams P, bool write, cudaStream_t st)
+template <int DT, bool VEC, bool E2M1, int LANES, int N>
+cudaError_t launch(const CacheParams &P, int parts, bool write, cudaStream_t st)
 {
-    P.warps = ceil_div(P.units, 32 / LANES * ROUNDS);
-    const long long ctas = ((long long)P.C.tokens * P.warps + WARPS - 1) / WARPS;
-    if (write) return launch_dependent("cache_write", cache_write_kernel<DT, VEC, E2M1, LANES, ROUNDS>, (int)ctas, THREADS, 0, st, P);
-    return launch_dependent("cache_read", cache_read_kernel<DT, VEC, E2M1, LANES, ROUNDS>, (int)ctas, THREADS, 0, st, P);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)ceil_div(P.C.tokens, N * P.groups), (unsigned)parts);
+    cfg.blockDim = dim3(THREADS);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = pdl_enabled("kv_cache") ? 1 : 0;
+    return write ? cudaLaunchKernelEx(&cfg, cache_write_kernel<DT, VEC, E2M1, LANES, N>, P) : cudaLaunchKernelEx(&cfg, cache_read_kernel<DT, VEC, E2M1, LANES, N>, P);
 }
 
-// few pieces: one to 8 or 16 lanes; more than fill the device twice over: four, so that the search for the token's place serves as many
+// Pieces of a token are dealt out evenly to CTAs of THREADS / LANES slots; what is left of the slots takes more tokens.  A thread takes one token
+// while that fills the device no more than once, then four, then eight.
 template <int DT, bool VEC, bool E2M1, int LANES>
-cudaError_t launch_rounds(const CacheParams &P, bool write, cudaStream_t st)
+cudaError_t launch_tokens(CacheParams P, bool write, cudaStream_t st)
 {
-    const long long warps = (long long)P.C.tokens * ceil_div(P.units, 32 / LANES);
-    if (warps <= (long long)device_sm_count() * 128) return launch<DT, VEC, E2M1, LANES, 1>(P, write, st);
-    return launch<DT, VEC, E2M1, LANES, 4>(P, write, st);
+    constexpr int SLOTS = THREADS / LANES;
+    const int parts = ceil_div(P.units, SLOTS);
+    P.width = ceil_div(P.units, parts);
+    P.groups = SLOTS / P.width;
+    const long long ctas = (long long)ceil_div(P.C.tokens, P.groups) * parts, resident = (long long)device_sm_count() * 8;
+    if (ctas <= resident) return launch<DT, VEC, E2M1, LANES, 1>(P, parts, write, st);
+    if (ctas <= 8 * resident) return launch<DT, VEC, E2M1, LANES, 4>(P, parts, write, st);
+    return launch<DT, VEC, E2M1, LANES, 8>(P, parts, write, st);
 }
 
 template <int DT, bool VEC>
 cudaError_t launch_form(const CacheParams &P, bool write, cudaStream_t st)
 {
-    if (P.C.e2m1) return P.C.dim <= 64 ? launch_rounds<DT, VEC, true, 8>(P, write, st) : launch_rounds<DT, VEC, true, 16>(P, write, st);
-    return P.C.dim <= 64 ? launch_rounds<DT, VEC, false, 8>(P, write, st) : launch_rounds<DT, VEC, false, 16>(P, write, st);
+    if (P.C.e2m1) return P.C.dim <= 64 ? launch_tokens<DT, VEC, true, 4>(P, write, st) : launch_tokens<DT, VEC, true, 8>(P, write, st);
+    return P.C.dim <= 64 ? launch_tokens<DT, VEC, false, 4>(P, write, st) : launch_tokens<DT, VEC, false, 8>(P, write, st);
 }
 
 cudaError_t launch_cache(const KvCache &C, bool write, cudaStream_t st)
@@ -194,9 +238,10 @@ cudaError_t launch_cache(const KvCache &C, bool write, cudaStream_t st)
     P.scales = ceil_div(C.dim, C.e2m1 ? FP4_BLOCK : FP8_BLOCK);
     P.chunks = ceil_div(C.dim, FP8_BLOCK);
     P.units = 2 * C.heads * P.chunks;
-    P.warps = 0;
+    P.width = P.groups = 0;
     const int bytes = C.x_dtype == VPTQ_DTYPE_FP32 ? 4 : 2, per = 16 / bytes;
     bool vec = C.dim % per == 0;
+    P.wide = C.dim % 16 == 0 && ((reinterpret_cast<uintptr_t>(C.x[0]) | reinterpret_cast<uintptr_t>(C.x[1])) & 31u) == 0;      // (read: packed)
     for (int i = 0; i < 2; i++)
         vec = vec && (reinterpret_cast<uintptr_t>(C.x[i]) & 15u) == 0 && (C.tokens == 1 || C.token_stride[i] % per == 0) && (C.heads == 1 || C.head_stride[i] % per == 0);
     switch (C.x_dtype) {

@@ -800,7 +800,7 @@ int64_t vptq_cache_row_scales(int32_t head_dim, int32_t cache_dtype)
 static int make_cache(const vptq_cache_desc *d, const vptq_cache_ptrs *p, const void *k, const void *v, int32_t n_tokens, KvCache *C)
 {
     if (d == nullptr) return VPTQ_E_NULL;
-    if (d->n_heads <= 0 || d->n_heads > 65536 || d->head_dim <= 0 || d->head_dim > VPTQ_CACHE_MAX_DIM || d->page_size <= 0 || d->page_size > FP8_MAX_SIZE ||
+    if (d->n_heads <= 0 || d->n_heads > 4096 || d->head_dim <= 0 || d->head_dim > VPTQ_CACHE_MAX_DIM || d->page_size <= 0 || d->page_size > FP8_MAX_SIZE ||
         d->n_pages <= 0 || d->n_pages > FP8_MAX_SIZE || d->n_seqs < 0 || d->n_seqs > FP8_MAX_SIZE || d->table_width < 0 || d->table_width > FP8_MAX_SIZE ||
         n_tokens < 0 || n_tokens > FP8_MAX_SIZE)
         return VPTQ_E_SHAPE;
