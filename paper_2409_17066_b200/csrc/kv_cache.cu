@@ -19,15 +19,19 @@ constexpr int THREADS = 256;
 
 struct CacheParams {
     KvCache C;
-    long long row_bytes, scales;               // of a row in the cache
+    int row_bytes, scale_bytes;                // of a row in the cache
     int chunks, units;                         // pieces of a row, and of a token (keys and values of all heads)
     int width, groups;                         // pieces of a token that a CTA takes, and tokens that it takes side by side
     int wide;                                  // rows to be read lie on 32 bytes, in pieces of 32 bytes
 };
 
-// Place of token t: the cache row of head 0, -1 when it has none, -2 when it is in no sequence.
-__device__ __forceinline__ long long find_row(const KvCache &C, int t)
+// Where a token's rows of head 0 begin, in bytes of codes and in bytes of scales; negative: GONE, it has no page, or NONE, it is in no sequence.
+constexpr long long GONE = -1, NONE = -2;
+struct __align__(16) Place { long long codes, scales; };
+
+__device__ __forceinline__ Place find_place(const CacheParams &P, int t)
 {
+    const KvCache &C = P.C;
     int lo = 0, n = C.seqs;                    // the last sequence that does not begin behind t is in [lo, lo + n)
     while (n > 1) {
         const int half = n / 2;
@@ -35,13 +39,14 @@ __device__ __forceinline__ long long find_row(const KvCache &C, int t)
         else n = half;
     }
     const int begin = __ldg(C.cu + lo), end = __ldg(C.cu + lo + 1), start = __ldg(C.start + lo);
-    if (t < begin || t >= end) return -2;
-    const long long token = (long long)start + (t - begin);
-    const long long slot = token / C.page;
-    if (token < 0 || slot >= C.width) return -1;
+    if (t < begin || t >= end) return {NONE, NONE};
+    const long long token = (long long)start + (t - begin);        // (less than 2^32)
+    const uint32_t slot = (uint32_t)token / (uint32_t)C.page;
+    if (token < 0 || slot >= (uint32_t)C.width) return {GONE, GONE};
     const int page = __ldg(C.table + (long long)lo * C.width + slot);
-    if ((unsigned)page >= (unsigned)C.pages) return -1;
-    return (long long)page * C.heads * C.page + token % C.page;
+    if ((unsigned)page >= (unsigned)C.pages) return {GONE, GONE};
+    const long long row = (long long)page * C.heads * C.page + ((uint32_t)token - slot * (uint32_t)C.page);
+    return {row * P.row_bytes, row * P.scale_bytes};
 }
 
 // What a thread works on: keys or values, a head, its first column of sixteen, and the tokens first, first + groups, ... of the CTA's.
@@ -76,21 +81,30 @@ __device__ __forceinline__ uint4 e4m3_codes16(const Sixteen<DT, VEC> &e, float f
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
+// the places of a CTA's tokens, the first of them t0
+__device__ __forceinline__ void find_places(const CacheParams &P, int t0, int tokens, Place *place)
+{
+    for (int i = threadIdx.x; i < tokens; i += THREADS) place[i] = t0 + i < P.C.tokens ? find_place(P, t0 + i) : Place{NONE, NONE};
+    __syncthreads();
+}
+
 // N tokens a thread
 template <int DT, bool VEC, bool E2M1, int LANES, int N>
 __global__ void __launch_bounds__(THREADS)
 cache_write_kernel(const __grid_constant__ CacheParams P)
 {
     constexpr int TOGETHER = N < BATCH ? N : BATCH;
-    __shared__ long long place[THREADS];
+    __shared__ Place place[THREADS / LANES / 2 * N];
     const KvCache &C = P.C;
     pdl_wait();
     const int tokens = N * P.groups, t0 = (int)blockIdx.x * tokens, lane = threadIdx.x % LANES;
     const Piece p = piece_of<LANES>(P);
     const long long step = P.groups * C.token_stride[p.kv] * Act<DT>::BYTES;
     const uint8_t *x = reinterpret_cast<const uint8_t *>(C.x[p.kv]) + ((t0 + p.first) * C.token_stride[p.kv] + p.head * C.head_stride[p.kv]) * Act<DT>::BYTES;
-    uint8_t *q = C.q[p.kv] + (E2M1 ? p.c / 2 : p.c), *scale = reinterpret_cast<uint8_t *>(C.scale[p.kv]);
     const long long head_rows = (long long)p.head * C.page;
+    uint8_t *q = C.q[p.kv] + head_rows * P.row_bytes + (E2M1 ? p.c / 2 : p.c);
+    uint8_t *scale = reinterpret_cast<uint8_t *>(C.scale[p.kv]) + head_rows * P.scale_bytes + (E2M1 ? p.c / FP4_BLOCK : p.c / FP8_BLOCK * 4);
+    const bool in_row = (E2M1 ? p.c / 2 : p.c) < P.row_bytes;
 #pragma unroll 1
     for (int k = 0; k < N; k += TOGETHER) {
         Sixteen<DT, VEC> e[TOGETHER];
@@ -100,26 +114,23 @@ cache_write_kernel(const __grid_constant__ CacheParams P)
             e[i] = load_sixteen<DT, VEC>(x, p.any && t0 + t < C.tokens ? p.c : C.dim, C.dim);
             x += step;
         }
-        if (k == 0) {
-            if (threadIdx.x < tokens) place[threadIdx.x] = t0 + (int)threadIdx.x < C.tokens ? find_row(C, t0 + threadIdx.x) : -2;
-            __syncthreads();
-        }
+        if (k == 0) find_places(P, t0, tokens, place);
 #pragma unroll
         for (int i = 0; i < TOGETHER; i++) {
             uint32_t m = magnitude(e[i]);
-            const long long at = p.any ? place[p.first + (k + i) * P.groups] : -1, row = at + head_rows;
+            const Place at = p.any ? place[p.first + (k + i) * P.groups] : Place{NONE, NONE};
             if constexpr (E2M1) {
                 const uint32_t b = fp4_pair_scale(m);
-                if (at < 0 || p.c / 2 >= P.row_bytes) continue;
-                *reinterpret_cast<uint2 *>(q + row * P.row_bytes) = fp4_codes16(e[i], b, C.dim - p.c);
-                if ((lane & 1) == 0) scale[row * P.scales + p.c / FP4_BLOCK] = (uint8_t)b;
+                if (at.codes < 0 || !in_row) continue;
+                *reinterpret_cast<uint2 *>(q + at.codes) = fp4_codes16(e[i], b, C.dim - p.c);
+                if ((lane & 1) == 0) scale[at.scales] = (uint8_t)b;
             } else {
 #pragma unroll
                 for (int o = LANES / 2; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
-                if (at < 0) continue;
+                if (at.codes < 0) continue;
                 const Fp8Scale s = fp8_scale(__uint_as_float(m));
-                if (p.c < P.row_bytes) *reinterpret_cast<uint4 *>(q + row * P.row_bytes) = e4m3_codes16(e[i], s.factor, C.dim - p.c);
-                if (lane == 0) reinterpret_cast<float *>(scale)[row * P.scales + p.c / FP8_BLOCK] = s.scale;
+                if (in_row) *reinterpret_cast<uint4 *>(q + at.codes) = e4m3_codes16(e[i], s.factor, C.dim - p.c);
+                if (lane == 0) *reinterpret_cast<float *>(scale + at.scales) = s.scale;
             }
         }
     }
@@ -143,18 +154,17 @@ __global__ void __launch_bounds__(THREADS)
 cache_read_kernel(const __grid_constant__ CacheParams P)
 {
     constexpr int TOGETHER = N < BATCH ? N : BATCH, BYTES = DT == VPTQ_DTYPE_FP32 ? 4 : 2;
-    __shared__ long long place[THREADS];
+    __shared__ Place place[THREADS / LANES / 2 * N];
     const KvCache &C = P.C;
     pdl_wait();
     const int tokens = N * P.groups, t0 = (int)blockIdx.x * tokens;
-    if (threadIdx.x < tokens) place[threadIdx.x] = t0 + (int)threadIdx.x < C.tokens ? find_row(C, t0 + threadIdx.x) : -2;
     const Piece p = piece_of<LANES>(P);
     const long long step = P.groups * C.token_stride[p.kv] * BYTES;
     uint8_t *x = reinterpret_cast<uint8_t *>(C.x[p.kv]) + ((t0 + p.first) * C.token_stride[p.kv] + p.head * C.head_stride[p.kv]) * BYTES;
     const long long head_rows = (long long)p.head * C.page;
     const uint8_t *q = C.q[p.kv] + head_rows * P.row_bytes + (E2M1 ? p.c / 2 : p.c);
-    const uint8_t *scale = reinterpret_cast<const uint8_t *>(C.scale[p.kv]) + (head_rows * P.scales + p.c / (E2M1 ? FP4_BLOCK : FP8_BLOCK)) * (E2M1 ? 1 : 4);
-    __syncthreads();
+    const uint8_t *scale = reinterpret_cast<const uint8_t *>(C.scale[p.kv]) + head_rows * P.scale_bytes + (E2M1 ? p.c / FP4_BLOCK : p.c / FP8_BLOCK * 4);
+    find_places(P, t0, tokens, place);
     if (!p.any || p.c >= C.dim) return;
 #pragma unroll 1
     for (int k = 0; k < N; k += TOGETHER) {
@@ -163,18 +173,18 @@ cache_read_kernel(const __grid_constant__ CacheParams P)
         bool in[TOGETHER];
 #pragma unroll
         for (int i = 0; i < TOGETHER; i++) {
-            const long long row = place[p.first + (k + i) * P.groups];
-            in[i] = row != -2;
+            const Place at = place[p.first + (k + i) * P.groups];
+            in[i] = at.codes != NONE;
             codes[i] = make_uint4(0, 0, 0, 0);
             s[i] = 0.f;
-            if (row < 0) continue;
+            if (at.codes < 0) continue;
             if constexpr (E2M1) {
-                const uint2 w = __ldcs(reinterpret_cast<const uint2 *>(q + row * P.row_bytes));
+                const uint2 w = __ldcs(reinterpret_cast<const uint2 *>(q + at.codes));
                 codes[i].x = w.x; codes[i].y = w.y;
-                s[i] = fp4_scale_value(__ldg(scale + row * P.scales));
+                s[i] = fp4_scale_value(__ldg(scale + at.scales));
             } else {
-                codes[i] = __ldcs(reinterpret_cast<const uint4 *>(q + row * P.row_bytes));
-                s[i] = __ldg(reinterpret_cast<const float *>(scale) + row * P.scales);
+                codes[i] = __ldcs(reinterpret_cast<const uint4 *>(q + at.codes));
+                s[i] = __ldg(reinterpret_cast<const float *>(scale + at.scales));
             }
         }
 #pragma unroll
@@ -209,7 +219,7 @@ cudaError_t launch(const CacheParams &P, int parts, bool write, cudaStream_t st)
 }
 
 // Pieces of a token are dealt out evenly to CTAs of THREADS / LANES slots; what is left of the slots takes more tokens.  A thread takes one token
-// while that fills the device no more than once, then four, then eight.
+// while that fills the device no more than once, then four, then sixteen.
 template <int DT, bool VEC, bool E2M1, int LANES>
 cudaError_t launch_tokens(CacheParams P, bool write, cudaStream_t st)
 {
@@ -220,7 +230,7 @@ cudaError_t launch_tokens(CacheParams P, bool write, cudaStream_t st)
     const long long ctas = (long long)ceil_div(P.C.tokens, P.groups) * parts, resident = (long long)device_sm_count() * 8;
     if (ctas <= resident) return launch<DT, VEC, E2M1, LANES, 1>(P, parts, write, st);
     if (ctas <= 8 * resident) return launch<DT, VEC, E2M1, LANES, 4>(P, parts, write, st);
-    return launch<DT, VEC, E2M1, LANES, 8>(P, parts, write, st);
+    return launch<DT, VEC, E2M1, LANES, 16>(P, parts, write, st);
 }
 
 template <int DT, bool VEC>
@@ -234,8 +244,8 @@ cudaError_t launch_cache(const KvCache &C, bool write, cudaStream_t st)
 {
     CacheParams P;
     P.C = C;
-    P.row_bytes = C.e2m1 ? fp4_row_bytes(C.dim) : fp8_row_bytes(C.dim);
-    P.scales = ceil_div(C.dim, C.e2m1 ? FP4_BLOCK : FP8_BLOCK);
+    P.row_bytes = (int)(C.e2m1 ? fp4_row_bytes(C.dim) : fp8_row_bytes(C.dim));
+    P.scale_bytes = C.e2m1 ? ceil_div(C.dim, FP4_BLOCK) : 4 * ceil_div(C.dim, FP8_BLOCK);
     P.chunks = ceil_div(C.dim, FP8_BLOCK);
     P.units = 2 * C.heads * P.chunks;
     P.width = P.groups = 0;
