@@ -552,6 +552,8 @@ int vptq_dequant_fp4(const vptq_layer_desc *desc, const vptq_layer_ptrs *p, uint
  *   every pointer is 16-byte aligned (VPTQ_E_ALIGN), but for x of 16 bits: any alignment of a value;  out_dtype FP16, BF16 or FP32
  *   flags: VPTQ_FLAG_CONCURRENT and VPTQ_FLAG_DETERMINISTIC are accepted and change nothing (no CTA waits for another launch's, every
  *           sum has a fixed order).
+ * At most 16 tokens take the kernel "fp4_few", which quantizes them itself, unless they have more columns than an SM has room for beside
+ * the weight's (on 148 SMs up to 15872 columns are always taken); all others take "fp4_tcgen05" (vptq_linear_fp4_path).
  * The workspace, 256-byte aligned, starts with a status word (vptq_workspace_status); its contents on entry are irrelevant, calls that may
  * overlap must not share one.  All device-side waits are bounded: one that gives up leaves NaN in the results that it concerns and
  * VPTQ_E_TIMEOUT in the status word. */
@@ -607,8 +609,8 @@ int vptq_cache_read(const vptq_cache_desc *desc, const vptq_cache_ptrs *p, void 
 
 const char *vptq_status_string(int code);
 const char *vptq_last_cuda_error(void);
-/* Five kernels — the batched tensor-core kernel and the one over prepared images, behind vptq_linear and
- * vptq_linear_fused, "assign_tcgen05" behind vptq_assign, "fp8_tcgen05" behind vptq_linear_fp8 and "fp4_tcgen05" behind vptq_linear_fp4 — keep an int32 status word at
+/* Six kernels — the batched tensor-core kernel and the one over prepared images, behind vptq_linear and
+ * vptq_linear_fused, "assign_tcgen05" behind vptq_assign, "fp8_tcgen05" behind vptq_linear_fp8 — and the two behind vptq_linear_fp4 keep an int32 status word at
  * byte 0 of their workspace; vptq_linear_has_status() and vptq_linear_fused_has_status() tell for which calls of the first two.  After any other call the workspace holds
  * no status and this call has no meaning.  It synchronises `stream`, reads the word and returns VPTQ_E_TIMEOUT if a
  * bounded device-side wait gave up during the call (the output is then invalid; the context stays

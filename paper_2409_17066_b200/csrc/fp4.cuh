@@ -32,9 +32,9 @@ struct Fp4Linear {
     const uint8_t *w, *w_scale;
     void *out;
 };
-long long linear_fp4_workspace_bytes(int N, int B, int x_dtype);
-int linear_fp4_launches(int B, int x_dtype);
-const char *linear_fp4_path(int B);
+long long linear_fp4_workspace_bytes(int M, int N, int B, int x_dtype);
+int linear_fp4_launches(int M, int N, int B, int x_dtype);
+const char *linear_fp4_path(int M, int N, int B);
 cudaError_t launch_linear_fp4(const Fp4Linear &P, void *ws, cudaStream_t st);
 
 #ifdef __CUDACC__

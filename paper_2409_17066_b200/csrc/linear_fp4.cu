@@ -6,12 +6,15 @@ namespace vptq {
 
 namespace {
 
-// workspace of the tensor-core kernel: the status word, then the activations' scales and e2m1 codes
+// 16-bit activations are quantized by a kernel of their own; that for few tokens does it itself
+bool quantizes_before(int M, int N, int B, int x_dtype) { return x_dtype != VPTQ_DTYPE_E2M1 && !linear_fp4_few_takes(M, N, B); }
+
+// workspace: the status word, then the activations' scales and e2m1 codes
 struct Workspace { long long scales, values, bytes; };
-Workspace workspace_of(int N, int B, int x_dtype)
+Workspace workspace_of(int M, int N, int B, int x_dtype)
 {
     Workspace w = {256, 256, 256};
-    if (x_dtype != VPTQ_DTYPE_E2M1) {
+    if (quantizes_before(M, N, B, x_dtype)) {
         w.values = w.scales + (fp4_scale_bytes(B, N) + 255) / 256 * 256;
         w.bytes = w.values + B * fp4_row_bytes(N);
     }
@@ -20,16 +23,17 @@ Workspace workspace_of(int N, int B, int x_dtype)
 
 }  // namespace
 
-long long linear_fp4_workspace_bytes(int N, int B, int x_dtype) { return workspace_of(N, B, x_dtype).bytes; }
-int linear_fp4_launches(int, int x_dtype) { return x_dtype != VPTQ_DTYPE_E2M1 ? 2 : 1; }
-const char *linear_fp4_path(int) { return "fp4_tcgen05"; }
+long long linear_fp4_workspace_bytes(int M, int N, int B, int x_dtype) { return workspace_of(M, N, B, x_dtype).bytes; }
+int linear_fp4_launches(int M, int N, int B, int x_dtype) { return quantizes_before(M, N, B, x_dtype) ? 2 : 1; }
+const char *linear_fp4_path(int M, int N, int B) { return linear_fp4_few_takes(M, N, B) ? "fp4_few" : "fp4_tcgen05"; }
 
 cudaError_t launch_linear_fp4(const Fp4Linear &P, void *ws, cudaStream_t st)
 {
+    if (linear_fp4_few_takes(P.M, P.N, P.B)) return launch_linear_fp4_few(P, reinterpret_cast<int *>(ws), st);
     uint8_t *w8 = reinterpret_cast<uint8_t *>(ws);
     Fp4Linear Q = P;
     if (P.x_dtype != VPTQ_DTYPE_E2M1) {
-        const Workspace w = workspace_of(P.N, P.B, P.x_dtype);
+        const Workspace w = workspace_of(P.M, P.N, P.B, P.x_dtype);
         const cudaError_t e = launch_fp4_quantize(P.x, P.x_dtype, P.B, P.N, P.N, w8 + w.values, w8 + w.scales, true, st);
         if (e != cudaSuccess) return e;
         Q.x = w8 + w.values;

@@ -208,6 +208,27 @@ def test_linear_of_many_shapes(b, M, N, B):
     assert same(y, b.vptq_linear_fp4(q, w, ws, x_scale=s, out_dtype="fp32"))            # bit for bit the same every time
 
 
+# (few tokens: a cluster's CTAs share the columns or not, one pass over the features or several, features that begin and end inside a tile of scales,
+# results whose rows are not aligned, and so many columns that the other kernel is taken)
+@pytest.mark.parametrize("B", [1, 2, 7, 8, 9, 15, 16])
+@pytest.mark.parametrize("M,N", [(1, 64), (32, 8192), (33, 2560), (100, 5000), (1024, 1000), (1001, 4096), (4100, 1100), (4736, 300), (9000, 640), (28672, 512), (37888, 260),
+                                 (40001, 130), (80000, 256), (300, 40000), (5000, 17000)])
+def test_linear_of_few_tokens(b, M, N, B):
+    g = gen(M + N + B)
+    w, ws = ref.random_weight(M, N, g, "cuda")
+    q, s = ref.random_weight(B, N, g, "cuda")
+    y = check_linear(b, q, w, ws, "fp32", N, ref.values(q, s, N), s)
+    assert same(y, b.vptq_linear_fp4(q, w, ws, x_scale=s, out_dtype="fp32"))
+    x = torch.randn(B, N, generator=g, device="cuda").half()
+    check_linear(b, x, w, ws, "bf16", N, ref.quantize(x)[0])
+
+
+def test_linear_paths(b):
+    path = lambda M, N, B: b.vptq_linear_fp4_path(b.make_fp4_desc(M, N), B)  # noqa: E731
+    assert [path(4096, 4096, B) for B in (1, 16, 17, 300)] == ["fp4_few"] * 2 + ["fp4_tcgen05"] * 2
+    assert path(28672, 8192, 16) == path(8192, 14336, 16) == "fp4_few" and path(300, 10 ** 6, 16) == "fp4_tcgen05"
+
+
 def test_linear_of_every_scale(b):
     """The rows' and the weight's scales run over all bytes, with sums that neither overflow nor lose to FP32's smallest values; 255 reads as NaN."""
     g = gen(9)
