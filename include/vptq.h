@@ -552,8 +552,8 @@ int vptq_dequant_fp4(const vptq_layer_desc *desc, const vptq_layer_ptrs *p, uint
  *   every pointer is 16-byte aligned (VPTQ_E_ALIGN), but for x of 16 bits: any alignment of a value;  out_dtype FP16, BF16 or FP32
  *   flags: VPTQ_FLAG_CONCURRENT and VPTQ_FLAG_DETERMINISTIC are accepted and change nothing (no CTA waits for another launch's, every
  *           sum has a fixed order).
- * At most 16 tokens take the kernel "fp4_few", which quantizes them itself, unless they have more columns than an SM has room for beside
- * the weight's (on 148 SMs up to 15872 columns are always taken); all others take "fp4_tcgen05" (vptq_linear_fp4_path).
+ * At most 16 tokens take the kernel "fp4_few" (which may quantize them itself), more "fp4_tcgen05" (vptq_linear_fp4_path).  A sum
+ * that overflows FP32 is an infinity or a NaN.
  * The workspace, 256-byte aligned, starts with a status word (vptq_workspace_status); its contents on entry are irrelevant, calls that may
  * overlap must not share one.  All device-side waits are bounded: one that gives up leaves NaN in the results that it concerns and
  * VPTQ_E_TIMEOUT in the status word. */

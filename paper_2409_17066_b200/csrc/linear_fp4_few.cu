@@ -1,18 +1,23 @@
-// out = x W^T for a few tokens over an e2m1 weight, in one kernel: the activations are quantized by the CTAs that multiply by them.
+// out = x W^T for at most 16 tokens over an e2m1 weight with a power of two for every 32 columns of a row.
 //
-// What counts is the weight's way from HBM; the products are the tensor cores' (tcgen05.mma, kind::mxf4, as in linear_fp4_tcgen05.cu), so that no
-// code of the weight passes through a register.  The tokens are rows of the MMA's first operand, of whose 128 rows only those that are tokens lie in
-// shared memory: the others are whatever follows there, and sums of lanes that nobody reads.
-// A CTA takes some groups of 32 features (a scale tile's columns of TMEM hold 32 rows each), at most seven at a time, dealt out evenly so that all
-// SMs load; a layer of fewer groups than SMs has its columns split over the CTAs of a cluster, which send each other their sums: every CTA adds
-// up its share of the results, in rank order.
-// Warps by role: 0 loads the weight and its scales (TMA) through a ring of stages of 256 columns, 1 copies scales to TMEM and issues the
-// MMAs, the others quantize the activations (the rule of fp4_quantize.cu; e2m1 activations: copy them) block by block into the layout of the operand,
-// where they stay; two of them read the sums in the end.
-// Every wait is bounded; sums of a CTA in which one gave up are NaN, and the workspace's status word is set.
+// Persistent CTAs, one per SM, own consecutive groups of 16 weight rows and take up to PASS of them (a pass) through all columns.  Each of
+// the warps takes every eighth (sixteenth) block of KB columns and feeds itself: a ring of stages in shared memory, a stage one block of the
+// pass's rows in one TMA box and the tiles of their scales, refilled as soon as it has been read.
+// The warp multiplies in FP16 (mma.sync m16n8k16), in which every code is exact: the order of the products inside a block of 32 columns is free, so
+// that lane 4g + t holds codes 8t .. 8t + 7 of rows g and g + 8 and of token g, a word that ldmatrix brings and four conversions widen.  A block's 32
+// products are exact in FP32; their sum is multiplied by the weight's power of two and added to the sum of all, times the token's, in one fma.
+// (Widened to e4m3 by table look-ups in registers the MMAs are half as many, but a look-up takes 18 clocks a word, the conversions 9.  The
+// tcgen05 form, tokens in 128 rows, took 12.0 us for 4096 x 4096 and one token: every block waits for its scales' way into TMEM and its MMAs, one after
+// the other, in front of 6 us of setting up.)
+// The activations, which no other warp of the CTA needs, come straight from global memory, a block ahead.  Where a CTA has one pass, those of 16 bits, of
+// at most 8 tokens, are quantized on the way by the rule of fp4_quantize.cu: a token's block is four lanes.  (Otherwise every CTA's work on all of
+// them, pass after pass, would take longer than a kernel in front that does it once.)
+// At the end of a pass the warps' sums meet in shared memory and are added in warp order: a result does not depend on timing.
+// Every wait is bounded; a warp whose wait gives up leaves NaN, and the workspace's status word is set.
 #include "fp4.cuh"
 #include "fp4_tcgen05.cuh"
-#include "tcgen05_pair.cuh"
+#include "tcgen05_ptx.cuh"
+#include "tma_2d.cuh"
 
 namespace vptq {
 
@@ -20,425 +25,371 @@ namespace {
 
 using namespace tc;
 
-constexpr int KB = 256, KB_BYTES = KB / 2;                // columns of a block: a swizzled row of 128 bytes
-constexpr int STEPS = KB / 64, CHUNKS = KB / FP4_TILE_COLS;            // MMAs, and scale tiles of 128 rows, along a block
-// Features of a group, groups of a pass at most.  An MMA's features begin at a multiple of 64: scale addresses in TMEM are even columns.  A pass that
-// begins at an odd group leaves the place of the group before it unused, in shared memory and among the sums.
-constexpr int GROUP = 32, GROUPS = 7;
-constexpr int GROUP_BYTES = GROUP * KB_BYTES, SCALES = CHUNKS * FP4_TILE_BYTES;
-constexpr int WARPS = 12, THREADS = 32 * WARPS, X_WARP0 = 2, SUM_WARP0 = 4, SUM_WARP1 = 8;      // (the warps that may read lanes 0..31 of TMEM)
-constexpr int X_HALVES = 2 * (WARPS - X_WARP0);
-constexpr int MAX_STAGES = 16;
-constexpr int MIN_RING = 16 * 1024;                       // an MMA reads 128 rows from its block of activations on
-constexpr int SMEM_MAX = 232448 - 1024;                  // (the static part takes a multiple of the dynamic part's alignment)
-// Two CTAs fit on an SM where their shared memory does: the next launch's are made ready beside these.  Together they never ask for more TMEM than
-// there is: one that wants more than half of its 512 columns has an SM to itself (CTAs of two clusters could wait for each other's).
-constexpr int HALF_SMEM = 113 * 1024, WHOLE_SMEM = 116 * 1024;
+constexpr int GROUP = 16;                                 // rows of an MMA
+constexpr int MAX_STAGES = 8;                             // of a warp
+constexpr int SMEM_MAX = 232448;
 
-struct Params {
-    int M, N, B, kbs, last_steps, col_tiles;
-    int groups, split;                                    // of the layer; CTAs of a cluster
-    int pass_groups, row_tiles;                           // groups and scale tiles that a stage has room for
-    int stages, x_rows;                                   // x_rows: tokens, rounded up to 8
-    int tmem_cols;
-    const void *x;
-    const uint8_t *x_scale;
-    void *out;
-    int out_dtype, wide_out;                              // wide_out: rows of `out` are 16-byte aligned
+__host__ __device__ constexpr int part_stride(int groups) { return groups * GROUP + 4; }               // (lanes of different tokens write different banks)
+// bytes of a stage: rows of KB / 2 bytes, tiles of KB / 128 times 512
+__host__ __device__ constexpr int group_bytes(int KB) { return GROUP * KB / 2; }
+__host__ __device__ constexpr int tile_bytes(int KB) { return KB / FP4_TILE_COLS * FP4_TILE_BYTES; }
+
+struct FewParams {
+    Fp4Linear L;
+    int col_tiles;
+    int passes;                // of every CTA
+    int stage_groups, stages;  // groups that a stage holds (the largest pass of any CTA), stages of a warp
     int *status;
+    uint32_t zero;
     unsigned long long wait_limit;
 };
 
-__device__ __forceinline__ void mma(uint32_t d_tmem, uint64_t a, uint64_t b, uint32_t idesc, uint32_t a_scale, uint32_t b_scale, uint32_t accumulate)
+__device__ __forceinline__ void load_matrices(uint32_t (&r)[4], uint32_t a)
 {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
-                 "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
-                 ::"r"(d_tmem), "l"(a), "l"(b), "r"(idesc), "r"(a_scale), "r"(b_scale), "r"(accumulate) : "memory");
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a));
 }
-__device__ __forceinline__ void copy_scales(uint32_t tmem, uint64_t desc)
+__device__ __forceinline__ uint32_t load_shared(uint32_t a)
 {
-    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+    uint32_t v;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(a));
+    return v;
 }
-__device__ __forceinline__ void store_peer4(uint32_t addr, uint32_t rank, float4 v)
+// eight codes as FP16
+__device__ __forceinline__ void widen(uint32_t q, uint32_t (&h)[4])
 {
-    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(address_in(addr, rank)), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
+    asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\tmov.b32 {b0, b1, b2, b3}, %4;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %0, b0;\n\tcvt.rn.f16x2.e2m1x2 %1, b1;\n\tcvt.rn.f16x2.e2m1x2 %2, b2;\n\tcvt.rn.f16x2.e2m1x2 %3, b3;\n\t}"
+        : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(q));
+}
+__device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+{
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// Byte i of a word of scales as a power of two; 0 is 2^-127, and 255 an infinity: what it is multiplied into is no number, or is told by that.
+__device__ __forceinline__ float scale_of(uint32_t w, int i)
+{
+    const uint32_t bits = (i == 3 ? w >> 1 : w << (23 - 8 * i)) & 0x7F800000u;
+    return __uint_as_float(max(bits, 0x00400000u));
+}
+// acc += (d * w) * s for a pair of sums
+__device__ __forceinline__ void add_scaled(float &a0, float &a1, float d0, float d1, float w, float s0, float s1)
+{
+    asm("{\n\t.reg .b64 a, d, w, s;\n\tmov.b64 a, {%0, %1};\n\tmov.b64 d, {%2, %3};\n\tmov.b64 w, {%4, %4};\n\tmov.b64 s, {%5, %6};\n\t"
+        "mul.rn.f32x2 d, d, w;\n\tfma.rn.f32x2 a, d, s, a;\n\tmov.b64 {%0, %1}, a;\n\t}" : "+f"(a0), "+f"(a1) : "f"(d0), "f"(d1), "f"(w), "f"(s0), "f"(s1));
 }
 
-// sixteen columns of a token: values that are to be quantized, or codes and their scale byte
-template <int DT, bool VEC> struct Item { Sixteen<DT, VEC> v; };
-template <> struct Item<VPTQ_DTYPE_E2M1, true> { uint2 q; uint32_t b; };
+// A lane's share of a token's KB columns, 8t .. 8t + 7 of each block of 32, as they lie in memory (16-bit values, two to a word) or as codes with
+// the scale bytes of four blocks to a word
+template <int DT, int KB> struct Raw { uint4 q[KB / 32]; };
+template <int KB> struct Raw<VPTQ_DTYPE_E2M1, KB> { uint32_t q[KB / 32], b[KB / 128]; };
 
-template <int DT, bool VEC>
-__device__ __forceinline__ void load_item(const Params &P, int row, int c, Item<DT, VEC> &e)
+// row: the token's, or null for one that is not there (zeros); c: the lane's first column
+template <int DT, bool VEC, int KB>
+__device__ __forceinline__ void load_block(Raw<DT, KB> &r, int i, const uint8_t *row, int c, int cols)
 {
+    c += 32 * i;
     if constexpr (DT == VPTQ_DTYPE_E2M1) {
-        const long long pitch = (long long)((P.N + FP4_BLOCK - 1) / FP4_BLOCK) * (FP4_BLOCK / 2);
-        e.q = make_uint2(0, 0);
-        e.b = 0;
-        if (row < P.B && c / 2 < pitch) {
-            e.q = __ldg(reinterpret_cast<const uint2 *>(reinterpret_cast<const uint8_t *>(P.x) + row * pitch + c / 2));
-            e.b = __ldg(P.x_scale + (long long)(c / FP4_TILE_COLS) * FP4_TILE_BYTES + fp4_scale_at(row, c / FP4_BLOCK % 4));
-        }
+        r.q[i] = row != nullptr && c < cols ? __ldg(reinterpret_cast<const uint32_t *>(row + c / 2)) : 0u;
+    } else if constexpr (VEC) {
+        r.q[i] = row != nullptr && c < cols ? __ldg(reinterpret_cast<const uint4 *>(row + 2ll * c)) : make_uint4(0, 0, 0, 0);
     } else {
-        e.v = load_sixteen<DT, VEC>(reinterpret_cast<const uint8_t *>(P.x) + (long long)row * P.N * Act<DT>::BYTES, row < P.B ? c : P.N, P.N);
+        uint32_t w[4] = {};
+#pragma unroll
+        for (int k = 0; k < 8; k++)
+            if (row != nullptr && c + k < cols) w[k / 2] |= (uint32_t)__ldg(reinterpret_cast<const uint16_t *>(row) + c + k) << (16 * (k & 1));
+        r.q[i] = make_uint4(w[0], w[1], w[2], w[3]);
     }
 }
-// its codes and scale byte; for a whole warp
-template <int DT, bool VEC>
-__device__ __forceinline__ uint2 codes_of(const Item<DT, VEC> &e, int n, uint32_t &b)
+
+// a token's block as an MMA operand, and its scale; for a whole warp.  n: columns from the lane's first on that exist.  zero: 0, which the compiler
+// does not know: conversions to e2m1 and back with nothing between them came out as zeros (nvcc 12.9).
+template <int DT, int KB>
+__device__ __forceinline__ float operand_of(const Raw<DT, KB> &r, int i, int n, uint32_t zero, uint32_t (&h)[4])
 {
     if constexpr (DT == VPTQ_DTYPE_E2M1) {
-        b = e.b;
-        return e.q;
+        widen(r.q[i], h);
+        return scale_of(r.b[i / 4], i & 3);
     } else {
-        b = fp4_pair_scale(magnitude(e.v));
-        return fp4_codes16(e.v, b, n);
+        Eight<DT, true> e;
+        e.q = r.q[i];
+        const uint32_t m = larger2(larger2(e.q.x & 0x7FFF7FFFu, e.q.y & 0x7FFF7FFFu), larger2(e.q.z & 0x7FFF7FFFu, e.q.w & 0x7FFF7FFFu));
+        const uint32_t b = fp4_block_scale(magnitude16<DT>(m));
+        float v[8];
+        values_of(e, v);
+        widen(fp4_codes(v, b, n) ^ zero, h);
+        return fp4_scale_value(b);
     }
 }
 
-template <int DT, bool VEC>
-__global__ void __launch_bounds__(THREADS, 2)
-linear_fp4_few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_ws, const __grid_constant__ Params P)
+template <int N> struct Count { static constexpr int value = N; };
+
+// map_full: boxes of stage_groups groups, map_less: of one fewer (passes differ by at most one).  VEC: activations are read 16 bytes at a time.
+// PASS: groups of a pass at most; NT: eight tokens, or twice that (e2m1 only).
+template <int DT, bool VEC, int PASS, int KB, int NT, int WARPS>
+__global__ void __launch_bounds__(32 * WARPS, 1)
+linear_fp4_few_kernel(const __grid_constant__ CUtensorMap map_full, const __grid_constant__ CUtensorMap map_less, const __grid_constant__ CUtensorMap map_scales,
+                      const __grid_constant__ FewParams D)
 {
+    const Fp4Linear &P = D.L;
+    constexpr int GB = group_bytes(KB), TB = tile_bytes(KB), ROW = KB / 2, BLOCKS = KB / 32;
+    constexpr int MAX_TILES = (PASS * GROUP + 2 * FP4_TILE_ROWS - GROUP - 1) / FP4_TILE_ROWS;      // that a pass's rows lie in
     extern __shared__ __align__(1024) uint8_t sm[];
-    __shared__ uint32_t tmem_slot, lost;                  // lost: a wait of this CTA gave up
-    __shared__ __align__(8) uint64_t barriers[2 * MAX_STAGES + 2];
-    // shared memory: activations by block, stages, the activations' scales by block, what the cluster's CTAs send, a barrier for every block
-    const int rank = P.split > 1 ? (int)cluster_rank() : 0, cluster = (int)blockIdx.x / P.split, clusters = (int)gridDim.x / P.split;
-    const int kb0 = (int)((long long)P.kbs * rank / P.split), kb1 = (int)((long long)P.kbs * (rank + 1) / P.split), blocks = kb1 - kb0;
-    const int most_blocks = (P.kbs + P.split - 1) / P.split;
-    const uint32_t x_block = (uint32_t)P.x_rows * KB_BYTES, xs_chunk = (uint32_t)P.x_rows * 16u;
-    const uint32_t places = P.pass_groups + 1, stage_bytes = places * GROUP_BYTES + (uint32_t)P.row_tiles * SCALES;
-    const uint32_t base = smem_addr(sm), ring = base + (most_blocks * x_block + 1023u & ~1023u), xs0 = ring + P.stages * stage_bytes;
-    const uint32_t sums = xs0 + (most_blocks * CHUNKS * xs_chunk + FP4_TILE_BYTES + 15u & ~15u);
-    const uint32_t x_bars = sums + (P.split > 1 ? (uint32_t)(P.x_rows * P.pass_groups * GROUP * 4 + 16 * P.split) : 0u);
-    const uint32_t bars = smem_addr(barriers);
-    auto bar_full = [&](int s) { return bars + 8u * s; };
-    auto bar_empty = [&](int s) { return bars + 8u * (MAX_STAGES + s); };
-    const uint32_t bar_acc_full = bars + 8u * 2 * MAX_STAGES, bar_acc_empty = bar_acc_full + 8;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t stages = (uint32_t)D.stages, codes_bytes = (uint32_t)(D.stage_groups * GB), stage_bytes = codes_bytes + MAX_TILES * TB;
+    const uint32_t ring = smem_addr(sm) + (uint32_t)warp * stages * stage_bytes;
+    float *part = reinterpret_cast<float *>(sm + WARPS * stages * stage_bytes);
+    const int stride = part_stride(D.stage_groups);
+    const uint32_t bars = smem_addr(part) + (uint32_t)(WARPS * 8 * NT * stride * 4 + warp * MAX_STAGES * 8);
 
-    if (threadIdx.x == 0) {
-        lost = 0;
-        for (int s = 0; s < P.stages; s++) { mbar_init(bar_full(s), 1); mbar_init(bar_empty(s), 1); }
-        mbar_init(bar_acc_full, 1);
-        mbar_init(bar_acc_empty, 2);
+    // this CTA's groups, in passes of nearly equal size
+    const int groups = (P.M + GROUP - 1) / GROUP, kbs = (P.N + KB - 1) / KB;
+    const int first = (int)((long long)groups * blockIdx.x / gridDim.x), count = (int)((long long)groups * (blockIdx.x + 1) / gridDim.x) - first;
+    const int passes = D.passes, pass_groups = count / passes, larger = count - pass_groups * passes;
+    auto pass_begin = [&](int p) { return first + p * pass_groups + min(p, larger); };
+    // this warp's loads, in the order it needs them; by one lane
+    int load_pass = warp < kbs ? 0 : passes, load_kb = warp, load_group = first, load_groups = pass_begin(1) - first;
+    auto load = [&](uint32_t slot) {
+        const uint32_t bar = bars + 8 * slot, to = ring + slot * stage_bytes;
+        const int tile = load_group * GROUP / FP4_TILE_ROWS, tiles = ((load_group + load_groups) * GROUP - 1) / FP4_TILE_ROWS - tile + 1;
+        mbar_expect_tx(bar, (uint32_t)(load_groups * GB + tiles * TB));
+        tma_load_2d(to, load_groups == D.stage_groups ? &map_full : &map_less, load_kb * ROW, load_group * GROUP, bar);
+#pragma unroll
+        for (int i = 0; i < MAX_TILES; i++)
+            if (i < tiles) tma_load_2d(to + codes_bytes + i * TB, &map_scales, 0, (tile + i) * D.col_tiles + load_kb * (KB / FP4_TILE_COLS), bar);
+    };
+    auto next_load = [&]() {
+        load_kb += WARPS;
+        if (load_kb >= kbs) {
+            load_kb = warp;
+            load_pass++;
+            load_group = pass_begin(load_pass);
+            load_groups = pass_begin(load_pass + 1) - load_group;
+        }
+    };
+    if (lane == 0) {
+        for (uint32_t s = 0; s < stages; s++) mbar_init(bars + 8 * s, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    for (int i = threadIdx.x; i < blocks; i += THREADS) mbar_init(x_bars + 8 * i, P.x_rows);
-    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    if (warp == 1) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&tmem_slot)), "r"(P.tmem_cols) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-    }
-    tc_fence_before();
-    __syncthreads();
-    if (P.split > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");       // (waited for before anything is sent)
-    tc_fence_after();
-    const uint32_t tmem = tmem_slot;
     pdl_launch_dependents();
-
-    // this cluster's groups, in passes of nearly the same number
-    const int g_first = (int)((long long)P.groups * cluster / clusters), g_end = (int)((long long)P.groups * (cluster + 1) / clusters);
-    const int passes = (g_end - g_first + P.pass_groups - 1) / P.pass_groups;
-    auto pass_begin = [&](int p) { return g_first + (int)((long long)(g_end - g_first) * p / passes); };
-    const uint32_t lost_at = smem_addr(&lost);
-    uint32_t gave_up = 0;
-    pdl_wait();                                                                // (weight and activations may be the preceding kernel's, and it may read the result's memory)
-
-    if (warp == 0) {
-        // ---- loads ----
-        uint32_t s = 0, round = 0;
-        for (int p = 0; p < passes; p++) {
-            const int g0 = pass_begin(p), n = pass_begin(p + 1) - g0, tiles = (g0 % 4 + n + 3) / 4;
-            for (int kb = kb0; kb < kb1; kb++) {
-                mbar_wait_or_flag(bar_empty(s), (round & 1) ^ 1u, lost_at, gave_up);
-                if (elect_one() && !gave_up) {
-                    const uint32_t at = ring + s * stage_bytes, full = bar_full(s);
-                    mbar_expect_tx(full, (uint32_t)(n * GROUP_BYTES + tiles * SCALES));
-                    for (int i = 0; i < n; i++) tma_load_2d(at + (g0 % 2 + i) * GROUP_BYTES, &map_w, kb * KB_BYTES, (g0 + i) * GROUP, full);
-                    for (int i = 0; i < tiles; i++)
-                        tma_load_2d(at + places * GROUP_BYTES + i * SCALES, &map_ws, 0, (g0 / 4 + i) * P.col_tiles + kb * CHUNKS, full);
-                }
-                __syncwarp();
-                if (++s == (uint32_t)P.stages) { s = 0; round++; }
-            }
-        }
-    } else if (warp == 1) {
-        // ---- scales to TMEM, then MMAs ----
-        const uint64_t a0 = make_smem_desc(base, 16, 1024, LAYOUT_SW128), b0 = make_smem_desc(ring, 16, 1024, LAYOUT_SW128);
-        const uint64_t as0 = make_smem_desc(xs0, 16, 128, 0), bs0 = make_smem_desc(ring + places * GROUP_BYTES, 16, 128, 0);
-        uint32_t s = 0, round = 0, turn = 0;
-        for (int p = 0; p < passes; p++) {
-            const int g0 = pass_begin(p), n = pass_begin(p + 1) - g0;
-            const uint32_t tiles = (uint32_t)(g0 % 4 + n + 3) / 4, inside = g0 % 4 / 2 * 2;
-            const uint32_t idesc = (1u << 7) | (1u << 10) | ((uint32_t)((g0 % 2 + n) * GROUP >> 3) << 17) | (1u << 23) | ((128u >> 4) << 24);
-            mbar_wait_or_flag(bar_acc_empty, (p & 1) ^ 1u, lost_at, gave_up);
-            for (int kb = kb0; kb < kb1; kb++, turn ^= 1) {
-                if (p == 0) mbar_wait_flagged(x_bars + 8 * (kb - kb0), 0, P.wait_limit, lost_at, gave_up);
-                mbar_wait_flagged(bar_full(s), round & 1, P.wait_limit, lost_at, gave_up);
-                tc_fence_after();
-                if (elect_one() && !gave_up) {
-                    const uint64_t at = (uint64_t)(s * stage_bytes >> 4), xa = (uint64_t)((kb - kb0) * x_block >> 4), xsa = (uint64_t)((kb - kb0) * CHUNKS * xs_chunk >> 4);
-                    const uint32_t xs = tmem + places * GROUP + turn * 32, ws = xs + 4 * CHUNKS;
-                    const int steps = kb == P.kbs - 1 ? P.last_steps : STEPS;
-#pragma unroll
-                    for (int c = 0; c < CHUNKS; c++) {
-                        if (2 * c >= steps) break;                             // (what lies behind the last columns is another row's)
-                        copy_scales(xs + 4 * c, as0 + xsa + c * (xs_chunk >> 4));
-                        for (uint32_t r = 0; r < tiles; r++) copy_scales(ws + 4 * (c * tiles + r), bs0 + at + (r * SCALES + c * FP4_TILE_BYTES >> 4));
-                    }
-#pragma unroll
-                    for (int k = 0; k < STEPS; k++) {
-                        if (k >= steps) break;
-                        const uint32_t id = idesc | (uint32_t)(k & 1) << 30 | (uint32_t)(k & 1) << 5;
-                        mma(tmem, a0 + xa + 2 * k, b0 + at + 2 * k, id, xs + 4 * (k / 2), ws + 4 * tiles * (k / 2) + inside, kb > kb0 || k > 0);
-                    }
-                    umma_commit(bar_empty(s));
-                    if (kb == kb1 - 1) umma_commit(bar_acc_full);
-                }
-                __syncwarp();
-                if (++s == (uint32_t)P.stages) { s = 0; round++; }
-            }
-        }
-    } else {
-        // ---- activations: half a warp takes a token's 256 columns ----
-        if (blockIdx.x == 0 && threadIdx.x == 32 * X_WARP0) *P.status = 0;
-        const int l = lane & 15, half = 2 * (warp - X_WARP0) + (lane >> 4), items = blocks * P.x_rows;
-        int kb = half / P.x_rows, row = half - kb * P.x_rows;
-        auto next = [&](int &kb, int &row) {
-            row += X_HALVES;
-            while (row >= P.x_rows) { row -= P.x_rows; kb++; }
-        };
-        Item<DT, VEC> e;
-        load_item<DT, VEC>(P, row, kb < blocks ? (kb0 + kb) * KB + 16 * l : KB * P.kbs, e);
-        for (int i = half - (lane >> 4); i < items; i += X_HALVES) {          // (a warp's halves run the same number of rounds: shuffles)
-            Item<DT, VEC> e2;
-            int kb2 = kb, row2 = row;
-            next(kb2, row2);
-            load_item<DT, VEC>(P, row2, kb2 < blocks ? (kb0 + kb2) * KB + 16 * l : KB * P.kbs, e2);
-            uint32_t b;
-            const uint2 q = codes_of<DT, VEC>(e, P.N - ((kb0 + kb) * KB + 16 * l), b);
-            if (kb < blocks) {
-                // 128-byte swizzle: the 16-byte pieces of a row are exchanged by the row's place among eight
-                const uint32_t at = base + kb * x_block + row * KB_BYTES + ((l / 2 ^ row & 7) << 4) + (l & 1) * 8;
-                asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(at), "r"(q.x), "r"(q.y) : "memory");
-                if ((l & 1) == 0) asm volatile("st.shared.u8 [%0], %1;" ::"r"(xs0 + (kb * CHUNKS + l / 8) * xs_chunk + row * 16 + l / 2 % 4), "r"(b) : "memory");
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            }
-            __syncwarp();
-            if (l == 0 && kb < blocks) mbar_arrive(x_bars + 8 * kb);
-            e = e2; kb = kb2; row = row2;
-        }
-        __syncwarp();
+    pdl_wait();                                           // (weight, scales and activations may all be the preceding kernel's output)
+    for (uint32_t s = 0; s < stages && load_pass < passes; s++) {
+        if (lane == 0) load(s);
+        next_load();
     }
+    if (blockIdx.x == 0 && threadIdx.x == 0) *D.status = 0;
     __syncwarp();
-    if (P.split > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");          // the cluster's CTAs have begun
-    const bool sums_up = warp == SUM_WARP0 || warp == SUM_WARP1;
+    uint32_t gave_up = 0;
+
+    const int g = lane >> 2, t = lane & 3;
+    // ldmatrix: this lane names row lane % 16 of a group and, of two adjacent blocks, the first (lanes 0..15) or the second; where that block's piece of
+    // the row lies is exchanged by the row's place (128- and 64-byte swizzle), for blocks j and j + 1 by j too
+    const int mrow = lane & 15, mblock = lane >> 4;
+    const uint32_t piece = (uint32_t)(KB == 256 ? mblock ^ (mrow & 7) : mblock ^ (mrow >> 1 & 3)) << 4;
+    const long long pitch = (P.N + FP4_BLOCK - 1ll) / FP4_BLOCK * (FP4_BLOCK / 2);
+    const int cols = DT == VPTQ_DTYPE_E2M1 ? (int)(2 * pitch) : P.N;
+    const uint8_t *xrow[NT];
+#pragma unroll
+    for (int u = 0; u < NT; u++)
+        xrow[u] = 8 * u + g < P.B ? reinterpret_cast<const uint8_t *>(P.x) + (8 * u + g) * (DT == VPTQ_DTYPE_E2M1 ? pitch : 2ll * P.N) : nullptr;
+    auto load_scales = [&](Raw<DT, KB> (&x)[NT], int kb) {
+        if constexpr (DT == VPTQ_DTYPE_E2M1) {
+#pragma unroll
+            for (int u = 0; u < NT; u++)
+#pragma unroll
+                for (int i = 0; i < KB / 128; i++) {
+                    const int tile = kb * (KB / 128) + i;
+                    x[u].b[i] = xrow[u] != nullptr && tile < D.col_tiles ? __ldg(reinterpret_cast<const uint32_t *>(P.x_scale + (long long)tile * FP4_TILE_BYTES + fp4_scale_at(8 * u + g, 0))) : 0u;
+                }
+        }
+    };
+    const int iterations = warp < kbs ? (kbs - warp + WARPS - 1) / WARPS : 0;
+    uint32_t slot = 0, parity = 0;
     for (int p = 0; p < passes; p++) {
-        const int g0 = pass_begin(p), n = pass_begin(p + 1) - g0, m0 = g0 * GROUP, cols = n * GROUP;
-        if (sums_up) {
-            mbar_wait_or_flag(bar_acc_full, p & 1, lost_at, gave_up);
-            tc_fence_after();
-            // (a lane that gave up, here or in another warp before this one was woken, leaves NaN)
-            const bool bad = __any_sync(0xffffffffu, gave_up != 0 || load_word(lost_at) != 0);
-            for (int c = warp == SUM_WARP0 ? 0 : 16; c < cols; c += 32) {
-                uint32_t d[16];
-                __syncwarp();
-                tmem_start16(tmem + g0 % 2 * GROUP + c, d);
-                tmem_wait16(d);
-                if (bad)
+        const int g0 = pass_begin(p), n_groups = pass_begin(p + 1) - g0;
+        Raw<DT, KB> x[NT];
 #pragma unroll
-                    for (int i = 0; i < 16; i++) d[i] = 0x7FFFFFFFu;
-                if (lane >= P.B) continue;
-                if (P.split > 1) {
-                    // pieces of four results, token by token, are dealt out over the ranks; a rank's are side by side for every sender
-                    const int all = P.B * (cols / 4);
+        for (int u = 0; u < NT; u++)
 #pragma unroll
-                    for (int i = 0; i < 4; i++) {
-                        const int piece = lane * (cols / 4) + c / 4 + i, owner = (int)((long long)(piece + 1) * P.split - 1) / all;
-                        const int first = (int)((long long)all * owner / P.split), count = (int)((long long)all * (owner + 1) / P.split) - first;
-                        store_peer4(sums + (uint32_t)(rank * count + piece - first) * 16u, (uint32_t)owner,
-                                    make_float4(__uint_as_float(d[4 * i]), __uint_as_float(d[4 * i + 1]), __uint_as_float(d[4 * i + 2]), __uint_as_float(d[4 * i + 3])));
+            for (int i = 0; i < BLOCKS; i++) load_block<DT, VEC, KB>(x[u], i, warp < kbs ? xrow[u] : nullptr, warp * KB + 8 * t, cols);
+        load_scales(x, warp);
+        float acc[PASS][NT][4] = {};
+        uint32_t scale_at[PASS];                          // of a group's row g, from a stage's scales on
+#pragma unroll
+        for (int r = 0; r < PASS; r++)
+            scale_at[r] = ((g0 + r) * GROUP / FP4_TILE_ROWS - g0 * GROUP / FP4_TILE_ROWS) * TB + fp4_scale_at((g0 + r) * GROUP % FP4_TILE_ROWS, 0) + g * 16;
+#pragma unroll 1
+        for (int it = 0, kb = warp; it < iterations; it++, kb += WARPS) {
+            const uint32_t stage = ring + slot * stage_bytes;
+            Raw<DT, KB> next[NT];                         // (e2m1: the next block's scales, whose words all of this one's blocks need)
+            load_scales(next, kb + WARPS);
+            bool waited = false;
+#pragma unroll
+            for (int j = 0; j < BLOCKS; j += 2) {
+                uint32_t h[NT][2][4];
+                float2 s[NT][2];
+#pragma unroll
+                for (int u = 0; u < NT; u++)
+#pragma unroll
+                    for (int i = 0; i < 2; i++) {
+                        const float own = operand_of<DT, KB>(x[u], j + i, P.N - (kb * KB + 32 * (j + i) + 8 * t), D.zero, h[u][i]);
+                        s[u][i] = make_float2(__shfl_sync(0xffffffffu, own, 8 * t), __shfl_sync(0xffffffffu, own, 8 * t + 4));      // of tokens 2t, 2t + 1
+                        load_block<DT, VEC, KB>(x[u], j + i, it + 1 < iterations ? xrow[u] : nullptr, (kb + WARPS) * KB + 8 * t, cols);
                     }
-                } else if (P.wide_out && m0 + c + 16 <= P.M) {
-                    const long long o = (long long)lane * P.M + m0 + c;
-                    if (P.out_dtype == VPTQ_DTYPE_FP32) {
+                if (!waited) mbar_wait_within(bars + 8 * slot, parity, D.wait_limit, gave_up);
+                waited = true;
+                const uint32_t matrices = stage + mrow * ROW + (piece ^ 16 * j), scales = stage + codes_bytes + j / 4 * FP4_TILE_BYTES;
+                // R groups from r0 on
+                auto multiply = [&](auto count, int r0) {
+                    constexpr int R = decltype(count)::value;
+                    uint32_t w[R][4], sw[R][2];
 #pragma unroll
-                        for (int i = 0; i < 4; i++) reinterpret_cast<uint4 *>(reinterpret_cast<float *>(P.out) + o)[i] = make_uint4(d[4 * i], d[4 * i + 1], d[4 * i + 2], d[4 * i + 3]);
-                    } else {
-                        uint32_t h[8];
-#pragma unroll
-                        for (int i = 0; i < 8; i++) h[i] = pair16(__uint_as_float(d[2 * i]), __uint_as_float(d[2 * i + 1]), P.out_dtype);
-#pragma unroll
-                        for (int i = 0; i < 2; i++) reinterpret_cast<uint4 *>(reinterpret_cast<uint16_t *>(P.out) + o)[i] = make_uint4(h[4 * i], h[4 * i + 1], h[4 * i + 2], h[4 * i + 3]);
+                    for (int r = 0; r < R; r++) {
+                        load_matrices(w[r], matrices + (r0 + r) * GB);
+                        sw[r][0] = load_shared(scales + scale_at[r0 + r]);         // of rows g and g + 8
+                        sw[r][1] = load_shared(scales + scale_at[r0 + r] + 8 * 16);
                     }
-                } else {
 #pragma unroll
-                    for (int i = 0; i < 16; i++)
-                        if (m0 + c + i < P.M) store_out(P.out, (long long)lane * P.M + m0 + c + i, __uint_as_float(d[i]), P.out_dtype);
+                    for (int i = 0; i < 2; i++) {
+                        uint32_t a[R][4], c[R][4];
+                        float d[R][NT][4] = {};
+#pragma unroll
+                        for (int r = 0; r < R; r++) {
+                            widen(w[r][2 * i], a[r]);
+                            widen(w[r][2 * i + 1], c[r]);
+                        }
+                        // step by step over all pairs: the two MMAs of a pair wait for one another
+#pragma unroll
+                        for (int k = 0; k < 2; k++)
+#pragma unroll
+                            for (int r = 0; r < R; r++)
+#pragma unroll
+                                for (int u = 0; u < NT; u++) mma_f16(d[r][u], a[r][2 * k], c[r][2 * k], a[r][2 * k + 1], c[r][2 * k + 1], h[u][i][2 * k], h[u][i][2 * k + 1]);
+#pragma unroll
+                        for (int r = 0; r < R; r++) {
+                            const float f0 = scale_of(sw[r][0], j % 4 + i), f1 = scale_of(sw[r][1], j % 4 + i);
+#pragma unroll
+                            for (int u = 0; u < NT; u++) {
+                                add_scaled(acc[r0 + r][u][0], acc[r0 + r][u][1], d[r][u][0], d[r][u][1], f0, s[u][i].x, s[u][i].y);
+                                add_scaled(acc[r0 + r][u][2], acc[r0 + r][u][3], d[r][u][2], d[r][u][3], f1, s[u][i].x, s[u][i].y);
+                            }
+                        }
+                    }
+                };
+#pragma unroll
+                for (int r0 = 0; r0 < PASS; r0 += 2) {
+                    if (r0 + 1 < n_groups) multiply(Count<2>{}, r0);
+                    else if (r0 < n_groups) multiply(Count<1>{}, r0);
                 }
             }
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0 && !gave_up) mbar_arrive(bar_acc_empty);
+            if constexpr (DT == VPTQ_DTYPE_E2M1)
+#pragma unroll
+                for (int u = 0; u < NT; u++)
+#pragma unroll
+                    for (int i = 0; i < KB / 128; i++) x[u].b[i] = next[u].b[i];
+            __syncwarp();                                 // every lane has read the stage
+            if (load_pass < passes && !__any_sync(0xffffffffu, gave_up != 0)) {
+                if (lane == 0) load(slot);
+                next_load();
+            }
+            if (++slot == stages) { slot = 0; parity ^= 1u; }
         }
-        if (P.split > 1) {                                                     // (one pass)
-            __syncwarp();
-            cluster_sync();
-            const int all = P.B * (cols / 4), first = (int)((long long)all * rank / P.split), count = (int)((long long)all * (rank + 1) / P.split) - first;
-            for (int i = threadIdx.x; i < count; i += THREADS) {
-                float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-                for (int r = 0; r < P.split; r++) {
-                    float4 a;
-                    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(a.x), "=f"(a.y), "=f"(a.z), "=f"(a.w) : "r"(sums + (uint32_t)(r * count + i) * 16u) : "memory");
-                    v.x += a.x; v.y += a.y; v.z += a.z; v.w += a.w;
-                }
-                const int token = (first + i) / (cols / 4), m = m0 + (first + i - token * (cols / 4)) * 4;
-                const long long o = (long long)token * P.M + m;
-                const float t[4] = {v.x, v.y, v.z, v.w};
-                if (P.wide_out && m + 4 <= P.M) {
-                    if (P.out_dtype == VPTQ_DTYPE_FP32) *reinterpret_cast<float4 *>(reinterpret_cast<float *>(P.out) + o) = v;
-                    else *reinterpret_cast<uint2 *>(reinterpret_cast<uint16_t *>(P.out) + o) = make_uint2(pair16(v.x, v.y, P.out_dtype), pair16(v.z, v.w, P.out_dtype));
-                } else {
-                    for (int k = 0; k < 4; k++)
-                        if (m + k < P.M) store_out(P.out, o + k, t[k], P.out_dtype);
-                }
-            }
+        // the warps' sums, in warp order
+        if (p > 0) asm volatile("bar.sync 1, %0;" ::"n"(32 * WARPS) : "memory");       // the last pass's have been read
+        float *mine = part + warp * 8 * NT * stride;
+        const bool lost = __any_sync(0xffffffffu, gave_up != 0);      // (every lane's sums hold products of all lanes' operands)
+#pragma unroll
+        for (int r = 0; r < PASS; r++) {
+            if (r >= n_groups) break;
+#pragma unroll
+            for (int u = 0; u < NT; u++)
+#pragma unroll
+                for (int i = 0; i < 4; i++)
+                    mine[(8 * u + 2 * t + (i & 1)) * stride + r * GROUP + g + 8 * (i >> 1)] = lost ? __int_as_float(0x7FFFFFFF) : acc[r][u][i];
+        }
+        asm volatile("bar.sync 1, %0;" ::"n"(32 * WARPS) : "memory");
+        const int rows = n_groups * GROUP, m0 = g0 * GROUP;
+        for (int i = threadIdx.x; i < P.B * rows; i += 32 * WARPS) {
+            const int token = i / rows, m = i % rows;
+            if (m0 + m >= P.M) continue;
+            float sum = 0.f;
+#pragma unroll
+            for (int w = 0; w < WARPS; w++) sum += part[(w * 8 * NT + token) * stride + m];
+            if (!(fabsf(sum) < __int_as_float(0x7F800000))) sum = __int_as_float(0x7FFFFFFF);           // (a weight's scale that is NaN)
+            store_out(P.out, (long long)token * P.M + m0 + m, sum, P.out_dtype);
         }
     }
-    tc_fence_before();
-    __syncthreads();
-    if (*reinterpret_cast<volatile uint32_t *>(&lost)) {
+    if (gave_up) {
         let_copies_land();
-        if (threadIdx.x == 0) atomicExch(P.status, VPTQ_E_TIMEOUT);            // (long after the word was cleared)
-        __syncthreads();
-    }
-    if (warp == 1) {
-        tc_fence_after();
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(P.tmem_cols) : "memory");
+        atomicExch(D.status, VPTQ_E_TIMEOUT);                          // (long after the word was cleared)
     }
 }
 
-// ---- host side ----------------------------------------------------------------------------------------
-
-struct Plan {
-    int split, clusters, pass_groups, row_tiles, stages, tmem_cols;
-    size_t smem;
-};
-
-// what a CTA needs beside its stages
-size_t fixed_bytes(int B, int kbs, int split, int pass_groups)
+template <int DT, bool VEC, int PASS, int KB, int NT, int WARPS>
+cudaError_t run(const Fp4Linear &P, int *status, cudaStream_t st)
 {
-    const int x_rows = (B + 7) / 8 * 8, blocks = ceil_div(kbs, split);
-    size_t n = ((size_t)blocks * x_rows * KB_BYTES + 1023) / 1024 * 1024 + ((size_t)blocks * CHUNKS * x_rows * 16 + FP4_TILE_BYTES + 15) / 16 * 16;
-    if (split > 1) n += (size_t)x_rows * pass_groups * GROUP * 4 + 16 * split;
-    return n + 8 * (size_t)blocks;
-}
-
-// Split, passes and stages by estimated time.
-bool make_plan(int M, int B, int kbs, Plan *best)
-{
-    const int groups = ceil_div(M, GROUP), sms = device_sm_count();
-    double best_cost = 1e300;
-    for (int split = 1; split <= 8; split *= 2) {
-        if (split > 1 && kbs < 2 * split) continue;
-        int room = sms / split;                                                // clusters that work at a time
-        if (split > 1) {
-            const int fit = max_resident_clusters(reinterpret_cast<const void *>(linear_fp4_few_kernel<VPTQ_DTYPE_FP16, true>), split, THREADS, SMEM_MAX);
-            if (fit < 1) continue;
-            if (fit < room) room = fit;
-        }
-        Plan p;
-        p.split = split;
-        p.clusters = groups < room ? groups : room;
-        const int most = ceil_div(groups, p.clusters);
-        if (split > 1 && most > GROUPS) continue;
-        const int passes = ceil_div(most, GROUPS);
-        p.pass_groups = ceil_div(most, passes);
-        p.row_tiles = (p.pass_groups + 3 + 3) / 4;                             // (a pass begins anywhere in a scale tile)
-        const size_t stage = (size_t)(p.pass_groups + 1) * GROUP_BYTES + (size_t)p.row_tiles * SCALES, fixed = fixed_bytes(B, kbs, split, p.pass_groups);
-        const int blocks = ceil_div(kbs, split);
-        // as many stages as there are blocks, within half of an SM's memory if that is 64 KB of them, else within all of it
-        auto fit = [&](size_t limit) { return limit > fixed ? (int)((limit - fixed) / stage) : 0; };
-        int stages = fit(HALF_SMEM);
-        if (stages < passes * blocks && stages * stage < 64 * 1024) stages = fit(SMEM_MAX);
-        if (stages > MAX_STAGES) stages = MAX_STAGES;
-        if (stages > passes * blocks) stages = passes * blocks;
-        while (stages * stage < (size_t)MIN_RING) stages++;                    // (never beyond MAX_STAGES: a stage has 9 KB at least)
-        if (stages < 1 || fixed + stages * stage > (size_t)SMEM_MAX || (stages < 2 && passes * blocks > 1)) continue;
-        p.stages = stages;
-        p.smem = fixed + stages * stage;
-        p.tmem_cols = 32;
-        while (p.tmem_cols < (p.pass_groups + 1) * GROUP + 64) p.tmem_cols *= 2;
-        if (p.tmem_cols > 256 && p.smem < (size_t)WHOLE_SMEM) p.smem = WHOLE_SMEM;
-        const double cost = (double)most * blocks + (split > 1 ? 8 : 0);       // groups of features by blocks of columns, 0.1 us each; the meeting 0.8 us
-        if (cost < best_cost) { best_cost = cost; *best = p; }
+    constexpr int MAX_TILES = (PASS * GROUP + 2 * FP4_TILE_ROWS - GROUP - 1) / FP4_TILE_ROWS;
+    const long long pitch = fp4_row_bytes(P.N);
+    const int groups = ceil_div(P.M, GROUP), sms = device_sm_count(), grid = groups < sms ? groups : sms, kbs = ceil_div(P.N, KB);
+    const int most = ceil_div(groups, grid);              // groups of a CTA
+    FewParams D;
+    D.L = P;
+    D.col_tiles = ceil_div(P.N, FP4_TILE_COLS);
+    D.passes = ceil_div(most, PASS);
+    D.stage_groups = ceil_div(most, D.passes);
+    D.status = status;
+    D.zero = 0;
+    D.wait_limit = wait_limit();
+    const int stage = D.stage_groups * group_bytes(KB) + MAX_TILES * tile_bytes(KB);
+    const int fixed = WARPS * 8 * NT * part_stride(D.stage_groups) * 4 + WARPS * MAX_STAGES * 8;
+    D.stages = (SMEM_MAX - fixed) / (WARPS * stage);
+    if (D.stages > MAX_STAGES) D.stages = MAX_STAGES;
+    const long long loads = (long long)ceil_div(kbs, WARPS) * D.passes;
+    if (D.stages > loads) D.stages = (int)loads;
+    const int smem = D.stages * WARPS * stage + fixed;
+    CUtensorMap map[2], map_scales;
+    for (int i = 0; i < 2; i++) {
+        const int rows = GROUP * (D.stage_groups - i > 0 ? D.stage_groups - i : 1);
+        if (!encode_tensor_map(&map[i], CU_TENSOR_MAP_DATA_TYPE_UINT8, P.w, pitch, P.M, pitch, 0, 0, KB / 2, rows, 1, KB == 256 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B))
+            return cudaErrorNotSupported;
     }
-    return best_cost < 1e300;
-}
-
-template <int DT, bool VEC>
-cudaError_t run(const Fp4Linear &L, const Plan &p, const Params &P, cudaStream_t st)
-{
-    CUtensorMap map_w, map_ws;
-    const long long pitch = fp4_row_bytes(L.N);
-    const uint64_t tiles = (uint64_t)(fp4_scale_bytes(L.M, L.N) / FP4_TILE_BYTES);
-    if (!encode_tensor_map(&map_w, CU_TENSOR_MAP_DATA_TYPE_UINT8, L.w, pitch, L.M, pitch, 0, 0, KB_BYTES, GROUP, 1, CU_TENSOR_MAP_SWIZZLE_128B) ||
-        !encode_tensor_map(&map_ws, CU_TENSOR_MAP_DATA_TYPE_UINT32, L.w_scale, FP4_TILE_BYTES / 4, tiles, FP4_TILE_BYTES, 0, 0, FP4_TILE_BYTES / 4, CHUNKS, 1,
-                           CU_TENSOR_MAP_SWIZZLE_NONE))
+    if (!encode_tensor_map(&map_scales, CU_TENSOR_MAP_DATA_TYPE_UINT32, P.w_scale, FP4_TILE_BYTES / 4, (uint64_t)(fp4_scale_bytes(P.M, P.N) / FP4_TILE_BYTES), FP4_TILE_BYTES, 0, 0,
+                           FP4_TILE_BYTES / 4, KB / FP4_TILE_COLS, 1, CU_TENSOR_MAP_SWIZZLE_NONE))
         return cudaErrorNotSupported;
-    auto kern = linear_fp4_few_kernel<DT, VEC>;
+    auto kern = linear_fp4_few_kernel<DT, VEC, PASS, KB, NT, WARPS>;
     const cudaError_t e = allow_dynamic_smem(reinterpret_cast<const void *>(kern), SMEM_MAX);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(p.clusters * p.split));
-    cfg.blockDim = dim3(THREADS);
-    cfg.dynamicSmemBytes = p.smem;
+    cfg.gridDim = dim3((unsigned)grid);
+    cfg.blockDim = dim3(32 * WARPS);
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
-    cudaLaunchAttribute attr[2];
-    int n = 0;
-    if (p.split > 1) {
-        attr[n].id = cudaLaunchAttributeClusterDimension;
-        attr[n].val.clusterDim.x = (unsigned)p.split; attr[n].val.clusterDim.y = 1; attr[n].val.clusterDim.z = 1;
-        n++;
-    }
-    if (pdl_enabled("linear_fp4")) {
-        attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        attr[n].val.programmaticStreamSerializationAllowed = 1;
-        n++;
-    }
-    cfg.attrs = attr; cfg.numAttrs = n;
-    return cudaLaunchKernelEx(&cfg, kern, map_w, map_ws, P);
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr; cfg.numAttrs = pdl_enabled("linear_fp4") ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, kern, map[0], map[1], map_scales, D);
 }
+
+// Up to two groups a CTA, in one pass: 16-bit activations are quantized on the way.  More, in passes of four: blocks of half as many columns, so that
+// two stages a warp fit.
+template <int DT, bool VEC, int NT>
+cudaError_t run_small(const Fp4Linear &P, int *status, cudaStream_t st) { return run<DT, VEC, 2, 256, NT, 16>(P, status, st); }
+template <int NT>
+cudaError_t run_large(const Fp4Linear &P, int *status, cudaStream_t st) { return run<VPTQ_DTYPE_E2M1, true, 4, 128, NT, 16>(P, status, st); }
+bool small(int M) { return ceil_div(M, GROUP) <= 2 * device_sm_count(); }
 
 }  // namespace
 
-bool linear_fp4_few_takes(int M, int N, int B)
-{
-    Plan p;
-    return B <= FP4_FEW_MAX_B && make_plan(M, B, ceil_div(N, KB), &p);
-}
+bool linear_fp4_few_quantizes(int M, int B) { return B <= 8 && small(M); }
 
-cudaError_t launch_linear_fp4_few(const Fp4Linear &L, int *status, cudaStream_t st)
+cudaError_t launch_linear_fp4_few(const Fp4Linear &P, int *status, cudaStream_t st)
 {
-    Plan p;
-    const int kbs = ceil_div(L.N, KB);
-    if (L.B > FP4_FEW_MAX_B || !make_plan(L.M, L.B, kbs, &p)) return cudaErrorNotSupported;
-    Params P;
-    P.M = L.M; P.N = L.N; P.B = L.B; P.kbs = kbs;
-    P.last_steps = ceil_div(L.N - (kbs - 1) * KB, 64);
-    P.col_tiles = ceil_div(L.N, FP4_TILE_COLS);
-    P.groups = ceil_div(L.M, GROUP); P.split = p.split;
-    P.pass_groups = p.pass_groups; P.row_tiles = p.row_tiles; P.stages = p.stages; P.x_rows = (L.B + 7) / 8 * 8; P.tmem_cols = p.tmem_cols;
-    P.x = L.x; P.x_scale = L.x_scale; P.out = L.out; P.out_dtype = L.out_dtype;
-    P.wide_out = (long long)L.M * (L.out_dtype == VPTQ_DTYPE_FP32 ? 4 : 2) % 16 == 0 ? 1 : 0;
-    P.status = status; P.wait_limit = wait_limit();
-    const bool vec = (reinterpret_cast<uintptr_t>(L.x) & 15u) == 0 && L.N % 8 == 0;
-    switch (L.x_dtype) {
-    case VPTQ_DTYPE_E2M1: return run<VPTQ_DTYPE_E2M1, true>(L, p, P, st);
-    case VPTQ_DTYPE_FP16: return vec ? run<VPTQ_DTYPE_FP16, true>(L, p, P, st) : run<VPTQ_DTYPE_FP16, false>(L, p, P, st);
-    default: return vec ? run<VPTQ_DTYPE_BF16, true>(L, p, P, st) : run<VPTQ_DTYPE_BF16, false>(L, p, P, st);
-    }
+    if (!small(P.M)) return P.B > 8 ? run_large<2>(P, status, st) : run_large<1>(P, status, st);
+    const bool vec = P.N % 8 == 0 && (reinterpret_cast<uintptr_t>(P.x) & 15u) == 0;
+    if (P.x_dtype == VPTQ_DTYPE_E2M1) return P.B > 8 ? run_small<VPTQ_DTYPE_E2M1, true, 2>(P, status, st) : run_small<VPTQ_DTYPE_E2M1, true, 1>(P, status, st);
+    if (P.x_dtype == VPTQ_DTYPE_BF16) return vec ? run_small<VPTQ_DTYPE_BF16, true, 1>(P, status, st) : run_small<VPTQ_DTYPE_BF16, false, 1>(P, status, st);
+    return vec ? run_small<VPTQ_DTYPE_FP16, true, 1>(P, status, st) : run_small<VPTQ_DTYPE_FP16, false, 1>(P, status, st);
 }
 
 }  // namespace vptq

@@ -772,14 +772,14 @@ int vptq_linear_fp4(const vptq_fp4_desc *desc, const void *x, const uint8_t *x_s
 const char *vptq_linear_fp4_path(const vptq_fp4_desc *desc, int32_t B)
 {
     if (check_fp4_desc(desc, B) != VPTQ_OK) return "invalid";
-    return linear_fp4_path(desc->M, desc->N, B);
+    return linear_fp4_path(B);
 }
 
 int vptq_linear_fp4_launches(const vptq_fp4_desc *desc, int32_t B)
 {
     const int rc = check_fp4_desc(desc, B);
     if (rc != VPTQ_OK) return rc;
-    return linear_fp4_launches(desc->M, desc->N, B, desc->x_dtype);
+    return linear_fp4_launches(desc->M, B, desc->x_dtype);
 }
 
 int64_t vptq_cache_row_bytes(int32_t head_dim, int32_t cache_dtype)

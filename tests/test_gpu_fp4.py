@@ -208,8 +208,7 @@ def test_linear_of_many_shapes(b, M, N, B):
     assert same(y, b.vptq_linear_fp4(q, w, ws, x_scale=s, out_dtype="fp32"))            # bit for bit the same every time
 
 
-# (few tokens: a cluster's CTAs share the columns or not, one pass over the features or several, features that begin and end inside a tile of scales,
-# results whose rows are not aligned, and so many columns that the other kernel is taken)
+# (few tokens: less than a block of columns a warp and many, one pass over the features or several, passes that begin and end inside a tile of scales)
 @pytest.mark.parametrize("B", [1, 2, 7, 8, 9, 15, 16])
 @pytest.mark.parametrize("M,N", [(1, 64), (32, 8192), (33, 2560), (100, 5000), (1024, 1000), (1001, 4096), (4100, 1100), (4736, 300), (9000, 640), (28672, 512), (37888, 260),
                                  (40001, 130), (80000, 256), (300, 40000), (5000, 17000)])
@@ -224,9 +223,10 @@ def test_linear_of_few_tokens(b, M, N, B):
 
 
 def test_linear_paths(b):
-    path = lambda M, N, B: b.vptq_linear_fp4_path(b.make_fp4_desc(M, N), B)  # noqa: E731
-    assert [path(4096, 4096, B) for B in (1, 16, 17, 300)] == ["fp4_few"] * 2 + ["fp4_tcgen05"] * 2
-    assert path(28672, 8192, 16) == path(8192, 14336, 16) == "fp4_few" and path(300, 10 ** 6, 16) == "fp4_tcgen05"
+    for x, launches in (("fp16", [1, 1, 2, 2, 2]), ("e2m1", [1, 1, 1, 1, 1])):
+        d = b.make_fp4_desc(4096, 4096, x)
+        assert [b.vptq_linear_fp4_path(d, B) for B in (1, 8, 16, 17, 300)] == ["fp4_few"] * 3 + ["fp4_tcgen05"] * 2
+        assert [b.vptq_linear_fp4_launches(d, B) for B in (1, 8, 16, 17, 300)] == launches
 
 
 def test_linear_of_every_scale(b):
