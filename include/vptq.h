@@ -552,11 +552,10 @@ int vptq_dequant_fp4(const vptq_layer_desc *desc, const vptq_layer_ptrs *p, uint
  *   every pointer is 16-byte aligned (VPTQ_E_ALIGN), but for x of 16 bits: any alignment of a value;  out_dtype FP16, BF16 or FP32
  *   flags: VPTQ_FLAG_CONCURRENT and VPTQ_FLAG_DETERMINISTIC are accepted and change nothing (no CTA waits for another launch's, every
  *           sum has a fixed order).
- * At most 16 tokens take the kernel "fp4_few" (which may quantize them itself), more "fp4_tcgen05" (vptq_linear_fp4_path).  A sum
- * that overflows FP32 is an infinity or a NaN.
- * The workspace, 256-byte aligned, starts with a status word (vptq_workspace_status); its contents on entry are irrelevant, calls that may
- * overlap must not share one.  All device-side waits are bounded: one that gives up leaves NaN in the results that it concerns and
- * VPTQ_E_TIMEOUT in the status word. */
+ * At most 8 tokens of 16 bits over a small weight (N <= 4096, M at most 32 rows to an SM) take the kernel "fp4_few" (no workspace), all others
+ * "fp4_tcgen05" (vptq_linear_fp4_path), whose workspace, 256-byte aligned, starts with a status word (vptq_workspace_status); its contents on entry
+ * are irrelevant, calls that may overlap must not share one.  All device-side waits are bounded: one that gives up leaves NaN in the results that it
+ * concerns and, with "fp4_tcgen05", VPTQ_E_TIMEOUT in the status word.  A sum that overflows FP32 is an infinity or a NaN. */
 typedef struct vptq_fp4_desc {
     int32_t M, N;        /* out_features, in_features */
     int32_t x_dtype;     /* VPTQ_DTYPE_E2M1, _FP16 or _BF16 */
@@ -609,8 +608,8 @@ int vptq_cache_read(const vptq_cache_desc *desc, const vptq_cache_ptrs *p, void 
 
 const char *vptq_status_string(int code);
 const char *vptq_last_cuda_error(void);
-/* Six kernels — the batched tensor-core kernel and the one over prepared images, behind vptq_linear and
- * vptq_linear_fused, "assign_tcgen05" behind vptq_assign, "fp8_tcgen05" behind vptq_linear_fp8 — and the two behind vptq_linear_fp4 keep an int32 status word at
+/* Five kernels — the batched tensor-core kernel and the one over prepared images, behind vptq_linear and
+ * vptq_linear_fused, "assign_tcgen05" behind vptq_assign, "fp8_tcgen05" behind vptq_linear_fp8 and "fp4_tcgen05" behind vptq_linear_fp4 — keep an int32 status word at
  * byte 0 of their workspace; vptq_linear_has_status() and vptq_linear_fused_has_status() tell for which calls of the first two.  After any other call the workspace holds
  * no status and this call has no meaning.  It synchronises `stream`, reads the word and returns VPTQ_E_TIMEOUT if a
  * bounded device-side wait gave up during the call (the output is then invalid; the context stays
@@ -628,7 +627,7 @@ int vptq_linear_fused_has_status(const vptq_layer_desc *descs, int32_t n_layers,
  * (0 restores the default).  With a limit of a few cycles a healthy kernel abandons its first wait that is
  * not already satisfied, reports VPTQ_E_TIMEOUT in its status word, leaves no copy in flight and returns;
  * the context stays usable.  Honoured by the path "decode_bucket_fma", by vptq_linear_fp8, vptq_linear_fp4 and
- * vptq_moe_fp8; "fp8_decode" and vptq_moe_fp8 have no status word and leave NaN in the results.  Process-wide; not for production. */
+ * vptq_moe_fp8; "fp8_decode", "fp4_few" and vptq_moe_fp8 have no status word and leave NaN in the results.  Process-wide; not for production. */
 void vptq_debug_set_wait_limit(uint64_t cycles);
 /* 1 when the kernels of vptq_linear / vptq_linear_fused for these arguments let one CTA wait for a flag that another CTA of
  * the same grid raises, 0 when no CTA waits for another, negative VPTQ_E_* on bad arguments.  Only the tensor-core kernel

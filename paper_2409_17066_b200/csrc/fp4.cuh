@@ -33,8 +33,8 @@ struct Fp4Linear {
     void *out;
 };
 long long linear_fp4_workspace_bytes(int M, int N, int B, int x_dtype);
-int linear_fp4_launches(int M, int B, int x_dtype);
-const char *linear_fp4_path(int B);
+int linear_fp4_launches(int M, int N, int B, int x_dtype);
+const char *linear_fp4_path(int M, int N, int B, int x_dtype);
 cudaError_t launch_linear_fp4(const Fp4Linear &P, void *ws, cudaStream_t st);
 
 #ifdef __CUDACC__

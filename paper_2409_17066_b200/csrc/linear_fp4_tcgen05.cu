@@ -13,6 +13,8 @@
 // tile's rows in rank order: one launch, no scratch, and a result that does not depend on timing.
 // Every wait is bounded.  A warp whose wait gives up stops: it loads, multiplies or hands on nothing more, so that the waits that depend
 // on it run out too and no sum is made of what has not arrived.  The results of a CTA with a wait that gave up are NaN, and the workspace's status word is set.
+#include <math.h>
+
 #include "fp4.cuh"
 #include "fp4_tcgen05.cuh"
 #include "tcgen05_pair.cuh"
@@ -30,31 +32,35 @@ constexpr int ACC_WARP0 = 4, ACC_WARPS = 8;
 constexpr int THREADS = 32 * (ACC_WARP0 + ACC_WARPS);
 // Registers: 12 warps of 168 at launch; the first four give some up, the others hold up to 128 sums a lane (4 x 104 + 8 x 200 = 12 x 168).
 constexpr int FEW_REGS = 104, ACC_REGS = 200;
-constexpr int X_BYTES = TM * KB_BYTES;                    // a stage's activations
-constexpr int SCALES = CHUNKS * FP4_TILE_BYTES;           // ... and the scales of 128 rows
-constexpr int STAGING = 2048;                             // per accumulating warp: 32 rows x 16 columns on their way out
+constexpr int SCALES = CHUNKS * FP4_TILE_BYTES;           // of 128 rows, along a stage
+constexpr int STAGING = 4096;                             // per accumulating warp: 32 rows of 128 bytes on their way out
 constexpr int SMEM_MAX = 232448 - 1024;                  // (the static part takes a multiple of the dynamic part's alignment)
 constexpr int BARRIERS = 256;
 constexpr int FIXED_BYTES = ACC_WARPS * STAGING + BARRIERS;
 
 // 128-row tiles of the weight's scales that a tile's features lie in
 template <int TN> constexpr int row_tiles() { return TN > 128 ? 2 : 1; }
-// a CTA's part of a stage: its tokens, the tile's features or (pairs) half of them, scales of its tokens and of all of the tile's features
-template <int TN, int PAIR> constexpr int stage_bytes() { return X_BYTES + TN / PAIR * KB_BYTES + (1 + row_tiles<TN>()) * SCALES; }
-template <int TN, int PAIR> constexpr int stages()
+// a CTA's part of a stage beside its tokens: the tile's features or (pairs) half of them, scales of 128 tokens and of all of the tile's features
+template <int TN, int PAIR> constexpr int weight_bytes() { return TN / PAIR * KB_BYTES + (1 + row_tiles<TN>()) * SCALES; }
+// stages that fit, at most MAX_STAGES.  Few tokens take less of a stage: an MMA reads 128 rows all the same, into what follows (behind the last stage that
+// is the staging), for sums that nobody reads.
+constexpr int MAX_STAGES = 12;
+template <int TN, int PAIR> constexpr int stages(int x_bytes)
 {
-    const int n = (SMEM_MAX - FIXED_BYTES) / stage_bytes<TN, PAIR>();
-    return n < 8 ? n : 8;
+    const int n = (SMEM_MAX - FIXED_BYTES) / (x_bytes + weight_bytes<TN, PAIR>());
+    return n < MAX_STAGES ? n : MAX_STAGES;
 }
-template <int TN, int PAIR> constexpr int smem_bytes() { return stages<TN, PAIR>() * stage_bytes<TN, PAIR>() + FIXED_BYTES; }
 // TMEM columns: one buffer of sums, or two; behind them two of scales, taken in turn by the stages
-template <int TN> constexpr int buffers() { return TN <= 192 ? 2 : 1; }
+template <int TN> constexpr int buffers() { return TN <= 128 ? 2 : 1; }
+// features that an accumulating warp takes: at least a piece of 128 bytes of 16-bit results (a tile of 64: four of the warps take all)
+template <int TN> constexpr int count() { return TN >= 128 ? TN / 2 : TN; }
 constexpr int SCALE_COLS = 32;
 
 struct Params {
     int M, B, kbs, last_steps;
     int col_tiles;                         // scale tiles along a row of 128-row tiles
     int tiles_t, tiles;
+    int x_bytes, stage_bytes, stages;      // of a CTA's part of a stage: activations, all of it; stages of the ring
     void *out;
     int out_dtype;
     int tma_out;           // rows of `out` are 16-byte aligned: stored by TMA
@@ -99,19 +105,48 @@ struct Sums {
     int t_rank;                            // pairs: this CTA's tokens of a tile start at t_rank * TM
 };
 
-// Half a tile's features, from c_first on, of the 32 tokens of lane quarter q.
+// 128 bytes of features from `col` on of 32 tokens from `row` on; `chunk` gives a lane's 16 bytes at place c of its row
+template <bool WIDE, typename Chunk>
+__device__ __forceinline__ void store_piece(const CUtensorMap &map_out, const Params &P, const Sums &S, int lane, int row, int col, Chunk chunk)
+{
+    constexpr int SIZE = WIDE ? 4 : 2, COLS = 128 / SIZE;
+    if (P.tma_out && lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+    __syncwarp();
+#pragma unroll
+    for (int c = 0; c < 8; c++) *reinterpret_cast<uint4 *>(S.staging_p + lane * 128 + ((c ^ (lane & 7)) << 4)) = chunk(c);
+    if (P.tma_out) {
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) {
+            if (col < P.M) tma_store(&map_out, S.staging, col, row);
+            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+        }
+    } else {
+        __syncwarp();
+        for (int r = 0; r < 32 && row + r < P.B; r++)
+            for (int c = lane; c < COLS && col + c < P.M; c += 32) {
+                const uint8_t *v = S.staging_p + r * 128 + ((c * SIZE / 16 ^ (r & 7)) << 4) + c * SIZE % 16;
+                const long long o = (long long)(row + r) * P.M + col + c;
+                if (WIDE) reinterpret_cast<float *>(P.out)[o] = *reinterpret_cast<const float *>(v);
+                else reinterpret_cast<uint16_t *>(P.out)[o] = *reinterpret_cast<const uint16_t *>(v);
+            }
+        __syncwarp();
+    }
+}
+
+// count<TN>() of a tile's features, from c_first on, of the 32 tokens of lane quarter q.
 template <int TN, int SPLIT, int PAIR>
 __device__ __forceinline__ void finish_tiles(const CUtensorMap &map_out, const Params &P, const Sums &S, int c_first, int q, int lane, uint32_t &gave_up)
 {
-    constexpr int COUNT = TN / 2, PIECES = COUNT / 16, BUF = buffers<TN>();
-    uint32_t it = 0, pieces = 0;
+    constexpr int COUNT = count<TN>(), PIECES = COUNT / 16, BUF = buffers<TN>();
+    uint32_t it = 0;
     for (int tile = S.first; tile < P.tiles; tile += S.step, it++) {
         const int t0 = (tile % P.tiles_t * PAIR + S.t_rank) * TM, n0 = tile / P.tiles_t * TN;
         const uint32_t buf = it % BUF;
         uint32_t d[PIECES][16];
         mbar_wait_or_flag(S.acc_full + 8 * buf, (it / BUF) & 1, S.lost_at, gave_up);
         tc_fence_after();
-        const bool any = t0 + 32 * q < P.B;                                // (the same for the warp's lanes)
+        const bool any = t0 + 32 * q < P.B && c_first < TN;                // (the same for the warp's lanes)
         if (any) {
 #pragma unroll
             for (int j = 0; j < PIECES; j++) tmem_start16(S.tmem + buf * TN + 16 * j, d[j]);
@@ -138,49 +173,25 @@ __device__ __forceinline__ void finish_tiles(const CUtensorMap &map_out, const P
                 }
             }
         } else {
-            // 16 features at a time through the warp's staging rows (32 or 64 bytes, swizzled as the store's map says)
-            const bool wide = P.out_dtype == VPTQ_DTYPE_FP32;
+            // through the warp's staging rows, 128 bytes (64 or 32 features) at a time, swizzled as the store's map says.  (In rows of 32 bytes the
+            // copies out took 2.4 us for a tile of 256 features, of 128 XXX.)
+            const int row = t0 + 32 * q, col = n0 + c_first;
+            if (P.out_dtype == VPTQ_DTYPE_FP32) {
 #pragma unroll
-            for (int j = 0; j < PIECES; j++) {
-                // (16-bit pieces take turns at two halves of the staging; every piece is a group of its own, stored or not)
-                const uint32_t at = wide ? 0u : (pieces++ & 1) * (STAGING / 2);
-                if (P.tma_out && lane == 0) {
-                    if (wide) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-                    else asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
-                }
-                __syncwarp();
-                if (wide) {
+                for (int j = 0; j < PIECES; j += 2)
+                    store_piece<true>(map_out, P, S, lane, row, col + 16 * j, [&](int c) {
+                        const uint32_t *v = d[j + c / 4] + c % 4 * 4;
+                        return make_uint4(v[0], v[1], v[2], v[3]);
+                    });
+            } else {
 #pragma unroll
-                    for (int c = 0; c < 4; c++)
-                        *reinterpret_cast<uint4 *>(S.staging_p + lane * 64 + ((c ^ ((lane >> 1) & 3)) << 4)) = make_uint4(d[j][4 * c], d[j][4 * c + 1], d[j][4 * c + 2], d[j][4 * c + 3]);
-                } else {
-#pragma unroll
-                    for (int c = 0; c < 2; c++) {
+                for (int j = 0; j < PIECES; j += 4)
+                    store_piece<false>(map_out, P, S, lane, row, col + 16 * j, [&](int c) {
                         uint32_t h[4];
 #pragma unroll
-                        for (int i = 0; i < 4; i++) h[i] = pair16(__uint_as_float(d[j][8 * c + 2 * i]), __uint_as_float(d[j][8 * c + 2 * i + 1]), P.out_dtype);
-                        *reinterpret_cast<uint4 *>(S.staging_p + at + lane * 32 + ((c ^ ((lane >> 2) & 1)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
-                    }
-                }
-                const int col = n0 + c_first + 16 * j;
-                if (P.tma_out) {
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                    __syncwarp();
-                    if (lane == 0) {
-                        if (col < P.M) tma_store(&map_out, S.staging + at, col, t0 + 32 * q);
-                        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-                    }
-                } else {
-                    __syncwarp();
-                    const int c = lane & 15;
-                    for (int r = lane >> 4; r < 32 && t0 + 32 * q + r < P.B; r += 2) {
-                        if (col + c >= P.M) break;
-                        const long long o = (long long)(t0 + 32 * q + r) * P.M + col + c;
-                        if (wide) reinterpret_cast<float *>(P.out)[o] = *reinterpret_cast<const float *>(S.staging_p + r * 64 + (((c >> 2) ^ ((r >> 1) & 3)) << 4) + (c & 3) * 4);
-                        else reinterpret_cast<uint16_t *>(P.out)[o] = *reinterpret_cast<const uint16_t *>(S.staging_p + at + r * 32 + (((c >> 3) ^ ((r >> 2) & 1)) << 4) + (c & 7) * 2);
-                    }
-                    __syncwarp();
-                }
+                        for (int i = 0; i < 4; i++) h[i] = pair16(__uint_as_float(d[j + c / 2][c % 2 * 8 + 2 * i]), __uint_as_float(d[j + c / 2][c % 2 * 8 + 2 * i + 1]), P.out_dtype);
+                        return make_uint4(h[0], h[1], h[2], h[3]);
+                    });
             }
             // a lane that gave up went on without handing anything on; the warp's sums are no good whichever lane it was
             if (__any_sync(0xffffffffu, load_word(S.lost_at) != 0)) {
@@ -199,24 +210,26 @@ __global__ void __launch_bounds__(THREADS, 1)
 linear_fp4_tcgen05_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_xs,
                           const __grid_constant__ CUtensorMap map_ws, const __grid_constant__ CUtensorMap map_out, const __grid_constant__ Params P)
 {
-    constexpr int ST = stages<TN, PAIR>(), SB = stage_bytes<TN, PAIR>(), RT = row_tiles<TN>(), BUF = buffers<TN>();
-    constexpr uint32_t XS_AT = X_BYTES + TN / PAIR * KB_BYTES, WS_AT = XS_AT + SCALES;          // of a stage: activations, weight, their scales
+    constexpr int RT = row_tiles<TN>(), BUF = buffers<TN>();
+    // of a stage: activations, weight, their scales
+    const uint32_t ST = P.stages, SB = P.stage_bytes, W_AT = P.x_bytes, XS_AT = W_AT + TN / PAIR * KB_BYTES, WS_AT = XS_AT + SCALES;
     extern __shared__ __align__(1024) uint8_t sm[];
     __shared__ uint32_t tmem_slot, lost;                  // lost: a wait of this CTA gave up (of a pair: of either)
     const uint32_t base = smem_addr(sm), staging0 = base + ST * SB, bars = staging0 + FIXED_BYTES - BARRIERS;
     auto bar_full = [&](int s) { return bars + 8u * s; };
-    auto bar_empty = [&](int s) { return bars + 8u * (ST + s); };
-    auto bar_acc_full = [&](int b) { return bars + 8u * (2 * ST + b); };
-    auto bar_acc_empty = [&](int b) { return bars + 8u * (2 * ST + 2 + b); };
+    auto bar_empty = [&](int s) { return bars + 8u * (MAX_STAGES + s); };
+    auto bar_acc_full = [&](int b) { return bars + 8u * (2 * MAX_STAGES + b); };
+    auto bar_acc_empty = [&](int b) { return bars + 8u * (2 * MAX_STAGES + 2 + b); };
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
     if (threadIdx.x == 0) {
         lost = 0;
-        for (int s = 0; s < ST; s++) { mbar_init(bar_full(s), 1); mbar_init(bar_empty(s), 1); }
+        for (uint32_t s = 0; s < ST; s++) { mbar_init(bar_full(s), 1); mbar_init(bar_empty(s), 1); }
         for (int b = 0; b < BUF; b++) { mbar_init(bar_acc_full(b), 1); mbar_init(bar_acc_empty(b), PAIR * ACC_WARPS); }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) tmem_alloc_all<PAIR>(smem_addr(&tmem_slot));
+    if (warp == 0 && elect_one()) { prefetch_map(&map_w); prefetch_map(&map_ws); prefetch_map(&map_x); prefetch_map(&map_xs); }
     tc_fence_before();
     __syncthreads();
     if constexpr (PAIR == 2) cluster_sync();              // the other CTA's barriers are ready, and its half of TMEM
@@ -242,46 +255,45 @@ linear_fp4_tcgen05_kernel(const __grid_constant__ CUtensorMap map_x, const __gri
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(FEW_REGS));
         if (warp == 0) {
             // ---- loads: this CTA's tokens, and its part of the tile's features; the bytes of a pair count on rank 0's barrier ----
-            uint32_t it = 0;
+            uint32_t s = 0, round = 0;
             const uint32_t full0 = PAIR > 1 ? address_in(bar_full(0), 0) : bar_full(0);
             const int n_part = t_rank * (TN / PAIR);
             pdl_wait();                                                        // (weight and activations may be the preceding kernel's)
             for (int tile = first; tile < P.tiles; tile += step) {
                 const int t0 = (tile % P.tiles_t * PAIR + t_rank) * TM, n0 = tile / P.tiles_t * TN;
-                for (int kb = kb0; kb < kb1; kb++, it++) {
-                    const uint32_t s = it % ST;
-                    mbar_wait_or_flag(bar_empty(s), ((it / ST) & 1) ^ 1u, lost_at, gave_up);
+                for (int kb = kb0; kb < kb1; kb++) {
+                    mbar_wait_or_flag(bar_empty(s), (round & 1) ^ 1u, lost_at, gave_up);
                     if (elect_one() && !gave_up) {
                         const uint32_t at = base + s * SB, full = full0 + 8 * s;
                         if (t_rank == 0) mbar_expect_tx(bar_full(s), PAIR * SB);
-                        tma_load<PAIR>(at + X_BYTES, &map_w, kb * KB_BYTES, n0 + n_part, full);
+                        tma_load<PAIR>(at + W_AT, &map_w, kb * KB_BYTES, n0 + n_part, full);
 #pragma unroll
                         for (int r = 0; r < RT; r++) tma_load<PAIR>(at + WS_AT + r * SCALES, &map_ws, 0, (n0 / FP4_TILE_ROWS + r) * P.col_tiles + kb * CHUNKS, full);
                         tma_load<PAIR>(at, &map_x, kb * KB_BYTES, t0, full);
                         tma_load<PAIR>(at + XS_AT, &map_xs, 0, t0 / FP4_TILE_ROWS * P.col_tiles + kb * CHUNKS, full);
                     }
                     __syncwarp();
+                    if (++s == ST) { s = 0; round++; }
                 }
             }
         } else if (warp == 1) {
             // ---- scales to TMEM, then MMAs: e2m1 x e2m1 -> FP32, both K-major; of a pair, rank 0's over the memory of both ----
             constexpr uint32_t IDESC = (1u << 7) | (1u << 10) | ((uint32_t)(TN >> 3) << 17) | (1u << 23) | ((uint32_t)(PAIR * TM >> 4) << 24);
-            const uint64_t a0 = make_smem_desc(base, 16, 1024, LAYOUT_SW128), b0 = make_smem_desc(base + X_BYTES, 16, 1024, LAYOUT_SW128);
+            const uint64_t a0 = make_smem_desc(base, 16, 1024, LAYOUT_SW128), b0 = make_smem_desc(base + W_AT, 16, 1024, LAYOUT_SW128);
             const uint64_t as0 = make_smem_desc(base + XS_AT, 16, 128, 0), bs0 = make_smem_desc(base + WS_AT, 16, 128, 0);
-            uint32_t it = 0, n = 0;
+            uint32_t s = 0, round = 0, turn = 0, n = 0;
             pdl_wait();                                                        // (a wait's time does not begin before the preceding kernel has ended)
             for (int tile = first; tile < P.tiles && t_rank == 0; tile += step, n++) {
                 const uint32_t buf = n % BUF, d = tmem + buf * TN;
                 // where the tile's features begin in their first scale tile: four columns hold 128 rows, 32 in each
                 const uint32_t inside = (uint32_t)(tile / P.tiles_t * TN) % FP4_TILE_ROWS / 32;
                 mbar_wait_or_flag(bar_acc_empty(buf), ((n / BUF) & 1) ^ 1u, lost_at, gave_up);
-                for (int kb = kb0; kb < kb1; kb++, it++) {
-                    const uint32_t s = it % ST;
-                    mbar_wait_flagged(bar_full(s), (it / ST) & 1, P.wait_limit, lost_at, gave_up);
+                for (int kb = kb0; kb < kb1; kb++, turn ^= 1) {
+                    mbar_wait_flagged(bar_full(s), round & 1, P.wait_limit, lost_at, gave_up);
                     tc_fence_after();
                     if (elect_one() && !gave_up) {
                         const uint64_t at = (uint64_t)((s * SB) >> 4);
-                        const uint32_t xs = tmem + BUF * TN + (it & 1) * SCALE_COLS, ws = xs + 4 * CHUNKS;
+                        const uint32_t xs = tmem + BUF * TN + turn * SCALE_COLS, ws = xs + 4 * CHUNKS;
                         const int steps = kb == P.kbs - 1 ? P.last_steps : STEPS;
 #pragma unroll
                         for (int c = 0; c < CHUNKS; c++) {
@@ -301,6 +313,7 @@ linear_fp4_tcgen05_kernel(const __grid_constant__ CUtensorMap map_x, const __gri
                         if (kb == kb1 - 1) commit<PAIR>(bar_acc_full(buf));
                     }
                     __syncwarp();
+                    if (++s == ST) { s = 0; round++; }
                 }
             }
         }
@@ -315,9 +328,9 @@ linear_fp4_tcgen05_kernel(const __grid_constant__ CUtensorMap map_x, const __gri
         const int w = warp - ACC_WARP0, q = warp & 3, share = w >> 2;          // TMEM lane quarter this warp may read, its part of the features
         pdl_wait();                                                            // (the result, and the status word, may be the preceding kernel's)
         if (blockIdx.x == 0 && threadIdx.x == 32 * ACC_WARP0) *P.status = 0;
-        const Sums S = {tmem + ((uint32_t)(32 * q) << 16) + share * (TN / 2), staging0 + w * STAGING, sm + ST * SB + w * STAGING, sm, lost_at,
+        const Sums S = {tmem + ((uint32_t)(32 * q) << 16) + share * count<TN>(), staging0 + w * STAGING, sm + ST * SB + w * STAGING, sm, lost_at,
                         bar_acc_full(0), PAIR > 1 ? address_in(bar_acc_empty(0), 0) : bar_acc_empty(0), first, step, t_rank};
-        finish_tiles<TN, SPLIT, PAIR>(map_out, P, S, share * (TN / 2), q, lane, gave_up);
+        finish_tiles<TN, SPLIT, PAIR>(map_out, P, S, share * count<TN>(), q, lane, gave_up);
         report();
         if constexpr (SPLIT > 1) {
             cluster_sync();
@@ -389,20 +402,25 @@ cudaError_t run(const Fp4Linear &L, const Params &P0, cudaStream_t st)
     Params P = P0;
     const long long pitch = fp4_row_bytes(L.N), out_bytes = L.out_dtype == VPTQ_DTYPE_FP32 ? 4 : 2;
     CUtensorMap map_x, map_w, map_xs, map_ws, map_out;
-    if (!encode_tensor_map(&map_x, CU_TENSOR_MAP_DATA_TYPE_UINT8, L.x, pitch, L.B, pitch, 0, 0, KB_BYTES, TM, 1, CU_TENSOR_MAP_SWIZZLE_128B) ||
+    // (rows that are no tokens are not filled either: a fill with zeros takes as long as a load, and their sums are not read)
+    const int x_rows = L.B < TM ? (L.B + 7) / 8 * 8 : TM;
+    P.x_bytes = x_rows * KB_BYTES;
+    P.stage_bytes = P.x_bytes + weight_bytes<TN, PAIR>();
+    P.stages = stages<TN, PAIR>(P.x_bytes);
+    if (!encode_tensor_map(&map_x, CU_TENSOR_MAP_DATA_TYPE_UINT8, L.x, pitch, L.B, pitch, 0, 0, KB_BYTES, x_rows, 1, CU_TENSOR_MAP_SWIZZLE_128B) ||
         !encode_tensor_map(&map_w, CU_TENSOR_MAP_DATA_TYPE_UINT8, L.w, pitch, L.M, pitch, 0, 0, KB_BYTES, TN / PAIR, 1, CU_TENSOR_MAP_SWIZZLE_128B) ||
         !map_scales(&map_xs, L.x_scale, L.B, L.N) || !map_scales(&map_ws, L.w_scale, L.M, L.N))
         return cudaErrorNotSupported;
     map_out = map_x;                                      // (not read unless tma_out)
     P.tma_out = L.M * out_bytes % 16 == 0 ? 1 : 0;
     if (P.tma_out &&
-        !encode_tensor_map(&map_out, out_bytes == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16, L.out, L.M, L.B, L.M * out_bytes, 0, 0, 16, 32, 1,
-                           out_bytes == 4 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_32B))
+        !encode_tensor_map(&map_out, out_bytes == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16, L.out, L.M, L.B, L.M * out_bytes, 0, 0, (uint32_t)(128 / out_bytes), 32, 1,
+                           CU_TENSOR_MAP_SWIZZLE_128B))
         return cudaErrorNotSupported;
     P.tiles_t = ceil_div(L.B, PAIR * TM);
     P.tiles = P.tiles_t * ceil_div(L.M, TN);
     auto kern = linear_fp4_tcgen05_kernel<TN, SPLIT, PAIR>;
-    constexpr int SMEM = smem_bytes<TN, PAIR>(), CLUSTER = SPLIT * PAIR;
+    constexpr int SMEM = SMEM_MAX, CLUSTER = SPLIT * PAIR;
     const cudaError_t e = allow_dynamic_smem(reinterpret_cast<const void *>(kern), SMEM);
     if (e != cudaSuccess) return e;
     int resident = device_sm_count();                     // clusters that work at a time
@@ -436,19 +454,20 @@ int resident_splits_of(int split)
 {
     const void *kern = split == 2 ? (const void *)linear_fp4_tcgen05_kernel<TN, 2, 1> : split == 4 ? (const void *)linear_fp4_tcgen05_kernel<TN, 4, 1>
                                                                                                    : (const void *)linear_fp4_tcgen05_kernel<TN, 8, 1>;
-    return max_resident_clusters(kern, split, THREADS, smem_bytes<TN, 1>());
+    return max_resident_clusters(kern, split, THREADS, SMEM_MAX);
 }
 // split tiles that work at a time: clusters of 8 do not fill the device (an SM partition holds two)
 int resident_splits(int tn, int split) { return tn == 64 ? resident_splits_of<64>(split) : resident_splits_of<128>(split); }
 
 struct Choice { int tn, split, pair; };
 
-// Tile width, split and pairs by estimated time.
-Choice choose(int M, int B, int kbs)
+// Tile width, split and pairs by estimated time.  A stage takes as long as its bytes take into shared memory, 113 to a nanosecond and SM (256 x 256 of a
+// pair: 350 ns, 128 x 128: 300), or its MMAs, 280 ns for 256 features; all of the weight takes as long as HBM needs for it.  A tile ends with 0.7 us for
+// its results, a split one with 1.5 for the meeting.
+Choice choose(int M, int N, int B, int kbs)
 {
-    constexpr int WIDTHS = 4;
-    const int widths[WIDTHS] = {256, 192, 128, 64}, splits[4] = {1, 2, 4, 8};
-    const double block_ns[2][WIDTHS] = {{520, 440, 350, 260}, {350, 300, 260, 0}};      // 0: there is no such kernel
+    constexpr int WIDTHS = 3;
+    const int widths[WIDTHS] = {256, 128, 64}, splits[4] = {1, 2, 4, 8};
     const int sms = device_sm_count();
     Choice best = {256, 1, 1};
     double best_time = 1e300;
@@ -456,13 +475,16 @@ Choice choose(int M, int B, int kbs)
         for (int i = 0; i < WIDTHS; i++)
             for (int j = 0; j < 4; j++) {
                 const int tn = widths[i], split = splits[j];
-                if (block_ns[pair - 1][i] == 0 || (pair > 1 && B <= TM)) continue;
+                if (pair > 1 && (B <= TM || tn < 128)) continue;
                 if (split > 1 && (tn > 128 || kbs < 2 * split || pair > 1)) continue;
                 const long long tiles = (long long)ceil_div(B, pair * TM) * ceil_div(M, tn);
                 if (split > 1 && tiles > resident_splits(tn, split)) continue;
                 const long long waves = split > 1 ? 1 : (tiles + sms / pair - 1) / (sms / pair);
-                const double time = waves * (ceil_div(kbs, split) * block_ns[pair - 1][i] + (split > 1 ? 1500 : 900));
-                if (time < best_time) { best_time = time; best = {tn, split, pair}; }
+                const int bytes = (B < TM ? B : TM) * KB_BYTES + tn / pair * KB_BYTES + (tn > 128 ? 3 : 2) * SCALES;
+                const double block = fmax(bytes / 113.0, 280.0 / 256 * tn);
+                const double time = waves * (ceil_div(kbs, split) * block + (split > 1 ? 1500 : 700)), hbm = M * (N * (17.0 / 32)) / 6000;
+                const double longer = fmax(time, hbm) + 0.01 * time;
+                if (longer < best_time) { best_time = longer; best = {tn, split, pair}; }
             }
     return best;
 }
@@ -477,16 +499,14 @@ cudaError_t launch_linear_fp4_tcgen05(const Fp4Linear &L, int *status, cudaStrea
     P.col_tiles = ceil_div(L.N, FP4_TILE_COLS);
     P.out = L.out; P.out_dtype = L.out_dtype; P.status = status;
     P.wait_limit = wait_limit();
-    P.tiles_t = P.tiles = P.tma_out = 0;
-    const Choice c = choose(L.M, L.B, P.kbs);
+    P.tiles_t = P.tiles = P.tma_out = P.x_bytes = P.stage_bytes = P.stages = 0;
+    const Choice c = choose(L.M, L.N, L.B, P.kbs);
     if (c.pair == 2) switch (c.tn) {
         case 256: return run<256, 1, 2>(L, P, st);
-        case 192: return run<192, 1, 2>(L, P, st);
         default: return run<128, 1, 2>(L, P, st);
         }
     switch (c.tn * 10 + c.split) {
     case 2561: return run<256, 1, 1>(L, P, st);
-    case 1921: return run<192, 1, 1>(L, P, st);
     case 1281: return run<128, 1, 1>(L, P, st);
     case 1282: return run<128, 2, 1>(L, P, st);
     case 1284: return run<128, 4, 1>(L, P, st);

@@ -760,8 +760,10 @@ int vptq_linear_fp4(const vptq_fp4_desc *desc, const void *x, const uint8_t *x_s
     if (x == nullptr || w == nullptr || w_scale == nullptr || out == nullptr || (e2m1 && x_scale == nullptr)) return VPTQ_E_NULL;
     if ((reinterpret_cast<uintptr_t>(x) & (e2m1 ? 15u : 1u)) || !aligned16(w) || !aligned16(w_scale) || !aligned16(out) || (e2m1 && !aligned16(x_scale))) return VPTQ_E_ALIGN;
     const long long need = linear_fp4_workspace_bytes(desc->M, desc->N, B, desc->x_dtype);
-    if (workspace == nullptr || (long long)workspace_bytes < need) return VPTQ_E_WORKSPACE;
-    if ((reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return VPTQ_E_ALIGN;
+    if (need > 0) {
+        if (workspace == nullptr || (long long)workspace_bytes < need) return VPTQ_E_WORKSPACE;
+        if ((reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return VPTQ_E_ALIGN;
+    }
     Fp4Linear P;
     P.M = desc->M; P.N = desc->N; P.B = B; P.x_dtype = desc->x_dtype; P.out_dtype = desc->out_dtype;
     P.x = x; P.x_scale = e2m1 ? x_scale : nullptr; P.w = w; P.w_scale = w_scale; P.out = out;
@@ -772,14 +774,14 @@ int vptq_linear_fp4(const vptq_fp4_desc *desc, const void *x, const uint8_t *x_s
 const char *vptq_linear_fp4_path(const vptq_fp4_desc *desc, int32_t B)
 {
     if (check_fp4_desc(desc, B) != VPTQ_OK) return "invalid";
-    return linear_fp4_path(B);
+    return linear_fp4_path(desc->M, desc->N, B, desc->x_dtype);
 }
 
 int vptq_linear_fp4_launches(const vptq_fp4_desc *desc, int32_t B)
 {
     const int rc = check_fp4_desc(desc, B);
     if (rc != VPTQ_OK) return rc;
-    return linear_fp4_launches(desc->M, B, desc->x_dtype);
+    return linear_fp4_launches(desc->M, desc->N, B, desc->x_dtype);
 }
 
 int64_t vptq_cache_row_bytes(int32_t head_dim, int32_t cache_dtype)

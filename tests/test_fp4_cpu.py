@@ -31,8 +31,10 @@ def test_sizes(b):
 def test_linear_queries(b):
     d = b.make_fp4_desc(4096, 4096)
     assert b.vptq_linear_fp4_path(b.make_fp4_desc(0, 4096), 1) == "invalid" and b.lib.vptq_linear_fp4_path(None, 1) == b"invalid"
-    # the workspace of 16-bit activations holds the quantized ones; of e2m1, the status word
-    for B in (1, 100, 5000):
+    # the workspace of 16-bit activations holds the quantized ones, that of e2m1 the status word; a few tokens over a small weight need none
+    assert [b.vptq_linear_fp4_workspace_bytes(d, B) for B in (1, 8)] == [0, 0] and b.vptq_linear_fp4_workspace_bytes(d, 9) > 256
+    assert b.vptq_linear_fp4_workspace_bytes(b.make_fp4_desc(4096, 4097), 1) > 256 and b.vptq_linear_fp4_workspace_bytes(b.make_fp4_desc(40960, 4096), 1) > 256
+    for B in (9, 100, 5000):
         q = b.vptq_linear_fp4_workspace_bytes(b.make_fp4_desc(4096, 4096, "e2m1"), B)
         assert 256 <= q <= b.vptq_linear_fp4_workspace_bytes(d, B) <= 1024 + q + B * 2048 + b.vptq_fp4_scale_bytes(B, 4096)
         assert 1 <= b.vptq_linear_fp4_launches(b.make_fp4_desc(4096, 4096, "e2m1"), B) <= b.vptq_linear_fp4_launches(d, B) <= 2
@@ -68,7 +70,7 @@ def test_refusals_of_the_c_abi(b):
         return L.vptq_linear_fp4(C.byref(desc), x, xs, 3, w, ws, out, room, n, None)
 
     assert linear(d, x=None) == linear(d, w=None) == linear(d, ws=None) == linear(d, out=None) == linear(e2m1) == b.E_NULL
-    assert linear(d, x=p + 1) == linear(e2m1, x=p + 8, xs=p) == linear(d, w=p + 8) == linear(d, ws=p + 4) == linear(d, out=p + 4) == linear(e2m1, xs=p + 1) == linear(d, room=p + 16) == b.E_ALIGN
+    assert linear(d, x=p + 1) == linear(e2m1, x=p + 8, xs=p) == linear(d, w=p + 8) == linear(d, ws=p + 4) == linear(d, out=p + 4) == linear(e2m1, xs=p + 1) == linear(e2m1, xs=p, room=p + 16) == b.E_ALIGN
     assert linear(e2m1, xs=p, room=None) == linear(e2m1, xs=p, n=8) == b.E_WORKSPACE
 
 

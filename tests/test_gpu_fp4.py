@@ -208,7 +208,7 @@ def test_linear_of_many_shapes(b, M, N, B):
     assert same(y, b.vptq_linear_fp4(q, w, ws, x_scale=s, out_dtype="fp32"))            # bit for bit the same every time
 
 
-# (few tokens: less than a block of columns a warp and many, one pass over the features or several, passes that begin and end inside a tile of scales)
+# (few tokens: warps with and without columns, rows that begin and end inside a tile of scales, one group or two a CTA; and those that the other kernel takes)
 @pytest.mark.parametrize("B", [1, 2, 7, 8, 9, 15, 16])
 @pytest.mark.parametrize("M,N", [(1, 64), (32, 8192), (33, 2560), (100, 5000), (1024, 1000), (1001, 4096), (4100, 1100), (4736, 300), (9000, 640), (28672, 512), (37888, 260),
                                  (40001, 130), (80000, 256), (300, 40000), (5000, 17000)])
@@ -223,10 +223,10 @@ def test_linear_of_few_tokens(b, M, N, B):
 
 
 def test_linear_paths(b):
-    for x, launches in (("fp16", [1, 1, 2, 2, 2]), ("e2m1", [1, 1, 1, 1, 1])):
-        d = b.make_fp4_desc(4096, 4096, x)
-        assert [b.vptq_linear_fp4_path(d, B) for B in (1, 8, 16, 17, 300)] == ["fp4_few"] * 3 + ["fp4_tcgen05"] * 2
-        assert [b.vptq_linear_fp4_launches(d, B) for B in (1, 8, 16, 17, 300)] == launches
+    path = lambda M, N, B, x="fp16": (b.vptq_linear_fp4_path(b.make_fp4_desc(M, N, x), B), b.vptq_linear_fp4_launches(b.make_fp4_desc(M, N, x), B))  # noqa: E731
+    few, two, one = ("fp4_few", 1), ("fp4_tcgen05", 2), ("fp4_tcgen05", 1)
+    assert [path(4096, 4096, B) for B in (1, 8, 9, 300)] == [few, few, two, two] and [path(4096, 4096, B, "e2m1") for B in (1, 300)] == [one, one]
+    assert [path(M, N, 1, "bf16") for M, N in ((4096, 4097), (40960, 64))] == [two, two]
 
 
 def test_linear_of_every_scale(b):

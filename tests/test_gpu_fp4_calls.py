@@ -199,6 +199,19 @@ def test_waits_that_run_out(b, M, N, B, x_type):
         assert same(call(), clean) and b.vptq_workspace_status(room) == b.OK
 
 
+@pytest.mark.parametrize("clocks", [1, 200, 1000])
+@pytest.mark.parametrize("M,N,B", [(4096, 4096, 1), (4736, 4096, 8), (300, 3990, 3)])
+def test_waits_of_a_few_tokens_that_run_out(b, M, N, B, clocks):
+    g = gen(M + B)
+    cold = [ref.random_weight(M, N, g, "cuda") for _ in range(20)]     # (more than L2 holds)
+    x = torch.randn(B, N, generator=g, device="cuda").half()
+    clean = [b.vptq_linear_fp4(x, w, s, out_dtype="fp32") for w, s in cold]
+    ys = with_short_waits(b, lambda: [b.vptq_linear_fp4(x, w, s, out_dtype="fp32") for w, s in cold], clocks)
+    for y, want, (w, s) in zip(ys, clean, cold):
+        right_or_nan(y, want, some=False)
+        assert torch.isfinite(want).all() and same(b.vptq_linear_fp4(x, w, s, out_dtype="fp32"), want)
+
+
 @pytest.mark.parametrize("clocks", [200, 800, 1600, 3200, 6400, 12800])
 def test_waits_that_run_out_midway(b, clocks):
     g = gen(5)
