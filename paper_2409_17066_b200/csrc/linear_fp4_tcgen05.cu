@@ -60,7 +60,7 @@ struct Params {
     int M, B, kbs, last_steps;
     int col_tiles;                         // scale tiles along a row of 128-row tiles
     int tiles_t, tiles;
-    int x_bytes, stage_bytes, stages;      // of a CTA's part of a stage: activations, all of it; stages of the ring
+    int x_bytes, stages;                   // of a CTA's part of a stage: activations; stages of the ring
     void *out;
     int out_dtype;
     int tma_out;           // rows of `out` are 16-byte aligned: stored by TMA
@@ -205,14 +205,15 @@ __device__ __forceinline__ void finish_tiles(const CUtensorMap &map_out, const P
     if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
 }
 
-template <int TN, int SPLIT, int PAIR>
+// FEW: fewer than 128 tokens (whose part of a stage is not known here)
+template <int TN, int SPLIT, int PAIR, bool FEW>
 __global__ void __launch_bounds__(THREADS, 1)
 linear_fp4_tcgen05_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_xs,
                           const __grid_constant__ CUtensorMap map_ws, const __grid_constant__ CUtensorMap map_out, const __grid_constant__ Params P)
 {
     constexpr int RT = row_tiles<TN>(), BUF = buffers<TN>();
     // of a stage: activations, weight, their scales
-    const uint32_t ST = P.stages, SB = P.stage_bytes, W_AT = P.x_bytes, XS_AT = W_AT + TN / PAIR * KB_BYTES, WS_AT = XS_AT + SCALES;
+    const uint32_t W_AT = FEW ? P.x_bytes : TM * KB_BYTES, SB = W_AT + weight_bytes<TN, PAIR>(), ST = FEW ? P.stages : stages<TN, PAIR>(TM * KB_BYTES), XS_AT = W_AT + TN / PAIR * KB_BYTES, WS_AT = XS_AT + SCALES;
     extern __shared__ __align__(1024) uint8_t sm[];
     __shared__ uint32_t tmem_slot, lost;                  // lost: a wait of this CTA gave up (of a pair: of either)
     const uint32_t base = smem_addr(sm), staging0 = base + ST * SB, bars = staging0 + FIXED_BYTES - BARRIERS;
@@ -295,6 +296,7 @@ linear_fp4_tcgen05_kernel(const __grid_constant__ CUtensorMap map_x, const __gri
                         const uint64_t at = (uint64_t)((s * SB) >> 4);
                         const uint32_t xs = tmem + BUF * TN + turn * SCALE_COLS, ws = xs + 4 * CHUNKS;
                         const int steps = kb == P.kbs - 1 ? P.last_steps : STEPS;
+                        // (with the next block's scales copied before these MMAs, a stage was held for one block longer: 8192 x 28672 at 2048 tokens 176 us, not 162)
 #pragma unroll
                         for (int c = 0; c < CHUNKS; c++) {
                             if (2 * c >= steps) break;                         // (what lies behind the last columns is another row's)
@@ -396,8 +398,8 @@ bool map_scales(CUtensorMap *map, const uint8_t *p, int rows, int cols)
     return encode_tensor_map(map, CU_TENSOR_MAP_DATA_TYPE_UINT32, p, FP4_TILE_BYTES / 4, tiles, FP4_TILE_BYTES, 0, 0, FP4_TILE_BYTES / 4, CHUNKS, 1, CU_TENSOR_MAP_SWIZZLE_NONE);
 }
 
-template <int TN, int SPLIT, int PAIR>
-cudaError_t run(const Fp4Linear &L, const Params &P0, cudaStream_t st)
+template <int TN, int SPLIT, int PAIR, bool FEW>
+cudaError_t run_as(const Fp4Linear &L, const Params &P0, cudaStream_t st)
 {
     Params P = P0;
     const long long pitch = fp4_row_bytes(L.N), out_bytes = L.out_dtype == VPTQ_DTYPE_FP32 ? 4 : 2;
@@ -405,7 +407,6 @@ cudaError_t run(const Fp4Linear &L, const Params &P0, cudaStream_t st)
     // (rows that are no tokens are not filled either: a fill with zeros takes as long as a load, and their sums are not read)
     const int x_rows = L.B < TM ? (L.B + 7) / 8 * 8 : TM;
     P.x_bytes = x_rows * KB_BYTES;
-    P.stage_bytes = P.x_bytes + weight_bytes<TN, PAIR>();
     P.stages = stages<TN, PAIR>(P.x_bytes);
     if (!encode_tensor_map(&map_x, CU_TENSOR_MAP_DATA_TYPE_UINT8, L.x, pitch, L.B, pitch, 0, 0, KB_BYTES, x_rows, 1, CU_TENSOR_MAP_SWIZZLE_128B) ||
         !encode_tensor_map(&map_w, CU_TENSOR_MAP_DATA_TYPE_UINT8, L.w, pitch, L.M, pitch, 0, 0, KB_BYTES, TN / PAIR, 1, CU_TENSOR_MAP_SWIZZLE_128B) ||
@@ -419,7 +420,7 @@ cudaError_t run(const Fp4Linear &L, const Params &P0, cudaStream_t st)
         return cudaErrorNotSupported;
     P.tiles_t = ceil_div(L.B, PAIR * TM);
     P.tiles = P.tiles_t * ceil_div(L.M, TN);
-    auto kern = linear_fp4_tcgen05_kernel<TN, SPLIT, PAIR>;
+    auto kern = linear_fp4_tcgen05_kernel<TN, SPLIT, PAIR, FEW>;
     constexpr int SMEM = SMEM_MAX, CLUSTER = SPLIT * PAIR;
     const cudaError_t e = allow_dynamic_smem(reinterpret_cast<const void *>(kern), SMEM);
     if (e != cudaSuccess) return e;
@@ -449,11 +450,19 @@ cudaError_t run(const Fp4Linear &L, const Params &P0, cudaStream_t st)
     return cudaLaunchKernelEx(&cfg, kern, map_x, map_w, map_xs, map_ws, map_out, P);
 }
 
+template <int TN, int SPLIT, int PAIR>
+cudaError_t run(const Fp4Linear &L, const Params &P, cudaStream_t st)
+{
+    if constexpr (PAIR == 1)
+        if (L.B <= TM - 8) return run_as<TN, SPLIT, 1, true>(L, P, st);
+    return run_as<TN, SPLIT, PAIR, false>(L, P, st);
+}
+
 template <int TN>
 int resident_splits_of(int split)
 {
-    const void *kern = split == 2 ? (const void *)linear_fp4_tcgen05_kernel<TN, 2, 1> : split == 4 ? (const void *)linear_fp4_tcgen05_kernel<TN, 4, 1>
-                                                                                                   : (const void *)linear_fp4_tcgen05_kernel<TN, 8, 1>;
+    const void *kern = split == 2 ? (const void *)linear_fp4_tcgen05_kernel<TN, 2, 1, false> : split == 4 ? (const void *)linear_fp4_tcgen05_kernel<TN, 4, 1, false>
+                                                                                                   : (const void *)linear_fp4_tcgen05_kernel<TN, 8, 1, false>;
     return max_resident_clusters(kern, split, THREADS, SMEM_MAX);
 }
 // split tiles that work at a time: clusters of 8 do not fill the device (an SM partition holds two)
@@ -462,7 +471,7 @@ int resident_splits(int tn, int split) { return tn == 64 ? resident_splits_of<64
 struct Choice { int tn, split, pair; };
 
 // Tile width, split and pairs by estimated time.  A stage takes as long as its bytes take into shared memory, 113 to a nanosecond and SM (256 x 256 of a
-// pair: 350 ns, 128 x 128: 300), or its MMAs, 280 ns for 256 features; all of the weight takes as long as HBM needs for it.  A tile ends with 0.7 us for
+// pair: 350 ns, 128 x 128: 300), or its MMAs, 280 ns for 256 features, and 250 at least; all of the weight takes as long as HBM needs for it.  A tile ends with 0.7 us for
 // its results, a split one with 1.5 for the meeting.
 Choice choose(int M, int N, int B, int kbs)
 {
@@ -481,7 +490,7 @@ Choice choose(int M, int N, int B, int kbs)
                 if (split > 1 && tiles > resident_splits(tn, split)) continue;
                 const long long waves = split > 1 ? 1 : (tiles + sms / pair - 1) / (sms / pair);
                 const int bytes = (B < TM ? B : TM) * KB_BYTES + tn / pair * KB_BYTES + (tn > 128 ? 3 : 2) * SCALES;
-                const double block = fmax(bytes / 113.0, 280.0 / 256 * tn);
+                const double block = fmax(bytes / 113.0, fmax(280.0 / 256 * tn, 250));
                 const double time = waves * (ceil_div(kbs, split) * block + (split > 1 ? 1500 : 700)), hbm = M * (N * (17.0 / 32)) / 6000;
                 const double longer = fmax(time, hbm) + 0.01 * time;
                 if (longer < best_time) { best_time = longer; best = {tn, split, pair}; }
@@ -499,7 +508,7 @@ cudaError_t launch_linear_fp4_tcgen05(const Fp4Linear &L, int *status, cudaStrea
     P.col_tiles = ceil_div(L.N, FP4_TILE_COLS);
     P.out = L.out; P.out_dtype = L.out_dtype; P.status = status;
     P.wait_limit = wait_limit();
-    P.tiles_t = P.tiles = P.tma_out = P.x_bytes = P.stage_bytes = P.stages = 0;
+    P.tiles_t = P.tiles = P.tma_out = P.x_bytes = P.stages = 0;
     const Choice c = choose(L.M, L.N, L.B, P.kbs);
     if (c.pair == 2) switch (c.tn) {
         case 256: return run<256, 1, 2>(L, P, st);
