@@ -552,7 +552,7 @@ int vptq_dequant_fp4(const vptq_layer_desc *desc, const vptq_layer_ptrs *p, uint
  *   every pointer is 16-byte aligned (VPTQ_E_ALIGN), but for x of 16 bits: any alignment of a value;  out_dtype FP16, BF16 or FP32
  *   flags: VPTQ_FLAG_CONCURRENT and VPTQ_FLAG_DETERMINISTIC are accepted and change nothing (no CTA waits for another launch's, every
  *           sum has a fixed order).
- * At most 8 tokens of 16 bits over a small weight (N <= 4096, M at most 32 rows to an SM) take the kernel "fp4_few" (no workspace), all others
+ * At most 8 tokens of 16 bits over a small weight (N a multiple of 8 up to 4096, M at most 32 rows to an SM) take the kernel "fp4_few" (no workspace), all others
  * "fp4_tcgen05" (vptq_linear_fp4_path), whose workspace, 256-byte aligned, starts with a status word (vptq_workspace_status); its contents on entry
  * are irrelevant, calls that may overlap must not share one.  All device-side waits are bounded: one that gives up leaves NaN in the results that it
  * concerns and, with "fp4_tcgen05", VPTQ_E_TIMEOUT in the status word.  A sum that overflows FP32 is an infinity or a NaN. */

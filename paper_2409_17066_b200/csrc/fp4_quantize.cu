@@ -12,7 +12,7 @@ namespace vptq {
 
 namespace {
 
-constexpr int THREADS = 256, STEPS = FP4_TILE_ROWS / 32;
+constexpr int THREADS = 256;
 
 struct QuantizeParams {
     const void *x;
@@ -23,17 +23,19 @@ struct QuantizeParams {
     int early;
 };
 
-template <int DT, bool VEC>
+// STEPS: rows of a thread; a tile is 4 / STEPS CTAs' work
+template <int DT, bool VEC, int STEPS>
 __global__ void __launch_bounds__(THREADS)
 fp4_quantize_kernel(const __grid_constant__ QuantizeParams P)
 {
     if (P.early) pdl_launch_dependents();
     pdl_wait();
     const int lane = threadIdx.x & 7, r = threadIdx.x >> 3;
-    const int rt = (int)(blockIdx.x / (unsigned)P.col_tiles), ct = (int)(blockIdx.x - (unsigned)rt * P.col_tiles);
-    const int row = rt * FP4_TILE_ROWS + r, c = ct * FP4_TILE_COLS + lane * 16;
+    const unsigned tile = STEPS == 4 ? blockIdx.x : blockIdx.x / (4 / STEPS);
+    const int rt = (int)(tile / (unsigned)P.col_tiles), ct = (int)(tile - (unsigned)rt * P.col_tiles), j0 = STEPS == 4 ? 0 : (int)(blockIdx.x % (4 / STEPS)) * STEPS;
+    const int row = rt * FP4_TILE_ROWS + 32 * j0 + r, c = ct * FP4_TILE_COLS + lane * 16;
     const uint8_t *x = reinterpret_cast<const uint8_t *>(P.x) + (long long)row * P.ld * Act<DT>::BYTES;
-    uint8_t *q = P.q + (long long)row * P.pitch + c / 2, *scale = P.scale + (long long)blockIdx.x * FP4_TILE_BYTES + fp4_scale_at(r, lane >> 1);
+    uint8_t *q = P.q + (long long)row * P.pitch + c / 2, *scale = P.scale + (long long)tile * FP4_TILE_BYTES + fp4_scale_at(32 * j0 + r, lane >> 1);
     const long long step = 32 * P.ld * Act<DT>::BYTES;
     Sixteen<DT, VEC> e[STEPS];
 #pragma unroll
@@ -46,13 +48,16 @@ fp4_quantize_kernel(const __grid_constant__ QuantizeParams P)
     }
 }
 
-template <int DT>
-cudaError_t launch(const QuantizeParams &P, bool vec, cudaStream_t st)
+// Where whole tiles would not give every SM two CTAs, a row to a thread: XXX.
+template <int DT, bool VEC>
+cudaError_t launch_as(const QuantizeParams &P, cudaStream_t st)
 {
     const int tiles = (int)((long long)ceil_div(P.rows, FP4_TILE_ROWS) * P.col_tiles);
-    return vec ? launch_dependent("fp4_quantize", fp4_quantize_kernel<DT, true>, tiles, THREADS, 0, st, P)
-               : launch_dependent("fp4_quantize", fp4_quantize_kernel<DT, false>, tiles, THREADS, 0, st, P);
+    if (tiles < 2 * device_sm_count()) return launch_dependent("fp4_quantize", fp4_quantize_kernel<DT, VEC, 1>, 4 * tiles, THREADS, 0, st, P);
+    return launch_dependent("fp4_quantize", fp4_quantize_kernel<DT, VEC, 4>, tiles, THREADS, 0, st, P);
 }
+template <int DT>
+cudaError_t launch(const QuantizeParams &P, bool vec, cudaStream_t st) { return vec ? launch_as<DT, true>(P, st) : launch_as<DT, false>(P, st); }
 
 }  // namespace
 

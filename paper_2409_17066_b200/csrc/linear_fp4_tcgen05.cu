@@ -109,7 +109,7 @@ struct Sums {
 template <bool WIDE, typename Chunk>
 __device__ __forceinline__ void store_piece(const CUtensorMap &map_out, const Params &P, const Sums &S, int lane, int row, int col, Chunk chunk)
 {
-    constexpr int SIZE = WIDE ? 4 : 2, COLS = 128 / SIZE;
+    constexpr int SIZE = WIDE ? 4 : 2;
     if (P.tma_out && lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
     __syncwarp();
 #pragma unroll
@@ -123,13 +123,27 @@ __device__ __forceinline__ void store_piece(const CUtensorMap &map_out, const Pa
         }
     } else {
         __syncwarp();
-        for (int r = 0; r < 32 && row + r < P.B; r++)
-            for (int c = lane; c < COLS && col + c < P.M; c += 32) {
-                const uint8_t *v = S.staging_p + r * 128 + ((c * SIZE / 16 ^ (r & 7)) << 4) + c * SIZE % 16;
-                const long long o = (long long)(row + r) * P.M + col + c;
-                if (WIDE) reinterpret_cast<float *>(P.out)[o] = *reinterpret_cast<const float *>(v);
-                else reinterpret_cast<uint16_t *>(P.out)[o] = *reinterpret_cast<const uint16_t *>(v);
+        // a lane's four bytes of eight rows at a time (row by row, value by value: 5001 x 700 at 2000 tokens 35 us instead of XXX)
+#pragma unroll 1
+        for (int r0 = 0; r0 < 32; r0 += 8) {
+            uint32_t v[8];
+#pragma unroll
+            for (int r = 0; r < 8; r++) v[r] = *reinterpret_cast<const uint32_t *>(S.staging_p + (r0 + r) * 128 + ((lane >> 2 ^ r) << 4) + (lane & 3) * 4);
+            const int c = col + lane * (4 / SIZE);
+#pragma unroll
+            for (int r = 0; r < 8; r++) {
+                if (row + r0 + r >= P.B || c >= P.M) continue;
+                const long long o = (long long)(row + r0 + r) * P.M + c;
+                if constexpr (WIDE) {
+                    reinterpret_cast<uint32_t *>(P.out)[o] = v[r];
+                } else if (c + 1 < P.M && (o & 1) == 0) {
+                    *reinterpret_cast<uint32_t *>(reinterpret_cast<uint16_t *>(P.out) + o) = v[r];
+                } else {
+                    reinterpret_cast<uint16_t *>(P.out)[o] = (uint16_t)v[r];
+                    if (c + 1 < P.M) reinterpret_cast<uint16_t *>(P.out)[o + 1] = (uint16_t)(v[r] >> 16);
+                }
             }
+        }
         __syncwarp();
     }
 }

@@ -226,7 +226,7 @@ def test_linear_paths(b):
     path = lambda M, N, B, x="fp16": (b.vptq_linear_fp4_path(b.make_fp4_desc(M, N, x), B), b.vptq_linear_fp4_launches(b.make_fp4_desc(M, N, x), B))  # noqa: E731
     few, two, one = ("fp4_few", 1), ("fp4_tcgen05", 2), ("fp4_tcgen05", 1)
     assert [path(4096, 4096, B) for B in (1, 8, 9, 300)] == [few, few, two, two] and [path(4096, 4096, B, "e2m1") for B in (1, 300)] == [one, one]
-    assert [path(M, N, 1, "bf16") for M, N in ((4096, 4097), (40960, 64))] == [two, two]
+    assert [path(M, N, 1, "bf16") for M, N in ((4096, 4104), (40960, 64), (64, 100))] == [two] * 3
 
 
 def test_linear_of_every_scale(b):
