@@ -88,12 +88,42 @@ __device__ __forceinline__ void fp4_values8(uint32_t q, float (&v)[8])
     }
 }
 
-// Sixteen consecutive values of a row, as two times eight; zeros beyond `cols`.
-template <int DT, bool VEC> struct Sixteen { Eight<DT, VEC> h[2]; };
+// Sixteen consecutive values of a row, as two times eight; zeros beyond `cols`.  Values of 16 bits are packed whether they were loaded so (VEC: 16 bytes at a
+// time) or in words, or halves of them at the ends, that lie anywhere.
+template <int DT, bool VEC> struct Sixteen { Eight<DT, VEC || DT != VPTQ_DTYPE_FP32> h[2]; };
 template <int DT, bool VEC>
 __device__ __forceinline__ Sixteen<DT, VEC> load_sixteen(const void *row, int c, int cols)
 {
-    return {{load_eight<DT, VEC>(row, c, cols), load_eight<DT, VEC>(row, c + 8, cols)}};
+    if constexpr (VEC || DT == VPTQ_DTYPE_FP32) {
+        return {{load_eight<DT, VEC>(row, c, cols), load_eight<DT, VEC>(row, c + 8, cols)}};
+    } else {
+        const uint16_t *p = reinterpret_cast<const uint16_t *>(row) + c;
+        uint32_t w[8] = {};
+        if (c + 16 <= cols) {
+            if ((reinterpret_cast<uintptr_t>(p) & 2u) == 0) {
+#pragma unroll
+                for (int i = 0; i < 8; i++) w[i] = __ldg(reinterpret_cast<const uint32_t *>(p) + i);
+            } else {
+                // a half, seven words, a half: no value beside these is touched
+                uint32_t last = __ldg(p);
+#pragma unroll
+                for (int i = 0; i < 7; i++) {
+                    const uint32_t next = __ldg(reinterpret_cast<const uint32_t *>(p + 1) + i);
+                    w[i] = i == 0 ? last | next << 16 : __funnelshift_r(last, next, 16);
+                    last = next;
+                }
+                w[7] = last >> 16 | (uint32_t)__ldg(p + 15) << 16;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; i++)
+                if (c + i < cols) w[i / 2] |= (uint32_t)__ldg(p + i) << (16 * (i & 1));
+        }
+        Sixteen<DT, VEC> e;
+        e.h[0].q = make_uint4(w[0], w[1], w[2], w[3]);
+        e.h[1].q = make_uint4(w[4], w[5], w[6], w[7]);
+        return e;
+    }
 }
 // the larger magnitudes of two words of packed 16-bit values, whose signs are cleared
 __device__ __forceinline__ uint32_t larger2(uint32_t a, uint32_t b)
@@ -105,14 +135,14 @@ __device__ __forceinline__ uint32_t larger2(uint32_t a, uint32_t b)
 template <int DT, bool VEC>
 __device__ __forceinline__ uint32_t magnitude(const Sixteen<DT, VEC> &e)
 {
-    if constexpr (VEC && DT != VPTQ_DTYPE_FP32) {
+    if constexpr (DT != VPTQ_DTYPE_FP32) {
         const uint32_t w[8] = {e.h[0].q.x, e.h[0].q.y, e.h[0].q.z, e.h[0].q.w, e.h[1].q.x, e.h[1].q.y, e.h[1].q.z, e.h[1].q.w};
         uint32_t m = w[0] & 0x7FFF7FFFu;
 #pragma unroll
         for (int i = 1; i < 8; i++) m = larger2(m, w[i] & 0x7FFF7FFFu);
         return magnitude16<DT>(m);
     } else {
-        return max(magnitude<8>(e.h[0].v), magnitude<8>(e.h[1].v));
+        return max(magnitude<8>(e.h[0].v), magnitude<8>(e.h[1].v));        // (an Eight of FP32 is the values)
     }
 }
 // Two adjacent lanes hold a block's 32 values: its scale byte.
