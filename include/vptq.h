@@ -580,7 +580,7 @@ int vptq_linear_fp4_launches(const vptq_fp4_desc *desc, int32_t B);
  * table[s][(start[s] + i) / page_size] (table [n_seqs][table_width]; entries that no token needs may be anything).
  *   vptq_cache_write: k and v [n_tokens][n_heads][head_dim] of x_dtype (FP16, BF16 or FP32) into the cache; a token's heads and the tokens are any
  *     distances apart (strides in values, not negative), a head's columns are adjacent; any alignment of a value
- *   vptq_cache_read: those tokens' keys and values into k and v, packed, rounded once to x_dtype
+ *   vptq_cache_read: those tokens' keys and values into k and v, packed: the FP32 product of code and scale, rounded to x_dtype
  * Tokens in no sequence (before cu[0], from cu[n_seqs] on) are left out: nothing is written for them.  A token whose position is negative or
  * beyond the table, or whose page is not in [0, n_pages), is not written, and reads as zeros.  Two tokens of one write that have the same
  * place (a page that two sequences share) leave it with codes and scales of either.

@@ -40,9 +40,10 @@ __device__ __forceinline__ Place find_place(const CacheParams &P, int t)
     }
     const int begin = __ldg(C.cu + lo), end = __ldg(C.cu + lo + 1), start = __ldg(C.start + lo);
     if (t < begin || t >= end) return {NONE, NONE};
-    const long long token = (long long)start + (t - begin);        // (less than 2^32)
+    const long long token = (long long)start + ((long long)t - begin);
+    if (token < 0 || token > 0xFFFFFFFFll) return {GONE, GONE};    // (a list that begins below zero may ask for more)
     const uint32_t slot = (uint32_t)token / (uint32_t)C.page;
-    if (token < 0 || slot >= (uint32_t)C.width) return {GONE, GONE};
+    if (slot >= (uint32_t)C.width) return {GONE, GONE};
     const int page = __ldg(C.table + (long long)lo * C.width + slot);
     if ((unsigned)page >= (unsigned)C.pages) return {GONE, GONE};
     const long long row = (long long)page * C.heads * C.page + ((uint32_t)token - slot * (uint32_t)C.page);

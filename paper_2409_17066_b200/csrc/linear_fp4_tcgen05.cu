@@ -191,7 +191,7 @@ __device__ __forceinline__ void finish_tiles(const CUtensorMap &map_out, const P
             }
         } else {
             // through the warp's staging rows, 128 bytes (64 or 32 features) at a time, swizzled as the store's map says.  (In rows of 32 bytes the
-            // copies out took 2.4 us for a tile of 256 features, of 128 XXX.)
+            // copies out took 2.4 us for a tile of 256 features; 16384 x 512 at 2048 tokens 24 us instead of 15.)
             const int row = t0 + 32 * q, col = n0 + c_first;
             if (P.out_dtype == VPTQ_DTYPE_FP32) {
 #pragma unroll

@@ -157,7 +157,8 @@ def test_tokens_without_a_sequence_or_a_page(b, fmt):
     g = gen(5)
     heads, dim, page, pages = 2, 64, 4, 6
     table = ints(0, -1, 6, 3, 2147483647, -2147483648, 5, 1, 2, 4).view(2, 5)
-    for starts, cu in (([0, 0], [2, 22, 41]), ([-3, 17], [0, 10, 20]), ([2147483647, -2147483648], [0, 20, 41]), ([0, 0], [0, 0, 0]), ([0, 0], [44, 44, 60])):
+    for starts, cu in (([0, 0], [2, 22, 41]), ([-3, 17], [0, 10, 20]), ([2147483647, -2147483648], [0, 20, 41]), ([0, 0], [0, 0, 0]), ([0, 0], [44, 44, 60]), ([0, 3], [-5, 20, 30]),
+                       ([2147483647, 0], [-2147483648, 30, 44])):
         start, cu = ints(*starts), ints(*cu)
         cache = junk(b, pages, page, heads, dim, fmt, g)
         k, v = (torch.randn(44, heads, dim, generator=g, device="cuda").half() for _ in range(2))

@@ -253,6 +253,26 @@ def test_linear_of_every_scale(b):
     assert y[~keep].isnan().all() and same(y[keep], clean[keep])
 
 
+@pytest.mark.parametrize("B", [1, 5])
+def test_linear_of_few_tokens_and_every_scale(b, B):
+    g = gen(B)
+    M, N = 300, 512
+    w, _ = ref.random_weight(M, N, g, "cuda")
+    bytes_ = torch.randint(100, 140, (M, 16), generator=g, device="cuda", dtype=torch.uint8)
+    bytes_[7], bytes_[8] = 0, 250                                      # powers below FP32's normal range, and near its end
+    w[8] &= 0x33
+    x = torch.randn(B, N, generator=g, device="cuda").bfloat16()
+    ws = ref.scale_tiles(bytes_)
+    clean = check_linear(b, x, w, ws, "fp32", N, ref.quantize(x)[0])
+    assert clean[:, 7].any() and b.vptq_linear_fp4_path(b.make_fp4_desc(M, N, "bf16"), B) == "fp4_few"
+    bytes_[5, 3] = bytes_[299, 15] = 255
+    w[299] = 0                                                         # zeros times what is no number
+    y = b.vptq_linear_fp4(x, w, ref.scale_tiles(bytes_), out_dtype="fp32")
+    keep = torch.ones(M, dtype=torch.bool, device="cuda")
+    keep[5] = keep[299] = False
+    assert y[:, ~keep].isnan().all() and same(y[:, keep], clean[:, keep])
+
+
 @pytest.mark.parametrize("B", [1, 40, 300])
 @pytest.mark.parametrize("bad", [float("nan"), float("inf")])
 def test_linear_keeps_what_is_not_a_number_in_its_row(b, B, bad):
