@@ -239,6 +239,13 @@ def test_linear_of_every_scale(b):
         bytes_ = torch.randint(middle - 3, middle + 4, (M, 16), generator=g, device="cuda", dtype=torch.uint8)
         ws, s = ref.scale_tiles(bytes_), ref.scale_tiles(254 - bytes_)
         check_linear(b, q, w, ws, "fp32", N, ref.values(q, s, N), s)
+    # powers below FP32's normal range, and near its end, of the weight and of the tokens
+    bytes_ = torch.randint(120, 130, (M, 16), generator=g, device="cuda", dtype=torch.uint8)
+    ends = bytes_.clone()
+    ends[7], ends[8], ends[9, ::2] = 0, 235, 0
+    y = check_linear(b, q, w, ref.scale_tiles(ends), "fp32", N, ref.values(q, ref.scale_tiles(bytes_), N), ref.scale_tiles(bytes_))
+    assert y[:, 7].any()
+    check_linear(b, q, w, ref.scale_tiles(bytes_), "fp32", N, ref.values(q, ref.scale_tiles(ends), N), ref.scale_tiles(ends))
     bytes_ = torch.full((M, 16), 127, device="cuda", dtype=torch.uint8)
     one = ref.scale_tiles(bytes_)
     bytes_ = bytes_.clone()
