@@ -58,7 +58,8 @@ constexpr int SCALE_COLS = 32;
 
 struct Params {
     int M, B, kbs, last_steps;
-    int col_tiles;                         // scale tiles along a row of 128-row tiles
+    int col_tiles, row_tiles;              // scale tiles along a row of 128-row tiles, and of those rows the weight's
+    const uint8_t *x_scale, *w_scale;
     int tiles_t, tiles;
     int x_bytes, stages;                   // of a CTA's part of a stage: activations; stages of the ring
     void *out;
@@ -247,7 +248,11 @@ linear_fp4_tcgen05_kernel(const __grid_constant__ CUtensorMap map_x, const __gri
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) tmem_alloc_all<PAIR>(smem_addr(&tmem_slot));
-    if (warp == 0 && elect_one()) { prefetch_map(&map_w); prefetch_map(&map_ws); prefetch_map(&map_x); prefetch_map(&map_xs); }
+    if (warp == 0 && elect_one()) {
+        prefetch_map(&map_w);
+        prefetch_map(&map_x);
+        if (PAIR == 2) { prefetch_map(&map_ws); prefetch_map(&map_xs); }
+    }
     tc_fence_before();
     __syncthreads();
     if constexpr (PAIR == 2) cluster_sync();              // the other CTA's barriers are ready, and its half of TMEM
@@ -283,12 +288,23 @@ linear_fp4_tcgen05_kernel(const __grid_constant__ CUtensorMap map_x, const __gri
                     mbar_wait_or_flag(bar_empty(s), (round & 1) ^ 1u, lost_at, gave_up);
                     if (elect_one() && !gave_up) {
                         const uint32_t at = base + s * SB, full = full0 + 8 * s;
-                        if (t_rank == 0) mbar_expect_tx(bar_full(s), PAIR * SB);
-                        tma_load<PAIR>(at + W_AT, &map_w, kb * KB_BYTES, n0 + n_part, full);
+                        const int x_tile = t0 / FP4_TILE_ROWS * P.col_tiles + kb * CHUNKS, w_tile = n0 / FP4_TILE_ROWS * P.col_tiles + kb * CHUNKS;
+                        if constexpr (PAIR == 2) {
+                            if (t_rank == 0) mbar_expect_tx(bar_full(s), PAIR * SB);
 #pragma unroll
-                        for (int r = 0; r < RT; r++) tma_load<PAIR>(at + WS_AT + r * SCALES, &map_ws, 0, (n0 / FP4_TILE_ROWS + r) * P.col_tiles + kb * CHUNKS, full);
+                            for (int r = 0; r < RT; r++) tma_load<PAIR>(at + WS_AT + r * SCALES, &map_ws, 0, w_tile + r * P.col_tiles, full);
+                            tma_load<PAIR>(at + XS_AT, &map_xs, 0, x_tile, full);
+                        } else {
+                            // scales as linear copies, of the tiles that there are: two maps fewer for the host to make (0.5 us of a call)
+                            const uint32_t bytes = min(CHUNKS, P.col_tiles - kb * CHUNKS) * FP4_TILE_BYTES, tiles = min(RT, P.row_tiles - n0 / FP4_TILE_ROWS);
+                            mbar_expect_tx(full, W_AT + TN * KB_BYTES + (1 + tiles) * bytes);
+#pragma unroll
+                            for (int r = 0; r < RT; r++)
+                                if (r < (int)tiles) bulk_load(at + WS_AT + r * SCALES, P.w_scale + (long long)(w_tile + r * P.col_tiles) * FP4_TILE_BYTES, bytes, full);
+                            bulk_load(at + XS_AT, P.x_scale + (long long)x_tile * FP4_TILE_BYTES, bytes, full);
+                        }
+                        tma_load<PAIR>(at + W_AT, &map_w, kb * KB_BYTES, n0 + n_part, full);
                         tma_load<PAIR>(at, &map_x, kb * KB_BYTES, t0, full);
-                        tma_load<PAIR>(at + XS_AT, &map_xs, 0, t0 / FP4_TILE_ROWS * P.col_tiles + kb * CHUNKS, full);
                     }
                     __syncwarp();
                     if (++s == ST) { s = 0; round++; }
@@ -427,8 +443,9 @@ cudaError_t run_as(const Fp4Linear &L, const Params &P0, cudaStream_t st)
     P.stages = stages<TN, PAIR>(P.x_bytes);
     if (!encode_tensor_map(&map_x, CU_TENSOR_MAP_DATA_TYPE_UINT8, L.x, pitch, L.B, pitch, 0, 0, KB_BYTES, x_rows, 1, CU_TENSOR_MAP_SWIZZLE_128B) ||
         !encode_tensor_map(&map_w, CU_TENSOR_MAP_DATA_TYPE_UINT8, L.w, pitch, L.M, pitch, 0, 0, KB_BYTES, TN / PAIR, 1, CU_TENSOR_MAP_SWIZZLE_128B) ||
-        !map_scales(&map_xs, L.x_scale, L.B, L.N) || !map_scales(&map_ws, L.w_scale, L.M, L.N))
+        (PAIR == 2 && (!map_scales(&map_xs, L.x_scale, L.B, L.N) || !map_scales(&map_ws, L.w_scale, L.M, L.N))))
         return cudaErrorNotSupported;
+    if (PAIR == 1) map_xs = map_ws = map_x;               // (not read)
     map_out = map_x;                                      // (not read unless tma_out)
     P.tma_out = L.M * out_bytes % 16 == 0 ? 1 : 0;
     if (P.tma_out &&
@@ -522,7 +539,8 @@ cudaError_t launch_linear_fp4_tcgen05(const Fp4Linear &L, int *status, cudaStrea
     Params P;
     P.M = L.M; P.B = L.B; P.kbs = ceil_div(L.N, KB);
     P.last_steps = ceil_div(L.N - (P.kbs - 1) * KB, 64);
-    P.col_tiles = ceil_div(L.N, FP4_TILE_COLS);
+    P.col_tiles = ceil_div(L.N, FP4_TILE_COLS); P.row_tiles = ceil_div(L.M, FP4_TILE_ROWS);
+    P.x_scale = L.x_scale; P.w_scale = L.w_scale;
     P.out = L.out; P.out_dtype = L.out_dtype; P.status = status;
     P.wait_limit = wait_limit();
     P.tiles_t = P.tiles = P.tma_out = P.x_bytes = P.stages = 0;
