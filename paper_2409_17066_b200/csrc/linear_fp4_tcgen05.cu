@@ -374,23 +374,35 @@ linear_fp4_tcgen05_kernel(const __grid_constant__ CUtensorMap map_x, const __gri
             const int t0 = first % P.tiles_t * TM, n0 = first / P.tiles_t * TN;
             constexpr int PIECES = TN / 4;
             const int all = min(TM, P.B - t0) * PIECES, i0 = (int)((long long)all * rank / SPLIT), i1 = (int)((long long)all * (rank + 1) / SPLIT);
-            for (int i = i0 + threadIdx.x - 32 * ACC_WARP0; i < i1; i += 32 * ACC_WARPS) {
-                const int row = i / PIECES, p = i % PIECES, col = n0 + 4 * p;
-                const uint32_t at = base + (uint32_t)(row * TN + 4 * (p ^ (row & 7))) * 4u;
-                float4 v[SPLIT];
+            // (two ranks: several pieces' reads under way at a time, 2048 x 8192 at 300 tokens 10.0 -> 9.8 us; four ranks, whose shares are smaller: 6.9 -> 7.3, not taken)
+            constexpr int TOGETHER = SPLIT == 2 ? 4 : 1, TAKERS = 32 * ACC_WARPS;
+#pragma unroll 1
+            for (int i = i0 + threadIdx.x - 32 * ACC_WARP0; i < i1; i += TAKERS * TOGETHER) {
+                float4 v[TOGETHER][SPLIT];
 #pragma unroll
-                for (int r = 0; r < SPLIT; r++) v[r] = load_peer(at, (uint32_t)r);
+                for (int u = 0; u < TOGETHER; u++) {
+                    const int k = min(i + u * TAKERS, i1 - 1), row = k / PIECES, p = k % PIECES;
+                    const uint32_t at = base + (uint32_t)(row * TN + 4 * (p ^ (row & 7))) * 4u;
 #pragma unroll
-                for (int r = 1; r < SPLIT; r++) { v[0].x += v[r].x; v[0].y += v[r].y; v[0].z += v[r].z; v[0].w += v[r].w; }
-                const long long o = (long long)(t0 + row) * P.M + col;
-                if (P.tma_out && col + 4 <= P.M) {                                 // rows of 16-byte multiples: a thread's four values are aligned
-                    if (P.out_dtype == VPTQ_DTYPE_FP32) *reinterpret_cast<float4 *>(reinterpret_cast<float *>(P.out) + o) = v[0];
-                    else *reinterpret_cast<uint2 *>(reinterpret_cast<uint16_t *>(P.out) + o) = make_uint2(pair16(v[0].x, v[0].y, P.out_dtype), pair16(v[0].z, v[0].w, P.out_dtype));
-                } else {
-                    const float e[4] = {v[0].x, v[0].y, v[0].z, v[0].w};
+                    for (int r = 0; r < SPLIT; r++) v[u][r] = load_peer(at, (uint32_t)r);
+                }
 #pragma unroll
-                    for (int k = 0; k < 4; k++)
-                        if (col + k < P.M) store_out(P.out, o + k, e[k], P.out_dtype);
+                for (int u = 0; u < TOGETHER; u++) {
+                    const int k = i + u * TAKERS, row = k / PIECES, col = n0 + 4 * (k % PIECES);
+                    if (k >= i1) break;
+                    float4 &t = v[u][0];
+#pragma unroll
+                    for (int r = 1; r < SPLIT; r++) { t.x += v[u][r].x; t.y += v[u][r].y; t.z += v[u][r].z; t.w += v[u][r].w; }
+                    const long long o = (long long)(t0 + row) * P.M + col;
+                    if (P.tma_out && col + 4 <= P.M) {                             // rows of 16-byte multiples: a thread's four values are aligned
+                        if (P.out_dtype == VPTQ_DTYPE_FP32) *reinterpret_cast<float4 *>(reinterpret_cast<float *>(P.out) + o) = t;
+                        else *reinterpret_cast<uint2 *>(reinterpret_cast<uint16_t *>(P.out) + o) = make_uint2(pair16(t.x, t.y, P.out_dtype), pair16(t.z, t.w, P.out_dtype));
+                    } else {
+                        const float e[4] = {t.x, t.y, t.z, t.w};
+#pragma unroll
+                        for (int c = 0; c < 4; c++)
+                            if (col + c < P.M) store_out(P.out, o + c, e[c], P.out_dtype);
+                    }
                 }
             }
             __syncwarp();
@@ -499,14 +511,17 @@ int resident_splits_of(int split)
                                                                                                    : (const void *)linear_fp4_tcgen05_kernel<TN, 8, 1, false>;
     return max_resident_clusters(kern, split, THREADS, SMEM_MAX);
 }
-// split tiles that work at a time: clusters of 8 do not fill the device (an SM partition holds two)
+// split tiles that work at a time
 int resident_splits(int tn, int split) { return tn == 64 ? resident_splits_of<64>(split) : resident_splits_of<128>(split); }
 
 struct Choice { int tn, split, pair; };
 
 // Tile width, split and pairs by estimated time.  A stage takes as long as its bytes take into shared memory, 113 to a nanosecond and SM (256 x 256 of a
-// pair: 350 ns, 128 x 128: 300), or its MMAs, 280 ns for 256 features, and 250 at least; all of the weight takes as long as HBM needs for it.  A tile ends with 0.7 us for
-// its results, a split one with 1.5 for the meeting.
+// pair: 350 ns, 128 x 128: 300), or its MMAs, 280 ns for 256 features, and 250 at least; all of the weight takes as long as HBM needs for it.
+// A tile ends with 0.5 us of 64 features, 0.7 of 128, 1.1 of 256 for its results (300 x 600 at 100 tokens: 3.8, 4.2, 6.6), a split one with 0.5 and
+// 0.08 ns a sum more for the meeting (128 x 128 sums 1.8 us, 16 x 128 0.7).  Clusters of 8 CTAs: of those that the occupancy query promises half came at
+// once (1024 x 8192 at 16 tokens: 16 clusters 8.4 us, 8 of tiles twice as wide 4.6).
+// Pairs do not split: clusters of two or four pairs came to 16.9 us instead of 17.8 for 4096 x 14336 at 300 tokens, and nowhere else to less.
 Choice choose(int M, int N, int B, int kbs)
 {
     constexpr int WIDTHS = 3;
@@ -521,11 +536,11 @@ Choice choose(int M, int N, int B, int kbs)
                 if (pair > 1 && (B <= TM || tn < 128)) continue;
                 if (split > 1 && (tn > 128 || kbs < 2 * split || pair > 1)) continue;
                 const long long tiles = (long long)ceil_div(B, pair * TM) * ceil_div(M, tn);
-                if (split > 1 && tiles > resident_splits(tn, split)) continue;
+                if (split > 1 && tiles > resident_splits(tn, split) / (split == 8 ? 2 : 1)) continue;
                 const long long waves = split > 1 ? 1 : (tiles + sms / pair - 1) / (sms / pair);
                 const int bytes = (B < TM ? B : TM) * KB_BYTES + tn / pair * KB_BYTES + (tn > 128 ? 3 : 2) * SCALES;
                 const double block = fmax(bytes / 113.0, fmax(280.0 / 256 * tn, 250));
-                const double time = waves * (ceil_div(kbs, split) * block + (split > 1 ? 1500 : 700)), hbm = M * (N * (17.0 / 32)) / 6000;
+                const double time = waves * (ceil_div(kbs, split) * block + 300 + 3 * tn + (split > 1 ? 500 + 0.08 * (B < TM ? B : TM) * tn : 0)), hbm = M * (N * (17.0 / 32)) / 6000;
                 const double longer = fmax(time, hbm) + 0.01 * time;
                 if (longer < best_time) { best_time = longer; best = {tn, split, pair}; }
             }

@@ -199,7 +199,8 @@ def test_linear(b, M, N, B, x_type):
 
 # (every form of the tensor-core kernel: pairs and single CTAs of each width, splits over clusters)
 @pytest.mark.parametrize("M,N,B", [(8192, 512, 2048), (6144, 512, 1000), (4096, 300, 1100), (14336, 520, 500), (28672, 256, 300), (9472, 1024, 16), (18944, 512, 16),
-                                   (128, 8192, 16), (300, 8192, 200), (2000, 16384, 30), (10000, 288, 128), (28416, 290, 120)])
+                                   (128, 8192, 16), (300, 8192, 200), (2000, 16384, 30), (10000, 288, 128), (28416, 290, 120), (4096, 8192, 300), (2000, 4096, 129), (1000, 2048, 500), (3000, 1100, 400), (520, 16384, 1000),
+                                   (1001, 4200, 257)])
 def test_linear_of_many_shapes(b, M, N, B):
     g = gen(M + N + B)
     w, ws = ref.random_weight(M, N, g, "cuda")

@@ -181,7 +181,7 @@ def test_results_behind_work_that_is_still_running(b):
 
 @pytest.mark.parametrize("x_type", ["bf16", "e2m1"])
 @pytest.mark.parametrize("M,N,B", [(37888, 320, 100), (9472, 4096, 100), (4096, 2048, 300), (8192, 8192, 2048), (4741, 416, 133), (128, 8192, 40), (1000, 4096, 77),
-                                   (2048, 2048, 128), (28672, 8192, 16), (28672, 8192, 1), (4096, 16384, 7)])
+                                   (2048, 2048, 128), (28672, 8192, 16), (28672, 8192, 1), (4096, 16384, 7), (4096, 14336, 300), (1000, 16384, 500)])
 def test_waits_that_run_out(b, M, N, B, x_type):
     g = gen(M + B)
     w, s = ref.random_weight(M, N, g, "cuda")
@@ -218,7 +218,7 @@ def test_waits_that_run_out_midway(b, clocks):
     w, s = ref.random_weight(8192, 8192, g, "cuda")
     x = torch.randn(600, 8192, generator=g, device="cuda").half()
     room = torch.zeros(1 << 23, dtype=torch.uint8, device="cuda")
-    for B in (1, 8, 16, 40, 100, 300, 600):
+    for B in (1, 8, 16, 40, 100, 130, 300, 600):
         call = lambda: b.vptq_linear_fp4(x[:B], w, s, out_dtype="fp32", workspace=room)  # noqa: E731, B023
         clean = call()
         for _ in range(3):
