@@ -547,8 +547,8 @@ int vptq_dequant_fp4(const vptq_layer_desc *desc, const vptq_layer_ptrs *p, uint
 
 /* out[B][M] = x[B][N] * W^T over an e2m1 weight: FP32 sums, the result rounded once to out_dtype.
  *   x_dtype VPTQ_DTYPE_E2M1: x [B][pitch(N)] with x_scale (tiles of its B rows)
- *           VPTQ_DTYPE_FP16 / _BF16: x [B][N], quantized inside the call by the rule (x_scale is not read): the same operands, and
- *           so the same result, as vptq_fp4_quantize followed by the call above
+ *           VPTQ_DTYPE_FP16 / _BF16: x [B][N], quantized inside the call by the rule (x_scale is not read): the same operands as
+ *           vptq_fp4_quantize followed by the call above, and the same result but for the order of "fp4_few"'s FP32 sums
  *   every pointer is 16-byte aligned (VPTQ_E_ALIGN), but for x of 16 bits: any alignment of a value;  out_dtype FP16, BF16 or FP32
  *   flags: VPTQ_FLAG_CONCURRENT and VPTQ_FLAG_DETERMINISTIC are accepted and change nothing (no CTA waits for another launch's, every
  *           sum has a fixed order).

@@ -82,6 +82,9 @@ __device__ __forceinline__ uint4 load_columns(const uint8_t *row, int c, int col
 
 // a token's block as an MMA operand, and its scale; for a whole warp.  n: columns from the lane's first on that exist.  zero: 0, which the compiler
 // does not know: conversions to e2m1 and back with nothing between them came out as zeros (nvcc 12.9).
+// A block's 32 products add up to at most 1152, times the weight's power of two at most 2^127: so that this does not overflow where the token's
+// power makes it small again, the operand is taken 2^11 smaller and its scale as much larger (all of it exact: the smallest step is 2^-140), unless
+// that scale is itself so large that the result overflows.
 template <int DT>
 __device__ __forceinline__ float operand_of(uint4 q, int n, uint32_t zero, uint32_t (&h)[4])
 {
@@ -92,7 +95,14 @@ __device__ __forceinline__ float operand_of(uint4 q, int n, uint32_t zero, uint3
     float v[8];
     values_of(e, v);
     widen(fp4_codes(v, b, n) ^ zero, h);
-    return fp4_scale_value(b);
+    const bool down = b < 243u;
+    const __half2 by = __half2half2(__ushort_as_half(down ? 0x1000 : 0x3C00));         // 2^-11 or 1
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        const __half2 p = __hmul2(*reinterpret_cast<const __half2 *>(&h[i]), by);
+        h[i] = *reinterpret_cast<const uint32_t *>(&p);
+    }
+    return __uint_as_float(b == 255u ? 0x7FFFFFFFu : (b + (down ? 11u : 0u)) << 23);
 }
 
 // map_full: boxes of stage_groups groups, map_less: of one fewer (CTAs differ by at most one).  VEC: activations are read 16 bytes at a time.

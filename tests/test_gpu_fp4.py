@@ -281,6 +281,22 @@ def test_linear_of_few_tokens_and_every_scale(b, B):
     assert y[:, ~keep].isnan().all() and same(y[:, keep], clean[:, keep])
 
 
+@pytest.mark.parametrize("B", [1, 5, 8, 40, 300])
+@pytest.mark.parametrize("size", [-126, -119, -110, -30, 0, 100, 116, 118, 124])
+def test_linear_of_scales_that_cancel(b, size, B):
+    """Weight and tokens near opposite ends of FP32's range: the results are in the middle of it."""
+    g = gen(B + size)
+    M, N = 300, 512
+    bytes_ = torch.randint(max(0, 119 - size), min(254, 127 - size) + 1, (M, 16), generator=g, device="cuda", dtype=torch.uint8)
+    w, _ = ref.random_weight(M, N, g, "cuda")
+    x = (torch.randn(B, N, generator=g, device="cuda").clamp(-3, 3) * 2.0 ** size).bfloat16()
+    ws = ref.scale_tiles(bytes_)
+    y = check_linear(b, x, w, ws, "fp32", N, ref.quantize(x)[0])
+    q, s = b.vptq_fp4_quantize(x)
+    check_linear(b, q, w, ws, "fp32", N, ref.values(q, s, N), s)
+    assert y.isfinite().all() and y.any()
+
+
 @pytest.mark.parametrize("B", [1, 40, 300])
 @pytest.mark.parametrize("bad", [float("nan"), float("inf")])
 def test_linear_keeps_what_is_not_a_number_in_its_row(b, B, bad):
