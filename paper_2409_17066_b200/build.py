@@ -37,7 +37,7 @@ def build_native(force: bool = False) -> str:
            os.path.join(root, "include", "torch", "csrc", "api", "include"), "/usr/local/cuda/include"]
     cmd = ["g++", "-O2", "-std=c++20", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
            *[f"-I{i}" for i in inc], NATIVE_SRC, "-o", NATIVE, f"-L{HERE}", f"-L{os.path.join(root, 'lib')}", "-l:libvptq.so",
-           "-ltorch_python", "-ltorch_cpu", "-lc10_cuda", "-lc10", "-Wl,-rpath,$ORIGIN"]
+           "-ltorch_python", "-ltorch_cpu", "-ltorch_cuda", "-lc10_cuda", "-lc10", "-Wl,-rpath,$ORIGIN"]
     subprocess.run(cmd, check=True)
     return NATIVE
 

@@ -5,6 +5,7 @@
 // attribute look-ups, ctypes conversions and torch.cuda.current_stream().
 #include <Python.h>
 
+#include <ATen/cuda/EmptyTensor.h>
 #include <ATen/detail/CUDAHooksInterface.h>
 #include <ATen/ops/clone.h>
 #include <ATen/ops/empty.h>
@@ -458,13 +459,19 @@ PyObject *py_moe_fp8(PyObject *, PyObject *const *a, Py_ssize_t n)
 
 // ---- 4-bit floating point ---------------------------------------------------------------------------------------------------
 
+// at::empty on the options' device, without the dispatcher: 0.2 us less of a call's 4 or 5 for every tensor
+at::Tensor new_tensor(at::IntArrayRef sizes, const at::TensorOptions &options)
+{
+    return at::Tensor(at::detail::empty_cuda(sizes, options.dtype().toScalarType(), options.device(), std::nullopt));
+}
+
 int64_t fp4_pitch(int64_t cols) { return (cols + 31) / 32 * 16; }
 
 // tensors of an e2m1 matrix: [rows][pitch] and its tiles of scales
 struct Fp4Tensors { at::Tensor q, scale; };
 Fp4Tensors empty_fp4(int64_t rows, int64_t cols, const at::TensorOptions &options)
 {
-    return {at::empty({rows, fp4_pitch(cols)}, options.dtype(at::kByte)), at::empty({(rows + 127) / 128, (cols + 127) / 128, 32, 16}, options.dtype(at::kByte))};
+    return {new_tensor({rows, fp4_pitch(cols)}, options.dtype(at::kByte)), new_tensor({(rows + 127) / 128, (cols + 127) / 128, 32, 16}, options.dtype(at::kByte))};
 }
 
 // [rows][pitch] e2m1 codes with tiles of scales
@@ -528,7 +535,7 @@ PyObject *py_fp4_values(PyObject *, PyObject *const *a, Py_ssize_t n)
     if (out && (!plain(*out) || out->dim() != 2 || out->size(0) != rows || out->size(1) != cols || code_of(out->scalar_type()) != dtype))
         return assertion("out [rows][cols], contiguous, of the type asked for");
     return guarded([&]() -> PyObject * {
-        at::Tensor result = out ? *out : at::empty({rows, cols}, q->options().dtype(dtype_of(dtype)));
+        at::Tensor result = out ? *out : new_tensor({rows, cols}, q->options().dtype(dtype_of(dtype)));
         int rc;
         Py_BEGIN_ALLOW_THREADS
         rc = vptq_fp4_values(static_cast<const uint8_t *>(q->data_ptr()), static_cast<const uint8_t *>(scale->data_ptr()), (int32_t)rows, (int32_t)cols, dtype,
@@ -576,7 +583,7 @@ PyObject *py_linear_fp4(PyObject *, PyObject *const *a, Py_ssize_t n)
     if (need < 0) return fail((int)need);
     return guarded([&]() -> PyObject * {
         CallMemory own;
-        const at::Tensor result = out ? *out : at::empty({B, M}, x->options().dtype(dtype_of(d.out_dtype)));
+        const at::Tensor result = out ? *out : new_tensor({B, M}, x->options().dtype(dtype_of(d.out_dtype)));
         if (B == 0) return out ? Py_NewRef(a[5]) : THPVariable_Wrap(result);           // no tokens: nothing to do
         if (need > 0 && ws == nullptr) {
             own.take(need);
@@ -675,7 +682,7 @@ PyObject *py_cache_read(PyObject *, PyObject *const *a, Py_ssize_t n)
             return assertion("k and v [tokens][heads][dim], contiguous, of the type asked for");
     return guarded([&]() -> PyObject * {
         const at::TensorOptions options = THPVariable_Unpack(a[0]).options().dtype(dtype_of(d.x_dtype));
-        at::Tensor k_out = k ? *k : at::empty({tokens, d.n_heads, dim}, options), v_out = v ? *v : at::empty({tokens, d.n_heads, dim}, options);
+        at::Tensor k_out = k ? *k : new_tensor({tokens, d.n_heads, dim}, options), v_out = v ? *v : new_tensor({tokens, d.n_heads, dim}, options);
         int rc;
         Py_BEGIN_ALLOW_THREADS
         rc = vptq_cache_read(&d, &p, k_out.data_ptr(), v_out.data_ptr(), (int32_t)tokens, current_stream());
