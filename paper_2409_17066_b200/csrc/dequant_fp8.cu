@@ -215,26 +215,28 @@ __device__ __forceinline__ void restore_block(const DequantFp8Params &P, int ind
         }
     }
     __syncthreads();
-    // 16 lanes a row, eight columns a lane (rows beyond M were not written: left out)
-    constexpr int ROWS = THREADS / 16, ROUNDS = FP8_BLOCK / ROWS;
-    const int lane = threadIdx.x & 15, sub = threadIdx.x >> 4, c = cb * FP8_BLOCK + lane * 8;
     if constexpr (E2M1) {
-        // four lanes are a block; the scales of 128 x 128 values are one tile, whose rows beyond M hold zeros
+        // 8 lanes a row, sixteen columns a lane, two lanes a block (eight columns a lane: 28672 x 8192 from 65536 + 256 entries 298 us instead of 256); the
+        // scales of 128 x 128 values are one tile, whose rows beyond M hold zeros
+        constexpr int ROWS = THREADS / 8;
+        const int lane = threadIdx.x & 7, c = cb * FP8_BLOCK + lane * 16;
         uint8_t *scales = P.tiles + ((long long)rb * P.col_blocks + cb) * FP4_TILE_BYTES;
 #pragma unroll
-        for (int i = 0; i < ROUNDS; i++) {
-            const int row = i * ROWS + sub;
+        for (int i = 0; i < FP8_BLOCK / ROWS; i++) {
+            const int row = i * ROWS + (int)(threadIdx.x >> 3);
             const bool in = m0 + row < m1;
-            Eight<VPTQ_DTYPE_FP16, true> e;
-            e.q = in && c < L.N ? *reinterpret_cast<const uint4 *>(&tile[row][lane * 8]) : make_uint4(0, 0, 0, 0);
-            const uint32_t b = fp4_block_scale(magnitude(e));
-            float v[8];
-            values_of(e, v);
-            if (in && c / 2 < P.pitch) *reinterpret_cast<uint32_t *>(P.q + (long long)(m0 + row) * P.pitch + c / 2) = fp4_codes(v, b, L.N - c);
-            if ((lane & 3) == 0) scales[fp4_scale_at(row, lane >> 2)] = (uint8_t)b;
+            Sixteen<VPTQ_DTYPE_FP16, true> e;
+#pragma unroll
+            for (int h = 0; h < 2; h++) e.h[h].q = in && c < L.N ? *reinterpret_cast<const uint4 *>(&tile[row][lane * 16 + 8 * h]) : make_uint4(0, 0, 0, 0);
+            const uint32_t b = fp4_pair_scale(magnitude(e));
+            if (in && c / 2 < P.pitch) *reinterpret_cast<uint2 *>(P.q + (long long)(m0 + row) * P.pitch + c / 2) = fp4_codes16(e, b, L.N - c);
+            if ((lane & 1) == 0) scales[fp4_scale_at(row, lane >> 1)] = (uint8_t)b;
         }
         return;
     }
+    // 16 lanes a row, eight columns a lane (rows beyond M were not written: left out)
+    constexpr int ROWS = THREADS / 16, ROUNDS = FP8_BLOCK / ROWS;
+    const int lane = threadIdx.x & 15, sub = threadIdx.x >> 4, c = cb * FP8_BLOCK + lane * 8;
     uint4 w[ROUNDS];
     uint32_t most = 0;
 #pragma unroll
