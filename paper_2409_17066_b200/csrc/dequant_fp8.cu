@@ -15,7 +15,8 @@
 // A table in L2 (1 MiB) makes a random read a vector, one a clock and SM; what it takes beyond them are dependent reads, indices and then
 // rows, with one block at a time a CTA (4096 x 4096 17.8 us, of which the reads are 8).  A small table is bound by the arithmetic (8192 x 28672
 // with 256 entries 201 us).
-// E2M1: the same to e2m1 with a power of two for every 32 columns of a row (fp4.cuh): only what follows the FP16 values differs.
+// E2M1: the same to e2m1 with a power of two for every 32 columns of a row (fp4.cuh), for layers that the kernel of dequant_fp4.cu does not take:
+// only what follows the FP16 values differs.
 #include "fp4.cuh"
 #include "index_words.cuh"
 #include "restore_words.cuh"
@@ -219,16 +220,16 @@ __device__ __forceinline__ void restore_block(const DequantFp8Params &P, int ind
         // 8 lanes a row, sixteen columns a lane, two lanes a block (eight columns a lane: 28672 x 8192 from 65536 + 256 entries 298 us instead of 256); the
         // scales of 128 x 128 values are one tile, whose rows beyond M hold zeros
         constexpr int ROWS = THREADS / 8;
-        const int lane = threadIdx.x & 7, c = cb * FP8_BLOCK + lane * 16;
+        const int lane = threadIdx.x >> 1 & 7, c = cb * FP8_BLOCK + lane * 16;       // (adjacent lanes in adjacent rows: in different banks)
         uint8_t *scales = P.tiles + ((long long)rb * P.col_blocks + cb) * FP4_TILE_BYTES;
 #pragma unroll
         for (int i = 0; i < FP8_BLOCK / ROWS; i++) {
-            const int row = i * ROWS + (int)(threadIdx.x >> 3);
+            const int row = i * ROWS + (int)(threadIdx.x >> 4 << 1 | (threadIdx.x & 1));
             const bool in = m0 + row < m1;
             Sixteen<VPTQ_DTYPE_FP16, true> e;
 #pragma unroll
             for (int h = 0; h < 2; h++) e.h[h].q = in && c < L.N ? *reinterpret_cast<const uint4 *>(&tile[row][lane * 16 + 8 * h]) : make_uint4(0, 0, 0, 0);
-            const uint32_t b = fp4_pair_scale(magnitude(e));
+            const uint32_t b = fp4_pair_scale<2>(magnitude(e));
             if (in && c / 2 < P.pitch) *reinterpret_cast<uint2 *>(P.q + (long long)(m0 + row) * P.pitch + c / 2) = fp4_codes16(e, b, L.N - c);
             if ((lane & 1) == 0) scales[fp4_scale_at(row, lane >> 1)] = (uint8_t)b;
         }
@@ -357,6 +358,7 @@ cudaError_t launch_dequant_fp8(const LayerView &L, uint8_t *q, float *scale, int
 
 cudaError_t launch_dequant_fp4(const LayerView &L, uint8_t *q, uint8_t *scale, int *inverse, cudaStream_t st)
 {
+    if (dequant_fp4_takes(L)) return launch_dequant_fp4_rows(L, q, scale, st);
     static_assert(FP4_TILE_ROWS == FP8_BLOCK && FP4_TILE_COLS == FP8_BLOCK, "a CTA's block is a tile of scales");
     DequantFp8Params P;
     P.L = L; P.q = q; P.scale = nullptr; P.tiles = scale;

@@ -23,6 +23,9 @@ cudaError_t launch_fp4_values(const uint8_t *q, const uint8_t *scale, int rows, 
 
 // a vector-quantized layer to e2m1 (dequant_fp8.cu); inverse: null or N words of scratch (a stored column order needs them)
 cudaError_t launch_dequant_fp4(const LayerView &L, uint8_t *q, uint8_t *scale, int *inverse, cudaStream_t st);
+// ... of the layers whose columns lie as they are stored (dequant_fp4.cu)
+bool dequant_fp4_takes(const LayerView &L);
+cudaError_t launch_dequant_fp4_rows(const LayerView &L, uint8_t *q, uint8_t *scale, cudaStream_t st);
 
 struct Fp4Linear {
     int M, N, B;
@@ -145,8 +148,9 @@ __device__ __forceinline__ uint32_t magnitude(const Sixteen<DT, VEC> &e)
         return max(magnitude<8>(e.h[0].v), magnitude<8>(e.h[1].v));        // (an Eight of FP32 is the values)
     }
 }
-// Two adjacent lanes hold a block's 32 values: its scale byte.
-__device__ __forceinline__ uint32_t fp4_pair_scale(uint32_t m) { return fp4_scale_byte(max(m, __shfl_xor_sync(0xffffffffu, m, 1))); }
+// Two lanes, OTHER apart, hold a block's 32 values: its scale byte.
+template <int OTHER = 1>
+__device__ __forceinline__ uint32_t fp4_pair_scale(uint32_t m) { return fp4_scale_byte(max(m, __shfl_xor_sync(0xffffffffu, m, OTHER))); }
 
 // Four adjacent lanes hold a block's 32 values: its scale byte, from each lane's largest magnitude (as bits).
 __device__ __forceinline__ uint32_t fp4_block_scale(uint32_t m)

@@ -154,7 +154,14 @@ def test_dequant_fp4_is_the_quantized_restored_weight(b, spec):
     check_quantized(*b.DeviceLayer(d).dequant_fp4(), torch.from_numpy(oracle.Layer.from_synth(d).dequant()).cuda())
 
 
-@pytest.mark.parametrize("spec", STAGED, ids=lambda s: s.name)
+# (a vector row of 128 columns to a warp: both tables staged or the residual's, with and without scale, outliers beside other columns, odd ends)
+ROWS = [synth.LayerSpec("q_r8", 4100, 2006, v=8, k1=65536, k2=256, n_out=5, v0=8, k0=256), synth.LayerSpec("q_r6", 4001, 1030, v=6, k1=65536, k2=200, n_out=33, v0=4, k0=16),
+        synth.LayerSpec("q_r8_plain", 2049, 1500, v=8, k1=2500, k2=200, has_scale=False), synth.LayerSpec("q_r6_wide", 1300, 4101, v=6, k1=4096, k2=256, n_out=130, v0=5, k0=100),
+        synth.LayerSpec("q_r8_both", 3001, 1001, v=8, k1=256, k2=256, n_out=3, v0=8, k0=16), synth.LayerSpec("q_r6_both", 6000, 2100, v=6, k1=200, k2=150, n_out=33, v0=4, k0=16),
+        synth.LayerSpec("q_r6_low", 7, 60001, v=6, k1=200, has_scale=False), synth.LayerSpec("q_r8_one", 1, 40000, v=8, k1=130)]
+
+
+@pytest.mark.parametrize("spec", STAGED + ROWS, ids=lambda s: s.name)
 def test_dequant_fp4_of_larger_layers(b, spec):
     dl = b.DeviceLayer(synth.make_layer(spec, 0, 3, 1))
     q, s = dl.dequant_fp4()
