@@ -15,9 +15,11 @@ inline long long fp4_scale_bytes(int rows, int cols)
     return (long long)ceil_div(rows, FP4_TILE_ROWS) * ceil_div(cols, FP4_TILE_COLS) * FP4_TILE_BYTES;
 }
 
-// `rows` rows to e2m1 (fp4_quantize.cu); ld = distance of x's rows in values; `early`: the kernel behind this one on the stream waits
-// for it by itself before it touches q or scale.
-cudaError_t launch_fp4_quantize(const void *x, int x_dtype, int rows, int cols, long long ld, uint8_t *q, uint8_t *scale, bool early, cudaStream_t st);
+// `rows` rows to e2m1 (fp4_quantize.cu); ld = distance of x's rows in values.  The kernel behind this one on the
+// stream may begin (and waits by itself before it touches q or scale) when this one has ended, at once, or when all those before this one have ended, what
+// they have written with them.
+enum class Behind { LAST, AT_ONCE, THEN };
+cudaError_t launch_fp4_quantize(const void *x, int x_dtype, int rows, int cols, long long ld, uint8_t *q, uint8_t *scale, Behind behind, cudaStream_t st);
 // ... and back to values [rows][cols] (fp4_values.cu)
 cudaError_t launch_fp4_values(const uint8_t *q, const uint8_t *scale, int rows, int cols, int out_dtype, void *out, cudaStream_t st);
 

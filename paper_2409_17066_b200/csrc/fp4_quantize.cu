@@ -20,7 +20,7 @@ struct QuantizeParams {
     long long ld, pitch;
     int col_tiles;
     uint8_t *q, *scale;
-    int early;
+    Behind behind;
 };
 
 // STEPS: rows of a thread; a tile is 4 / STEPS CTAs' work
@@ -28,8 +28,9 @@ template <int DT, bool VEC, int STEPS>
 __global__ void __launch_bounds__(THREADS)
 fp4_quantize_kernel(const __grid_constant__ QuantizeParams P)
 {
-    if (P.early) pdl_launch_dependents();
+    if (P.behind == Behind::AT_ONCE) pdl_launch_dependents();
     pdl_wait();
+    if (P.behind == Behind::THEN) pdl_launch_dependents();
     const int lane = threadIdx.x & 7, r = threadIdx.x >> 3;
     const unsigned tile = STEPS == 4 ? blockIdx.x : blockIdx.x / (4 / STEPS);
     const int rt = (int)(tile / (unsigned)P.col_tiles), ct = (int)(tile - (unsigned)rt * P.col_tiles), j0 = STEPS == 4 ? 0 : (int)(blockIdx.x % (4 / STEPS)) * STEPS;
@@ -61,12 +62,12 @@ cudaError_t launch(const QuantizeParams &P, bool vec, cudaStream_t st) { return 
 
 }  // namespace
 
-cudaError_t launch_fp4_quantize(const void *x, int x_dtype, int rows, int cols, long long ld, uint8_t *q, uint8_t *scale, bool early, cudaStream_t st)
+cudaError_t launch_fp4_quantize(const void *x, int x_dtype, int rows, int cols, long long ld, uint8_t *q, uint8_t *scale, Behind behind, cudaStream_t st)
 {
     QuantizeParams P;
     P.x = x; P.rows = rows; P.cols = cols; P.ld = ld; P.pitch = fp4_row_bytes(cols);
     P.col_tiles = ceil_div(cols, FP4_TILE_COLS);
-    P.q = q; P.scale = scale; P.early = early ? 1 : 0;
+    P.q = q; P.scale = scale; P.behind = behind;
     const int bytes = x_dtype == VPTQ_DTYPE_FP32 ? 4 : 2, per = 16 / bytes;
     const bool vec = (reinterpret_cast<uintptr_t>(x) & 15u) == 0 && cols % per == 0 && (rows == 1 || ld % per == 0);
     switch (x_dtype) {

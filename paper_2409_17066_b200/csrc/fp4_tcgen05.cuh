@@ -4,8 +4,8 @@
 
 namespace vptq {
 
-// P.x in e2m1 with scales; *status is cleared, and set when a bounded wait gave up
-cudaError_t launch_linear_fp4_tcgen05(const Fp4Linear &P, int *status, cudaStream_t st);
+// P.x in e2m1 with scales, early: by the kernel launched just before (Behind::THEN); *status is cleared, and set when a bounded wait gave up
+cudaError_t launch_linear_fp4_tcgen05(const Fp4Linear &P, int *status, bool early, cudaStream_t st);
 
 // a few tokens in 16 bits over a small weight, quantized on the way; no status word
 bool linear_fp4_few_takes(int M, int N, int B, int x_dtype);

@@ -66,6 +66,7 @@ struct Params {
     int out_dtype;
     int tma_out;           // rows of `out` are 16-byte aligned: stored by TMA
     int *status;
+    int weight_early;      // all that came before the preceding kernel of the stream has ended, and that one does not write the weight
     unsigned long long wait_limit;
 };
 
@@ -281,30 +282,47 @@ linear_fp4_tcgen05_kernel(const __grid_constant__ CUtensorMap map_x, const __gri
             uint32_t s = 0, round = 0;
             const uint32_t full0 = PAIR > 1 ? address_in(bar_full(0), 0) : bar_full(0);
             const int n_part = t_rank * (TN / PAIR);
+            // the weight's part of a stage, and what the stage waits for; then the tokens'.  (One lane calls them.)
+            auto scale_bytes = [&](int kb) { return (uint32_t)(min(CHUNKS, P.col_tiles - kb * CHUNKS) * FP4_TILE_BYTES); };
+            auto load_weight = [&](uint32_t s, int kb, int n0) {
+                const uint32_t at = base + s * SB, full = full0 + 8 * s;
+                const int w_tile = n0 / FP4_TILE_ROWS * P.col_tiles + kb * CHUNKS;
+                if constexpr (PAIR == 2) {
+                    if (t_rank == 0) mbar_expect_tx(bar_full(s), PAIR * SB);
+#pragma unroll
+                    for (int r = 0; r < RT; r++) tma_load<PAIR>(at + WS_AT + r * SCALES, &map_ws, 0, w_tile + r * P.col_tiles, full);
+                } else {
+                    // scales as linear copies, of the tiles that there are: two maps fewer for the host to make (0.5 us of a call)
+                    const uint32_t bytes = scale_bytes(kb), tiles = min(RT, P.row_tiles - n0 / FP4_TILE_ROWS);
+                    mbar_expect_tx(full, W_AT + TN * KB_BYTES + (1 + tiles) * bytes);
+#pragma unroll
+                    for (int r = 0; r < RT; r++)
+                        if (r < (int)tiles) bulk_load(at + WS_AT + r * SCALES, P.w_scale + (long long)(w_tile + r * P.col_tiles) * FP4_TILE_BYTES, bytes, full);
+                }
+                tma_load<PAIR>(at + W_AT, &map_w, kb * KB_BYTES, n0 + n_part, full);
+            };
+            auto load_tokens = [&](uint32_t s, int kb, int t0) {
+                const uint32_t at = base + s * SB, full = full0 + 8 * s;
+                const int x_tile = t0 / FP4_TILE_ROWS * P.col_tiles + kb * CHUNKS;
+                if constexpr (PAIR == 2) tma_load<PAIR>(at + XS_AT, &map_xs, 0, x_tile, full);
+                else bulk_load(at + XS_AT, P.x_scale + (long long)x_tile * FP4_TILE_BYTES, scale_bytes(kb), full);
+                tma_load<PAIR>(at, &map_x, kb * KB_BYTES, t0, full);
+            };
+            // Behind the kernel that quantizes the tokens the weight need not wait for it.
+            int begun = P.weight_early ? min((int)ST, kb1 - kb0) : 0;
+            if (first >= P.tiles) begun = 0;
+            for (int i = 0; i < begun; i++) {
+                if (elect_one()) load_weight((uint32_t)i, kb0 + i, first / P.tiles_t * TN);
+                __syncwarp();
+            }
             pdl_wait();                                                        // (weight and activations may be the preceding kernel's)
             for (int tile = first; tile < P.tiles; tile += step) {
                 const int t0 = (tile % P.tiles_t * PAIR + t_rank) * TM, n0 = tile / P.tiles_t * TN;
-                for (int kb = kb0; kb < kb1; kb++) {
+                for (int kb = kb0; kb < kb1; kb++, begun--) {
                     mbar_wait_or_flag(bar_empty(s), (round & 1) ^ 1u, lost_at, gave_up);
                     if (elect_one() && !gave_up) {
-                        const uint32_t at = base + s * SB, full = full0 + 8 * s;
-                        const int x_tile = t0 / FP4_TILE_ROWS * P.col_tiles + kb * CHUNKS, w_tile = n0 / FP4_TILE_ROWS * P.col_tiles + kb * CHUNKS;
-                        if constexpr (PAIR == 2) {
-                            if (t_rank == 0) mbar_expect_tx(bar_full(s), PAIR * SB);
-#pragma unroll
-                            for (int r = 0; r < RT; r++) tma_load<PAIR>(at + WS_AT + r * SCALES, &map_ws, 0, w_tile + r * P.col_tiles, full);
-                            tma_load<PAIR>(at + XS_AT, &map_xs, 0, x_tile, full);
-                        } else {
-                            // scales as linear copies, of the tiles that there are: two maps fewer for the host to make (0.5 us of a call)
-                            const uint32_t bytes = min(CHUNKS, P.col_tiles - kb * CHUNKS) * FP4_TILE_BYTES, tiles = min(RT, P.row_tiles - n0 / FP4_TILE_ROWS);
-                            mbar_expect_tx(full, W_AT + TN * KB_BYTES + (1 + tiles) * bytes);
-#pragma unroll
-                            for (int r = 0; r < RT; r++)
-                                if (r < (int)tiles) bulk_load(at + WS_AT + r * SCALES, P.w_scale + (long long)(w_tile + r * P.col_tiles) * FP4_TILE_BYTES, bytes, full);
-                            bulk_load(at + XS_AT, P.x_scale + (long long)x_tile * FP4_TILE_BYTES, bytes, full);
-                        }
-                        tma_load<PAIR>(at + W_AT, &map_w, kb * KB_BYTES, n0 + n_part, full);
-                        tma_load<PAIR>(at, &map_x, kb * KB_BYTES, t0, full);
+                        if (begun <= 0) load_weight(s, kb, n0);
+                        load_tokens(s, kb, t0);
                     }
                     __syncwarp();
                     if (++s == ST) { s = 0; round++; }
@@ -549,7 +567,7 @@ Choice choose(int M, int N, int B, int kbs)
 
 }  // namespace
 
-cudaError_t launch_linear_fp4_tcgen05(const Fp4Linear &L, int *status, cudaStream_t st)
+cudaError_t launch_linear_fp4_tcgen05(const Fp4Linear &L, int *status, bool early, cudaStream_t st)
 {
     Params P;
     P.M = L.M; P.B = L.B; P.kbs = ceil_div(L.N, KB);
@@ -558,6 +576,7 @@ cudaError_t launch_linear_fp4_tcgen05(const Fp4Linear &L, int *status, cudaStrea
     P.x_scale = L.x_scale; P.w_scale = L.w_scale;
     P.out = L.out; P.out_dtype = L.out_dtype; P.status = status;
     P.wait_limit = wait_limit();
+    P.weight_early = early ? 1 : 0;
     P.tiles_t = P.tiles = P.tma_out = P.x_bytes = P.stages = 0;
     const Choice c = choose(L.M, L.N, L.B, P.kbs);
     if (c.pair == 2) switch (c.tn) {

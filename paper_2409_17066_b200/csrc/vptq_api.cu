@@ -708,7 +708,7 @@ int vptq_fp4_quantize(const void *x, int32_t x_dtype, int32_t n_rows, int32_t n_
     if (n_rows == 0) return VPTQ_OK;
     if (x == nullptr || q == nullptr || scale == nullptr) return VPTQ_E_NULL;
     if (!aligned16(q) || !aligned16(scale) || (reinterpret_cast<uintptr_t>(x) & (x_dtype == VPTQ_DTYPE_FP32 ? 3u : 1u))) return VPTQ_E_ALIGN;
-    const cudaError_t e = launch_fp4_quantize(x, x_dtype, n_rows, n_cols, ld, q, scale, false, reinterpret_cast<cudaStream_t>(stream));
+    const cudaError_t e = launch_fp4_quantize(x, x_dtype, n_rows, n_cols, ld, q, scale, Behind::LAST, reinterpret_cast<cudaStream_t>(stream));
     return e == cudaSuccess ? VPTQ_OK : cuda_fail(e);
 }
 

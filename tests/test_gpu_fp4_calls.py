@@ -141,9 +141,9 @@ def test_products_in_a_replayed_graph(b, B):
         assert same(y, want)
 
 
-@pytest.mark.parametrize("permuted", [False, True])
-def test_a_restore_in_a_replayed_graph(b, permuted):
-    dl = b.DeviceLayer(synth.make_layer(synth.LayerSpec("q_graph", 1000, 1100, v=8, k1=256, k2=16, permuted=permuted), 0, 3, 1))
+@pytest.mark.parametrize("k2,permuted", [(16, False), (16, True), (0, False)])
+def test_a_restore_in_a_replayed_graph(b, k2, permuted):
+    dl = b.DeviceLayer(synth.make_layer(synth.LayerSpec("q_graph", 1000, 1100, v=8, k1=256, k2=k2, permuted=permuted), 0, 3, 1))
     dl.dequant_fp4()
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
@@ -178,6 +178,43 @@ def test_results_behind_work_that_is_still_running(b):
 
 
 # ---- waits that run out: every result is right or a NaN, and the next call is right ----------------------------
+
+@pytest.mark.parametrize("graph", [False, True])
+@pytest.mark.parametrize("B", [1, 16, 300])
+def test_products_right_behind_their_weight(b, B, graph):
+    """A weight that the kernel just before makes, of a size whose loads begin ahead of the tokens' quantization; another one every time."""
+    M, N = 28672, 2080
+    g = gen(B)
+    x = torch.randn(B, N, generator=g, device="cuda").bfloat16()
+    weights = [torch.randn(M, N, generator=g, device="cuda").bfloat16() for _ in range(3)]
+    want = []
+    for v in weights:
+        w, s = b.vptq_fp4_quantize(v)
+        torch.cuda.synchronize()
+        want.append(b.vptq_linear_fp4(x, w, s))
+        torch.cuda.synchronize()
+    given, q = weights[0].clone(), torch.empty(M, N, device="cuda", dtype=torch.bfloat16)
+
+    def both():
+        q.copy_(given)
+        return b.vptq_linear_fp4(x, *b.vptq_fp4_quantize(q))
+
+    if graph:
+        both()
+        torch.cuda.synchronize()
+        captured = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(captured):
+            y = both()
+    got = []
+    for i in range(9):
+        given.copy_(weights[i % 3])
+        if graph:
+            captured.replay()
+            got.append(y.clone())
+        else:
+            got.append(both())
+    assert all(same(r, want[i % 3]) for i, r in enumerate(got))
+
 
 @pytest.mark.parametrize("x_type", ["bf16", "e2m1"])
 @pytest.mark.parametrize("M,N,B", [(37888, 320, 100), (9472, 4096, 100), (4096, 2048, 300), (8192, 8192, 2048), (4741, 416, 133), (128, 8192, 40), (1000, 4096, 77),
