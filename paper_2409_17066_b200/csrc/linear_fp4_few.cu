@@ -7,7 +7,7 @@
 // products are exact in FP32; their sum is multiplied by the weight's power of two and added to the sum of all, times the token's, in one fma.
 // The activations, which no other warp of the CTA needs, come straight from global memory and are quantized by the rule of fp4_quantize.cu: a
 // token's block is four lanes.  At the end the warps' sums meet in shared memory and are added in warp order.
-// 4096 x 4096, one token, 5.7 us: launch and first reads, then a warp's steps for a block, bound by the integer pipe (a word's widening is 7 of its
+// 4096 x 4096, one token, 5.2 us: launch and first reads, then a warp's steps for a block, bound by the integer pipe (a word's widening is 7 of its
 // instructions, four conversions and the bytes' ways to them; by table look-ups to e4m3 it would be 9).  That is also why larger weights go to
 // linear_fp4_tcgen05.cu behind a quantizing kernel, whose products cost no instructions: 28672 x 8192 takes 36 us this way, in passes.
 // Every wait is bounded; a warp whose wait gives up leaves NaN.
