@@ -34,7 +34,7 @@ static_assert(8 * STRIDE * 4 <= STAGE_BYTES, "a warp's sums take its operands' p
 
 struct FewParams {
     Fp4Linear L;
-    int col_tiles, stage_groups;              // stage_groups: the most of any CTA
+    int stage_groups;                         // the most of any CTA
     uint32_t zero;
     unsigned long long wait_limit;
 };
@@ -130,8 +130,9 @@ linear_fp4_few_kernel(const __grid_constant__ CUtensorMap map_full, const __grid
     if (lane == 0 && any) {
         mbar_expect_tx(bar, (uint32_t)(n_groups * GROUP_BYTES + tiles * CHUNKS * FP4_TILE_BYTES));
         tma_load_2d(stage, n_groups == D.stage_groups ? &map_full : &map_less, warp * ROW, g0 * GROUP, bar);
+        // (zeros beyond a row's last tile, as the codes there: what follows in memory is the next 128 rows', and 0 * NaN is not 0)
         for (int i = 0; i < tiles; i++)
-            tma_load_2d(stage + GROUPS * GROUP_BYTES + i * CHUNKS * FP4_TILE_BYTES, &map_scales, 0, (tile0 + i) * D.col_tiles + warp * CHUNKS, bar);
+            tma_load_3d(stage + GROUPS * GROUP_BYTES + i * CHUNKS * FP4_TILE_BYTES, &map_scales, 0, warp * CHUNKS, tile0 + i, bar);
     }
     __syncwarp();
     uint32_t gave_up = 0;
@@ -221,7 +222,6 @@ cudaError_t run(const Fp4Linear &P, cudaStream_t st)
     const int groups = ceil_div(P.M, GROUP), sms = device_sm_count(), grid = groups < sms ? groups : sms;
     FewParams D;
     D.L = P;
-    D.col_tiles = ceil_div(P.N, FP4_TILE_COLS);
     D.stage_groups = ceil_div(groups, grid);
     D.zero = 0;
     D.wait_limit = wait_limit();
@@ -230,7 +230,8 @@ cudaError_t run(const Fp4Linear &P, cudaStream_t st)
         const int rows = GROUP * (D.stage_groups - i > 0 ? D.stage_groups - i : 1);
         if (!encode_tensor_map(&map[i], CU_TENSOR_MAP_DATA_TYPE_UINT8, P.w, pitch, P.M, pitch, 0, 0, ROW, rows, 1, CU_TENSOR_MAP_SWIZZLE_128B)) return cudaErrorNotSupported;
     }
-    if (!encode_tensor_map(&map_scales, CU_TENSOR_MAP_DATA_TYPE_UINT32, P.w_scale, FP4_TILE_BYTES / 4, (uint64_t)(fp4_scale_bytes(P.M, P.N) / FP4_TILE_BYTES), FP4_TILE_BYTES, 0, 0,
+    const uint64_t col_tiles = (uint64_t)ceil_div(P.N, FP4_TILE_COLS), row_tiles = (uint64_t)ceil_div(P.M, FP4_TILE_ROWS);
+    if (!encode_tensor_map(&map_scales, CU_TENSOR_MAP_DATA_TYPE_UINT32, P.w_scale, FP4_TILE_BYTES / 4, col_tiles, FP4_TILE_BYTES, row_tiles, col_tiles * FP4_TILE_BYTES,
                            FP4_TILE_BYTES / 4, CHUNKS, 1, CU_TENSOR_MAP_SWIZZLE_NONE))
         return cudaErrorNotSupported;
     auto kern = linear_fp4_few_kernel<DT, VEC>;
