@@ -214,17 +214,19 @@ PyObject *py_dequant(PyObject *, PyObject *const *a, Py_ssize_t n)
 
 // ---- 8-bit floating point: these allocate their results (and workspaces) themselves, from torch's allocator -----------------
 
-// a contiguous CUDA tensor on the device of the current stream
-bool on_current_device(const at::Tensor &t) { return t.is_cuda() && t.get_device() == c10::cuda::current_device(); }
+// a CUDA tensor on the device of the current stream, with memory and strides (a sparse one throws when asked for either), and a contiguous one
+bool on_current_device(const at::Tensor &t) { return t.is_cuda() && t.layout() == at::kStrided && t.get_device() == c10::cuda::current_device(); }
 bool plain(const at::Tensor &t) { return on_current_device(t) && t.is_contiguous(); }
 
 // workspace argument: a contiguous tensor of the current device (its bytes are written) or None
 bool room_of(PyObject *o, void **p, size_t *bytes)
 {
-    if (!workspace_of(o, p, bytes)) return false;
-    if (o == Py_None || plain(THPVariable_Unpack(o))) return true;
-    assertion("workspace: a contiguous tensor of the current device");
-    return false;
+    if (o != Py_None) {
+        const at::Tensor *t = tensor_of(o);
+        if (!t) return false;
+        if (!plain(*t)) { assertion("workspace: a contiguous tensor of the current device"); return false; }
+    }
+    return workspace_of(o, p, bytes);
 }
 
 // whether an address that came without a tensor is memory of the current device
@@ -237,7 +239,7 @@ bool address_on_current_device(const void *p)
     }
 }
 
-// runs a call that may throw (torch's allocator) and turns what it throws into a Python error
+// runs a call that may throw (torch's allocator, questions that a tensor does not answer) and turns what it throws into a Python error
 template <typename F>
 PyObject *guarded(F f)
 {
@@ -698,21 +700,30 @@ PyObject *py_set_error_class(PyObject *, PyObject *cls)
     Py_RETURN_NONE;
 }
 
+// A method as the table takes it.  Nothing that its C++ throws gets past it: in the interpreter's C frames that would end the process.
+template <PyObject *(*CALL)(PyObject *, PyObject *const *, Py_ssize_t)>
+PyObject *entry(PyObject *self, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded([&]() { return CALL(self, a, n); });
+}
+template <PyObject *(*CALL)(PyObject *, PyObject *const *, Py_ssize_t)>
+PyCFunction method() { return reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(entry<CALL>)); }
+
 PyMethodDef methods[] = {
-    {"linear", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_linear)), METH_FASTCALL, "vptq_linear on torch tensors"},
-    {"dequant", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_dequant)), METH_FASTCALL, "vptq_dequant on torch tensors"},
-    {"layer_linear", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_layer_linear)), METH_FASTCALL, "DeviceLayer.linear"},
-    {"fused_linear", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_fused_linear)), METH_FASTCALL, "FusedLayers.linear"},
-    {"fp8_quantize", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_fp8_quantize)), METH_FASTCALL, "vptq_fp8_quantize on torch tensors"},
-    {"dequant_fp8", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_dequant_fp8)), METH_FASTCALL, "vptq_dequant_fp8 on torch tensors"},
-    {"linear_fp8", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_linear_fp8)), METH_FASTCALL, "vptq_linear_fp8 on torch tensors"},
-    {"moe_fp8", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_moe_fp8)), METH_FASTCALL, "vptq_moe_fp8 on torch tensors"},
-    {"fp4_quantize", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_fp4_quantize)), METH_FASTCALL, "vptq_fp4_quantize on torch tensors"},
-    {"fp4_values", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_fp4_values)), METH_FASTCALL, "vptq_fp4_values on torch tensors"},
-    {"dequant_fp4", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_dequant_fp4)), METH_FASTCALL, "vptq_dequant_fp4 on torch tensors"},
-    {"linear_fp4", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_linear_fp4)), METH_FASTCALL, "vptq_linear_fp4 on torch tensors"},
-    {"cache_write", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_cache_write)), METH_FASTCALL, "vptq_cache_write on torch tensors"},
-    {"cache_read", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_cache_read)), METH_FASTCALL, "vptq_cache_read on torch tensors"},
+    {"linear", method<py_linear>(), METH_FASTCALL, "vptq_linear on torch tensors"},
+    {"dequant", method<py_dequant>(), METH_FASTCALL, "vptq_dequant on torch tensors"},
+    {"layer_linear", method<py_layer_linear>(), METH_FASTCALL, "DeviceLayer.linear"},
+    {"fused_linear", method<py_fused_linear>(), METH_FASTCALL, "FusedLayers.linear"},
+    {"fp8_quantize", method<py_fp8_quantize>(), METH_FASTCALL, "vptq_fp8_quantize on torch tensors"},
+    {"dequant_fp8", method<py_dequant_fp8>(), METH_FASTCALL, "vptq_dequant_fp8 on torch tensors"},
+    {"linear_fp8", method<py_linear_fp8>(), METH_FASTCALL, "vptq_linear_fp8 on torch tensors"},
+    {"moe_fp8", method<py_moe_fp8>(), METH_FASTCALL, "vptq_moe_fp8 on torch tensors"},
+    {"fp4_quantize", method<py_fp4_quantize>(), METH_FASTCALL, "vptq_fp4_quantize on torch tensors"},
+    {"fp4_values", method<py_fp4_values>(), METH_FASTCALL, "vptq_fp4_values on torch tensors"},
+    {"dequant_fp4", method<py_dequant_fp4>(), METH_FASTCALL, "vptq_dequant_fp4 on torch tensors"},
+    {"linear_fp4", method<py_linear_fp4>(), METH_FASTCALL, "vptq_linear_fp4 on torch tensors"},
+    {"cache_write", method<py_cache_write>(), METH_FASTCALL, "vptq_cache_write on torch tensors"},
+    {"cache_read", method<py_cache_read>(), METH_FASTCALL, "vptq_cache_read on torch tensors"},
     {"set_error_class", py_set_error_class, METH_O, "exception raised for VPTQ_E_* codes"},
     {nullptr, nullptr, 0, nullptr}};
 
