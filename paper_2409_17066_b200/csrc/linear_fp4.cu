@@ -18,6 +18,16 @@ Workspace workspace_of(int M, int N, int B, int x_dtype)
     return w;
 }
 
+// Loads of the weight may go ahead of the tokens' quantization only if the product is let in when all before that has ended, not at once: worth it
+// where the loads take longer than the wait, and with some tokens, whose quantization takes longer too.  Gains over weights of 2560 to 11008 columns, in a
+// graph / call by call, weights one after the other out of HBM:
+//   9 to 48 tokens:  14 MB -7 % / +2 %, 35 MB -4 / +1, 58 MB -4 / +1, 72 MB -3 / +3, 96 MB +1 / +4
+//   96 to 700:       14 MB -1 % / +3 %, 21 MB 0 / +3, 35 MB +1 / +3, 58 MB +1 / +3, 96 MB +1 / +3
+// and with one weight that stays in L2
+//   9 to 48:         35 MB -6 % / -4 %, 58 MB -2 / -1, 72 MB +2 / 0, 96 MB +2 / +4
+//   96 to 700:       14 MB -5 % / 0 %, 25 MB -2 / +1, 35 MB -1 / 0, 58 MB +2 / +2, 96 MB +1 / +3
+bool loads_early(long long weight_bytes, int tokens) { return weight_bytes >= (tokens < 96 ? 80 << 20 : 24 << 20); }
+
 }  // namespace
 
 long long linear_fp4_workspace_bytes(int M, int N, int B, int x_dtype) { return workspace_of(M, N, B, x_dtype).bytes; }
@@ -29,10 +39,7 @@ cudaError_t launch_linear_fp4(const Fp4Linear &P, void *ws, cudaStream_t st)
     if (linear_fp4_few_takes(P.M, P.N, P.B, P.x_dtype)) return launch_linear_fp4_few(P, st);
     uint8_t *w8 = reinterpret_cast<uint8_t *>(ws);
     Fp4Linear Q = P;
-    // Loads of the weight may go ahead of the tokens' quantization only if the product is let in when all before that has ended, not at once: worth it for
-    // weights that come from HBM (one after the other, 28672 x 8192 at 16 tokens 25.9 -> 24.6 us, 14336 x 4096 at 500 22.5 -> 21.5; still in L2 17.3 ->
-    // 17.4), too late for small ones (in a graph 300 x 600 at 40 tokens 6.9 -> 7.9, 11008 x 4096 at 128 9.5 -> 10.0).
-    const bool early = P.x_dtype != VPTQ_DTYPE_E2M1 && P.M * fp4_row_bytes(P.N) >= 28 << 20;
+    const bool early = P.x_dtype != VPTQ_DTYPE_E2M1 && loads_early(P.M * fp4_row_bytes(P.N), P.B);
     if (P.x_dtype != VPTQ_DTYPE_E2M1) {
         const Workspace w = workspace_of(P.M, P.N, P.B, P.x_dtype);
         const cudaError_t e = launch_fp4_quantize(P.x, P.x_dtype, P.B, P.N, P.N, w8 + w.values, w8 + w.scales, early ? Behind::THEN : Behind::AT_ONCE, st);
