@@ -204,8 +204,8 @@ cache_read_kernel(const __grid_constant__ CacheParams P)
     }
 }
 
-template <int DT, bool VEC, bool E2M1, int LANES, int N>
-cudaError_t launch(const CacheParams &P, int parts, bool write, cudaStream_t st)
+template <int DT, bool VEC, bool E2M1, int LANES, bool WRITE, int N>
+cudaError_t launch(const CacheParams &P, int parts, cudaStream_t st)
 {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)ceil_div(P.C.tokens, N * P.groups), (unsigned)parts);
@@ -216,32 +216,44 @@ cudaError_t launch(const CacheParams &P, int parts, bool write, cudaStream_t st)
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = pdl_enabled("kv_cache") ? 1 : 0;
-    return write ? cudaLaunchKernelEx(&cfg, cache_write_kernel<DT, VEC, E2M1, LANES, N>, P) : cudaLaunchKernelEx(&cfg, cache_read_kernel<DT, VEC, E2M1, LANES, N>, P);
+    if constexpr (WRITE) return cudaLaunchKernelEx(&cfg, cache_write_kernel<DT, VEC, E2M1, LANES, N>, P);
+    else return cudaLaunchKernelEx(&cfg, cache_read_kernel<DT, VEC, E2M1, LANES, N>, P);
 }
 
-// Pieces of a token are dealt out evenly to CTAs of THREADS / LANES slots; what is left of the slots takes more tokens.  A thread takes one token
-// while that fills the device no more than once, then four, then sixteen.
-template <int DT, bool VEC, bool E2M1, int LANES>
-cudaError_t launch_tokens(CacheParams P, bool write, cudaStream_t st)
+// Pieces of a token are dealt out evenly to CTAs of THREADS / LANES slots; what is left of the slots takes more tokens.  A thread takes one, four or
+// sixteen tokens: the more, the fewer look-ups and addresses, but the more registers (CTAs that an SM holds: reading 8, 4 or 5, 3 or 4; writing 6, 4, 3;
+// writing out of FP32 6, 2, 2) and the fewer threads.  The steps are by the CTAs of the one-token form, in units of eight an SM.  Measured over heads of
+// 40 to 256 columns, the time of the next form over that of the one before:
+//   reading, four tokens:              0.5 units 1.1, 1 0.9 to 1.0, 2 0.84, 8 0.8 to 0.9, 96 0.7 to 0.9
+//   reading, sixteen instead of four:  2 1.2 to 1.6, 8 0.94 to 1.24, 16 0.98 to 1.08, 48 0.95 to 1.05, 96 0.90 to 1.02
+//   writing, four:                     0.5 1.0 to 1.2, 1 0.9 to 1.0, 2 0.9, 8 0.8, 96 0.7; sixteen instead of four: 1.0 to 1.2 from 8 on, not taken
+//   writing out of FP32, four:         1.1 to 1.2 from 1 on, not taken; sixteen instead of one: 8 1.0, 24 1.0, 48 1.0, 64 0.9, 96 0.9
+template <int DT, bool VEC, bool E2M1, int LANES, bool WRITE>
+cudaError_t launch_tokens(CacheParams P, cudaStream_t st)
 {
     constexpr int SLOTS = THREADS / LANES;
     const int parts = ceil_div(P.units, SLOTS);
     P.width = ceil_div(P.units, parts);
     P.groups = SLOTS / P.width;
-    const long long ctas = (long long)ceil_div(P.C.tokens, P.groups) * parts, resident = (long long)device_sm_count() * 8;
-    if (ctas <= resident) return launch<DT, VEC, E2M1, LANES, 1>(P, parts, write, st);
-    if (ctas <= 8 * resident) return launch<DT, VEC, E2M1, LANES, 4>(P, parts, write, st);
-    return launch<DT, VEC, E2M1, LANES, 16>(P, parts, write, st);
+    const long long ctas = (long long)ceil_div(P.C.tokens, P.groups) * parts, unit = (long long)device_sm_count() * 8;
+    if constexpr (!(WRITE && DT == VPTQ_DTYPE_FP32)) {
+        if (ctas > unit && (WRITE || ctas < 48 * unit)) return launch<DT, VEC, E2M1, LANES, WRITE, 4>(P, parts, st);
+    }
+    if constexpr (!(WRITE && DT != VPTQ_DTYPE_FP32)) {
+        if (ctas >= 48 * unit) return launch<DT, VEC, E2M1, LANES, WRITE, 16>(P, parts, st);
+    }
+    return launch<DT, VEC, E2M1, LANES, WRITE, 1>(P, parts, st);
 }
 
-template <int DT, bool VEC>
-cudaError_t launch_form(const CacheParams &P, bool write, cudaStream_t st)
+template <int DT, bool VEC, bool WRITE>
+cudaError_t launch_form(const CacheParams &P, cudaStream_t st)
 {
-    if (P.C.e2m1) return P.C.dim <= 64 ? launch_tokens<DT, VEC, true, 4>(P, write, st) : launch_tokens<DT, VEC, true, 8>(P, write, st);
-    return P.C.dim <= 64 ? launch_tokens<DT, VEC, false, 4>(P, write, st) : launch_tokens<DT, VEC, false, 8>(P, write, st);
+    if (P.C.e2m1) return P.C.dim <= 64 ? launch_tokens<DT, VEC, true, 4, WRITE>(P, st) : launch_tokens<DT, VEC, true, 8, WRITE>(P, st);
+    return P.C.dim <= 64 ? launch_tokens<DT, VEC, false, 4, WRITE>(P, st) : launch_tokens<DT, VEC, false, 8, WRITE>(P, st);
 }
 
-cudaError_t launch_cache(const KvCache &C, bool write, cudaStream_t st)
+template <bool WRITE>
+cudaError_t launch_cache(const KvCache &C, cudaStream_t st)
 {
     CacheParams P;
     P.C = C;
@@ -256,15 +268,15 @@ cudaError_t launch_cache(const KvCache &C, bool write, cudaStream_t st)
     for (int i = 0; i < 2; i++)
         vec = vec && (reinterpret_cast<uintptr_t>(C.x[i]) & 15u) == 0 && (C.tokens == 1 || C.token_stride[i] % per == 0) && (C.heads == 1 || C.head_stride[i] % per == 0);
     switch (C.x_dtype) {
-    case VPTQ_DTYPE_FP16: return vec ? launch_form<VPTQ_DTYPE_FP16, true>(P, write, st) : launch_form<VPTQ_DTYPE_FP16, false>(P, write, st);
-    case VPTQ_DTYPE_BF16: return vec ? launch_form<VPTQ_DTYPE_BF16, true>(P, write, st) : launch_form<VPTQ_DTYPE_BF16, false>(P, write, st);
-    default: return vec ? launch_form<VPTQ_DTYPE_FP32, true>(P, write, st) : launch_form<VPTQ_DTYPE_FP32, false>(P, write, st);
+    case VPTQ_DTYPE_FP16: return vec ? launch_form<VPTQ_DTYPE_FP16, true, WRITE>(P, st) : launch_form<VPTQ_DTYPE_FP16, false, WRITE>(P, st);
+    case VPTQ_DTYPE_BF16: return vec ? launch_form<VPTQ_DTYPE_BF16, true, WRITE>(P, st) : launch_form<VPTQ_DTYPE_BF16, false, WRITE>(P, st);
+    default: return vec ? launch_form<VPTQ_DTYPE_FP32, true, WRITE>(P, st) : launch_form<VPTQ_DTYPE_FP32, false, WRITE>(P, st);
     }
 }
 
 }  // namespace
 
-cudaError_t launch_cache_write(const KvCache &C, cudaStream_t st) { return launch_cache(C, true, st); }
-cudaError_t launch_cache_read(const KvCache &C, cudaStream_t st) { return launch_cache(C, false, st); }
+cudaError_t launch_cache_write(const KvCache &C, cudaStream_t st) { return launch_cache<true>(C, st); }
+cudaError_t launch_cache_read(const KvCache &C, cudaStream_t st) { return launch_cache<false>(C, st); }
 
 }  // namespace vptq
