@@ -534,7 +534,8 @@ int vptq_moe_fp8(const vptq_moe_desc *desc, const vptq_moe_ptrs *p, const void *
  *   the type), to q and scale (16-byte aligned).  rows = 0 does nothing; rows and cols are at most 2^30, else VPTQ_E_SHAPE (M, N and B of the calls
  *   below too).
  * vptq_fp4_values: such a matrix back to out [rows][cols], packed, of out_dtype (FP16, BF16 or FP32; FP16 rounds and overflows as a conversion
- *   does, the others hold every value that the quantization makes). */
+ *   does, the others hold every value that the quantization makes but one: magnitudes from 3.5 * 2^126 on, which FP32 and BF16 still have, become
+ *   2^128, and read back as an infinity). */
 int64_t vptq_fp4_row_bytes(int32_t n_cols);
 int64_t vptq_fp4_scale_bytes(int32_t n_rows, int32_t n_cols);
 int vptq_fp4_quantize(const void *x, int32_t x_dtype, int32_t n_rows, int32_t n_cols, int64_t ld, uint8_t *q, uint8_t *scale, void *stream);
@@ -580,10 +581,10 @@ int vptq_linear_fp4_launches(const vptq_fp4_desc *desc, int32_t B);
  * table[s][(start[s] + i) / page_size] (table [n_seqs][table_width]; entries that no token needs may be anything).
  *   vptq_cache_write: k and v [n_tokens][n_heads][head_dim] of x_dtype (FP16, BF16 or FP32) into the cache; a token's heads and the tokens are any
  *     distances apart (strides in values, not negative), a head's columns are adjacent; any alignment of a value
- *   vptq_cache_read: those tokens' keys and values into k and v, packed: the FP32 product of code and scale, rounded to x_dtype
+ *   vptq_cache_read: those tokens' keys and values into k and v, packed: the FP32 product of code and scale, rounded to x_dtype (e2m1's 2^128: an infinity)
  * Tokens in no sequence (before cu[0], from cu[n_seqs] on) are left out: nothing is written for them.  A token whose position is negative or
  * beyond the table, or whose page is not in [0, n_pages), is not written, and reads as zeros.  Two tokens of one write that have the same
- * place (a page that two sequences share) leave it with codes and scales of either.
+ * place (a page that two sequences share) leave undefined values there: codes of the one may stand beside scales of the other.
  * Codes are 16-byte aligned, FP32 scales and the int32 arrays 4-byte aligned.  n_heads, page_size and n_pages are positive, head_dim is 1 to
  * VPTQ_CACHE_MAX_DIM, n_heads at most 4096, the others at most 2^30, else VPTQ_E_SHAPE; no tokens or no sequences: nothing is done. */
 #define VPTQ_CACHE_MAX_DIM 4096

@@ -602,7 +602,8 @@ def vptq_cache_read(k_cache: torch.Tensor, k_scale: torch.Tensor, v_cache: torch
                     start: torch.Tensor, cu: torch.Tensor, n_tokens: int, head_dim: int, out_dtype: Optional[str] = None,
                     k: Optional[torch.Tensor] = None, v: Optional[torch.Tensor] = None):
     """(k, v) [n_tokens][heads][head_dim] of those tokens out of the cache; out_dtype "fp16", "bf16" or "fp32" (default: that of k and v, else
-    "bf16").  Rows of tokens in no sequence (from cu[-1] on) are left as they are; in tensors that the call makes they are undefined."""
+    "bf16").  Rows of tokens in no sequence (from cu[-1] on) are left as they are; in tensors that the call makes they are undefined: a padded batch whose
+    padding is looked at later brings k and v of its own."""
     return _native.cache_read(k_cache, k_scale, v_cache, v_scale, table, start, cu, n_tokens, head_dim,
                               None if out_dtype is None else _DT[out_dtype], k, v)
 

@@ -70,3 +70,20 @@ def test_a_weights_block_of_the_next_128_rows(b, N):
         x = torch.randn(B, N, generator=g, device="cuda").half()
         clean, y = (b.vptq_linear_fp4(x, w, s, out_dtype="fp32") for s in (good, bad))
         assert clean.isfinite().all() and y[:, 128:].isnan().all() and same(y[:, :128], clean[:, :128])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_the_largest_magnitudes(b, dtype):
+    """From 3.5 * 2^126 on a value becomes 2^128, which FP32 and BF16 do not have; what is smaller reads back as a number."""
+    x = torch.zeros(4, 64, device="cuda", dtype=dtype)
+    x[0, 0], x[1, 0], x[2, 0], x[3, 5] = 3.5 * 2.0 ** 126, 3.46875 * 2.0 ** 126, torch.finfo(dtype).max, -torch.finfo(dtype).max
+    q, s = b.vptq_fp4_quantize(x)
+    assert [int(v) for v in ref.scale_rows(s, 4, 64)[:, 0]] == [253, 252, 253, 253]
+    want = torch.zeros(4, 64, dtype=torch.float64, device="cuda")
+    want[0, 0], want[1, 0], want[2, 0], want[3, 5] = 2.0 ** 128, 6 * 2.0 ** 125, 2.0 ** 128, -2.0 ** 128
+    assert torch.equal(ref.values(q, s, 64), want)
+    cache, i = b.make_cache(1, 4, 1, 64, "e2m1"), lambda *v: torch.tensor(v, dtype=torch.int32, device="cuda")
+    b.vptq_cache_write(x.view(4, 1, 64), x.view(4, 1, 64), *cache, i(0).view(1, 1), i(0), i(0, 4))
+    for out, t in (("fp32", torch.float32), ("bf16", torch.bfloat16)):
+        assert torch.equal(b.vptq_fp4_values(q, s, 64, out), want.float().to(t))
+        assert all(torch.equal(r.view(4, 64), want.float().to(t)) for r in b.vptq_cache_read(*cache, i(0).view(1, 1), i(0), i(0, 4), 4, 64, out))
