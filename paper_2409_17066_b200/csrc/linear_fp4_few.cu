@@ -7,9 +7,10 @@
 // products are exact in FP32; their sum is multiplied by the weight's power of two and added to the sum of all, times the token's, in one fma.
 // The activations, which no other warp of the CTA needs, come straight from global memory and are quantized by the rule of fp4_quantize.cu: a
 // token's block is four lanes.  At the end the warps' sums meet in shared memory and are added in warp order.
-// 4096 x 4096, one token, 5.2 us: launch and first reads, then a warp's steps for a block, bound by the integer pipe (a word's widening is 7 of its
-// instructions, four conversions and the bytes' ways to them; by table look-ups to e4m3 it would be 9).  That is also why larger weights go to
-// linear_fp4_tcgen05.cu behind a quantizing kernel, whose products cost no instructions: 28672 x 8192 takes 36 us this way, in passes.
+// 4096 x 4096, one token, 5.6 us, weights out of HBM in a graph: launch, first reads and a warp's eight dependent steps.  No pipe is used up (issue slots
+// 48 % busy, the integer pipe 40 %, for which a word's widening is 7 instructions, four conversions and the bytes' ways to them).
+// Larger weights go to linear_fp4_tcgen05.cu behind a quantizing kernel, whose products cost no instructions.  A form of this kernel that went over them
+// in passes, the integer pipe its bound, took 36 us for 28672 x 8192 and one token, that one 22.
 // Every wait is bounded; a warp whose wait gives up leaves NaN.
 #include "fp4.cuh"
 #include "fp4_tcgen05.cuh"
@@ -251,8 +252,12 @@ cudaError_t run(const Fp4Linear &P, cudaStream_t st)
 
 }  // namespace
 
-// One launch instead of two (4096 x 4096, one token, 5.2 us against 6.1 on the device, and 2 less of the host's time).  Rows that are no multiples of 16
-// bytes, read value by value, would take longer than the other launch.
+// One launch instead of two, and 2 to 3 us less of the host's time.  In a graph, this kernel / the two, weights out of HBM, one token:
+//   512 rows:   128 columns 2.8 / 3.7 us, 1024 2.9 / 4.5, 2048 3.4 / 4.6, 4096 4.5 / 4.9
+//   4096 rows:  128 columns 2.9 / 3.5, 1024 3.2 / 5.0, 2048 4.1 / 6.0, 4096 5.6 / 7.5 (8 tokens 6.6 / 7.6)
+//   4736 rows (32 an SM):  4096 columns 5.8 / 8.1
+// A warp's columns are one step of loads: more than 4096 would take a second, while the gain is already shrinking (64 rows of 4096, 8 tokens: 4.7 / 4.5).
+// Rows that are no multiples of 16 bytes, read value by value, would take longer than the other launch.
 bool linear_fp4_few_takes(int M, int N, int B, int x_dtype)
 {
     return x_dtype != VPTQ_DTYPE_E2M1 && B <= 8 && N <= MAX_COLS && N % 8 == 0 && ceil_div(M, GROUP) <= GROUPS * device_sm_count();
