@@ -48,6 +48,19 @@ def test_a_weights_block(b, N, B):
     assert y[:, ~keep].isnan().all() and same(y[:, keep], clean[:, keep])
 
 
+# (pairs of CTAs and single ones, wide tiles and narrow ones, columns split over clusters)
+@pytest.mark.parametrize("M,N,B", [(8192, 384, 2048), (4096, 640, 1000), (28672, 128, 300), (37888, 384, 100), (18944, 640, 16), (300, 8320, 16), (2000, 5760, 30), (1000, 2176, 500)])
+def test_a_weights_block_and_many_tokens(b, M, N, B):
+    g = gen(M)
+    last = ref.up(N, 32) - 1
+    w, _ = ref.random_weight(M, N, g, "cuda")
+    q, s = ref.random_weight(B, N, g, "cuda")
+    good, bad, keep = not_numbers(M, N, [(128 + 5, 0), (128 + 37, 1), (256 + 10, 2), (256 + 43, 3), (M - 1, last), (M - 40, 0)])
+    clean = check_linear(b, q, w, good, "fp32", N, ref.values(q, s, N), s)
+    y = b.vptq_linear_fp4(q, w, bad, x_scale=s, out_dtype="fp32")
+    assert y[:, ~keep].isnan().all() and same(y[:, keep], clean[:, keep])
+
+
 @pytest.mark.parametrize("N", COLS)
 def test_a_tokens_block(b, N):
     g = gen(N)
