@@ -8,7 +8,7 @@
 // The activations, which no other warp of the CTA needs, come straight from global memory and are quantized by the rule of fp4_quantize.cu: a
 // token's block is four lanes.  At the end the warps' sums meet in shared memory and are added in warp order.
 // 4096 x 4096, one token, 5.6 us, weights out of HBM in a graph: launch, first reads and a warp's eight dependent steps.  No pipe is used up (issue slots
-// 48 % busy, the integer pipe 40 %, for which a word's widening is 7 instructions, four conversions and the bytes' ways to them).
+// 49 % busy, the integer pipe 41 %, for which a word's widening is 7 instructions, four conversions and the bytes' ways to them).
 // Larger weights go to linear_fp4_tcgen05.cu behind a quantizing kernel, whose products cost no instructions.  A form of this kernel that went over them
 // in passes, the integer pipe its bound, took 36 us for 28672 x 8192 and one token, that one 22.
 // Every wait is bounded; a warp whose wait gives up leaves NaN.
